@@ -64,7 +64,9 @@ typedef enum apb_status {
     APB_ERR_VALUE = -4,    /* delta is NaN; alpha negative or infinite; step not finite or <= 0 */
     APB_ERR_NOMEM = -5,    /* host or device allocation failed                             */
     APB_ERR_HIP = -6,      /* a HIP call failed; see apb_last_hip_error()                  */
-    APB_ERR_SCRATCH = -7   /* apb_quantize_forward_static: sizes beyond the static scratch array */
+    APB_ERR_SCRATCH = -7,  /* apb_quantize_forward_static: sizes beyond the static scratch array */
+    APB_ERR_TYPE = -8,     /* an element type is not one of apb_type                       */
+    APB_ERR_ALIGN = -9     /* a 4-bit matrix is not 16-byte aligned, or an array not aligned to its elements */
 } apb_status;
 
 /* Opaque compressed layer.  Holds, in device memory: the sign words, the CSR of
@@ -298,6 +300,117 @@ size_t apb_train_workspace_bytes(void);
 int apb_train_forward(const float* W, long long n, float alpha, float delta, float* out, void* stream);
 int apb_train_backward(const float* W, const float* G, long long n, float alpha, float delta, float* grad_w,
                        double* grad_alpha_delta, long long* n_binarized, void* workspace, void* stream);
+
+/* ---- Microscaled 4-bit matrices: quantization, products, gradients --------------------------------
+ *
+ * The step above 2 bits that the matrix cores multiply as it is stored.  The rows of a matrix are cut
+ * into blocks of 32 consecutive values; a block has one scale 2^e (8 bits) and each value 4 bits, a sign
+ * and one of the levels 0, 1/2, 1, 3/2, 2, 3, 4, 6:
+ *      e  = clamp(floor(log2(max |x|)) - 2, -127, 125)      (-127 for a block of zeros)
+ *      x^ = 2^e * nearest level of x * 2^-e                 (midway: the level of even index; beyond 6: 6)
+ * A block that holds a NaN or an infinity gets the scale code of NaN: all its values read as NaN and so
+ * does every sum they enter.  Quantization is exact float arithmetic, so its result is defined to the bit.
+ *
+ * Layout of a 4-bit matrix of `rows` x K, with Kp = 256 * ceil(K / 256); 16-byte aligned:
+ *   uint8 codes[rows][Kp/2]          value k in byte k/2, even k in the low nibble; bit 3 the sign, bits
+ *                                    0..2 the index of the level.  Values k >= K are zero.
+ *   uint8 scales[Kp/256][rows][8]    byte (k mod 256) / 32: e + 127, or 255 for NaN
+ * It is plain device memory, like packed activations: it carries no record of rows and K, and reading it
+ * with others is unspecified, never out of bounds as long as it has apb_mx4_bytes(rows, K) bytes.
+ *
+ * Unlike the K x M activations above, operands here have the values that are summed over side by side:
+ * rows are tokens (or output channels), row-major, as language models hold them.  A K x M matrix is
+ * quantized through its strides, and since both operands of a product have the same form, exchanging them
+ * gives the transposed product.
+ *
+ * Groups: `offsets` (DEVICE, E+1 int32, ascending, offsets[0] = 0) gives every expert e the rows
+ * offsets[e] .. offsets[e+1]-1 of the left operand; the right operand then is E <= APB_MOE_MAX_E matrices of
+ * N rows each (one 4-bit matrix of E*N rows).  Experts may have no rows.  Rows from offsets[E] on belong to no expert and
+ * their results are 0.  offsets == NULL: one matrix, E must be 1.  The offsets are read on the device; values
+ * that are not ascending or leave 0 .. M give unspecified results, never an access out of bounds.
+ *
+ * Element types of the float matrices: apb_type.  Row strides (ld...) count elements and may be any number
+ * >= the row length; any alignment that suits the elements is taken, 16-byte alignment is faster.
+ * Sums are float32.  Everything only enqueues on `stream`, allocates nothing and records no memset. */
+enum apb_type { APB_F32 = 0, APB_BF16 = 1, APB_F16 = 2 };
+
+/* Bytes of a 4-bit matrix; 0 on bad arguments (rows or K <= 0, K > 2^22, or rows * ceil(K/256) >= 2^27). */
+size_t apb_mx4_bytes(int rows, int K);
+
+/*   X           DEVICE, element (r, k) at X[r * row_stride + k * col_stride]; strides of any sign or order.
+ *   rows_from   NULL, or DEVICE `rows` int32: row i of the result is row rows_from[i] of X (a gather);
+ *               an entry outside 0 .. rows_in-1 gives a row of zeros.  NULL: rows_in must equal rows.
+ *   mx          DEVICE, apb_mx4_bytes(rows, K) bytes, fully overwritten. */
+int apb_mx4_quantize(const void* X, int type, long long row_stride, long long col_stride, int rows_in,
+                     const int32_t* rows_from, int rows, int K, void* mx, void* stream);
+
+/* The values a 4-bit matrix stands for, rounded once to `type` (exact in APB_F32 and APB_BF16).
+ *   X  DEVICE, `rows` rows of K elements, ldx >= K apart. */
+int apb_mx4_dequantize(const void* mx, int rows, int K, int type, void* X, long long ldx, void* stream);
+
+/* Y[m, n] = sum_k A^[m, k] * B^[n, k]     (grouped: B^[e*N + n, k] with the expert e of row m)
+ *   A  DEVICE, 4-bit matrix of M rows.     B  DEVICE, 4-bit matrix of E*N rows.
+ *   Y  DEVICE, M rows of N elements of `type`, ldy apart, fully overwritten. */
+int apb_mx4_gemm(const void* A, const void* B, const int32_t* offsets, int E, int M, int N, int K, int type, void* Y,
+                 long long ldy, void* stream);
+
+/* apb_mx4_quantize of the activations and apb_mx4_gemm as one call, with the same Y.  Few rows (per expert, on
+ * average) run as a single kernel that quantizes in registers and streams the weights once: the form for
+ * single tokens.  X, x_type, ldx, rows_in, rows_from: as in apb_mx4_quantize with col_stride 1.
+ *   scratch  DEVICE, apb_mx4_bytes(M, K) bytes; contents unspecified afterwards. */
+int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const void* W,
+                   const int32_t* offsets, int E, int M, int N, int K, void* scratch, int y_type, void* Y, long long ldy,
+                   void* stream);
+
+/* The gradients at the quantized operands (straight-through, as apb_train_backward has it):
+ *      dX[m, k]     = sum_n G[m, n] * W^[n, k]                (grouped: W^ of the row's expert)
+ *      dW[e][n, k]  = sum over the rows m of expert e of G[m, n] * X^[m, k]
+ * G keeps every bit of its type: the matrix cores multiply bfloat16, in which 4-bit values are exact, and a
+ * G of APB_F16 or APB_F32 goes through them as two or three bfloat16 parts whose sum it is.
+ *   G   DEVICE, M rows of N elements of g_type, ldg apart.
+ *   W   DEVICE, 4-bit matrix of E*N rows of K.     X  DEVICE, 4-bit matrix of M rows of K.
+ *   dX  DEVICE, M rows of K elements of `type`, ldx apart, fully overwritten.
+ *   dW  DEVICE, E*N rows of K elements of `type`, ldw apart, fully overwritten (0 for an expert without rows). */
+int apb_mx4_backward_input(const void* G, int g_type, long long ldg, const void* W, const int32_t* offsets, int E, int M,
+                           int N, int K, int type, void* dX, long long ldx, void* stream);
+int apb_mx4_backward_weight(const void* G, int g_type, long long ldg, const void* X, const int32_t* offsets, int E, int M,
+                            int N, int K, int type, void* dW, long long ldw, void* stream);
+
+/* ---- Routing tokens to experts ---------------------------------------------------------------------
+ *
+ * apb_moe_route: every token takes its k largest logits, the lowest index among equals, in descending order.
+ * A logit of -inf or NaN is never taken.  Slot (t, j) is token t's j-th choice:
+ *      expert[t, j]   its expert, -1 if the token has fewer than k logits to take
+ *      weight[t, j]   softmax over the logits the token took (0 for slots of expert -1)
+ * The slots become rows, ordered by expert and, within one, by slot; slots of expert -1 come last:
+ *      offsets[e]     first row of expert e (E+1 entries; offsets[E] = rows that have an expert)
+ *      row_token[r]   the token of row r (T*k entries: what apb_mx4_linear takes as rows_from)
+ *      slot_row[t,j]  the row of the slot (a permutation of 0 .. T*k-1)
+ *   logits     DEVICE, T rows of E elements of `type`, ld apart; k <= E, k <= APB_MOE_MAX_K,
+ *              E <= APB_MOE_MAX_E, T * k < 2^24.
+ *   workspace  DEVICE, apb_moe_workspace_bytes(T, E, k) bytes, 4-byte aligned. */
+#define APB_MOE_MAX_E 1024
+#define APB_MOE_MAX_K 32
+size_t apb_moe_workspace_bytes(int T, int E, int k);
+int apb_moe_route(const void* logits, int type, long long ld, int T, int E, int k, int32_t* expert, float* weight,
+                  int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* workspace, void* stream);
+
+/* dlogits[t, expert[t,j]] = weight[t,j] * (dweight[t,j] - sum_i weight[t,i] * dweight[t,i]), 0 elsewhere; expert,
+ * weight as apb_moe_route left them, dweight DEVICE, T*k floats.  dlogits: T rows of E elements of `type`, ld apart. */
+int apb_moe_route_backward(const int32_t* expert, const float* weight, const float* dweight, int T, int E, int k, int type,
+                           void* dlogits, long long ld, void* stream);
+
+/* Y[t] = sum_j weight[t,j] * Z[slot_row[t,j]], and its gradients dZ[slot_row[t,j]] = weight[t,j] * dY[t] and
+ * dweight[t,j] = <dY[t], Z[slot_row[t,j]]>.  weight == NULL: all 1 (the gradient of the gather that rows_from is).
+ * A slot of weight 0 adds nothing, whatever its row holds, and its dZ is 0.  Sums over j in the order of j.
+ *   Z, dZ  DEVICE, T*k rows of N elements, ldz / lddz apart.   Y, dY  DEVICE, T rows of N elements, ldy / lddy apart.
+ *   An entry of slot_row outside 0 .. T*k-1 is a row of zeros and its dZ is not written.
+ *   dZ is fully overwritten if slot_row is a permutation.  dweight: T*k floats, or NULL. */
+int apb_moe_combine(const void* Z, int type, long long ldz, const int32_t* slot_row, const float* weight, int T, int k,
+                    int N, void* Y, long long ldy, void* stream);
+int apb_moe_combine_backward(const void* dY, int type, long long lddy, const void* Z, long long ldz, const int32_t* slot_row,
+                             const float* weight, int T, int k, int N, void* dZ, long long lddz, float* dweight,
+                             void* stream);
 
 /* ---- Measurement support: instruction-rate probes ---------------------------------------------
  *

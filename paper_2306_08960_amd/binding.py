@@ -25,12 +25,15 @@ EXPORTS = (
     "apb_w2_pack", "apb_w2_export", "apb_w2_free", "apb_gemm_2_2_int", "apb_gemm_2_2",
     "apb_train_workspace_bytes", "apb_train_forward", "apb_train_backward",
     "apb_probe_out_bytes", "apb_probe_rate",
+    "apb_mx4_bytes", "apb_mx4_quantize", "apb_mx4_dequantize", "apb_mx4_gemm", "apb_mx4_linear",
+    "apb_mx4_backward_input", "apb_mx4_backward_weight",
+    "apb_moe_workspace_bytes", "apb_moe_route", "apb_moe_route_backward", "apb_moe_combine", "apb_moe_combine_backward",
     "apb_strerror", "apb_last_hip_error",
 )
 
 APB_OK = 0
 APB_ERR_NULL, APB_ERR_SHAPE, APB_ERR_BITS, APB_ERR_VALUE, APB_ERR_NOMEM, APB_ERR_HIP = -1, -2, -3, -4, -5, -6
-APB_ERR_SCRATCH = -7
+APB_ERR_SCRATCH, APB_ERR_TYPE, APB_ERR_ALIGN = -7, -8, -9
 APB_STATIC_SCRATCH_BYTES = 32 << 20
 
 _lib: Optional[ctypes.CDLL] = None
@@ -109,6 +112,23 @@ def load() -> ctypes.CDLL:
     lib.apb_probe_out_bytes.restype = ctypes.c_size_t
     lib.apb_probe_rate.argtypes = [ci, ci, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.apb_probe_rate.restype = ci
+    ll = ctypes.c_longlong
+    lib.apb_mx4_bytes.argtypes = [ci, ci]
+    lib.apb_mx4_bytes.restype = ctypes.c_size_t
+    lib.apb_moe_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.apb_moe_workspace_bytes.restype = ctypes.c_size_t
+    for name, args in (("apb_mx4_quantize", [vp, ci, ll, ll, ci, vp, ci, ci, vp, vp]),
+                       ("apb_mx4_dequantize", [vp, ci, ci, ci, vp, ll, vp]),
+                       ("apb_mx4_gemm", [vp, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp]),
+                       ("apb_mx4_linear", [vp, ci, ll, ci, vp, vp, vp, ci, ci, ci, ci, vp, ci, vp, ll, vp]),
+                       ("apb_mx4_backward_input", [vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp]),
+                       ("apb_mx4_backward_weight", [vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp]),
+                       ("apb_moe_route", [vp, ci, ll, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp]),
+                       ("apb_moe_route_backward", [vp, vp, vp, ci, ci, ci, ci, vp, ll, vp]),
+                       ("apb_moe_combine", [vp, ci, ll, vp, vp, ci, ci, ci, vp, ll, vp]),
+                       ("apb_moe_combine_backward", [vp, ci, ll, vp, ll, vp, vp, ci, ci, ci, vp, ll, vp, vp])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ci
     lib.apb_strerror.argtypes = [ci]
     lib.apb_strerror.restype = ctypes.c_char_p
     lib.apb_last_hip_error.argtypes = []
@@ -579,3 +599,259 @@ def apb_train_backward(W: torch.Tensor, G: torch.Tensor, alpha: float, delta: fl
                                      sums.data_ptr(), count.data_ptr(), workspace.data_ptr(), _stream(stream)),
            "apb_train_backward")
     return grad_w, sums, count
+
+
+# ----------------------------------------------------------------------------- microscaled 4-bit matrices
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # apb_type
+
+
+def _type(dtype: torch.dtype) -> int:
+    if dtype not in _TYPES:
+        raise TypeError("element type must be float32, bfloat16 or float16")
+    return _TYPES[dtype]
+
+
+def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
+    """(pointer, apb_type, row stride) of a 2-D float matrix whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise TypeError(f"{name} must be a 2-D tensor on the GPU")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise TypeError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), _type(t.dtype), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _result(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dtype, device, name: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}")
+    return t
+
+
+def _ints(t: Optional[torch.Tensor], count: Optional[int], name: str) -> Optional[int]:
+    """Pointer of an int32 array of `count` entries, None for None."""
+    if t is None:
+        return None
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{name} must hold {count} int32")
+    return _dev_ptr(t, torch.int32, name)
+
+
+def _floats(t: Optional[torch.Tensor], count: int, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.numel() != count:
+        raise ValueError(f"{name} must hold {count} floats")
+    return _dev_ptr(t, torch.float32, name)
+
+
+def apb_mx4_bytes(rows: int, K: int) -> int:
+    return int(load().apb_mx4_bytes(int(rows), int(K)))
+
+
+def alloc_mx4(rows: int, K: int, device=None) -> torch.Tensor:
+    """Memory for a 4-bit matrix of `rows` rows of K values (uint8, see the header for the layout)."""
+    nbytes = apb_mx4_bytes(rows, K)
+    if nbytes == 0:
+        raise ApbError(APB_ERR_SHAPE, "apb_mx4_bytes")
+    dev = device if device is not None else torch.device("cuda", torch.cuda.current_device())
+    return torch.empty(nbytes, dtype=torch.uint8, device=dev)
+
+
+def _mx4_ptr(mx: torch.Tensor, rows: int, K: int, name: str) -> int:
+    need = apb_mx4_bytes(rows, K)
+    if need == 0:
+        raise ApbError(APB_ERR_SHAPE, "apb_mx4_bytes")
+    if mx.numel() * mx.element_size() < need:
+        raise ValueError(f"{name} smaller than apb_mx4_bytes({rows}, {K})")
+    return _dev_ptr(mx, torch.uint8, name)
+
+
+def _experts(offsets: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+    """(pointer, number of groups) of the offsets; (None, 1) without."""
+    if offsets is None:
+        return None, 1
+    if offsets.numel() < 2:
+        raise ValueError("offsets must hold E + 1 int32")
+    return _ints(offsets, None, "offsets"), offsets.numel() - 1
+
+
+def apb_mx4_quantize(X: torch.Tensor, mx: Optional[torch.Tensor] = None, rows_from: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """X: [rows, K] on the GPU, any strides (X.t() of a K x M matrix as well) -> its 4-bit form.  rows_from: int32 [rows],
+    the rows of X to take."""
+    if X.dim() != 2 or not X.is_cuda:
+        raise TypeError("X must be a 2-D tensor on the GPU")
+    rows_in, K = X.shape
+    rows = rows_in if rows_from is None else rows_from.numel()
+    if mx is None:
+        mx = alloc_mx4(rows, K, X.device)
+    _check(load().apb_mx4_quantize(X.data_ptr(), _type(X.dtype), X.stride(0), 1 if K == 1 else X.stride(1), rows_in,
+                                   _ints(rows_from, rows, "rows_from"), rows, K, _mx4_ptr(mx, rows, K, "mx"), _stream(stream)),
+           "apb_mx4_quantize")
+    return mx
+
+
+def apb_mx4_dequantize(mx: torch.Tensor, rows: int, K: int, dtype: torch.dtype = torch.float32,
+                       X: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    X = _result(X, (rows, K), dtype, mx.device, "X")
+    ptr, t, ld = _matrix(X, "X")
+    _check(load().apb_mx4_dequantize(_mx4_ptr(mx, rows, K, "mx"), int(rows), int(K), t, ptr, ld, _stream(stream)),
+           "apb_mx4_dequantize")
+    return X
+
+
+def apb_mx4_gemm(A: torch.Tensor, B: torch.Tensor, M: int, N: int, K: int, dtype: torch.dtype = torch.float32,
+                 Y: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y[M, N] = A^ B^T of two 4-bit matrices; with offsets (int32 [E+1]) the rows of A are grouped by expert and B holds
+    E*N rows."""
+    off, E = _experts(offsets)
+    Y = _result(Y, (M, N), dtype, A.device, "Y")
+    ptr, t, ld = _matrix(Y, "Y")
+    _check(load().apb_mx4_gemm(_mx4_ptr(A, M, K, "A"), _mx4_ptr(B, E * N, K, "B"), off, E, int(M), int(N), int(K), t, ptr, ld,
+                               _stream(stream)), "apb_mx4_gemm")
+    return Y
+
+
+def apb_mx4_linear(X: torch.Tensor, W: torch.Tensor, N: int, dtype: Optional[torch.dtype] = None,
+                   Y: Optional[torch.Tensor] = None, rows_from: Optional[torch.Tensor] = None,
+                   offsets: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """apb_mx4_quantize of X [rows_in, K] + apb_mx4_gemm with the 4-bit weights W in one call; Y has X's type by default."""
+    xp, xt, ldx = _matrix(X, "X")
+    rows_in, K = X.shape
+    M = rows_in if rows_from is None else rows_from.numel()
+    off, E = _experts(offsets)
+    if scratch is None:
+        scratch = alloc_mx4(M, K, X.device)
+    Y = _result(Y, (M, N), dtype or X.dtype, X.device, "Y")
+    yp, yt, ldy = _matrix(Y, "Y")
+    _check(load().apb_mx4_linear(xp, xt, ldx, rows_in, _ints(rows_from, M, "rows_from"), _mx4_ptr(W, E * N, K, "W"), off, E, M,
+                                 int(N), K, _mx4_ptr(scratch, M, K, "scratch"), yt, yp, ldy, _stream(stream)), "apb_mx4_linear")
+    return Y
+
+
+def apb_mx4_backward_input(G: torch.Tensor, W: torch.Tensor, K: int, dtype: Optional[torch.dtype] = None,
+                           dX: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """dX[M, K] = G W^ for the gradient G [M, N] of the product with the 4-bit weights W; dX has G's type by default."""
+    gp, gt, ldg = _matrix(G, "G")
+    M, N = G.shape
+    off, E = _experts(offsets)
+    dX = _result(dX, (M, K), dtype or G.dtype, G.device, "dX")
+    xp, xt, ldx = _matrix(dX, "dX")
+    _check(load().apb_mx4_backward_input(gp, gt, ldg, _mx4_ptr(W, E * N, K, "W"), off, E, M, N, int(K), xt, xp, ldx, _stream(stream)),
+           "apb_mx4_backward_input")
+    return dX
+
+
+def apb_mx4_backward_weight(G: torch.Tensor, X: torch.Tensor, K: int, dtype: torch.dtype = torch.float32,
+                            dW: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """dW[E*N, K] = G^T X^ (per expert with offsets) for the 4-bit activations X of the product."""
+    gp, gt, ldg = _matrix(G, "G")
+    M, N = G.shape
+    off, E = _experts(offsets)
+    dW = _result(dW, (E * N, K), dtype, G.device, "dW")
+    wp, wt, ldw = _matrix(dW, "dW")
+    _check(load().apb_mx4_backward_weight(gp, gt, ldg, _mx4_ptr(X, M, K, "X"), off, E, M, N, int(K), wt, wp, ldw, _stream(stream)),
+           "apb_mx4_backward_weight")
+    return dW
+
+
+# ----------------------------------------------------------------------------- routing tokens to experts
+
+def apb_moe_workspace_bytes(T: int, E: int, k: int) -> int:
+    return int(load().apb_moe_workspace_bytes(int(T), int(E), int(k)))
+
+
+def alloc_moe_workspace(T: int, E: int, k: int, device=None) -> torch.Tensor:
+    nbytes = apb_moe_workspace_bytes(T, E, k)
+    if nbytes == 0:
+        raise ApbError(APB_ERR_SHAPE, "apb_moe_workspace_bytes")
+    dev = device if device is not None else torch.device("cuda", torch.cuda.current_device())
+    return torch.empty((nbytes + 3) // 4, dtype=torch.int32, device=dev)
+
+
+def apb_moe_route(logits: torch.Tensor, k: int, workspace: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> dict:
+    """logits [T, E] -> expert int32 [T, k], weight float32 [T, k], offsets int32 [E+1], row_token int32 [T*k],
+    slot_row int32 [T, k] (see the header)."""
+    ptr, t, ld = _matrix(logits, "logits")
+    T, E = logits.shape
+    if workspace is None:
+        workspace = alloc_moe_workspace(T, E, k, logits.device)
+    elif workspace.numel() * workspace.element_size() < apb_moe_workspace_bytes(T, E, k):
+        raise ValueError("workspace smaller than apb_moe_workspace_bytes(T, E, k)")
+    new = lambda *shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device=logits.device)
+    out = {"expert": new(T, k), "weight": new(T, k, dtype=torch.float32), "offsets": new(E + 1), "row_token": new(T * k),
+           "slot_row": new(T, k)}
+    _check(load().apb_moe_route(ptr, t, ld, T, E, int(k), *(v.data_ptr() for v in out.values()),
+                                _dev_ptr(workspace, torch.int32, "workspace"), _stream(stream)), "apb_moe_route")
+    return out
+
+
+def apb_moe_route_backward(expert: torch.Tensor, weight: torch.Tensor, dweight: torch.Tensor, E: int,
+                           dtype: torch.dtype = torch.float32, dlogits: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    if expert.dim() != 2:
+        raise ValueError("expert must be [T, k]")
+    T, k = expert.shape
+    dlogits = _result(dlogits, (T, E), dtype, expert.device, "dlogits")
+    ptr, t, ld = _matrix(dlogits, "dlogits")
+    _check(load().apb_moe_route_backward(_ints(expert, T * k, "expert"), _floats(weight, T * k, "weight"),
+                                         _floats(dweight, T * k, "dweight"), T, int(E), k, t, ptr, ld, _stream(stream)),
+           "apb_moe_route_backward")
+    return dlogits
+
+
+def _slots(slot_row: torch.Tensor, Z: Optional[torch.Tensor], name: str) -> Tuple[int, int]:
+    if slot_row.dim() != 2:
+        raise ValueError("slot_row must be [T, k]")
+    T, k = slot_row.shape
+    if Z is not None and Z.shape[0] != T * k:
+        raise ValueError(f"{name} must have T*k rows")
+    return T, k
+
+
+def apb_moe_combine(Z: torch.Tensor, slot_row: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                    Y: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y[t] = sum_j weight[t, j] * Z[slot_row[t, j]]; weight None: all 1.  Y has Z's type."""
+    T, k = _slots(slot_row, Z, "Z")
+    zp, zt, ldz = _matrix(Z, "Z")
+    N = Z.shape[1]
+    Y = _result(Y, (T, N), Z.dtype, Z.device, "Y")
+    yp, yt, ldy = _matrix(Y, "Y")
+    if yt != zt:
+        raise TypeError("Y must have Z's type")
+    _check(load().apb_moe_combine(zp, zt, ldz, _ints(slot_row, T * k, "slot_row"), _floats(weight, T * k, "weight"), T, k, N, yp,
+                                  ldy, _stream(stream)), "apb_moe_combine")
+    return Y
+
+
+def apb_moe_combine_backward(dY: torch.Tensor, Z: Optional[torch.Tensor], slot_row: torch.Tensor,
+                             weight: Optional[torch.Tensor] = None, dZ: Optional[torch.Tensor] = None,
+                             stream: Optional[torch.cuda.Stream] = None):
+    """(dZ [T*k, N], dweight float32 [T, k]); Z None: only dZ is computed, dweight is None."""
+    T, k = _slots(slot_row, Z, "Z")
+    gp, gt, ldg = _matrix(dY, "dY")
+    N = dY.shape[1]
+    if dY.shape[0] != T:
+        raise ValueError("dY must have T rows")
+    zp, ldz, dweight = None, N, None
+    if Z is not None:
+        zp, zt, ldz = _matrix(Z, "Z")
+        if Z.shape[1] != N or zt != gt:
+            raise ValueError("Z must have dY's columns and type")
+        dweight = torch.empty((T, k), dtype=torch.float32, device=dY.device)
+    dZ = _result(dZ, (T * k, N), dY.dtype, dY.device, "dZ")
+    dp, dt, lddz = _matrix(dZ, "dZ")
+    if dt != gt:
+        raise TypeError("dZ must have dY's type")
+    _check(load().apb_moe_combine_backward(gp, gt, ldg, zp, ldz, _ints(slot_row, T * k, "slot_row"),
+                                           _floats(weight, T * k, "weight"), T, k, N, dp, lddz,
+                                           None if dweight is None else dweight.data_ptr(), _stream(stream)),
+           "apb_moe_combine_backward")
+    return dZ, dweight

@@ -524,6 +524,8 @@ const char* apb_strerror(int code) {
         case APB_ERR_NOMEM: return "out of memory";
         case APB_ERR_HIP: return "a HIP call failed (see apb_last_hip_error)";
         case APB_ERR_SCRATCH: return "the packed activations of this K, M and bits do not fit the library's static scratch array";
+        case APB_ERR_TYPE: return "an element type is not one of apb_type";
+        case APB_ERR_ALIGN: return "a pointer is not aligned as its contents need";
         default: return "unknown apb status";
     }
 }

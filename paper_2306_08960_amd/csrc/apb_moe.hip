@@ -1,0 +1,412 @@
+// Routing tokens to experts: the k largest logits of a token, softmax over them, the slots (token, choice) ordered by expert;
+// joining the experts' results; and both gradients.
+//
+// The order is that of a stable counting sort by expert.  A token takes an expert once at most, so the slots of an expert
+// among 64 tokens are a 64-bit mask, the rank of one the number of mask bits below it, and nothing depends on the order in
+// which atomics arrive.
+#include "apb_mx4.h"
+
+namespace apb {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTokens = 64;                   // tokens of a workgroup: bits of a mask
+constexpr int kScanThreads = 1024;
+constexpr long long kMaxSlots = 1LL << 24;    // a workgroup of 256 lanes per token: the lanes of a launch fit 32 bits
+
+// An order-preserving map of the logits that can be taken to positive whole numbers; -inf and NaN: 0.
+__device__ __forceinline__ uint32_t order_key(float v) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);      // (-0 and 0 are equal)
+    if (!(v > -INFINITY)) return 0u;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t key) {
+    return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d, kWave));
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d >>= 1) v += __shfl_xor(v, d, kWave);
+    return v;
+}
+
+// One wave: the choices of token t.  Lane j gets choice j (-1: none) and its weight; lanes hold EPL experts each, expert
+// 64 * r + lane.
+template <int EPL>
+__device__ __forceinline__ int choose(const void* logits, int type, long long at, int E, int k, float& weight) {
+    const int lane = threadIdx.x & (kWave - 1);
+    uint32_t key[EPL];
+#pragma unroll
+    for (int r = 0; r < EPL; ++r) {
+        const int e = r * kWave + lane;
+        key[r] = e < E ? order_key(load_f32(logits, type, at + e)) : 0u;
+    }
+    int mine = -1;
+    uint32_t mine_key = 0, top = 0;
+    for (int j = 0; j < k; ++j) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int r = 1; r < EPL; ++r) best = max(best, key[r]);
+        best = wave_max(best);
+        if (best == 0u) break;
+        if (j == 0) top = best;
+        bool found = false;
+#pragma unroll
+        for (int r = 0; r < EPL; ++r) {
+            const unsigned long long hit = __ballot(key[r] == best);
+            if (!found && hit) {
+                const int src = __ffsll((long long)hit) - 1;
+                found = true;
+                if (lane == j) {
+                    mine = r * kWave + src;
+                    mine_key = best;
+                }
+                if (lane == src) key[r] = 0u;
+            }
+        }
+    }
+    const float p = mine >= 0 ? expf(key_value(mine_key) - key_value(top)) : 0.0f;
+    const float sum = wave_sum(p);
+    weight = mine >= 0 ? p / sum : 0.0f;
+    return mine;
+}
+
+// What a workgroup knows of its 64 tokens: mask[e], which of them took expert e; drop[t], how many choices of token t there
+// are not.
+struct Block {
+    unsigned long long mask[APB_MOE_MAX_E];
+    int drop[kTokens];
+};
+
+__device__ __forceinline__ void clear(Block& b, int E) {
+    for (int e = threadIdx.x; e < E; e += kThreads) b.mask[e] = 0ull;
+    if (threadIdx.x < kTokens) b.drop[threadIdx.x] = 0;
+}
+__device__ __forceinline__ void note(Block& b, int token, int expert) {
+    if (expert >= 0) atomicOr(&b.mask[expert], 1ull << token);
+    else atomicAdd(&b.drop[token], 1);
+}
+// rank of slot (token, j) among the workgroup's slots of its expert (-1: among those without)
+__device__ __forceinline__ int rank_of(const Block& b, int token, int expert, int j, int k) {
+    if (expert >= 0) return __popcll(b.mask[expert] & ((1ull << token) - 1ull));
+    int n = j - (k - b.drop[token]);                             // (a token's missing choices are its last ones)
+    for (int i = 0; i < token; ++i) n += b.drop[i];
+    return n;
+}
+
+// ALONE: one workgroup has all tokens and does everything.  Otherwise count[e][workgroup] is written (e == E: slots without
+// an expert) and the scan and placement kernels follow.
+template <int EPL, bool ALONE>
+__global__ __launch_bounds__(kThreads) void k_moe_choose(const void* __restrict__ logits, int type, long long ld, int T, int E,
+                                                         int k, int32_t* __restrict__ expert, float* __restrict__ weight,
+                                                         int32_t* __restrict__ offsets, int32_t* __restrict__ row_token,
+                                                         int32_t* __restrict__ slot_row, int32_t* __restrict__ count) {
+    __shared__ Block b;
+    __shared__ int start[ALONE ? APB_MOE_MAX_E + 1 : 1];
+    clear(b, E);
+    __syncthreads();
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int t0 = blockIdx.x * kTokens;
+    for (int i = wave; i < kTokens && t0 + i < T; i += kThreads / kWave) {
+        float w;
+        const int e = choose<EPL>(logits, type, (long long)(t0 + i) * ld, E, k, w);
+        if (lane < k) {
+            expert[(t0 + i) * k + lane] = e;
+            weight[(t0 + i) * k + lane] = w;
+            note(b, i, e);
+        }
+    }
+    __syncthreads();
+    if (!ALONE) {
+        for (int e = threadIdx.x; e <= E; e += kThreads) {
+            int n = 0;
+            if (e < E) n = __popcll(b.mask[e]);
+            else
+                for (int i = 0; i < kTokens; ++i) n += b.drop[i];
+            count[(size_t)e * gridDim.x + blockIdx.x] = n;
+        }
+        return;
+    }
+    if (wave == 0) {
+        int before = 0;
+        for (int base = 0; base < E; base += kWave) {
+            const int e = base + lane;
+            const int n = e < E ? __popcll(b.mask[e]) : 0;
+            int upto = n;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const int v = __shfl_up(upto, d, kWave);
+                if (lane >= d) upto += v;
+            }
+            if (e < E) {
+                start[e] = before + upto - n;
+                offsets[e] = before + upto - n;
+            }
+            before += __shfl(upto, kWave - 1, kWave);
+        }
+        if (lane == 0) {
+            start[E] = before;
+            offsets[E] = before;
+        }
+    }
+    __syncthreads();
+    for (int s = threadIdx.x; s < T * k; s += kThreads) {
+        const int t = s / k, e = expert[s];                      // (written by this workgroup, before its barrier)
+        const int row = start[e >= 0 ? e : E] + rank_of(b, t, e, s - t * k, k);
+        slot_row[s] = row;
+        row_token[row] = t;
+    }
+}
+
+// One workgroup: count[e][..] becomes the number of slots of e before each workgroup, offsets the first row of each expert.
+__global__ __launch_bounds__(kScanThreads) void k_moe_scan(int32_t* __restrict__ count, int blocks, int E,
+                                                           int32_t* __restrict__ offsets) {
+    __shared__ int total[APB_MOE_MAX_E + 1];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    for (int e = wave; e <= E; e += kScanThreads / kWave) {
+        int before = 0;
+        for (int base = 0; base < blocks; base += kWave) {
+            const int i = base + lane;
+            const int n = i < blocks ? count[(size_t)e * blocks + i] : 0;
+            int upto = n;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const int v = __shfl_up(upto, d, kWave);
+                if (lane >= d) upto += v;
+            }
+            if (i < blocks) count[(size_t)e * blocks + i] = before + upto - n;
+            before += __shfl(upto, kWave - 1, kWave);
+        }
+        if (lane == 0) total[e] = before;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        int before = 0;
+        for (int base = 0; base <= E; base += kWave) {
+            const int e = base + lane;
+            const int n = e <= E ? total[e] : 0;
+            int upto = n;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const int v = __shfl_up(upto, d, kWave);
+                if (lane >= d) upto += v;
+            }
+            if (e <= E) offsets[e] = before + upto - n;
+            before += __shfl(upto, kWave - 1, kWave);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void k_moe_place(const int32_t* __restrict__ expert, int T, int E, int k,
+                                                        const int32_t* __restrict__ count, const int32_t* __restrict__ offsets,
+                                                        int32_t* __restrict__ row_token, int32_t* __restrict__ slot_row) {
+    __shared__ Block b;
+    clear(b, E);
+    __syncthreads();
+    const int t0 = blockIdx.x * kTokens;
+    const int slots = min(kTokens, T - t0) * k;
+    for (int s = threadIdx.x; s < slots; s += kThreads) note(b, s / k, expert[t0 * k + s]);
+    __syncthreads();
+    for (int s = threadIdx.x; s < slots; s += kThreads) {
+        const int t = s / k, e = expert[t0 * k + s], g = e >= 0 ? e : E;
+        const int row = offsets[g] + count[(size_t)g * gridDim.x + blockIdx.x] + rank_of(b, t, e, s - t * k, k);
+        slot_row[t0 * k + s] = row;
+        row_token[row] = t0 + t;
+    }
+}
+
+// One wave per token; its row of dlogits is put together in LDS.
+__global__ __launch_bounds__(kThreads) void k_moe_route_backward(const int32_t* __restrict__ expert,
+                                                                 const float* __restrict__ weight,
+                                                                 const float* __restrict__ dweight, int T, int E, int k,
+                                                                 int type, void* __restrict__ dlogits, long long ld) {
+    __shared__ float rows[kThreads / kWave][APB_MOE_MAX_E];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int t = blockIdx.x * (kThreads / kWave) + wave;
+    float* row = rows[wave];
+    for (int e = lane; e < E; e += kWave) row[e] = 0.0f;
+    __syncthreads();
+    if (t < T) {
+        const bool slot = lane < k;
+        const int e = slot ? expert[t * k + lane] : -1;
+        const bool there = e >= 0 && e < E;
+        const float w = there ? weight[t * k + lane] : 0.0f, d = there ? dweight[t * k + lane] : 0.0f;
+        const float inner = wave_sum(w * d);
+        if (there) row[e] = w * (d - inner);
+    }
+    __syncthreads();
+    if (t < T)
+        for (int e = lane; e < E; e += kWave) store_f32(dlogits, type, (long long)t * ld + e, row[e]);
+}
+
+// A lane makes eight neighbours of a row of Y.  grid.x: tokens, grid.y: pieces of 2048 columns.
+template <int TYPE, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_moe_combine(const void* __restrict__ Z, long long ldz,
+                                                          const int32_t* __restrict__ slot_row,
+                                                          const float* __restrict__ weight, int T, int k, int N,
+                                                          void* __restrict__ Y, long long ldy) {
+    const int t = blockIdx.x, n = (blockIdx.y * kThreads + threadIdx.x) * 8;
+    if (n >= N) return;
+    float acc[8] = {};
+    for (int j = 0; j < k; ++j) {
+        const int row = slot_row[t * k + j];
+        const float w = weight ? weight[t * k + j] : 1.0f;
+        if (w == 0.0f || row < 0 || row >= T * k) continue;
+        float v[8];
+        load8<TYPE, VEC>(Z, (long long)row * ldz + n, N - n, v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) acc[q] = fmaf(w, v[q], acc[q]);
+    }
+    store8<TYPE, VEC>(Y, (long long)t * ldy + n, N - n, acc);
+}
+
+// One wave per slot: its row of dZ and its dweight.
+template <int TYPE, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* __restrict__ dY, long long lddy,
+                                                                   const void* __restrict__ Z, long long ldz,
+                                                                   const int32_t* __restrict__ slot_row,
+                                                                   const float* __restrict__ weight, int slots, FastDiv by_k, int N,
+                                                                   void* __restrict__ dZ, long long lddz,
+                                                                   float* __restrict__ dweight) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int s = blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+    if (s >= slots) return;
+    const int t = (int)by_k.div((uint32_t)s), row = slot_row[s];
+    const float w = weight ? weight[s] : 1.0f;
+    const bool there = row >= 0 && row < slots;
+    float dot = 0.0f;
+    if (there) {
+        for (int n = lane * 8; n < N; n += kWave * 8) {
+            float g[8], z[8], d[8];
+            load8<TYPE, VEC>(dY, (long long)t * lddy + n, N - n, g);
+            if (dweight) {
+                load8<TYPE, VEC>(Z, (long long)row * ldz + n, N - n, z);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) dot = fmaf(g[q], z[q], dot);
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) d[q] = w == 0.0f ? 0.0f : w * g[q];
+            store8<TYPE, VEC>(dZ, (long long)row * lddz + n, N - n, d);
+        }
+    }
+    if (dweight) {
+        dot = wave_sum(dot);
+        if (lane == 0) dweight[s] = dot;
+    }
+}
+
+template <int EPL>
+void launch_choose(bool alone, int blocks, hipStream_t s, const void* logits, int type, long long ld, int T, int E, int k,
+                   int32_t* expert, float* weight, int32_t* offsets, int32_t* row_token, int32_t* slot_row, int32_t* count) {
+    if (alone)
+        hipLaunchKernelGGL((k_moe_choose<EPL, true>), dim3(blocks), dim3(kThreads), 0, s, logits, type, ld, T, E, k, expert, weight,
+                           offsets, row_token, slot_row, count);
+    else
+        hipLaunchKernelGGL((k_moe_choose<EPL, false>), dim3(blocks), dim3(kThreads), 0, s, logits, type, ld, T, E, k, expert, weight,
+                           offsets, row_token, slot_row, count);
+}
+
+bool bad_route(int T, int E, int k) {
+    return T <= 0 || E <= 0 || k <= 0 || k > E || E > APB_MOE_MAX_E || k > APB_MOE_MAX_K || (long long)T * k >= kMaxSlots;
+}
+int route_blocks(int T) { return (T + kTokens - 1) / kTokens; }
+
+}  // namespace
+}  // namespace apb
+
+using namespace apb;
+
+extern "C" {
+
+size_t apb_moe_workspace_bytes(int T, int E, int k) {
+    if (bad_route(T, E, k)) return 0;
+    return (size_t)route_blocks(T) * (E + 1) * sizeof(int32_t);
+}
+
+int apb_moe_route(const void* logits, int type, long long ld, int T, int E, int k, int32_t* expert, float* weight,
+                  int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* workspace, void* stream) {
+    if (!logits || !expert || !weight || !offsets || !row_token || !slot_row || !workspace) return APB_ERR_NULL;
+    if (bad_type(type)) return APB_ERR_TYPE;
+    if (bad_route(T, E, k) || ld < E) return APB_ERR_SHAPE;
+    if (!aligned(logits, type_size(type)) || !aligned(expert, 4) || !aligned(weight, 4) || !aligned(offsets, 4) ||
+        !aligned(row_token, 4) || !aligned(slot_row, 4) || !aligned(workspace, 4))
+        return APB_ERR_ALIGN;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const int blocks = route_blocks(T);
+    int32_t* count = static_cast<int32_t*>(workspace);
+    const bool alone = blocks == 1;
+    if (E <= 64) launch_choose<1>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else if (E <= 128) launch_choose<2>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else if (E <= 256) launch_choose<4>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else launch_choose<16>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    if (!alone) {
+        hipLaunchKernelGGL(k_moe_scan, dim3(1), dim3(kScanThreads), 0, s, count, blocks, E, offsets);
+        hipLaunchKernelGGL(k_moe_place, dim3(blocks), dim3(kThreads), 0, s, expert, T, E, k, count, offsets, row_token, slot_row);
+    }
+    APB_HIP(hipGetLastError());
+    return APB_OK;
+}
+
+int apb_moe_route_backward(const int32_t* expert, const float* weight, const float* dweight, int T, int E, int k, int type,
+                           void* dlogits, long long ld, void* stream) {
+    if (!expert || !weight || !dweight || !dlogits) return APB_ERR_NULL;
+    if (bad_type(type)) return APB_ERR_TYPE;
+    if (bad_route(T, E, k) || ld < E) return APB_ERR_SHAPE;
+    if (!aligned(expert, 4) || !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dlogits, type_size(type))) return APB_ERR_ALIGN;
+    const int per = kThreads / kWave;
+    hipLaunchKernelGGL(k_moe_route_backward, dim3((T + per - 1) / per), dim3(kThreads), 0, reinterpret_cast<hipStream_t>(stream), expert,
+                       weight, dweight, T, E, k, type, dlogits, ld);
+    APB_HIP(hipGetLastError());
+    return APB_OK;
+}
+
+#define APB_BY_TYPE_AND_ALIGNMENT(kernel, grid, ...)                                                                            \
+    do {                                                                                                                        \
+        if (type == APB_F32 && vec) hipLaunchKernelGGL((kernel<APB_F32, true>), grid, dim3(kThreads), 0, s, __VA_ARGS__);       \
+        else if (type == APB_F32) hipLaunchKernelGGL((kernel<APB_F32, false>), grid, dim3(kThreads), 0, s, __VA_ARGS__);        \
+        else if (type == APB_BF16 && vec) hipLaunchKernelGGL((kernel<APB_BF16, true>), grid, dim3(kThreads), 0, s, __VA_ARGS__); \
+        else if (type == APB_BF16) hipLaunchKernelGGL((kernel<APB_BF16, false>), grid, dim3(kThreads), 0, s, __VA_ARGS__);      \
+        else if (vec) hipLaunchKernelGGL((kernel<APB_F16, true>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                     \
+        else hipLaunchKernelGGL((kernel<APB_F16, false>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                             \
+    } while (0)
+
+int apb_moe_combine(const void* Z, int type, long long ldz, const int32_t* slot_row, const float* weight, int T, int k,
+                    int N, void* Y, long long ldy, void* stream) {
+    if (!Z || !slot_row || !Y) return APB_ERR_NULL;
+    if (bad_type(type)) return APB_ERR_TYPE;
+    if (T <= 0 || k <= 0 || k > APB_MOE_MAX_K || N <= 0 || N > kMxMaxK || (long long)T * k >= kMaxSlots || ldz < N || ldy < N) return APB_ERR_SHAPE;
+    if (!aligned(Z, type_size(type)) || !aligned(Y, type_size(type)) || !aligned(slot_row, 4) || !aligned(weight, 4)) return APB_ERR_ALIGN;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const bool vec = rows_aligned16(Z, ldz, type) && rows_aligned16(Y, ldy, type);
+    const dim3 grid((unsigned)T, (unsigned)((N + kThreads * 8 - 1) / (kThreads * 8)));
+    APB_BY_TYPE_AND_ALIGNMENT(k_moe_combine, grid, Z, ldz, slot_row, weight, T, k, N, Y, ldy);
+    APB_HIP(hipGetLastError());
+    return APB_OK;
+}
+
+int apb_moe_combine_backward(const void* dY, int type, long long lddy, const void* Z, long long ldz, const int32_t* slot_row,
+                             const float* weight, int T, int k, int N, void* dZ, long long lddz, float* dweight,
+                             void* stream) {
+    if (!dY || (!Z && dweight) || !slot_row || !dZ) return APB_ERR_NULL;
+    if (bad_type(type)) return APB_ERR_TYPE;
+    if (T <= 0 || k <= 0 || k > APB_MOE_MAX_K || N <= 0 || N > kMxMaxK || (long long)T * k >= kMaxSlots || (Z && ldz < N) || lddy < N || lddz < N)
+        return APB_ERR_SHAPE;
+    if (!aligned(dY, type_size(type)) || !aligned(Z, type_size(type)) || !aligned(dZ, type_size(type)) || !aligned(slot_row, 4) ||
+        !aligned(weight, 4) || !aligned(dweight, 4))
+        return APB_ERR_ALIGN;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const bool vec = rows_aligned16(dY, lddy, type) && rows_aligned16(dZ, lddz, type) && (!dweight || rows_aligned16(Z, ldz, type));
+    const int slots = T * k, per = kThreads / kWave;
+    const dim3 grid((unsigned)((slots + per - 1) / per));
+    APB_BY_TYPE_AND_ALIGNMENT(k_moe_combine_backward, grid, dY, lddy, Z, ldz, slot_row, weight, slots, FastDiv((uint32_t)k), N, dZ, lddz,
+                              dweight);
+    APB_HIP(hipGetLastError());
+    return APB_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,225 @@
+// What the kernels of the microscaled 4-bit matrices share: the layout, element types, groups of rows.
+#pragma once
+
+#include <algorithm>
+
+#include "apb_internal.h"
+
+namespace apb {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kMxBlock = 32;                  // values that share a scale
+constexpr int kMxSeg = 256;                   // a row is padded to whole segments of 256 values: one 128-byte line of
+                                              // codes, 8 scale bytes
+constexpr int kMxSegBytes = kMxSeg / 2;
+
+// A 4-bit matrix in memory (the layout of apb.h).
+struct Mx {
+    const uint8_t* codes;                     // [rows][segs * 128]
+    const uint8_t* scales;                    // [segs][rows][8]
+    int rows, segs;
+};
+
+inline int mx_segs(int K) { return (int)(((long long)K + kMxSeg - 1) / kMxSeg); }
+constexpr int kMxMaxK = 1 << 22;
+// rows * segs < 2^27 (34 G values): eight segments to a workgroup of 256 lanes, the lanes of a launch fit 32 bits
+inline bool bad_shape_mx(long long rows, int K) {
+    return rows <= 0 || K <= 0 || K > kMxMaxK || rows * mx_segs(K) >= (1LL << 27);
+}
+inline Mx mx_view(const void* p, int rows, int K) {
+    const int segs = mx_segs(K);
+    const uint8_t* b = static_cast<const uint8_t*>(p);
+    return Mx{b, b + (size_t)rows * segs * kMxSegBytes, rows, segs};
+}
+
+// The sizes of a product and of its gradients: M rows in E groups (offsets) against E matrices of N rows.
+inline bool bad_product(int E, int M, int N, int K, const int32_t* offsets) {
+    return E <= 0 || E > APB_MOE_MAX_E || N <= 0 || (!offsets && E != 1) || bad_shape_mx(M, K) ||
+           bad_shape_mx((long long)E * N, K) || (N + 127) / 128 > 65535;
+}
+
+inline bool bad_type(int t) { return t != APB_F32 && t != APB_BF16 && t != APB_F16; }
+inline int type_size(int t) { return t == APB_F32 ? 4 : 2; }
+inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+// Rows that start at 16-byte boundaries: element pointer and row stride.
+inline bool rows_aligned16(const void* p, long long ld, int type) {
+    return aligned(p, 16) && (ld * type_size(type)) % 16 == 0;
+}
+
+// n / d for any 32-bit n without a division: m = ceil(2^(32+s) / d) with 2^s >= d is less than 1 above 2^(32+s) / d, so n * m
+// is less than 2^(32+s) / d above n * 2^(32+s) / d: too little to reach the next whole quotient.
+struct FastDiv {
+    uint32_t mul, shift, d;
+    __host__ explicit FastDiv(uint32_t div) : d(div) {
+        uint32_t s = 0;
+        while ((1ull << s) < div) ++s;
+        shift = s;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << s) - div)) / div + 1);       // the multiplier without its bit 32
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (uint32_t)(((uint64_t)__umulhi(n, mul) + n) >> shift); }
+};
+
+// ---- element types ------------------------------------------------------------------------------
+
+__device__ __forceinline__ float load_f32(const void* p, int type, long long i) {
+    if (type == APB_F32) return static_cast<const float*>(p)[i];
+    if (type == APB_BF16) return (float)static_cast<const __bf16*>(p)[i];
+    return (float)static_cast<const _Float16*>(p)[i];
+}
+// one rounding, to nearest even
+__device__ __forceinline__ void store_f32(void* p, int type, long long i, float v) {
+    if (type == APB_F32) static_cast<float*>(p)[i] = v;
+    else if (type == APB_BF16) static_cast<__bf16*>(p)[i] = (__bf16)v;
+    else static_cast<_Float16*>(p)[i] = (_Float16)v;
+}
+__device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
+    if (type == APB_BF16) {
+        const bf16x2 v = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+    const f16x2 v = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+// four neighbours at element i, of which `count` exist; `vec`: i is a multiple of 4 and rows start at 16-byte boundaries
+__device__ __forceinline__ void store4(void* p, int type, long long i, const float (&v)[4], int count, bool vec) {
+    if (vec && count >= 4) {
+        if (type == APB_F32) {
+            *reinterpret_cast<f32x4*>(static_cast<float*>(p) + i) = f32x4{v[0], v[1], v[2], v[3]};
+        } else {
+            *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p) + i) = u32x2{pack2(type, v[0], v[1]), pack2(type, v[2], v[3])};
+        }
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (q < count) store_f32(p, type, i + q, v[q]);
+}
+
+// Eight neighbours of a row as floats; `have` of them exist.
+template <int TYPE, bool VEC>
+__device__ __forceinline__ void load8(const void* X, long long at, int have, float (&v)[8]) {
+    if (VEC && have >= 8) {
+        if (TYPE == APB_F32) {
+            const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
+            const f32x4 a = p[0], b = p[1];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = a[q], v[4 + q] = b[q];
+        } else {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(X) + at);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t pair = w[q];                      // (a bit cast of w[q] itself would take w[0]'s place)
+                if (TYPE == APB_BF16) {
+                    v[2 * q] = __builtin_bit_cast(float, pair << 16);
+                    v[2 * q + 1] = __builtin_bit_cast(float, pair & 0xffff0000u);
+                } else {
+                    const f16x2 h = __builtin_bit_cast(f16x2, pair);
+                    v[2 * q] = (float)h[0];
+                    v[2 * q + 1] = (float)h[1];
+                }
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = q < have ? load_f32(X, TYPE, at + q) : 0.0f;
+}
+template <int TYPE, bool VEC>
+__device__ __forceinline__ void store8(void* X, long long at, int have, const float (&v)[8]) {
+    if (VEC && have >= 8) {
+        if (TYPE == APB_F32) {
+            f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(X) + at);
+            p[0] = f32x4{v[0], v[1], v[2], v[3]};
+            p[1] = f32x4{v[4], v[5], v[6], v[7]};
+        } else {
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(X) + at) =
+                u32x4{pack2(TYPE, v[0], v[1]), pack2(TYPE, v[2], v[3]), pack2(TYPE, v[4], v[5]), pack2(TYPE, v[6], v[7])};
+        }
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < have) store_f32(X, TYPE, at + q, v[q]);
+}
+
+// ---- the scale of a block -------------------------------------------------------------------------
+
+// from the largest magnitude's float bits (sign cleared): e + 127 of the block, 255 if it is not finite.  floor(log2) of a
+// subnormal is below -126, so its e is -127 whatever it is.
+__device__ __forceinline__ uint32_t scale_code(uint32_t top) {
+    const uint32_t ex = top >> 23;
+    return ex >= 255u ? 255u : ex > 2u ? ex - 2u : 0u;
+}
+// 2^-e as a float; e <= 125 and >= -127, so it is a normal number
+__device__ __forceinline__ float scale_inverse(uint32_t code) { return __builtin_bit_cast(float, (254u - code) << 23); }
+// 2^e as a float (2^-127 is subnormal); NaN for 255
+__device__ __forceinline__ float scale_value(uint32_t code) {
+    return __builtin_bit_cast(float, code == 0u ? 0x00400000u : code == 255u ? 0x7fc00000u : code << 23);
+}
+
+// ---- groups of rows ---------------------------------------------------------------------------------
+
+// Where a workgroup's tile of rows lies: rows row0 .. row0 + rows - 1 of group e; e == E: the rows that belong to no expert;
+// rows == 0: no such tile.
+struct RowTile {
+    int e, row0, rows;
+};
+
+// Tiles of `tile` rows that R rows in E groups (and the rows behind them) take at most.
+inline long long max_row_tiles(int R, int E, bool grouped, int tile) {
+    const long long whole = ((long long)R + tile - 1) / tile;
+    return grouped ? whole + std::min<long long>((long long)E + 1, R) : whole;
+}
+
+// The t-th tile of `tile` rows.  Called by whole waves, all lanes with the same t; each lane takes a group, a prefix sum over
+// the lanes counts tiles, 64 groups at a time.
+__device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ offsets, int E, int R, int tile, int t) {
+    if (offsets == nullptr) {
+        const int row0 = t * tile;
+        return RowTile{0, row0, min(tile, R - row0)};
+    }
+    const int lane = threadIdx.x & (kWave - 1);
+    int before = 0;
+    for (int base = 0; base <= E; base += kWave) {
+        const int e = base + lane;
+        int a = 0, b = 0;
+        if (e <= E) {
+            a = min(max(offsets[e], 0), R);
+            b = e < E ? max(a, min(offsets[e + 1], R)) : R;
+        }
+        const int tiles = (b - a + tile - 1) / tile;
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int v = __shfl_up(upto, d, kWave);
+            if (lane >= d) upto += v;
+        }
+        const unsigned long long hit = __ballot(t < before + upto);
+        if (hit) {
+            const int src = __ffsll((long long)hit) - 1;
+            const int first = __shfl(before + upto - tiles, src, kWave);
+            const int ra = __shfl(a, src, kWave), rb = __shfl(b, src, kWave);
+            const int row0 = ra + (t - first) * tile;
+            return RowTile{base + src, row0, min(tile, rb - row0)};
+        }
+        before += __shfl(upto, kWave - 1, kWave);
+    }
+    return RowTile{E, R, 0};
+}
+
+// ---- launchers (one translation unit each) -----------------------------------------------------------
+
+int launch_mx4_quantize(const void* X, int type, long long row_stride, long long col_stride, int rows_in,
+                        const int32_t* rows_from, int rows, int K, void* mx, hipStream_t s);
+int launch_mx4_gemm(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy,
+                    hipStream_t s);
+
+}  // namespace apb

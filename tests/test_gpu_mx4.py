@@ -1,0 +1,368 @@
+"""The microscaled 4-bit matrices through the C ABI against the CPU oracle in float64.
+
+Tolerances, fixed before the first run.  Quantization: none, bytes are compared.  Dequantization: the value rounded once.
+Products and gradients: 4-bit values, their products and the parts of G are exact, so an error is made only where float32 sums
+are rounded.  A sum passes through at most (terms / 16 + 64) additions in a row (matrix instructions chained over at least 16
+terms each, a tree of no more than 64 inside one, joins of partial sums), each within 2^-23 of the sum of the magnitudes of the
+terms, whether it rounds or cuts off; then one rounding to the output's type."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4_oracle as o
+
+pytestmark = pytest.mark.gpu
+
+TYPE = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF_ULP = {t: torch.finfo(d).eps / 2 for t, d in TYPE.items()}
+TINY = {"f32": 2.0 ** -149, "bf16": 2.0 ** -133, "f16": 2.0 ** -24}
+PARTS = {"f32": 3, "bf16": 1, "f16": 2}
+
+
+@pytest.fixture(scope="module")
+def b():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2306_08960_amd import binding
+    binding.load()
+    return binding
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _in(a, t):
+    """float array -> GPU tensor of type t, and the same values in float32."""
+    x = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(TYPE[t])
+    return x.cuda(), x.float().numpy()
+
+
+def _close(got, want, mag, terms, t, parts=1):
+    tol = (parts * terms / 16 + 64) * 2.0 ** -23 * mag + HALF_ULP[t] * 1.001 * (np.abs(want) + 2.0 ** -10 * mag) + TINY[t]
+    err = np.abs(got - want)
+    assert np.isfinite(got).all()
+    worst = np.unravel_index(np.argmax(err - tol), err.shape)
+    assert (err <= tol).all(), (worst, got[worst], want[worst], tol[worst])
+
+
+def _acts(seed, M, K):
+    g = np.random.default_rng(seed)
+    return (g.standard_normal((M, K)) * np.exp(g.standard_normal(K))).astype(np.float32)
+
+
+def _weights(seed, rows, K):
+    return (np.random.default_rng(seed + 7919).standard_normal((rows, K)) * 0.02).astype(np.float32)
+
+
+# ------------------------------------------------------------------------------------------ quantization
+
+def _special(M, K):
+    """Values where rounding and scales go wrong: midway points, saturation, subnormals, zeros, the extremes."""
+    g = np.random.default_rng(M * 10007 + K)
+    x = _acts(M + K, M, K)
+    mids = np.array([0, .25, .5, .75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6, 6.5, 7, 7.99], np.float32)
+    for r in range(0, M, 2):
+        x[r] = g.choice(mids, K) * g.choice([-1, 1], K) * np.float32(2.0) ** int(g.integers(-6, 7))
+    x[1 % M] = 0
+    x[-1, :] *= np.float32(1e-4)
+    return x
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 31), (3, 32), (5, 33), (2, 255), (7, 256), (3, 257), (16, 517), (33, 1024), (9, 4096)])
+def test_quantize_and_back(b, M, K, t):
+    x, v = _in(_special(M, K), t)
+    codes, scales = o.quantize(v)
+    mx = b.apb_mx4_quantize(x)
+    assert np.array_equal(mx.cpu().numpy(), o.pack(codes, scales))
+    want = o.values(codes, scales, K)
+    for back in ("f32", "bf16", "f16"):
+        got = b.apb_mx4_dequantize(mx, M, K, TYPE[back])
+        assert torch.equal(got.cpu(), torch.from_numpy(want).to(TYPE[back]))
+
+
+def test_quantize_extremes(b):
+    x = np.zeros((8, 64), np.float32)
+    x[0, :40] = 3.4028235e38
+    x[1, :4] = 1e-45, -3e-39, 1.1754944e-38, 5e-39
+    x[2, 3], x[2, 40] = np.inf, 1.0
+    x[3, 3], x[3, 40] = np.nan, -1.0
+    x[4, 0], x[4, 1] = -np.inf, 5.0
+    x[5, :2] = 1e30, 1e-30
+    x[6, :] = -0.0
+    codes, scales = o.quantize(x)
+    mx = b.apb_mx4_quantize(torch.from_numpy(x).cuda())
+    assert np.array_equal(mx.cpu().numpy(), o.pack(codes, scales))
+    got = b.apb_mx4_dequantize(mx, 8, 64).cpu().numpy()
+    assert np.array_equal(got, o.values(codes, scales, 64).astype(np.float32), equal_nan=True)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_quantize_strides_and_gather(b, t):
+    M, K = 70, 300
+    x, v = _in(_special(M, K), t)
+    want = o.pack(*o.quantize(v))
+    wide = torch.full((M, K + 5), 99.0, dtype=TYPE[t], device="cuda")
+    wide[:, 3:K + 3] = x
+    every = torch.full((2 * M, 3 * K), 99.0, dtype=TYPE[t], device="cuda")
+    every[::2, ::3] = x
+    for view in (x, wide[:, 3:K + 3], x.t().contiguous().t(), every[::2, ::3]):
+        mx = torch.full((b.apb_mx4_bytes(M, K),), 0xa5, dtype=torch.uint8, device="cuda")
+        assert np.array_equal(b.apb_mx4_quantize(view, mx=mx).cpu().numpy(), want)
+    rows = np.array([5, 5, -1, 69, 0, 70, 2 ** 31 - 1, 3], np.int32)
+    there = (rows >= 0) & (rows < M)
+    picked = np.where(there[:, None], v[np.where(there, rows, 0)], 0).astype(np.float32)
+    for view in (x, x.t().contiguous().t()):
+        mx = b.apb_mx4_quantize(view, rows_from=torch.from_numpy(rows).cuda())
+        assert np.array_equal(mx.cpu().numpy(), o.pack(*o.quantize(picked)))
+
+
+def test_dequantize_into_a_wider_matrix(b):
+    x, v = _in(_special(6, 70), "f32")
+    mx = b.apb_mx4_quantize(x)
+    for pad in (1, 2):                                               # rows that start at odd and at even places
+        out = torch.full((6, 70 + pad), 7.0, device="cuda")
+        b.apb_mx4_dequantize(mx, 6, 70, X=out[:, :70])
+        assert np.array_equal(out[:, :70].cpu().numpy(), o.quantized(v).astype(np.float32)) and (out[:, 70:] == 7.0).all()
+
+
+# ------------------------------------------------------------------------------------------ products
+
+SHAPES = [(1, 1, 1), (1, 33, 40), (2, 64, 256), (3, 100, 300), (15, 129, 512), (16, 200, 513), (17, 48, 1000), (31, 77, 2048),
+          (33, 517, 96), (64, 256, 768), (65, 130, 257), (127, 255, 512), (130, 300, 1024), (257, 259, 600), (1, 1000, 4096),
+          (300, 513, 4200), (520, 528, 300)]
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("t,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32")])
+def test_linear(b, M, N, K, t, out):
+    print(f"[case] mx4 linear {M} {N} {K} {t} {out}", flush=True)
+    x, v = _in(_acts(M + N + K, M, K), t)
+    wf = _weights(N + K, N, K)
+    w4 = b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    want, mag = o.product(o.quantized(v), o.quantized(wf), N)
+    guard = torch.full((M + 2, N + 3), 7.0, dtype=TYPE[out], device="cuda")
+    y = guard[1:M + 1, :N]
+    b.apb_mx4_linear(x, w4, N, Y=y)
+    _close(_np(y), want, mag, K, out)
+    assert (guard[0] == 7).all() and (guard[-1] == 7).all() and (guard[:, N:] == 7).all()
+    y2 = b.apb_mx4_gemm(b.apb_mx4_quantize(x), w4, M, N, K, dtype=TYPE[out])
+    _close(_np(y2), want, mag, K, out)
+    # exchanged operands: the transposed product
+    y3 = b.apb_mx4_gemm(w4, b.apb_mx4_quantize(x), N, M, K, dtype=TYPE[out])
+    _close(_np(y3).T, want, mag, K, out)
+
+
+def _groups(kind, M, E, seed=0):
+    g = np.random.default_rng(seed + M + E)
+    if kind == "even":
+        cut = np.arange(E + 1) * M // E
+    elif kind == "one":                                              # one expert has all rows
+        cut = np.array([0] * (E // 2 + 1) + [M] * (E - E // 2))
+    elif kind == "none":                                             # no row has an expert
+        cut = np.zeros(E + 1)
+    else:                                                            # ragged, some empty, some rows behind the last
+        cut = np.sort(np.concatenate([[0], g.integers(0, M + 1, E)]))
+        cut[E // 2] = cut[E // 2 + 1] if E > 1 else cut[E // 2]
+        cut = np.minimum(np.sort(cut), max(M - 3, 0))
+    return cut.astype(np.int32)
+
+
+GROUPS = [("even", 8, 4, 64, 256), ("ragged", 37, 5, 100, 300), ("ragged", 1, 3, 33, 70), ("one", 40, 6, 96, 512),
+          ("none", 20, 3, 40, 128), ("ragged", 300, 7, 257, 520), ("even", 640, 3, 200, 1024), ("ragged", 200, 130, 48, 256),
+          ("ragged", 70, 1, 130, 300), ("one", 600, 4, 300, 768), ("ragged", 900, 2, 520, 300)]
+
+
+@pytest.mark.parametrize("kind,M,E,N,K", GROUPS)
+@pytest.mark.parametrize("t,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+def test_grouped(b, kind, M, E, N, K, t, out):
+    print(f"[case] mx4 grouped {kind} {M} {E} {N} {K} {t}", flush=True)
+    tokens = M // 2 + 1
+    x, v = _in(_acts(M + N + K, tokens, K), t)
+    rows = np.random.default_rng(M).integers(0, tokens, M).astype(np.int32)
+    off = _groups(kind, M, E)
+    wf = _weights(N + K, E * N, K)
+    w4 = b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    want, mag = o.product(o.quantized(v)[rows], o.quantized(wf), N, off)
+    y = torch.full((M, N), 7.0, dtype=TYPE[out], device="cuda")
+    dev = torch.from_numpy(off).cuda()
+    b.apb_mx4_linear(x, w4, N, Y=y, rows_from=torch.from_numpy(rows).cuda(), offsets=dev)
+    _close(_np(y), want, mag, K, out)
+    assert (_np(y)[off[-1]:] == 0).all()
+    y2 = torch.full((M, N), 7.0, dtype=TYPE[out], device="cuda")
+    b.apb_mx4_gemm(b.apb_mx4_quantize(x, rows_from=torch.from_numpy(rows).cuda()), w4, M, N, K, Y=y2, offsets=dev)
+    _close(_np(y2), want, mag, K, out)
+
+
+@pytest.mark.parametrize("M", [3, 200])
+def test_nan_stays_in_its_row(b, M):
+    x = _acts(5, M, 300)
+    x[1, 290], x[2, 0] = np.nan, np.inf
+    w4 = b.apb_mx4_quantize(torch.from_numpy(_weights(5, 70, 300)).cuda())
+    for y in (b.apb_mx4_linear(torch.from_numpy(x).cuda(), w4, 70),
+              b.apb_mx4_gemm(b.apb_mx4_quantize(torch.from_numpy(x).cuda()), w4, M, 70, 300)):
+        assert torch.isnan(y[1]).all() and torch.isnan(y[2]).all()
+        assert torch.isfinite(y[0]).all() and torch.isfinite(y[3:]).all()
+
+
+def test_offsets_that_make_no_sense_stay_in_bounds(b):
+    M, E, N, K = 50, 4, 40, 300
+    x = torch.from_numpy(_acts(1, M, K)).cuda()
+    w4 = b.apb_mx4_quantize(torch.from_numpy(_weights(1, E * N, K)).cuda())
+    x4 = b.apb_mx4_quantize(x)
+    g = torch.randn(M, N, device="cuda")
+    for bad in ([0, 60, 10, 2 ** 31 - 1, 50], [-5, -1, 40, 20, 90], [50, 40, 30, 20, 10]):
+        off = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        guard = torch.full((M + 2, N), 7.0, device="cuda")
+        b.apb_mx4_linear(x, w4, N, Y=guard[1:-1], offsets=off)
+        b.apb_mx4_gemm(x4, w4, M, N, K, Y=guard[1:-1], offsets=off)
+        assert (guard[0] == 7).all() and (guard[-1] == 7).all()
+        b.apb_mx4_backward_input(g, w4, K, offsets=off)
+        b.apb_mx4_backward_weight(g, x4, K, offsets=off)
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------ gradients
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 33, 40), (3, 100, 300), (17, 64, 256), (64, 130, 513), (130, 70, 257),
+                                   (200, 300, 520), (333, 257, 130), (520, 300, 300)])
+@pytest.mark.parametrize("t,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32")])
+def test_gradients(b, M, N, K, t, out):
+    print(f"[case] mx4 gradients {M} {N} {K} {t} {out}", flush=True)
+    xf, wf = _acts(M + K, M, K), _weights(N + K, N, K)
+    g, gv = _in(np.random.default_rng(M * N).standard_normal((M, N)) * 1e-2, t)
+    x4, w4 = b.apb_mx4_quantize(torch.from_numpy(xf).cuda()), b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    dx, dw, mx, mw = o.gradients(gv, o.quantized(xf), o.quantized(wf))
+    gx, gw = torch.full((M, K + 2), 7.0, dtype=TYPE[out], device="cuda"), torch.full((N, K + 2), 7.0, dtype=TYPE[out], device="cuda")
+    b.apb_mx4_backward_input(g, w4, K, dX=gx[:, :K])
+    b.apb_mx4_backward_weight(g, x4, K, dW=gw[:, :K])
+    _close(_np(gx[:, :K]), dx, mx, N, out, PARTS[t])
+    _close(_np(gw[:, :K]), dw, mw, M, out, PARTS[t])
+    assert (gx[:, K:] == 7).all() and (gw[:, K:] == 7).all()
+    # a gradient whose rows do not start at 16-byte boundaries
+    odd = torch.zeros((M, N + 3), dtype=TYPE[t], device="cuda")
+    odd[:, 1:N + 1] = g
+    _close(_np(b.apb_mx4_backward_input(odd[:, 1:N + 1], w4, K, dtype=TYPE[out])), dx, mx, N, out, PARTS[t])
+    _close(_np(b.apb_mx4_backward_weight(odd[:, 1:N + 1], x4, K, dtype=TYPE[out])), dw, mw, M, out, PARTS[t])
+
+
+@pytest.mark.parametrize("kind,M,E,N,K", GROUPS)
+@pytest.mark.parametrize("t,out", [("f32", "f32"), ("bf16", "bf16")])
+def test_grouped_gradients(b, kind, M, E, N, K, t, out):
+    print(f"[case] mx4 grouped gradients {kind} {M} {E} {N} {K} {t}", flush=True)
+    xf, wf, off = _acts(M + K, M, K), _weights(N + K, E * N, K), _groups(kind, M, E)
+    g, gv = _in(np.random.default_rng(M * N).standard_normal((M, N)) * 1e-2, t)
+    x4, w4 = b.apb_mx4_quantize(torch.from_numpy(xf).cuda()), b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    dx, dw, mx, mw = o.gradients(gv, o.quantized(xf), o.quantized(wf), off)
+    dev = torch.from_numpy(off).cuda()
+    gx, gw = torch.full((M, K), 7.0, dtype=TYPE[out], device="cuda"), torch.full((E * N, K), 7.0, device="cuda")
+    b.apb_mx4_backward_input(g, w4, K, dX=gx, offsets=dev)
+    b.apb_mx4_backward_weight(g, x4, K, dW=gw, offsets=dev)
+    _close(_np(gx), dx, mx, N, out, PARTS[t])
+    _close(_np(gw), dw, mw, M, "f32", PARTS[t])
+
+
+def test_gradients_by_differences(b):
+    """The product is linear in either operand: <G, Y(X, W1) - Y(X, W2)> = <dW, W1^ - W2^>, and the same for X."""
+    M, N, K = 96, 80, 320
+    x1, x2, w1, w2 = (torch.from_numpy(a).cuda() for a in (_acts(1, M, K), _acts(2, M, K), _weights(1, N, K), _weights(2, N, K)))
+    g = torch.randn(M, N, device="cuda")
+    q = {n: b.apb_mx4_quantize(v) for n, v in (("x1", x1), ("x2", x2), ("w1", w1), ("w2", w2))}
+    y = lambda x, w: b.apb_mx4_gemm(q[x], q[w], M, N, K).double()
+    val = lambda n, rows: b.apb_mx4_dequantize(q[n], rows, K).double()
+    left = ((y("x1", "w1") - y("x1", "w2")) * g.double()).sum().item()
+    term = b.apb_mx4_backward_weight(g, q["x1"], K).double() * (val("w1", N) - val("w2", N))
+    # either side: the errors of its float32 sums, (terms / 16 + 64) * 2^-23 of magnitudes that Cauchy-Schwarz bounds
+    scale = g.double().norm().item() * val("x1", M).norm().item() * (val("w1", N).norm() + val("w2", N).norm()).item()
+    assert abs(left - term.sum().item()) <= 2 * (3 * K / 16 + 64) * 2.0 ** -23 * scale
+    left = ((y("x1", "w1") - y("x2", "w1")) * g.double()).sum().item()
+    term = b.apb_mx4_backward_input(g, q["w1"], K).double() * (val("x1", M) - val("x2", M))
+    scale = g.double().norm().item() * val("w1", N).norm().item() * (val("x1", M).norm() + val("x2", M).norm()).item()
+    assert abs(left - term.sum().item()) <= 2 * (3 * K / 16 + 64) * 2.0 ** -23 * scale
+
+
+@pytest.mark.parametrize("t", ["f32", "f16"])
+def test_every_bit_of_the_gradient_counts(b, t):
+    """G times a matrix that holds one 1 per row is G itself, to the last bit of its type."""
+    N = 64
+    w = torch.zeros(N, N)
+    w[torch.arange(N), torch.arange(N)] = 1.0
+    w4 = b.apb_mx4_quantize(w.cuda())
+    g = (torch.randn(40, N) * torch.exp(torch.randn(40, 1) * (3 if t == "f16" else 20))).to(TYPE[t])
+    got = b.apb_mx4_backward_input(g.cuda(), w4, N, dtype=torch.float32)
+    assert torch.equal(got.cpu(), g.float())
+
+
+def test_gradient_infinities_and_nan(b):
+    for t in ("f32", "bf16", "f16"):
+        g = torch.ones(40, 64, dtype=TYPE[t])
+        g[3, 5], g[4, 6] = float("inf"), float("nan")
+        w = torch.ones(64, 64)
+        dx = b.apb_mx4_backward_input(g.cuda(), b.apb_mx4_quantize(w.cuda()), 64, dtype=torch.float32).cpu()
+        assert (dx[3] == float("inf")).all() and torch.isnan(dx[4]).all()
+        assert torch.isfinite(dx[:3]).all() and torch.isfinite(dx[5:]).all()
+
+
+# ------------------------------------------------------------------------------------------ streams, graphs, repeats
+
+def test_same_bits_again_on_another_stream_and_in_a_graph(b):
+    M, E, N, K = 70, 5, 130, 520
+    x = torch.from_numpy(_acts(9, M, K)).cuda().bfloat16()
+    w4 = b.apb_mx4_quantize(torch.from_numpy(_weights(9, E * N, K)).cuda())
+    off = torch.from_numpy(_groups("ragged", M, E)).cuda()
+    g = torch.randn(M, N, device="cuda").bfloat16()
+    x4, scratch = b.alloc_mx4(M, K), b.alloc_mx4(M, K)
+    y, dx, dw = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda"), torch.empty(E * N, K, device="cuda")
+
+    def step(stream=None):
+        b.apb_mx4_quantize(x, mx=x4, stream=stream)
+        b.apb_mx4_linear(x, w4, N, Y=y, offsets=off, scratch=scratch, stream=stream)
+        b.apb_mx4_backward_input(g, w4, K, dX=dx, offsets=off, stream=stream)
+        b.apb_mx4_backward_weight(g, x4, K, dW=dw, offsets=off, stream=stream)
+
+    def wipe():
+        for t in (y, dx, dw):
+            t.fill_(7.0)
+        x4.fill_(3)
+
+    step()
+    first = [t.clone() for t in (x4, y, dx, dw)]
+    same = lambda: all(torch.equal(a, c) for a, c in zip(first, (x4, y, dx, dw)))
+    side = torch.cuda.Stream()
+    wipe()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    assert same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        wipe()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same()
+        (torch.ones(1000, device="cuda") * 2).sum().item()           # eager work in between
+
+
+def test_binding_refusals(b):
+    x, w4 = torch.zeros(4, 64, device="cuda"), b.alloc_mx4(8, 64)
+    with pytest.raises(ValueError):
+        b.apb_mx4_linear(x, w4, 9)                                    # weights too small
+    with pytest.raises(ValueError):
+        b.apb_mx4_linear(x, w4, 8, Y=torch.zeros(4, 9, device="cuda"))
+    with pytest.raises(TypeError):
+        b.apb_mx4_quantize(torch.zeros(4, 64))                        # not on the GPU
+    with pytest.raises(TypeError):
+        b.apb_mx4_quantize(x.double())
+    with pytest.raises(TypeError):
+        b.apb_mx4_linear(x.t(), w4, 8)                                # rows not contiguous
+    with pytest.raises(TypeError):
+        b.apb_mx4_linear(x, w4, 8, offsets=torch.zeros(2, device="cuda"))
+    with pytest.raises(b.ApbError) as e:
+        b.alloc_mx4(0, 64)
+    assert e.value.code == b.APB_ERR_SHAPE
+    with pytest.raises(b.ApbError) as e:
+        b.apb_mx4_quantize(x, mx=torch.empty(10000, dtype=torch.uint8, device="cuda")[1:])
+    assert e.value.code == b.APB_ERR_ALIGN

@@ -1,0 +1,117 @@
+"""The 4-bit products and the routing without a GPU: the oracle's definitions at values worked out by hand, and the
+library's checks of arguments, each of which answers before anything is launched."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+from oracle import mx4_oracle as o
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2306_08960_amd", "libapb.so")
+built = pytest.mark.skipif(not os.path.exists(LIB), reason="libapb.so not built (run __graft_entry__.build())")
+
+
+def test_levels_ties_and_saturation():
+    # the largest is 7: scale 2^0, and 7 itself goes to 6; midway values go to the even index
+    x = np.array([[7, .25, .26, .75, .74, 1.25, 1.75, 2.5, 2.51, 3.5, 3.49, 5, 5.01, -.25, -.75, -5, 6.5, 0]], np.float32)
+    want = [6, 0, .5, 1, .5, 1, 2, 2, 3, 4, 3, 4, 6, -0., -1, -4, 6, 0]
+    assert o.quantized(x)[0].tolist() == want
+
+
+def test_scales():
+    x = np.zeros((7, 32), np.float32)
+    x[0, 3], x[1, 0], x[2, 0], x[3, 0], x[4, 5], x[5, 31] = 4.0, 3.999, np.float32(3.4e38), 1e-45, np.inf, np.nan
+    codes, scales = o.quantize(x)
+    assert scales[:, 0].tolist() == [127, 126, 252, 0, 255, 255, 0]
+    assert o.values(codes, scales, 32)[3, 0] == 0.0 and np.isnan(o.values(codes, scales, 32)[4]).all()
+    assert (scales[:, 1:] == 0).all() and (codes[:, 32:] == 0).all()
+
+
+def test_gradients_by_differences():
+    g = np.random.default_rng(3)
+    x, w, d = g.standard_normal((5, 40)), g.standard_normal((14, 40)), g.standard_normal((5, 7))
+    off, h = [0, 3, 4], 1e-6
+    dx, dw, _, _ = o.gradients(d, x, w, off)
+    loss = lambda x, w: float((o.product(x, w, 7, off)[0] * d).sum())
+    for a, grad, f in ((x, dx, lambda a: loss(a, w)), (w, dw, lambda a: loss(x, a))):
+        for i in ((0, 0), (2, 39), (3, 5), (4, 1)):
+            hi, lo = a.copy(), a.copy()
+            hi[i] += h
+            lo[i] -= h
+            assert abs((f(hi) - f(lo)) / (2 * h) - grad[i]) < 1e-7
+    assert (dx[4] == 0).all()                                         # behind the last group
+
+
+def test_route_and_its_gradient_by_differences():
+    g = np.random.default_rng(4)
+    z = g.standard_normal((6, 9))
+    z[1] = -np.inf
+    z[2, :8] = np.nan
+    z[3, 2] = z[3, 5] = 9.0
+    r = o.route(z, 3)
+    assert r["expert"][1].tolist() == [-1, -1, -1] and r["expert"][2].tolist() == [8, -1, -1]
+    assert r["expert"][3, :2].tolist() == [2, 5] and r["offsets"][-1] == 6 * 3 - 5
+    assert sorted(r["slot_row"].reshape(-1)) == list(range(18))
+    d = g.standard_normal((6, 3))
+    grad = o.route_backward(r["expert"], r["weight"], d, 9)
+    for i in ((0, int(r["expert"][0, 1])), (2, 8), (4, int(r["expert"][4, 0])), (5, int(np.argmin(z[5])))):
+        hi, lo = z.copy(), z.copy()
+        hi[i] += 1e-6
+        lo[i] -= 1e-6
+        diff = ((o.route(hi, 3)["weight"] - o.route(lo, 3)["weight"]) * d).sum() / 2e-6
+        assert abs(diff - grad[i]) < 1e-8
+
+
+@pytest.fixture()
+def b():
+    from paper_2306_08960_amd import binding
+    binding.load()
+    return binding
+
+
+@built
+def test_sizes(b):
+    assert b.apb_mx4_bytes(1, 1) == 128 + 8 and b.apb_mx4_bytes(3, 257) == 3 * 2 * 136
+    for bad in ((0, 4), (4, 0), (-1, 4), (4, (1 << 22) + 1), (1 << 27, 1)):
+        assert b.apb_mx4_bytes(*bad) == 0
+    assert b.apb_moe_workspace_bytes(1, 4, 2) > 0
+    for bad in ((0, 4, 2), (4, 0, 1), (4, 4, 0), (4, 4, 5), (4, 1025, 2), (4, 64, 33), (1 << 24, 4, 1)):
+        assert b.apb_moe_workspace_bytes(*bad) == 0
+
+
+@built
+def test_refusals(b):
+    lib, p, odd = b.load(), ctypes.c_void_p(4096), ctypes.c_void_p(4098)     # never dereferenced
+    S, N, T, A = b.APB_ERR_SHAPE, b.APB_ERR_NULL, b.APB_ERR_TYPE, b.APB_ERR_ALIGN
+    q = lambda X=p, t=0, rs=8, cs=1, ri=4, f=None, r=4, K=8, mx=p: lib.apb_mx4_quantize(X, t, rs, cs, ri, f, r, K, mx, None)
+    assert [q(X=None), q(mx=None), q(t=3), q(t=-1), q(r=0), q(K=0), q(ri=0, f=p), q(ri=5), q(K=(1 << 22) + 1), q(mx=odd),
+            q(X=odd), q(f=odd)] == [N, N, T, T, S, S, S, S, S, A, A, A]
+    d = lambda mx=p, r=4, K=8, t=0, X=p, ld=8: lib.apb_mx4_dequantize(mx, r, K, t, X, ld, None)
+    assert [d(mx=None), d(X=None), d(r=0), d(K=-1), d(t=9), d(ld=7), d(mx=odd), d(X=odd)] == [N, N, S, S, T, S, A, A]
+    g = lambda a=p, b_=p, off=None, E=1, M=4, n=4, K=8, t=0, Y=p, ld=4: lib.apb_mx4_gemm(a, b_, off, E, M, n, K, t, Y, ld, None)
+    assert [g(a=None), g(b_=None), g(Y=None), g(E=2), g(E=0, off=p), g(E=1025, off=p), g(M=0), g(n=0), g(K=0), g(t=3), g(ld=3),
+            g(a=odd), g(b_=odd), g(Y=odd), g(off=odd)] == [N, N, N, S, S, S, S, S, S, T, S, A, A, A, A]
+    l = lambda X=p, xt=0, ldx=8, ri=4, f=None, W=p, off=None, E=1, M=4, n=4, K=8, sc=p, yt=0, Y=p, ld=4: lib.apb_mx4_linear(
+        X, xt, ldx, ri, f, W, off, E, M, n, K, sc, yt, Y, ld, None)
+    assert [l(X=None), l(W=None), l(sc=None), l(Y=None), l(xt=3), l(yt=3), l(ldx=7), l(ri=3), l(ri=0, f=p), l(E=3), l(M=0),
+            l(ld=2), l(X=odd), l(W=odd), l(sc=odd), l(f=odd)] == [N, N, N, N, T, T, S, S, S, S, S, S, A, A, A, A]
+    for call in (lib.apb_mx4_backward_input, lib.apb_mx4_backward_weight):
+        w = lambda G=p, gt=0, ldg=4, Q=p, off=None, E=1, M=4, n=4, K=8, t=0, out=p, ld=8: call(G, gt, ldg, Q, off, E, M, n, K, t, out, ld, None)
+        assert [w(G=None), w(Q=None), w(out=None), w(gt=3), w(t=3), w(ldg=3), w(ld=7), w(E=2), w(M=0), w(n=-1), w(K=0), w(G=odd),
+                w(Q=odd), w(out=odd)] == [N, N, N, T, T, S, S, S, S, S, S, A, A, A]
+    r = lambda x=p, t=0, ld=8, T_=4, E=8, k=2, e=p, ws=p: lib.apb_moe_route(x, t, ld, T_, E, k, e, p, p, p, p, ws, None)
+    assert [r(x=None), r(e=None), r(ws=None), r(t=5), r(ld=7), r(T_=0), r(E=0), r(k=0), r(k=9), r(E=2000, ld=2000), r(x=odd),
+            r(ws=odd)] == [N, N, N, T, S, S, S, S, S, S, A, A]
+    rb = lambda e=p, T_=4, E=8, k=2, t=0, out=p, ld=8: lib.apb_moe_route_backward(e, p, p, T_, E, k, t, out, ld, None)
+    assert [rb(e=None), rb(out=None), rb(T_=0), rb(k=9), rb(t=7), rb(ld=7), rb(e=odd)] == [N, N, S, S, T, S, A]
+    c = lambda Z=p, t=0, ldz=8, s=p, w=None, T_=4, k=2, n=8, Y=p, ld=8: lib.apb_moe_combine(Z, t, ldz, s, w, T_, k, n, Y, ld, None)
+    assert [c(Z=None), c(s=None), c(Y=None), c(t=3), c(ldz=7), c(ld=7), c(T_=0), c(k=33), c(n=0), c(Z=odd), c(w=odd)] == \
+        [N, N, N, T, S, S, S, S, S, A, A]
+    cb = lambda dY=p, t=0, ldy=8, Z=p, ldz=8, s=p, T_=4, k=2, n=8, dZ=p, ldd=8, dw=p: lib.apb_moe_combine_backward(
+        dY, t, ldy, Z, ldz, s, None, T_, k, n, dZ, ldd, dw, None)
+    assert [cb(dY=None), cb(Z=None), cb(s=None), cb(dZ=None), cb(t=3), cb(ldy=7), cb(ldz=7), cb(ldd=7), cb(k=0), cb(dZ=odd),
+            cb(dw=odd)] == [N, N, N, N, T, S, S, S, S, A, A]
+    for code in (b.APB_ERR_TYPE, b.APB_ERR_ALIGN):
+        assert "unknown" not in b.strerror(code)
