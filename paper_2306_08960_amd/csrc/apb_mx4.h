@@ -204,13 +204,13 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ off
         }
         const unsigned long long hit = __ballot(t < before + upto);
         if (hit) {
-            const int src = __ffsll((long long)hit) - 1;
-            const int first = __shfl(before + upto - tiles, src, kWave);
-            const int ra = __shfl(a, src, kWave), rb = __shfl(b, src, kWave);
+            const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
+            const int first = __builtin_amdgcn_readlane(before + upto - tiles, src);     // (scalars: what follows is uniform)
+            const int ra = __builtin_amdgcn_readlane(a, src), rb = __builtin_amdgcn_readlane(b, src);
             const int row0 = ra + (t - first) * tile;
             return RowTile{base + src, row0, min(tile, rb - row0)};
         }
-        before += __shfl(upto, kWave - 1, kWave);
+        before += __builtin_amdgcn_readlane(upto, kWave - 1);
     }
     return RowTile{E, R, 0};
 }
