@@ -330,7 +330,7 @@ int apb_train_backward(const float* W, const float* G, long long n, float alpha,
  * that are not ascending or leave 0 .. M give unspecified results, never an access out of bounds.
  *
  * Element types of the float matrices: apb_type.  Row strides (ld...) count elements and may be any number
- * >= the row length; any alignment that suits the elements is taken, 16-byte alignment is faster.
+ * >= the row length; any alignment that suits the elements is taken.
  * Sums are float32.  Everything only enqueues on `stream`, allocates nothing and records no memset. */
 enum apb_type { APB_F32 = 0, APB_BF16 = 1, APB_F16 = 2 };
 

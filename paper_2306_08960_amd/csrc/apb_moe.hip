@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_route_backward(const int32_t* 
 }
 
 // A lane makes eight neighbours of a row of Y.  grid.x: tokens, grid.y: pieces of 2048 columns.
-template <int TYPE, bool VEC>
+template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_moe_combine(const void* __restrict__ Z, long long ldz,
                                                           const int32_t* __restrict__ slot_row,
                                                           const float* __restrict__ weight, int T, int k, int N,
@@ -258,15 +258,15 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine(const void* __restrict
         const float w = weight ? weight[t * k + j] : 1.0f;
         if (w == 0.0f || row < 0 || row >= T * k) continue;
         float v[8];
-        load8<TYPE, VEC>(Z, (long long)row * ldz + n, N - n, v);
+        load8<TYPE>(Z, (long long)row * ldz + n, N - n, v);
 #pragma unroll
         for (int q = 0; q < 8; ++q) acc[q] = fmaf(w, v[q], acc[q]);
     }
-    store8<TYPE, VEC>(Y, (long long)t * ldy + n, N - n, acc);
+    store8<TYPE>(Y, (long long)t * ldy + n, N - n, acc);
 }
 
 // One wave per slot: its row of dZ and its dweight.
-template <int TYPE, bool VEC>
+template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* __restrict__ dY, long long lddy,
                                                                    const void* __restrict__ Z, long long ldz,
                                                                    const int32_t* __restrict__ slot_row,
@@ -283,15 +283,15 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* _
     if (there) {
         for (int n = lane * 8; n < N; n += kWave * 8) {
             float g[8], z[8], d[8];
-            load8<TYPE, VEC>(dY, (long long)t * lddy + n, N - n, g);
+            load8<TYPE>(dY, (long long)t * lddy + n, N - n, g);
             if (dweight) {
-                load8<TYPE, VEC>(Z, (long long)row * ldz + n, N - n, z);
+                load8<TYPE>(Z, (long long)row * ldz + n, N - n, z);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) dot = fmaf(g[q], z[q], dot);
             }
 #pragma unroll
             for (int q = 0; q < 8; ++q) d[q] = w == 0.0f ? 0.0f : w * g[q];
-            store8<TYPE, VEC>(dZ, (long long)row * lddz + n, N - n, d);
+            store8<TYPE>(dZ, (long long)row * lddz + n, N - n, d);
         }
     }
     if (dweight) {
@@ -365,14 +365,11 @@ int apb_moe_route_backward(const int32_t* expert, const float* weight, const flo
     return APB_OK;
 }
 
-#define APB_BY_TYPE_AND_ALIGNMENT(kernel, grid, ...)                                                                            \
-    do {                                                                                                                        \
-        if (type == APB_F32 && vec) hipLaunchKernelGGL((kernel<APB_F32, true>), grid, dim3(kThreads), 0, s, __VA_ARGS__);       \
-        else if (type == APB_F32) hipLaunchKernelGGL((kernel<APB_F32, false>), grid, dim3(kThreads), 0, s, __VA_ARGS__);        \
-        else if (type == APB_BF16 && vec) hipLaunchKernelGGL((kernel<APB_BF16, true>), grid, dim3(kThreads), 0, s, __VA_ARGS__); \
-        else if (type == APB_BF16) hipLaunchKernelGGL((kernel<APB_BF16, false>), grid, dim3(kThreads), 0, s, __VA_ARGS__);      \
-        else if (vec) hipLaunchKernelGGL((kernel<APB_F16, true>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                     \
-        else hipLaunchKernelGGL((kernel<APB_F16, false>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                             \
+#define APB_BY_TYPE(kernel, grid, ...)                                                                         \
+    do {                                                                                                       \
+        if (type == APB_F32) hipLaunchKernelGGL((kernel<APB_F32>), grid, dim3(kThreads), 0, s, __VA_ARGS__);   \
+        else if (type == APB_BF16) hipLaunchKernelGGL((kernel<APB_BF16>), grid, dim3(kThreads), 0, s, __VA_ARGS__); \
+        else hipLaunchKernelGGL((kernel<APB_F16>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                   \
     } while (0)
 
 int apb_moe_combine(const void* Z, int type, long long ldz, const int32_t* slot_row, const float* weight, int T, int k,
@@ -382,9 +379,8 @@ int apb_moe_combine(const void* Z, int type, long long ldz, const int32_t* slot_
     if (T <= 0 || k <= 0 || k > APB_MOE_MAX_K || N <= 0 || N > kMxMaxK || (long long)T * k >= kMaxSlots || ldz < N || ldy < N) return APB_ERR_SHAPE;
     if (!aligned(Z, type_size(type)) || !aligned(Y, type_size(type)) || !aligned(slot_row, 4) || !aligned(weight, 4)) return APB_ERR_ALIGN;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const bool vec = rows_aligned16(Z, ldz, type) && rows_aligned16(Y, ldy, type);
     const dim3 grid((unsigned)T, (unsigned)((N + kThreads * 8 - 1) / (kThreads * 8)));
-    APB_BY_TYPE_AND_ALIGNMENT(k_moe_combine, grid, Z, ldz, slot_row, weight, T, k, N, Y, ldy);
+    APB_BY_TYPE(k_moe_combine, grid, Z, ldz, slot_row, weight, T, k, N, Y, ldy);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
@@ -400,10 +396,9 @@ int apb_moe_combine_backward(const void* dY, int type, long long lddy, const voi
         !aligned(weight, 4) || !aligned(dweight, 4))
         return APB_ERR_ALIGN;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const bool vec = rows_aligned16(dY, lddy, type) && rows_aligned16(dZ, lddz, type) && (!dweight || rows_aligned16(Z, ldz, type));
     const int slots = T * k, per = kThreads / kWave;
     const dim3 grid((unsigned)((slots + per - 1) / per));
-    APB_BY_TYPE_AND_ALIGNMENT(k_moe_combine_backward, grid, dY, lddy, Z, ldz, slot_row, weight, slots, FastDiv((uint32_t)k), N, dZ, lddz,
+    APB_BY_TYPE(k_moe_combine_backward, grid, dY, lddy, Z, ldz, slot_row, weight, slots, FastDiv((uint32_t)k), N, dZ, lddz,
                               dweight);
     APB_HIP(hipGetLastError());
     return APB_OK;

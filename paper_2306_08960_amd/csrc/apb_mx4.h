@@ -49,10 +49,6 @@ inline bool bad_product(int E, int M, int N, int K, const int32_t* offsets) {
 inline bool bad_type(int t) { return t != APB_F32 && t != APB_BF16 && t != APB_F16; }
 inline int type_size(int t) { return t == APB_F32 ? 4 : 2; }
 inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-// Rows that start at 16-byte boundaries: element pointer and row stride.
-inline bool rows_aligned16(const void* p, long long ld, int type) {
-    return aligned(p, 16) && (ld * type_size(type)) % 16 == 0;
-}
 
 // n / d for any 32-bit n without a division: m = ceil(2^(32+s) / d) with 2^s >= d is less than 1 above 2^(32+s) / d, so n * m
 // is less than 2^(32+s) / d above n * 2^(32+s) / d: too little to reach the next whole quotient.
@@ -88,14 +84,22 @@ __device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
     const f16x2 v = {(_Float16)a, (_Float16)b};
     return __builtin_bit_cast(uint32_t, v);
 }
-// four neighbours at element i, of which `count` exist; `vec`: i is a multiple of 4 and rows start at 16-byte boundaries
-__device__ __forceinline__ void store4(void* p, int type, long long i, const float (&v)[4], int count, bool vec) {
-    if (vec && count >= 4) {
-        if (type == APB_F32) {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(p) + i) = f32x4{v[0], v[1], v[2], v[3]};
-        } else {
-            *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p) + i) = u32x2{pack2(type, v[0], v[1]), pack2(type, v[2], v[3])};
-        }
+// Vectors at any address: global memory takes them unaligned, so rows of any stride are read and written alike.
+typedef u32x4 u32x4_any __attribute__((aligned(1)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+__device__ __forceinline__ u32x4 load16_any(const void* p) { return *static_cast<const u32x4_any*>(p); }
+__device__ __forceinline__ void store16_any(void* p, const u32x4& v) { *static_cast<u32x4_any*>(p) = v; }
+__device__ __forceinline__ void store8_any(void* p, const u32x2& v) { *static_cast<u32x2_any*>(p) = v; }
+
+__device__ __forceinline__ uint32_t float_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
+
+// four neighbours at element i, of which `count` exist
+__device__ __forceinline__ void store4(void* p, int type, long long i, const float (&v)[4], int count) {
+    if (count >= 4) {
+        if (type == APB_F32)
+            store16_any(static_cast<float*>(p) + i, u32x4{float_bits(v[0]), float_bits(v[1]), float_bits(v[2]), float_bits(v[3])});
+        else
+            store8_any(static_cast<uint16_t*>(p) + i, u32x2{pack2(type, v[0], v[1]), pack2(type, v[2], v[3])});
         return;
     }
 #pragma unroll
@@ -103,28 +107,32 @@ __device__ __forceinline__ void store4(void* p, int type, long long i, const flo
         if (q < count) store_f32(p, type, i + q, v[q]);
 }
 
-// Eight neighbours of a row as floats; `have` of them exist.
-template <int TYPE, bool VEC>
+// eight neighbours of a row, of which `have` exist
+template <int TYPE>
 __device__ __forceinline__ void load8(const void* X, long long at, int have, float (&v)[8]) {
-    if (VEC && have >= 8) {
+    if (have >= 8) {
+        const uint8_t* p = static_cast<const uint8_t*>(X) + at * (TYPE == APB_F32 ? 4 : 2);
+        const u32x4 w = load16_any(p);
         if (TYPE == APB_F32) {
-            const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
-            const f32x4 a = p[0], b = p[1];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = a[q], v[4 + q] = b[q];
-        } else {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(X) + at);
+            const u32x4 x = load16_any(p + 16);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t pair = w[q];                      // (a bit cast of w[q] itself would take w[0]'s place)
-                if (TYPE == APB_BF16) {
-                    v[2 * q] = __builtin_bit_cast(float, pair << 16);
-                    v[2 * q + 1] = __builtin_bit_cast(float, pair & 0xffff0000u);
-                } else {
-                    const f16x2 h = __builtin_bit_cast(f16x2, pair);
-                    v[2 * q] = (float)h[0];
-                    v[2 * q + 1] = (float)h[1];
-                }
+                const uint32_t a = w[q], b = x[q];
+                v[q] = __builtin_bit_cast(float, a);
+                v[4 + q] = __builtin_bit_cast(float, b);
+            }
+            return;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t pair = w[q];                          // (a bit cast of w[q] itself would take w[0]'s place)
+            if (TYPE == APB_BF16) {
+                v[2 * q] = __builtin_bit_cast(float, pair << 16);
+                v[2 * q + 1] = __builtin_bit_cast(float, pair & 0xffff0000u);
+            } else {
+                const f16x2 h = __builtin_bit_cast(f16x2, pair);
+                v[2 * q] = (float)h[0];
+                v[2 * q + 1] = (float)h[1];
             }
         }
         return;
@@ -132,22 +140,16 @@ __device__ __forceinline__ void load8(const void* X, long long at, int have, flo
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] = q < have ? load_f32(X, TYPE, at + q) : 0.0f;
 }
-template <int TYPE, bool VEC>
+template <int TYPE>
 __device__ __forceinline__ void store8(void* X, long long at, int have, const float (&v)[8]) {
-    if (VEC && have >= 8) {
-        if (TYPE == APB_F32) {
-            f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(X) + at);
-            p[0] = f32x4{v[0], v[1], v[2], v[3]};
-            p[1] = f32x4{v[4], v[5], v[6], v[7]};
-        } else {
-            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(X) + at) =
-                u32x4{pack2(TYPE, v[0], v[1]), pack2(TYPE, v[2], v[3]), pack2(TYPE, v[4], v[5]), pack2(TYPE, v[6], v[7])};
-        }
+    if (have >= 8 && TYPE != APB_F32) {
+        store16_any(static_cast<uint16_t*>(X) + at,
+                    u32x4{pack2(TYPE, v[0], v[1]), pack2(TYPE, v[2], v[3]), pack2(TYPE, v[4], v[5]), pack2(TYPE, v[6], v[7])});
         return;
     }
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-        if (q < have) store_f32(X, TYPE, at + q, v[q]);
+    const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+    store4(X, TYPE, at, a, have);
+    store4(X, TYPE, at + 4, b, have - 4);
 }
 
 // ---- the scale of a block -------------------------------------------------------------------------

@@ -47,8 +47,7 @@ __device__ __forceinline__ void tile_of(int id, int tiles_n, int& t, int& n) {
 // scales are one word.  Rows of B go in the first operand: a lane then holds four neighbours of a row of Y.
 template <int F>
 __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx B, const int32_t* __restrict__ offsets, int E, int N,
-                                                                       int tiles_n, int type, void* __restrict__ Y, long long ldy,
-                                                                       bool vec) {
+                                                                       int tiles_n, int type, void* __restrict__ Y, long long ldy) {
     constexpr int kRows = 64 * F;                                // of either operand
     constexpr int kLoads = 2 * kRows / 8 / 4;                    // instructions of a wave that fetch a segment's codes
     constexpr int kScaleLoads = 2 * kRows / 32 / 4;              // ... its scales
@@ -66,7 +65,7 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
         const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int i = threadIdx.x; i < t.rows * (kRows / 4); i += kThreads) {
             const int n = n0 + i % (kRows / 4) * 4;
-            store4(Y, type, (long long)(t.row0 + i / (kRows / 4)) * ldy + n, zero, N - n, vec);
+            store4(Y, type, (long long)(t.row0 + i / (kRows / 4)) * ldy + n, zero, N - n);
         }
         return;
     }
@@ -172,7 +171,7 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
             for (int g = 0; g < 4; ++g) {
                 const int n = n0 + wn + 32 * y + 8 * g + 4 * h;
                 const float v[4] = {acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-                store4(Y, type, row + n, v, N - n, vec);
+                store4(Y, type, row + n, v, N - n);
             }
     }
 }
@@ -182,8 +181,7 @@ void launch_tiles(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M
     const long long tiles_m = (max_row_tiles(M, E, offsets != nullptr, 64 * F) + 3) / 4 * 4;
     const int tiles_n = (N + 64 * F - 1) / (64 * F);
     const unsigned blocks = (unsigned)((tiles_m * tiles_n + 127) / 128 * 128);
-    hipLaunchKernelGGL((k_mx4_gemm<F>), dim3(blocks), dim3(kThreads), 0, s, A, B, offsets, E, N, tiles_n, type, Y, ldy,
-                       rows_aligned16(Y, ldy, type));
+    hipLaunchKernelGGL((k_mx4_gemm<F>), dim3(blocks), dim3(kThreads), 0, s, A, B, offsets, E, N, tiles_n, type, Y, ldy);
 }
 
 }  // namespace

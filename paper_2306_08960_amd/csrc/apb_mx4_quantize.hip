@@ -30,7 +30,7 @@ __device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t code) 
 
 // Rows whose values lie side by side.  32 lanes take a segment of 256 values of a row, eight each; the four lanes of a block
 // exchange their maxima.  `item` counts segments row by row.
-template <int TYPE, bool VEC>
+template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_mx4_quantize(const void* __restrict__ X, long long row_stride, int rows_in,
                                                            const int32_t* __restrict__ rows_from, int rows, int K, int segs,
                                                            FastDiv by_segs, uint8_t* __restrict__ codes,
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantize(const void* __restric
     const int src = rows_from ? rows_from[r] : r;
     const int k = seg * kMxSeg + 8 * l;
     float v[8];
-    load8<TYPE, VEC>(X, (long long)src * row_stride + k, src >= 0 && src < rows_in ? K - k : 0, v);
+    load8<TYPE>(X, (long long)src * row_stride + k, src >= 0 && src < rows_in ? K - k : 0, v);
     uint32_t top = top_bits(v);
     top = max(top, (uint32_t)__shfl_xor((int)top, 1, 32));
     top = max(top, (uint32_t)__shfl_xor((int)top, 2, 32));
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantize_strided(const void* _
 }
 
 __global__ __launch_bounds__(kThreads) void k_mx4_dequantize(Mx mx, int K, FastDiv by_segs, int type, void* __restrict__ X,
-                                                             long long ldx, bool vec) {
+                                                             long long ldx) {
     const uint32_t item = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     const int l = threadIdx.x & 31;
     const int r = (int)by_segs.div(item), seg = (int)(item - (uint32_t)r * mx.segs);
@@ -100,8 +100,8 @@ __global__ __launch_bounds__(kThreads) void k_mx4_dequantize(Mx mx, int K, FastD
         v[q / 2][2 * (q & 1) + 1] = p[1] * scale;
     }
     const long long at = (long long)r * ldx + k;
-    store4(X, type, at, v[0], K - k, vec);
-    store4(X, type, at + 4, v[1], K - k - 4, vec);
+    store4(X, type, at, v[0], K - k);
+    store4(X, type, at + 4, v[1], K - k - 4);
 }
 
 template <int TYPE>
@@ -111,12 +111,8 @@ void quantize_type(const void* X, long long row_stride, long long col_stride, in
     if (col_stride == 1) {
         const unsigned blocks = (unsigned)(((long long)rows * segs + kThreads / 32 - 1) / (kThreads / 32));
         const FastDiv by_segs((uint32_t)segs);
-        if (rows_aligned16(X, row_stride, TYPE))
-            hipLaunchKernelGGL((k_mx4_quantize<TYPE, true>), dim3(blocks), dim3(kThreads), 0, s, X, row_stride, rows_in, rows_from,
-                               rows, K, segs, by_segs, codes, scales);
-        else
-            hipLaunchKernelGGL((k_mx4_quantize<TYPE, false>), dim3(blocks), dim3(kThreads), 0, s, X, row_stride, rows_in, rows_from,
-                               rows, K, segs, by_segs, codes, scales);
+        hipLaunchKernelGGL((k_mx4_quantize<TYPE>), dim3(blocks), dim3(kThreads), 0, s, X, row_stride, rows_in, rows_from, rows, K, segs,
+                           by_segs, codes, scales);
         return;
     }
     const dim3 grid((unsigned)((rows + kWave - 1) / kWave), (unsigned)(segs * 2));
@@ -165,7 +161,7 @@ int apb_mx4_dequantize(const void* mx, int rows, int K, int type, void* X, long 
     const Mx m = mx_view(mx, rows, K);
     const unsigned blocks = (unsigned)(((long long)rows * m.segs + kThreads / 32 - 1) / (kThreads / 32));
     hipLaunchKernelGGL(k_mx4_dequantize, dim3(blocks), dim3(kThreads), 0, reinterpret_cast<hipStream_t>(stream), m, K,
-                       FastDiv((uint32_t)m.segs), type, X, ldx, rows_aligned16(X, ldx, type));
+                       FastDiv((uint32_t)m.segs), type, X, ldx);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
