@@ -148,8 +148,9 @@ def _check(code: int, what: str) -> None:
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return int(s.cuda_stream)
+    if stream is None:                                   # (the handle alone: a Stream object takes 2.6 us to make)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return int(stream.cuda_stream)
 
 
 def _dev_ptr(t: torch.Tensor, dtype: torch.dtype, name: str) -> int:
@@ -607,43 +608,44 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # apb_type
 
 
 def _type(dtype: torch.dtype) -> int:
-    if dtype not in _TYPES:
+    t = _TYPES.get(dtype)
+    if t is None:
         raise TypeError("element type must be float32, bfloat16 or float16")
-    return _TYPES[dtype]
+    return t
 
 
 def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
     """(pointer, apb_type, row stride) of a 2-D float matrix whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda:
+    if not t.is_cuda or t.dim() != 2:
         raise TypeError(f"{name} must be a 2-D tensor on the GPU")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise TypeError(f"the rows of {name} must be contiguous")
-    return t.data_ptr(), _type(t.dtype), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return t.data_ptr(), _type(t.dtype), ld if rows > 1 else max(cols, ld)
 
 
-def _result(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dtype, device, name: str) -> torch.Tensor:
+def _result(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dtype, like: torch.Tensor, name: str):
+    """(tensor, pointer, apb_type, row stride) of an output: `t`, or a new one beside `like`."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        if shape[0] < 0 or shape[1] < 0:
+            raise ApbError(APB_ERR_SHAPE, name)
+        t = like.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr(), _type(dtype), shape[1]
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {list(shape)}")
-    return t
+    return (t, *_matrix(t, name))
 
 
-def _ints(t: Optional[torch.Tensor], count: Optional[int], name: str) -> Optional[int]:
-    """Pointer of an int32 array of `count` entries, None for None."""
+def _array(t: Optional[torch.Tensor], dtype: torch.dtype, count: Optional[int], name: str) -> Optional[int]:
+    """Pointer of a contiguous array of `count` entries, None for None."""
     if t is None:
         return None
     if count is not None and t.numel() != count:
-        raise ValueError(f"{name} must hold {count} int32")
-    return _dev_ptr(t, torch.int32, name)
-
-
-def _floats(t: Optional[torch.Tensor], count: int, name: str) -> Optional[int]:
-    if t is None:
-        return None
-    if t.numel() != count:
-        raise ValueError(f"{name} must hold {count} floats")
-    return _dev_ptr(t, torch.float32, name)
+        raise ValueError(f"{name} must hold {count} entries")
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor on the GPU")
+    return t.data_ptr()
 
 
 def apb_mx4_bytes(rows: int, K: int) -> int:
@@ -660,12 +662,10 @@ def alloc_mx4(rows: int, K: int, device=None) -> torch.Tensor:
 
 
 def _mx4_ptr(mx: torch.Tensor, rows: int, K: int, name: str) -> int:
-    need = apb_mx4_bytes(rows, K)
-    if need == 0:
-        raise ApbError(APB_ERR_SHAPE, "apb_mx4_bytes")
-    if mx.numel() * mx.element_size() < need:
+    # (what apb_mx4_bytes says; the library refuses the sizes it has no answer for)
+    if mx.numel() < rows * ((K + 255) // 256) * 136:
         raise ValueError(f"{name} smaller than apb_mx4_bytes({rows}, {K})")
-    return _dev_ptr(mx, torch.uint8, name)
+    return _array(mx, torch.uint8, None, name)
 
 
 def _experts(offsets: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
@@ -674,7 +674,7 @@ def _experts(offsets: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
         return None, 1
     if offsets.numel() < 2:
         raise ValueError("offsets must hold E + 1 int32")
-    return _ints(offsets, None, "offsets"), offsets.numel() - 1
+    return _array(offsets, torch.int32, None, "offsets"), offsets.numel() - 1
 
 
 def apb_mx4_quantize(X: torch.Tensor, mx: Optional[torch.Tensor] = None, rows_from: Optional[torch.Tensor] = None,
@@ -688,15 +688,14 @@ def apb_mx4_quantize(X: torch.Tensor, mx: Optional[torch.Tensor] = None, rows_fr
     if mx is None:
         mx = alloc_mx4(rows, K, X.device)
     _check(load().apb_mx4_quantize(X.data_ptr(), _type(X.dtype), X.stride(0), 1 if K == 1 else X.stride(1), rows_in,
-                                   _ints(rows_from, rows, "rows_from"), rows, K, _mx4_ptr(mx, rows, K, "mx"), _stream(stream)),
+                                   _array(rows_from, torch.int32, rows, "rows_from"), rows, K, _mx4_ptr(mx, rows, K, "mx"), _stream(stream)),
            "apb_mx4_quantize")
     return mx
 
 
 def apb_mx4_dequantize(mx: torch.Tensor, rows: int, K: int, dtype: torch.dtype = torch.float32,
                        X: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    X = _result(X, (rows, K), dtype, mx.device, "X")
-    ptr, t, ld = _matrix(X, "X")
+    X, ptr, t, ld = _result(X, (rows, K), dtype, mx, "X")
     _check(load().apb_mx4_dequantize(_mx4_ptr(mx, rows, K, "mx"), int(rows), int(K), t, ptr, ld, _stream(stream)),
            "apb_mx4_dequantize")
     return X
@@ -708,8 +707,7 @@ def apb_mx4_gemm(A: torch.Tensor, B: torch.Tensor, M: int, N: int, K: int, dtype
     """Y[M, N] = A^ B^T of two 4-bit matrices; with offsets (int32 [E+1]) the rows of A are grouped by expert and B holds
     E*N rows."""
     off, E = _experts(offsets)
-    Y = _result(Y, (M, N), dtype, A.device, "Y")
-    ptr, t, ld = _matrix(Y, "Y")
+    Y, ptr, t, ld = _result(Y, (M, N), dtype, A, "Y")
     _check(load().apb_mx4_gemm(_mx4_ptr(A, M, K, "A"), _mx4_ptr(B, E * N, K, "B"), off, E, int(M), int(N), int(K), t, ptr, ld,
                                _stream(stream)), "apb_mx4_gemm")
     return Y
@@ -726,9 +724,8 @@ def apb_mx4_linear(X: torch.Tensor, W: torch.Tensor, N: int, dtype: Optional[tor
     off, E = _experts(offsets)
     if scratch is None:
         scratch = alloc_mx4(M, K, X.device)
-    Y = _result(Y, (M, N), dtype or X.dtype, X.device, "Y")
-    yp, yt, ldy = _matrix(Y, "Y")
-    _check(load().apb_mx4_linear(xp, xt, ldx, rows_in, _ints(rows_from, M, "rows_from"), _mx4_ptr(W, E * N, K, "W"), off, E, M,
+    Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y")
+    _check(load().apb_mx4_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), _mx4_ptr(W, E * N, K, "W"), off, E, M,
                                  int(N), K, _mx4_ptr(scratch, M, K, "scratch"), yt, yp, ldy, _stream(stream)), "apb_mx4_linear")
     return Y
 
@@ -740,8 +737,7 @@ def apb_mx4_backward_input(G: torch.Tensor, W: torch.Tensor, K: int, dtype: Opti
     gp, gt, ldg = _matrix(G, "G")
     M, N = G.shape
     off, E = _experts(offsets)
-    dX = _result(dX, (M, K), dtype or G.dtype, G.device, "dX")
-    xp, xt, ldx = _matrix(dX, "dX")
+    dX, xp, xt, ldx = _result(dX, (M, K), dtype or G.dtype, G, "dX")
     _check(load().apb_mx4_backward_input(gp, gt, ldg, _mx4_ptr(W, E * N, K, "W"), off, E, M, N, int(K), xt, xp, ldx, _stream(stream)),
            "apb_mx4_backward_input")
     return dX
@@ -754,8 +750,7 @@ def apb_mx4_backward_weight(G: torch.Tensor, X: torch.Tensor, K: int, dtype: tor
     gp, gt, ldg = _matrix(G, "G")
     M, N = G.shape
     off, E = _experts(offsets)
-    dW = _result(dW, (E * N, K), dtype, G.device, "dW")
-    wp, wt, ldw = _matrix(dW, "dW")
+    dW, wp, wt, ldw = _result(dW, (E * N, K), dtype, G, "dW")
     _check(load().apb_mx4_backward_weight(gp, gt, ldg, _mx4_ptr(X, M, K, "X"), off, E, M, N, int(K), wt, wp, ldw, _stream(stream)),
            "apb_mx4_backward_weight")
     return dW
@@ -781,16 +776,21 @@ def apb_moe_route(logits: torch.Tensor, k: int, workspace: Optional[torch.Tensor
     slot_row int32 [T, k] (see the header)."""
     ptr, t, ld = _matrix(logits, "logits")
     T, E = logits.shape
+    need = apb_moe_workspace_bytes(T, E, k)
+    if need == 0:
+        raise ApbError(APB_ERR_SHAPE, "apb_moe_route")
     if workspace is None:
         workspace = alloc_moe_workspace(T, E, k, logits.device)
-    elif workspace.numel() * workspace.element_size() < apb_moe_workspace_bytes(T, E, k):
+    elif workspace.numel() * workspace.element_size() < need:
         raise ValueError("workspace smaller than apb_moe_workspace_bytes(T, E, k)")
-    new = lambda *shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device=logits.device)
-    out = {"expert": new(T, k), "weight": new(T, k, dtype=torch.float32), "offsets": new(E + 1), "row_token": new(T * k),
-           "slot_row": new(T, k)}
-    _check(load().apb_moe_route(ptr, t, ld, T, E, int(k), *(v.data_ptr() for v in out.values()),
-                                _dev_ptr(workspace, torch.int32, "workspace"), _stream(stream)), "apb_moe_route")
-    return out
+    ints = torch.int32
+    expert, weight = logits.new_empty((T, k), dtype=ints), logits.new_empty((T, k), dtype=torch.float32)
+    offsets, row_token = logits.new_empty(E + 1, dtype=ints), logits.new_empty(T * k, dtype=ints)
+    slot_row = logits.new_empty((T, k), dtype=ints)
+    _check(load().apb_moe_route(ptr, t, ld, T, E, k, expert.data_ptr(), weight.data_ptr(), offsets.data_ptr(),
+                                row_token.data_ptr(), slot_row.data_ptr(), _array(workspace, ints, None, "workspace"),
+                                _stream(stream)), "apb_moe_route")
+    return {"expert": expert, "weight": weight, "offsets": offsets, "row_token": row_token, "slot_row": slot_row}
 
 
 def apb_moe_route_backward(expert: torch.Tensor, weight: torch.Tensor, dweight: torch.Tensor, E: int,
@@ -799,10 +799,9 @@ def apb_moe_route_backward(expert: torch.Tensor, weight: torch.Tensor, dweight: 
     if expert.dim() != 2:
         raise ValueError("expert must be [T, k]")
     T, k = expert.shape
-    dlogits = _result(dlogits, (T, E), dtype, expert.device, "dlogits")
-    ptr, t, ld = _matrix(dlogits, "dlogits")
-    _check(load().apb_moe_route_backward(_ints(expert, T * k, "expert"), _floats(weight, T * k, "weight"),
-                                         _floats(dweight, T * k, "dweight"), T, int(E), k, t, ptr, ld, _stream(stream)),
+    dlogits, ptr, t, ld = _result(dlogits, (T, E), dtype, expert, "dlogits")
+    _check(load().apb_moe_route_backward(_array(expert, torch.int32, T * k, "expert"), _array(weight, torch.float32, T * k, "weight"),
+                                         _array(dweight, torch.float32, T * k, "dweight"), T, int(E), k, t, ptr, ld, _stream(stream)),
            "apb_moe_route_backward")
     return dlogits
 
@@ -822,11 +821,10 @@ def apb_moe_combine(Z: torch.Tensor, slot_row: torch.Tensor, weight: Optional[to
     T, k = _slots(slot_row, Z, "Z")
     zp, zt, ldz = _matrix(Z, "Z")
     N = Z.shape[1]
-    Y = _result(Y, (T, N), Z.dtype, Z.device, "Y")
-    yp, yt, ldy = _matrix(Y, "Y")
+    Y, yp, yt, ldy = _result(Y, (T, N), Z.dtype, Z, "Y")
     if yt != zt:
         raise TypeError("Y must have Z's type")
-    _check(load().apb_moe_combine(zp, zt, ldz, _ints(slot_row, T * k, "slot_row"), _floats(weight, T * k, "weight"), T, k, N, yp,
+    _check(load().apb_moe_combine(zp, zt, ldz, _array(slot_row, torch.int32, T * k, "slot_row"), _array(weight, torch.float32, T * k, "weight"), T, k, N, yp,
                                   ldy, _stream(stream)), "apb_moe_combine")
     return Y
 
@@ -845,13 +843,12 @@ def apb_moe_combine_backward(dY: torch.Tensor, Z: Optional[torch.Tensor], slot_r
         zp, zt, ldz = _matrix(Z, "Z")
         if Z.shape[1] != N or zt != gt:
             raise ValueError("Z must have dY's columns and type")
-        dweight = torch.empty((T, k), dtype=torch.float32, device=dY.device)
-    dZ = _result(dZ, (T * k, N), dY.dtype, dY.device, "dZ")
-    dp, dt, lddz = _matrix(dZ, "dZ")
+        dweight = slot_row.new_empty((T, k), dtype=torch.float32)
+    dZ, dp, dt, lddz = _result(dZ, (T * k, N), dY.dtype, dY, "dZ")
     if dt != gt:
         raise TypeError("dZ must have dY's type")
-    _check(load().apb_moe_combine_backward(gp, gt, ldg, zp, ldz, _ints(slot_row, T * k, "slot_row"),
-                                           _floats(weight, T * k, "weight"), T, k, N, dp, lddz,
+    _check(load().apb_moe_combine_backward(gp, gt, ldg, zp, ldz, _array(slot_row, torch.int32, T * k, "slot_row"),
+                                           _array(weight, torch.float32, T * k, "weight"), T, k, N, dp, lddz,
                                            None if dweight is None else dweight.data_ptr(), _stream(stream)),
            "apb_moe_combine_backward")
     return dZ, dweight

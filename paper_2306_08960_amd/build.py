@@ -21,7 +21,7 @@ LIB = os.path.join(HERE, "libapb.so")
 SOURCES = ["apb_api.hip", "apb_compress.hip", "apb_digits.hip", "apb_quantize.hip", "apb_forward.hip", "apb_sparse.hip", "apb_rows.hip",
            "apb_binary_mfma.hip", "apb_binary_mfma_d1.hip", "apb_binary_mfma_d2.hip", "apb_binary_mfma_22i.hip",
            "apb_binary_mfma_22f.hip", "apb_noalloc.hip", "apb_probe.hip", "apb_train.hip",
-           "apb_mx4_quantize.hip", "apb_mx4_gemm.hip", "apb_mx4_backward.hip", "apb_moe.hip"]
+           "apb_mx4_quantize.hip", "apb_mx4_gemm.hip", "apb_mx4_few.hip", "apb_mx4_backward.hip", "apb_moe.hip"]
 
 # Packed-FP32 VALU forms are disabled on purpose; contraction is off so that every fused
 # multiply-add in the kernels is one written explicitly.

@@ -167,6 +167,56 @@ __device__ __forceinline__ float scale_value(uint32_t code) {
     return __builtin_bit_cast(float, code == 0u ? 0x00400000u : code == 255u ? 0x7fc00000u : code << 23);
 }
 
+__device__ __forceinline__ uint32_t top_bits(const float (&v)[8]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) top = max(top, __builtin_bit_cast(uint32_t, v[q]) & 0x7fffffffu);
+    return top;
+}
+
+// eight values -> eight nibbles
+__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t code) {
+    if (code == 255u) return 0u;
+    const float inv = scale_inverse(code);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * inv, v[1] * inv, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inv, v[3] * inv, 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * inv, v[5] * inv, 1.0f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * inv, v[7] * inv, 1.0f, 3);
+    return w;
+}
+
+// ---- matrix instructions ----------------------------------------------------------------------------
+
+// (the instruction reads the low four words of a 4-bit operand)
+__device__ __forceinline__ i32x8 operand(const u32x4& w) { return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}; }
+
+// Products of 4-bit operands, 32 x 32 x 64 and 16 x 16 x 128; S: which byte of a scale word counts.  Sums within a block of 32 are
+// exact, each block is added with one rounding.
+template <int S>
+__device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, const f32x16& c, int sa, int sb) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, 4, 4, S, sa, S, sb);
+}
+template <int S>
+__device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f32x4& c, int sa, int sb) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a), operand(b), c, 4, 4, S, sa, S, sb);
+}
+
+// ---- loads to LDS --------------------------------------------------------------------------------------
+
+// A load of 16 (4) bytes per lane that goes to LDS, to 16 (4) bytes per lane from `to` on, without passing through registers.  Written
+// out because several segments can be under way: the compiler would wait for all of them before each read of LDS.  Whoever
+// reads what arrived waits for it first (s_waitcnt vmcnt).
+__device__ __forceinline__ void load16_to_lds(uint32_t to, const void* base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base));
+}
+__device__ __forceinline__ void load4_to_lds(uint32_t to, const void* base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base));
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
 // ---- groups of rows ---------------------------------------------------------------------------------
 
 // Where a workgroup's tile of rows lies: rows row0 .. row0 + rows - 1 of group e; e == E: the rows that belong to no expert;
@@ -221,6 +271,11 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ off
 
 int launch_mx4_quantize(const void* X, int type, long long row_stride, long long col_stride, int rows_in,
                         const int32_t* rows_from, int rows, int K, void* mx, hipStream_t s);
+// Few rows: may it run as the one kernel that streams the weights (apb_mx4_few.hip)?
+bool mx4_few_applies(const int32_t* offsets, int E, int M, int K);
+int launch_mx4_few(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const Mx& W, const int32_t* offsets,
+                   int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s);
+int launch_mx4_few(const Mx& A, const Mx& W, const int32_t* offsets, int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s);
 int launch_mx4_gemm(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy,
                     hipStream_t s);
 

@@ -6,29 +6,8 @@ namespace {
 
 constexpr int kThreads = 256;                 // four waves, two by two
 
-// (the instruction reads the low four words of a 4-bit operand)
-__device__ __forceinline__ i32x8 operand(const u32x4& w) { return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}; }
-
-template <int S>
-__device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, const f32x16& c, int sa, int sb) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, 4, 4, S, sa, S, sb);
-}
-
-// A load of 16 (4) bytes per lane that goes to LDS, to 16 (4) bytes per lane from `to` on, without passing through registers.  Written
-// out because several segments can be under way: the compiler would wait for all of them before each read of LDS.  Whoever
-// reads what arrived waits with arrived() first.
-__device__ __forceinline__ void load16_to_lds(uint32_t to, const void* base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base));
-}
-__device__ __forceinline__ void load4_to_lds(uint32_t to, const void* base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base));
-}
 // Every wave's loads are in LDS and every wave's reads of LDS before this point have been answered.
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
-}
-
 // Which tile a workgroup takes: workgroups go to the eight XCDs in turn, and sixteen in a row on one XCD take a block of 4 x 4
 // tiles, which shares its operands in that XCD's cache.
 __device__ __forceinline__ void tile_of(int id, int tiles_n, int& t, int& n) {
@@ -129,7 +108,7 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
 #define APB_MULTIPLY(S, SET)                                                                               \
     __builtin_amdgcn_sched_barrier(0);                                                                     \
     _Pragma("unroll") for (int x = 0; x < F; ++x) _Pragma("unroll") for (int y = 0; y < F; ++y)            \
-        acc[x][y] = mfma<S>(fn[SET][y], fm[SET][x], acc[x][y], vn[y], vm[x]);                              \
+        acc[x][y] = mfma32<S>(fn[SET][y], fm[SET][x], acc[x][y], vn[y], vm[x]);                              \
     __builtin_amdgcn_sched_barrier(0)
     // A segment per pass.  The last step's operands are in registers before the barrier, behind which the segment after next takes
     // this one's place in LDS and the next one's first operands are read, under the last step's products.  (The last segment is
@@ -208,8 +187,10 @@ int apb_mx4_gemm(const void* A, const void* B, const int32_t* offsets, int E, in
     if (bad_type(type)) return APB_ERR_TYPE;
     if (bad_product(E, M, N, K, offsets) || ldy < N) return APB_ERR_SHAPE;
     if (!aligned(A, 16) || !aligned(B, 16) || !aligned(Y, type_size(type)) || !aligned(offsets, 4)) return APB_ERR_ALIGN;
-    return launch_mx4_gemm(mx_view(A, M, K), mx_view(B, E * N, K), offsets, E, M, N, type, Y, ldy,
-                           reinterpret_cast<hipStream_t>(stream));
+    const Mx a = mx_view(A, M, K), b = mx_view(B, E * N, K);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (mx4_few_applies(offsets, E, M, K)) return launch_mx4_few(a, b, offsets, E, M, N, K, type, Y, ldy, s);
+    return launch_mx4_gemm(a, b, offsets, E, M, N, type, Y, ldy, s);
 }
 
 int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const void* W,
@@ -222,6 +203,8 @@ int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const 
         !aligned(offsets, 4) || !aligned(rows_from, 4))
         return APB_ERR_ALIGN;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (mx4_few_applies(offsets, E, M, K))
+        return launch_mx4_few(X, x_type, ldx, rows_in, rows_from, mx_view(W, E * N, K), offsets, E, M, N, K, y_type, Y, ldy, s);
     const int rc = launch_mx4_quantize(X, x_type, ldx, 1, rows_in, rows_from, M, K, scratch, s);
     if (rc != APB_OK) return rc;
     return launch_mx4_gemm(mx_view(scratch, M, K), mx_view(W, E * N, K), offsets, E, M, N, y_type, Y, ldy, s);

@@ -9,25 +9,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ uint32_t top_bits(const float (&v)[8]) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) top = max(top, __builtin_bit_cast(uint32_t, v[q]) & 0x7fffffffu);
-    return top;
-}
-
-// eight values -> eight nibbles
-__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t code) {
-    if (code == 255u) return 0u;
-    const float inv = scale_inverse(code);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * inv, v[1] * inv, 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inv, v[3] * inv, 1.0f, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * inv, v[5] * inv, 1.0f, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * inv, v[7] * inv, 1.0f, 3);
-    return w;
-}
-
 // Rows whose values lie side by side.  32 lanes take a segment of 256 values of a row, eight each; the four lanes of a block
 // exchange their maxima.  `item` counts segments row by row.
 template <int TYPE>
