@@ -107,6 +107,38 @@ __device__ __forceinline__ void store4(void* p, int type, long long i, const flo
         if (q < count) store_f32(p, type, i + q, v[q]);
 }
 
+// Eight neighbours of a row as they lie in memory.
+template <int TYPE>
+struct Eight {
+    u32x4 w[TYPE == APB_F32 ? 2 : 1];
+};
+
+template <int TYPE>
+__device__ __forceinline__ Eight<TYPE> load_eight(const void* X, long long at) {
+    Eight<TYPE> v;
+    const uint8_t* p = static_cast<const uint8_t*>(X) + at * (TYPE == APB_F32 ? 4 : 2);
+    v.w[0] = load16_any(p);
+    if constexpr (TYPE == APB_F32) v.w[1] = load16_any(p + 16);
+    return v;
+}
+// ... of which `have` exist; the others are zero
+template <int TYPE>
+__device__ __forceinline__ Eight<TYPE> load_some(const void* X, long long at, int have) {
+    if (have >= 8) return load_eight<TYPE>(X, at);
+    Eight<TYPE> v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if constexpr (TYPE == APB_F32) {
+            v.w[0][q] = q < have ? static_cast<const uint32_t*>(X)[at + q] : 0u;
+            v.w[1][q] = q + 4 < have ? static_cast<const uint32_t*>(X)[at + q + 4] : 0u;
+        } else {
+            const uint16_t* p = static_cast<const uint16_t*>(X) + at + 2 * q;
+            v.w[0][q] = (2 * q < have ? (uint32_t)p[0] : 0u) | (2 * q + 1 < have ? (uint32_t)p[1] << 16 : 0u);
+        }
+    }
+    return v;
+}
+
 // eight neighbours of a row, of which `have` exist
 template <int TYPE>
 __device__ __forceinline__ void load8(const void* X, long long at, int have, float (&v)[8]) {
@@ -160,30 +192,61 @@ __device__ __forceinline__ uint32_t scale_code(uint32_t top) {
     const uint32_t ex = top >> 23;
     return ex >= 255u ? 255u : ex > 2u ? ex - 2u : 0u;
 }
-// 2^-e as a float; e <= 125 and >= -127, so it is a normal number
-__device__ __forceinline__ float scale_inverse(uint32_t code) { return __builtin_bit_cast(float, (254u - code) << 23); }
 // 2^e as a float (2^-127 is subnormal); NaN for 255
 __device__ __forceinline__ float scale_value(uint32_t code) {
     return __builtin_bit_cast(float, code == 0u ? 0x00400000u : code == 255u ? 0x7fc00000u : code << 23);
 }
 
-__device__ __forceinline__ uint32_t top_bits(const float (&v)[8]) {
-    uint32_t top = 0;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// The largest magnitude of eight values as the bits of a float (bits without their sign order like magnitudes; a NaN is above
+// infinity).
+template <int TYPE>
+__device__ __forceinline__ uint32_t top_bits(const Eight<TYPE>& v) {
+    if constexpr (TYPE == APB_F32) {
+        uint32_t top = 0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) top = max(top, __builtin_bit_cast(uint32_t, v[q]) & 0x7fffffffu);
-    return top;
+        for (int q = 0; q < 8; ++q) top = max(top, v.w[q / 4][q & 3] & 0x7fffffffu);
+        return top;
+    } else {
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t pair = v.w[0][q] & 0x7fff7fffu;
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, pair));
+        }
+        const uint16_t most = max(top[0], top[1]);
+        if constexpr (TYPE == APB_BF16) return (uint32_t)most << 16;
+        else return float_bits((float)__builtin_bit_cast(_Float16, most));
+    }
+}
+// the larger of it among the four lanes of a block of 32
+__device__ __forceinline__ uint32_t top_of_four(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));      // lanes 1 0 3 2
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));   // lanes 2 3 0 1
 }
 
-// eight values -> eight nibbles
-__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t code) {
-    if (code == 255u) return 0u;
-    const float inv = scale_inverse(code);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * inv, v[1] * inv, 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inv, v[3] * inv, 1.0f, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * inv, v[5] * inv, 1.0f, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * inv, v[7] * inv, 1.0f, 3);
-    return w;
+// Eight values -> eight nibbles.  The conversion divides by the power of two whose float has the scale code as its exponent and
+// rounds once, to nearest even; that holds for codes 0 and 252 as well.
+template <int TYPE, int B>
+__device__ __forceinline__ uint32_t encode_pair(uint32_t w, const Eight<TYPE>& v, float scale) {
+    if constexpr (TYPE == APB_F32) {
+        const uint32_t a = v.w[B / 2][2 * B & 3], c = v.w[B / 2][(2 * B & 3) + 1];
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __builtin_bit_cast(float, a), __builtin_bit_cast(float, c), scale, B);
+    } else {
+        const uint32_t pair = v.w[0][B];
+        if constexpr (TYPE == APB_BF16) return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, pair), scale, B);
+        else return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(f16x2, pair), scale, B);
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t encode8(const Eight<TYPE>& v, uint32_t code) {
+    const float scale = __builtin_bit_cast(float, code << 23);
+    uint32_t w = encode_pair<TYPE, 0>(0u, v, scale);
+    w = encode_pair<TYPE, 1>(w, v, scale);
+    w = encode_pair<TYPE, 2>(w, v, scale);
+    w = encode_pair<TYPE, 3>(w, v, scale);
+    return code == 255u ? 0u : w;
 }
 
 // ---- matrix instructions ----------------------------------------------------------------------------

@@ -24,38 +24,6 @@ struct Parts {
 // successive rows meets a bank twice.
 __device__ __forceinline__ int lds_at(int row, int chunk) { return row * kStep + 8 * (chunk ^ ((row + (row >> 3)) & 7)); }
 
-// Eight neighbours of G in eight times their size of memory words.
-template <int TYPE>
-struct Eight {
-    u32x4 w[TYPE == APB_F32 ? 2 : 1];
-};
-
-template <int TYPE>
-__device__ __forceinline__ Eight<TYPE> load_eight(const void* G, long long at) {
-    Eight<TYPE> v;
-    const uint8_t* p = static_cast<const uint8_t*>(G) + at * (TYPE == APB_F32 ? 4 : 2);
-    v.w[0] = load16_any(p);
-    if (TYPE == APB_F32) v.w[TYPE == APB_F32 ? 1 : 0] = load16_any(p + 16);
-    return v;
-}
-// ... of which `have` exist; the others are zero
-template <int TYPE>
-__device__ __forceinline__ Eight<TYPE> load_some(const void* G, long long at, int have) {
-    if (have >= 8) return load_eight<TYPE>(G, at);
-    Eight<TYPE> v;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (TYPE == APB_F32) {
-            v.w[0][q] = q < have ? static_cast<const uint32_t*>(G)[at + q] : 0u;
-            v.w[TYPE == APB_F32 ? 1 : 0][q] = q + 4 < have ? static_cast<const uint32_t*>(G)[at + q + 4] : 0u;
-        } else {
-            const uint16_t* p = static_cast<const uint16_t*>(G) + at + 2 * q;
-            v.w[0][q] = (2 * q < have ? (uint32_t)p[0] : 0u) | (2 * q + 1 < have ? (uint32_t)p[1] << 16 : 0u);
-        }
-    }
-    return v;
-}
-
 // The bfloat16 parts of eight values, pairs of neighbours in a word: each takes the leading 8 significant bits of what is left
 // (cut off, so that no part is larger than the value and none overflows).  Bits below 2^-133, which bfloat16 has not, are lost.
 template <int TYPE>

@@ -1,6 +1,8 @@
 // Y = Q(X) W^T for few rows, plain or grouped by expert: what bounds it is reading the weights once.  One kernel: a workgroup
 // brings its rows of X into LDS as 4-bit blocks (quantizing them on the way) while its first weights are already under way, then
 // streams weights through registers into the matrix cores.
+#include <type_traits>
+
 #include "apb_mx4.h"
 
 namespace apb {
@@ -22,18 +24,18 @@ struct Rows {                                 // the left operand: float rows or
     Mx mx;
 };
 
-// MT: tiles of 16 rows.  A wave computes 16 outputs (rows of W) x 16 * MT rows; WK = 2^wk_log2 waves split the segments of a tile
+// A wave computes 16 outputs (rows of W) x 16 rows; WK = 2^wk_log2 waves split the segments of a tile
 // among them and join their sums through LDS in a fixed order.  Weights go from memory to a ring of the wave's own in LDS, whole
 // lines of 128 bytes per row (loaded to registers in the order of the operands they would come in half lines, at half the
 // speed), so a wave waits for nobody but its own loads.  Lane (r, g) holds row r; of a segment of 256, step s multiplies blocks
 // 4 s .. 4 s + 3.
-template <int TYPE, int MT>
+template <int TYPE>
 __global__ __launch_bounds__(kThreads, 4) void k_mx4_few(Rows X, Mx W, const int32_t* __restrict__ offsets, int E, int M, int N,
                                                          int K, int lds_rows, int wk_log2, int type, void* __restrict__ Y,
                                                          long long ldy) {
     extern __shared__ __align__(16) uint8_t lds[];
     const int segs = W.segs;
-    const RowTile t = find_row_tile(offsets, E, M, 16 * MT, blockIdx.x);
+    const RowTile t = find_row_tile(offsets, E, M, 16, blockIdx.x);
     if (t.rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int tiles_n = (N + 15) / 16;
@@ -83,33 +85,48 @@ __global__ __launch_bounds__(kThreads, 4) void k_mx4_few(Rows X, Mx W, const int
     for (int i = 0; i < min(kRing, items); ++i) fetch();
 
     // X: row i's 16-byte blocks, permuted by the row's number (no bank is met twice by eight rows), then the scales of all rows
-    const int per_row = segs * 32;
-    for (int i = tid; i < t.rows * per_row; i += kThreads) {
-        const int row = i / per_row, unit = i - row * per_row;   // unit: eight values
-        const int at = row * pitch + 16 * ((unit >> 2) ^ (row & 7)) + 4 * (unit & 3);
-        if (TYPE == kFourBit) {
-            const size_t src = (size_t)(t.row0 + row);
-            *reinterpret_cast<uint32_t*>(lds + at) = *reinterpret_cast<const uint32_t*>(X.mx.codes + src * pitch + 4 * unit);
-            if ((unit & 3) == 0) x_scales[(row * segs) * 8 + (unit >> 2)] = X.mx.scales[((size_t)(unit >> 5) * X.mx.rows + src) * 8 + ((unit >> 2) & 7)];
-        } else {
-            const int src = X.rows_from ? X.rows_from[t.row0 + row] : t.row0 + row;
-            float v[8];
-            load8<TYPE>(X.x, (long long)src * X.ld + 8 * unit, src >= 0 && src < X.rows_in ? K - 8 * unit : 0, v);
-            uint32_t top = top_bits(v);
-            top = max(top, (uint32_t)__shfl_xor((int)top, 1, kWave));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 2, kWave));
-            const uint32_t code = scale_code(top);
-            *reinterpret_cast<uint32_t*>(lds + at) = encode8(v, code);
-            if ((unit & 3) == 0) x_scales[(row * segs) * 8 + (unit >> 2)] = (uint8_t)code;
+    // A wave takes pieces of 512 values of a row, eight for each lane, four pieces at a time as long as it has as many.
+    const int pieces = (segs + 1) / 2, all = t.rows * pieces;
+    auto bring = [&](int first, auto count) {
+        constexpr int kCount = decltype(count)::value;
+        Eight<TYPE == kFourBit ? APB_BF16 : TYPE> v[kCount];
+        uint32_t word[kCount], mark[kCount];
+        int row[kCount], unit[kCount];
+#pragma unroll
+        for (int u = 0; u < kCount; ++u) {
+            const int i = first + u * kWaves;
+            row[u] = i / pieces;
+            unit[u] = (i - row[u] * pieces) * kWave + lane;
+            if (unit[u] >= segs * 32) unit[u] -= 32;             // (half a piece: the other half does the same again)
+            if constexpr (TYPE == kFourBit) {
+                const size_t src = (size_t)(t.row0 + row[u]);
+                word[u] = *reinterpret_cast<const uint32_t*>(X.mx.codes + src * pitch + 4 * unit[u]);
+                mark[u] = X.mx.scales[((size_t)(unit[u] >> 5) * X.mx.rows + src) * 8 + ((unit[u] >> 2) & 7)];
+            } else {
+                const int src = X.rows_from ? X.rows_from[t.row0 + row[u]] : t.row0 + row[u];
+                v[u] = load_some<TYPE>(X.x, (long long)src * X.ld + 8 * unit[u], src >= 0 && src < X.rows_in ? K - 8 * unit[u] : 0);
+            }
         }
-    }
+#pragma unroll
+        for (int u = 0; u < kCount; ++u) {
+            if constexpr (TYPE != kFourBit) {
+                mark[u] = scale_code(top_of_four(top_bits(v[u])));
+                word[u] = encode8(v[u], mark[u]);
+            }
+            *reinterpret_cast<uint32_t*>(lds + row[u] * pitch + 16 * ((unit[u] >> 2) ^ (row[u] & 7)) + 4 * (unit[u] & 3)) = word[u];
+            if ((unit[u] & 3) == 0) x_scales[row[u] * segs * 8 + (unit[u] >> 2)] = (uint8_t)mark[u];
+        }
+    };
+    int piece = wave;
+    for (; piece + 3 * kWaves < all; piece += 4 * kWaves) bring(piece, std::integral_constant<int, 4>{});
+    for (; piece < all; piece += kWaves) bring(piece, std::integral_constant<int, 1>{});
     __syncthreads();
 
+    const int row = min(r, t.rows - 1);
+    const uint8_t* x_codes = lds + row * pitch;
     int item = 0, slot = 0, nt = nt0;
     for (int base = blockIdx.y * wn_n; base < tiles_n; base += step_n, nt += step_n) {
-        f32x4 acc[MT];
-#pragma unroll
-        for (int x = 0; x < MT; ++x) acc[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int seg = nt < tiles_n ? wk : segs; seg < segs; seg += wk_n, ++item) {
             // all but the loads of the segments behind this one
             if (item + kRing <= items) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (kRing - 1)) : "memory");
@@ -118,59 +135,44 @@ __global__ __launch_bounds__(kThreads, 4) void k_mx4_few(Rows X, Mx W, const int
             const u32x4 w0 = *reinterpret_cast<const u32x4*>(from + r * kMxSegBytes + 16 * (g ^ (r & 7)));
             const u32x4 w1 = *reinterpret_cast<const u32x4*>(from + r * kMxSegBytes + 16 * ((4 + g) ^ (r & 7)));
             const int sw0 = from[2048 + 8 * r + g], sw1 = from[2048 + 8 * r + 4 + g];
-#pragma unroll
-            for (int x = 0; x < MT; ++x) {
-                const int row = min(16 * x + r, t.rows - 1);
-                const uint8_t* sx = x_scales + (row * segs + seg) * 8 + g;
-                const uint8_t* p = lds + row * pitch;
-                const u32x4 x0 = *reinterpret_cast<const u32x4*>(p + 16 * ((8 * seg + g) ^ (row & 7)));
-                const u32x4 x1 = *reinterpret_cast<const u32x4*>(p + 16 * ((8 * seg + 4 + g) ^ (row & 7)));
-                acc[x] = mfma16<0>(w0, x0, acc[x], sw0, sx[0]);
-                acc[x] = mfma16<0>(w1, x1, acc[x], sw1, sx[4]);
-            }
+            const uint8_t* sx = x_scales + (row * segs + seg) * 8 + g;
+            const u32x4 x0 = *reinterpret_cast<const u32x4*>(x_codes + 16 * ((8 * seg + g) ^ (row & 7)));
+            const u32x4 x1 = *reinterpret_cast<const u32x4*>(x_codes + 16 * ((8 * seg + 4 + g) ^ (row & 7)));
+            acc = mfma16<0>(w0, x0, acc, sw0, sx[0]);
+            acc = mfma16<0>(w1, x1, acc, sw1, sx[4]);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (this slot has been read)
             if (item + kRing < items) fetch();
             slot = slot + 1 == kRing ? 0 : slot + 1;
         }
         if (wk_n > 1) {
             // (the barrier at the end of the loop keeps this round's readers ahead of the next round's writers)
-#pragma unroll
-            for (int x = 0; x < MT; ++x) *reinterpret_cast<f32x4*>(sums + ((wave * MT + x) * kWave + lane) * 4) = acc[x];
+            *reinterpret_cast<f32x4*>(sums + (wave * kWave + lane) * 4) = acc;
             __syncthreads();
-            if (wk == 0) {
-                for (int w = 1; w < wk_n; ++w)
+            if (wk == 0)
+                for (int w = 1; w < wk_n; ++w) {
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(sums + ((wave + w) * kWave + lane) * 4);
 #pragma unroll
-                    for (int x = 0; x < MT; ++x) {
-                        const f32x4 v = *reinterpret_cast<const f32x4*>(sums + (((wave + w) * MT + x) * kWave + lane) * 4);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) acc[x][q] += v[q];
-                    }
-            }
+                    for (int q = 0; q < 4; ++q) acc[q] += v[q];
+                }
         }
-        if (wk == 0 && nt < tiles_n) {
+        if (wk == 0 && nt < tiles_n && r < t.rows) {
             const int n = nt * 16 + 4 * g;
-#pragma unroll
-            for (int x = 0; x < MT; ++x) {
-                const float v[4] = {acc[x][0], acc[x][1], acc[x][2], acc[x][3]};
-                if (16 * x + r < t.rows) store4(Y, type, (long long)(t.row0 + 16 * x + r) * ldy + n, v, N - n);
-            }
+            const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+            store4(Y, type, (long long)(t.row0 + r) * ldy + n, v, N - n);
         }
         if (wk_n > 1) __syncthreads();
     }
 }
 
-size_t lds_bytes(int rows, int segs, int tiles) {
+size_t lds_bytes(int rows, int segs) {
     return (size_t)rows * segs * kMxSegBytes + ((size_t)rows * segs * 8 + 15) / 16 * 16 + (size_t)kWaves * kRing * kSlot +
-           (size_t)kWaves * tiles * kWave * 16;
+           (size_t)kWaves * kWave * 16;
 }
-// rows of an expert, were they all alike
-int mean_rows(const int32_t* offsets, int E, int M) { return offsets ? (M + E - 1) / E : M; }
-
-template <int TYPE, int MT>
+template <int TYPE>
 int launch(const Rows& X, const Mx& W, const int32_t* offsets, int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s) {
-    const int lds_rows = std::min(M, 16 * MT);
-    const size_t lds = lds_bytes(lds_rows, W.segs, MT);
-    const long long row_tiles = max_row_tiles(M, E, offsets != nullptr, 16 * MT);
+    const int lds_rows = std::min(M, 16);
+    const size_t lds = lds_bytes(lds_rows, W.segs);
+    const long long row_tiles = max_row_tiles(M, E, offsets != nullptr, 16);
     const int tiles_n = (N + 15) / 16;
     // Waves share a tile only where there would be fewer workgroups than compute units without.
     int wk = 0;
@@ -178,33 +180,31 @@ int launch(const Rows& X, const Mx& W, const int32_t* offsets, int E, int M, int
     const int groups = (tiles_n + (kWaves >> wk) - 1) / (kWaves >> wk);
     const long long per_row_tile = std::max<long long>(1, kWorkgroups / row_tiles);
     const dim3 grid((unsigned)row_tiles, (unsigned)std::min<long long>(groups, per_row_tile));
-    hipLaunchKernelGGL((k_mx4_few<TYPE, MT>), grid, dim3(kThreads), lds, s, X, W, offsets, E, M, N, K, lds_rows, wk, type, Y, ldy);
+    hipLaunchKernelGGL((k_mx4_few<TYPE>), grid, dim3(kThreads), lds, s, X, W, offsets, E, M, N, K, lds_rows, wk, type, Y, ldy);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
 
-template <int TYPE>
-int launch_rows(const Rows& X, const Mx& W, const int32_t* offsets, int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s) {
-    if (mean_rows(offsets, E, M) <= 16) return launch<TYPE, 1>(X, W, offsets, E, M, N, K, type, Y, ldy, s);
-    return launch<TYPE, 2>(X, W, offsets, E, M, N, K, type, Y, ldy, s);
-}
-
 }  // namespace
 
+// A workgroup quantizes every row it multiplies with, so the rows must be few and short.  Measured against quantization and
+// tiles (us): 4096 x 4096, 1 row 5.0 : 11.7, 16 rows 10.4 : 12.2, 32 rows 16.9 : 12.4; 8192 x 8192, 4 rows 12.2 : 19.9, 16 rows
+// 20.5 : 20.0; 64 experts of 2048 x 2048, a row each 20.5 : 26.1, 4 rows 33.9 : 36.1, 8 rows 38.4 : 36.8; 16 experts of
+// 2048 x 4096, 8 rows each 28.4 : 17.2.
 bool mx4_few_applies(const int32_t* offsets, int E, int M, int K) {
-    const int mean = mean_rows(offsets, E, M), tile = mean <= 16 ? 16 : 32;
-    return mean <= 32 && lds_bytes(std::min(M, tile), mx_segs(K), tile / 16) <= kMaxLds;
+    const int mean = offsets ? (M + E - 1) / E : M;              // rows of an expert, were they all alike
+    return mean <= 16 && (long long)mean * K <= (offsets ? 8192 : 65536) && lds_bytes(std::min(M, 16), mx_segs(K)) <= kMaxLds;
 }
 
 int launch_mx4_few(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const Mx& W, const int32_t* offsets,
                    int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s) {
     const Rows rows{X, ldx, rows_in, rows_from, Mx{}};
-    if (x_type == APB_F32) return launch_rows<APB_F32>(rows, W, offsets, E, M, N, K, type, Y, ldy, s);
-    if (x_type == APB_BF16) return launch_rows<APB_BF16>(rows, W, offsets, E, M, N, K, type, Y, ldy, s);
-    return launch_rows<APB_F16>(rows, W, offsets, E, M, N, K, type, Y, ldy, s);
+    if (x_type == APB_F32) return launch<APB_F32>(rows, W, offsets, E, M, N, K, type, Y, ldy, s);
+    if (x_type == APB_BF16) return launch<APB_BF16>(rows, W, offsets, E, M, N, K, type, Y, ldy, s);
+    return launch<APB_F16>(rows, W, offsets, E, M, N, K, type, Y, ldy, s);
 }
 int launch_mx4_few(const Mx& A, const Mx& W, const int32_t* offsets, int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s) {
-    return launch_rows<kFourBit>(Rows{nullptr, 0, 0, nullptr, A}, W, offsets, E, M, N, K, type, Y, ldy, s);
+    return launch<kFourBit>(Rows{nullptr, 0, 0, nullptr, A}, W, offsets, E, M, N, K, type, Y, ldy, s);
 }
 
 }  // namespace apb

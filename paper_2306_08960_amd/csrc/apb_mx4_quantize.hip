@@ -1,7 +1,7 @@
 // Quantization to microscaled 4-bit blocks and back.  A block is 32 neighbours along K with one scale 2^e,
 // e = floor(log2(max |x|)) - 2, so that the largest magnitude lies in [4, 8) * 2^e, and each value becomes the nearest of
-// +-{0, .5, 1, 1.5, 2, 3, 4, 6} * 2^e (ties to the even index, beyond 6: 6).  x * 2^-e is exact, the conversion instruction
-// rounds once, so the codes are defined to the bit.  Both directions are one pass over memory and bound by it.
+// +-{0, .5, 1, 1.5, 2, 3, 4, 6} * 2^e (ties to the even index, beyond 6: 6).  The conversion instruction scales and rounds
+// once, so the codes are defined to the bit.  Both directions are one pass over memory and bound by it.
 #include "apb_mx4.h"
 
 namespace apb {
@@ -22,12 +22,8 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantize(const void* __restric
     if (r >= rows) return;
     const int src = rows_from ? rows_from[r] : r;
     const int k = seg * kMxSeg + 8 * l;
-    float v[8];
-    load8<TYPE>(X, (long long)src * row_stride + k, src >= 0 && src < rows_in ? K - k : 0, v);
-    uint32_t top = top_bits(v);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 32));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 32));
-    const uint32_t code = scale_code(top);
+    const Eight<TYPE> v = load_some<TYPE>(X, (long long)src * row_stride + k, src >= 0 && src < rows_in ? K - k : 0);
+    const uint32_t code = scale_code(top_of_four(top_bits(v)));
     *reinterpret_cast<uint32_t*>(codes + ((size_t)r * segs + seg) * kMxSegBytes + 4 * l) = encode8(v, code);
     if ((l & 3) == 0) scales[((size_t)seg * rows + r) * 8 + l / 4] = (uint8_t)code;
 }
@@ -45,12 +41,20 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantize_strided(const void* _
     const int src = rows_from ? rows_from[r] : r;
     const int have = src >= 0 && src < rows_in ? K - block * kMxBlock : 0;
     const long long at = (long long)src * row_stride + (long long)block * kMxBlock * col_stride;
-    float v[4][8];
+    Eight<TYPE> v[4];
     uint32_t top = 0;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[g][q] = 8 * g + q < have ? load_f32(X, TYPE, at + (8 * g + q) * col_stride) : 0.0f;
+        for (int q = 0; q < 8; ++q) {
+            const long long i = at + (8 * g + q) * col_stride;
+            if constexpr (TYPE == APB_F32) {
+                v[g].w[q / 4][q & 3] = 8 * g + q < have ? static_cast<const uint32_t*>(X)[i] : 0u;
+            } else {
+                const uint32_t x = 8 * g + q < have ? static_cast<const uint16_t*>(X)[i] : 0u;
+                v[g].w[0][q / 2] = q & 1 ? v[g].w[0][q / 2] | x << 16 : x;
+            }
+        }
         top = max(top, top_bits(v[g]));
     }
     const uint32_t code = scale_code(top);
