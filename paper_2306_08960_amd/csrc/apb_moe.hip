@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTokens = 64;                   // tokens of a workgroup: bits of a mask
-constexpr int kScanThreads = 1024;
+constexpr int kChooseThreads = 1024;          // four waves for a SIMD to switch between: a choice is a chain of dependent steps
 constexpr long long kMaxSlots = 1LL << 24;    // a workgroup of 256 lanes per token: the lanes of a launch fit 32 bits
 
 // An order-preserving map of the logits that can be taken to positive whole numbers; -inf and NaN: 0.
@@ -24,9 +24,26 @@ __device__ __forceinline__ float key_value(uint32_t key) {
     return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
+// Over the lanes of a wave, in six steps of lane-permuted operands; lanes without a partner take 0.
+template <int CTRL>
+__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false); }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d, kWave));
+    v = max(v, (uint32_t)from_lane<0x111>((int)v));              // from the lane 1, 2, 4, 8 below, in rows of 16
+    v = max(v, (uint32_t)from_lane<0x112>((int)v));
+    v = max(v, (uint32_t)from_lane<0x114>((int)v));
+    v = max(v, (uint32_t)from_lane<0x118>((int)v));
+    v = max(v, (uint32_t)from_lane<0x142>((int)v));              // from the last lane of the row before
+    v = max(v, (uint32_t)from_lane<0x143>((int)v));              // from lane 31
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, kWave - 1);
+}
+// sum over this lane and those below
+__device__ __forceinline__ int wave_prefix(int v) {
+    v += from_lane<0x111>(v);
+    v += from_lane<0x112>(v);
+    v += from_lane<0x114>(v);
+    v += from_lane<0x118>(v);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // into rows 2 and 3
     return v;
 }
 __device__ __forceinline__ float wave_sum(float v) {
@@ -84,7 +101,7 @@ struct Block {
 };
 
 __device__ __forceinline__ void clear(Block& b, int E) {
-    for (int e = threadIdx.x; e < E; e += kThreads) b.mask[e] = 0ull;
+    for (int e = threadIdx.x; e < E; e += blockDim.x) b.mask[e] = 0ull;
     if (threadIdx.x < kTokens) b.drop[threadIdx.x] = 0;
 }
 __device__ __forceinline__ void note(Block& b, int token, int expert) {
@@ -99,20 +116,28 @@ __device__ __forceinline__ int rank_of(const Block& b, int token, int expert, in
     return n;
 }
 
+// First rows of the experts from how many slots each has; a whole wave.
+__device__ __forceinline__ int start_of(int n, int lane, int& before) {
+    const int upto = wave_prefix(n);
+    const int start = before + upto - n;
+    before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    return start;
+}
+
 // ALONE: one workgroup has all tokens and does everything.  Otherwise count[e][workgroup] is written (e == E: slots without
 // an expert) and the scan and placement kernels follow.
 template <int EPL, bool ALONE>
-__global__ __launch_bounds__(kThreads) void k_moe_choose(const void* __restrict__ logits, int type, long long ld, int T, int E,
-                                                         int k, int32_t* __restrict__ expert, float* __restrict__ weight,
-                                                         int32_t* __restrict__ offsets, int32_t* __restrict__ row_token,
-                                                         int32_t* __restrict__ slot_row, int32_t* __restrict__ count) {
+__global__ __launch_bounds__(kChooseThreads) void k_moe_choose(const void* __restrict__ logits, int type, long long ld, int T, int E,
+                                                               int k, int32_t* __restrict__ expert, float* __restrict__ weight,
+                                                               int32_t* __restrict__ offsets, int32_t* __restrict__ row_token,
+                                                               int32_t* __restrict__ slot_row, int32_t* __restrict__ count) {
     __shared__ Block b;
     __shared__ int start[ALONE ? APB_MOE_MAX_E + 1 : 1];
     clear(b, E);
     __syncthreads();
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int t0 = blockIdx.x * kTokens;
-    for (int i = wave; i < kTokens && t0 + i < T; i += kThreads / kWave) {
+    for (int i = wave; i < kTokens && t0 + i < T; i += blockDim.x / kWave) {
         float w;
         const int e = choose<EPL>(logits, type, (long long)(t0 + i) * ld, E, k, w);
         if (lane < k) {
@@ -123,7 +148,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_choose(const void* __restrict_
     }
     __syncthreads();
     if (!ALONE) {
-        for (int e = threadIdx.x; e <= E; e += kThreads) {
+        for (int e = threadIdx.x; e <= E; e += blockDim.x) {
             int n = 0;
             if (e < E) n = __popcll(b.mask[e]);
             else
@@ -134,28 +159,17 @@ __global__ __launch_bounds__(kThreads) void k_moe_choose(const void* __restrict_
     }
     if (wave == 0) {
         int before = 0;
-        for (int base = 0; base < E; base += kWave) {
+        for (int base = 0; base <= E; base += kWave) {
             const int e = base + lane;
-            const int n = e < E ? __popcll(b.mask[e]) : 0;
-            int upto = n;
-#pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const int v = __shfl_up(upto, d, kWave);
-                if (lane >= d) upto += v;
+            const int first = start_of(e < E ? __popcll(b.mask[e]) : 0, lane, before);
+            if (e <= E) {
+                start[e] = first;
+                offsets[e] = first;
             }
-            if (e < E) {
-                start[e] = before + upto - n;
-                offsets[e] = before + upto - n;
-            }
-            before += __shfl(upto, kWave - 1, kWave);
-        }
-        if (lane == 0) {
-            start[E] = before;
-            offsets[E] = before;
         }
     }
     __syncthreads();
-    for (int s = threadIdx.x; s < T * k; s += kThreads) {
+    for (int s = threadIdx.x; s < T * k; s += blockDim.x) {
         const int t = s / k, e = expert[s];                      // (written by this workgroup, before its barrier)
         const int row = start[e >= 0 ? e : E] + rank_of(b, t, e, s - t * k, k);
         slot_row[s] = row;
@@ -163,58 +177,56 @@ __global__ __launch_bounds__(kThreads) void k_moe_choose(const void* __restrict_
     }
 }
 
-// One workgroup: count[e][..] becomes the number of slots of e before each workgroup, offsets the first row of each expert.
-__global__ __launch_bounds__(kScanThreads) void k_moe_scan(int32_t* __restrict__ count, int blocks, int E,
-                                                           int32_t* __restrict__ offsets) {
-    __shared__ int total[APB_MOE_MAX_E + 1];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    for (int e = wave; e <= E; e += kScanThreads / kWave) {
-        int before = 0;
-        for (int base = 0; base < blocks; base += kWave) {
-            const int i = base + lane;
-            const int n = i < blocks ? count[(size_t)e * blocks + i] : 0;
-            int upto = n;
+// One wave per expert: count[e][..] becomes the number of slots of e before each workgroup, total[e] that of all of them.
+__global__ __launch_bounds__(kWave) void k_moe_scan(int32_t* __restrict__ count, int blocks, int32_t* __restrict__ total) {
+    constexpr int kEach = 4;                                     // workgroups to a lane
+    const int lane = threadIdx.x;
+    int32_t* row = count + (size_t)blockIdx.x * blocks;
+    int before = 0;
+    for (int base = 0; base < blocks; base += kWave * kEach) {
+        const int i0 = base + lane * kEach;
+        int n[kEach], sum = 0;
 #pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const int v = __shfl_up(upto, d, kWave);
-                if (lane >= d) upto += v;
-            }
-            if (i < blocks) count[(size_t)e * blocks + i] = before + upto - n;
-            before += __shfl(upto, kWave - 1, kWave);
-        }
-        if (lane == 0) total[e] = before;
-    }
-    __syncthreads();
-    if (wave == 0) {
-        int before = 0;
-        for (int base = 0; base <= E; base += kWave) {
-            const int e = base + lane;
-            const int n = e <= E ? total[e] : 0;
-            int upto = n;
+        for (int i = 0; i < kEach; ++i) n[i] = i0 + i < blocks ? row[i0 + i] : 0;
 #pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const int v = __shfl_up(upto, d, kWave);
-                if (lane >= d) upto += v;
-            }
-            if (e <= E) offsets[e] = before + upto - n;
-            before += __shfl(upto, kWave - 1, kWave);
+        for (int i = 0; i < kEach; ++i) sum += n[i];
+        int at = start_of(sum, lane, before);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (i0 + i < blocks) row[i0 + i] = at;
+            at += n[i];
         }
     }
+    if (lane == 0) total[blockIdx.x] = before;
 }
 
 __global__ __launch_bounds__(kThreads) void k_moe_place(const int32_t* __restrict__ expert, int T, int E, int k,
-                                                        const int32_t* __restrict__ count, const int32_t* __restrict__ offsets,
-                                                        int32_t* __restrict__ row_token, int32_t* __restrict__ slot_row) {
+                                                        const int32_t* __restrict__ count, const int32_t* __restrict__ total,
+                                                        int32_t* __restrict__ offsets, int32_t* __restrict__ row_token,
+                                                        int32_t* __restrict__ slot_row) {
     __shared__ Block b;
+    __shared__ int start[APB_MOE_MAX_E + 1];
     clear(b, E);
     __syncthreads();
     const int t0 = blockIdx.x * kTokens;
     const int slots = min(kTokens, T - t0) * k;
     for (int s = threadIdx.x; s < slots; s += kThreads) note(b, s / k, expert[t0 * k + s]);
+    if (threadIdx.x < kWave) {
+        const int lane = threadIdx.x;
+        int before = 0;
+        for (int base = 0; base <= E; base += kWave) {
+            const int e = base + lane;
+            const int first = start_of(e < E ? total[e] : 0, lane, before);
+            if (e <= E) {
+                start[e] = first + count[(size_t)e * gridDim.x + blockIdx.x];
+                if (blockIdx.x == 0) offsets[e] = first;
+            }
+        }
+    }
     __syncthreads();
     for (int s = threadIdx.x; s < slots; s += kThreads) {
-        const int t = s / k, e = expert[t0 * k + s], g = e >= 0 ? e : E;
-        const int row = offsets[g] + count[(size_t)g * gridDim.x + blockIdx.x] + rank_of(b, t, e, s - t * k, k);
+        const int t = s / k, e = expert[t0 * k + s];
+        const int row = start[e >= 0 ? e : E] + rank_of(b, t, e, s - t * k, k);
         slot_row[t0 * k + s] = row;
         row_token[row] = t0 + t;
     }
@@ -253,19 +265,33 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine(const void* __restrict
     const int t = blockIdx.x, n = (blockIdx.y * kThreads + threadIdx.x) * 8;
     if (n >= N) return;
     float acc[8] = {};
-    for (int j = 0; j < k; ++j) {
-        const int row = slot_row[t * k + j];
-        const float w = weight ? weight[t * k + j] : 1.0f;
-        if (w == 0.0f || row < 0 || row >= T * k) continue;
-        float v[8];
-        load8<TYPE>(Z, (long long)row * ldz + n, N - n, v);
+    constexpr int kAhead = 4;                                    // rows under way
+    for (int j = 0; j < k; j += kAhead) {
+        int row[kAhead];
+        float w[kAhead];
+        Eight<TYPE> v[kAhead];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) acc[q] = fmaf(w, v[q], acc[q]);
+        for (int u = 0; u < kAhead; ++u) {
+            row[u] = j + u < k ? slot_row[t * k + j + u] : -1;
+            w[u] = j + u < k ? weight ? weight[t * k + j + u] : 1.0f : 0.0f;
+            if (row[u] < 0 || row[u] >= T * k) w[u] = 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (w[u] != 0.0f) v[u] = load_some<TYPE>(Z, (long long)row[u] * ldz + n, N - n);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (w[u] == 0.0f) continue;
+            float x[8];
+            floats(v[u], x);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) acc[q] = fmaf(w[u], x[q], acc[q]);
+        }
     }
     store8<TYPE>(Y, (long long)t * ldy + n, N - n, acc);
 }
 
-// One wave per slot: its row of dZ and its dweight.
+// One workgroup per slot: its row of dZ and its dweight.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* __restrict__ dY, long long lddy,
                                                                    const void* __restrict__ Z, long long ldz,
@@ -273,42 +299,54 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* _
                                                                    const float* __restrict__ weight, int slots, FastDiv by_k, int N,
                                                                    void* __restrict__ dZ, long long lddz,
                                                                    float* __restrict__ dweight) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int s = blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
-    if (s >= slots) return;
-    const int t = (int)by_k.div((uint32_t)s), row = slot_row[s];
+    __shared__ float sums[kThreads / kWave];
+    const int s = blockIdx.x, t = (int)by_k.div((uint32_t)s), row = slot_row[s];
     const float w = weight ? weight[s] : 1.0f;
-    const bool there = row >= 0 && row < slots;
+    if (row < 0 || row >= slots) {
+        if (dweight && threadIdx.x == 0) dweight[s] = 0.0f;
+        return;
+    }
     float dot = 0.0f;
-    if (there) {
-        for (int n = lane * 8; n < N; n += kWave * 8) {
-            float g[8], z[8], d[8];
-            load8<TYPE>(dY, (long long)t * lddy + n, N - n, g);
-            if (dweight) {
-                load8<TYPE>(Z, (long long)row * ldz + n, N - n, z);
+    for (int n = threadIdx.x * 8; n < N; n += kThreads * 8) {
+        const Eight<TYPE> a = load_some<TYPE>(dY, (long long)t * lddy + n, N - n);
+        float g[8], d[8];
+        if (dweight) {
+            const Eight<TYPE> b = load_some<TYPE>(Z, (long long)row * ldz + n, N - n);
+            float z[8];
+            floats(a, g);
+            floats(b, z);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) dot = fmaf(g[q], z[q], dot);
-            }
-#pragma unroll
-            for (int q = 0; q < 8; ++q) d[q] = w == 0.0f ? 0.0f : w * g[q];
-            store8<TYPE>(dZ, (long long)row * lddz + n, N - n, d);
+            for (int q = 0; q < 8; ++q) dot = fmaf(g[q], z[q], dot);
+        } else {
+            floats(a, g);
         }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) d[q] = w == 0.0f ? 0.0f : w * g[q];
+        store8<TYPE>(dZ, (long long)row * lddz + n, N - n, d);
     }
     if (dweight) {
         dot = wave_sum(dot);
-        if (lane == 0) dweight[s] = dot;
+        if ((threadIdx.x & (kWave - 1)) == 0) sums[threadIdx.x / kWave] = dot;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float all = sums[0];
+#pragma unroll
+            for (int i = 1; i < kThreads / kWave; ++i) all += sums[i];
+            dweight[s] = all;
+        }
     }
 }
 
 template <int EPL>
-void launch_choose(bool alone, int blocks, hipStream_t s, const void* logits, int type, long long ld, int T, int E, int k,
-                   int32_t* expert, float* weight, int32_t* offsets, int32_t* row_token, int32_t* slot_row, int32_t* count) {
-    if (alone)
-        hipLaunchKernelGGL((k_moe_choose<EPL, true>), dim3(blocks), dim3(kThreads), 0, s, logits, type, ld, T, E, k, expert, weight,
-                           offsets, row_token, slot_row, count);
+void launch_choose(int blocks, hipStream_t s, const void* logits, int type, long long ld, int T, int E, int k, int32_t* expert,
+                   float* weight, int32_t* offsets, int32_t* row_token, int32_t* slot_row, int32_t* count) {
+    const dim3 threads(std::min(kChooseThreads, kWave * T));
+    if (blocks == 1)
+        hipLaunchKernelGGL((k_moe_choose<EPL, true>), dim3(blocks), threads, 0, s, logits, type, ld, T, E, k, expert, weight, offsets,
+                           row_token, slot_row, count);
     else
-        hipLaunchKernelGGL((k_moe_choose<EPL, false>), dim3(blocks), dim3(kThreads), 0, s, logits, type, ld, T, E, k, expert, weight,
-                           offsets, row_token, slot_row, count);
+        hipLaunchKernelGGL((k_moe_choose<EPL, false>), dim3(blocks), threads, 0, s, logits, type, ld, T, E, k, expert, weight, offsets,
+                           row_token, slot_row, count);
 }
 
 bool bad_route(int T, int E, int k) {
@@ -325,7 +363,7 @@ extern "C" {
 
 size_t apb_moe_workspace_bytes(int T, int E, int k) {
     if (bad_route(T, E, k)) return 0;
-    return (size_t)route_blocks(T) * (E + 1) * sizeof(int32_t);
+    return ((size_t)route_blocks(T) + 1) * (E + 1) * sizeof(int32_t);
 }
 
 int apb_moe_route(const void* logits, int type, long long ld, int T, int E, int k, int32_t* expert, float* weight,
@@ -339,14 +377,14 @@ int apb_moe_route(const void* logits, int type, long long ld, int T, int E, int 
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const int blocks = route_blocks(T);
     int32_t* count = static_cast<int32_t*>(workspace);
-    const bool alone = blocks == 1;
-    if (E <= 64) launch_choose<1>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
-    else if (E <= 128) launch_choose<2>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
-    else if (E <= 256) launch_choose<4>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
-    else launch_choose<16>(alone, blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
-    if (!alone) {
-        hipLaunchKernelGGL(k_moe_scan, dim3(1), dim3(kScanThreads), 0, s, count, blocks, E, offsets);
-        hipLaunchKernelGGL(k_moe_place, dim3(blocks), dim3(kThreads), 0, s, expert, T, E, k, count, offsets, row_token, slot_row);
+    if (E <= 64) launch_choose<1>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else if (E <= 128) launch_choose<2>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else if (E <= 256) launch_choose<4>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else launch_choose<16>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    if (blocks > 1) {
+        int32_t* total = count + (size_t)blocks * (E + 1);
+        hipLaunchKernelGGL(k_moe_scan, dim3(E + 1), dim3(kWave), 0, s, count, blocks, total);
+        hipLaunchKernelGGL(k_moe_place, dim3(blocks), dim3(kThreads), 0, s, expert, T, E, k, count, total, offsets, row_token, slot_row);
     }
     APB_HIP(hipGetLastError());
     return APB_OK;
@@ -396,8 +434,8 @@ int apb_moe_combine_backward(const void* dY, int type, long long lddy, const voi
         !aligned(weight, 4) || !aligned(dweight, 4))
         return APB_ERR_ALIGN;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const int slots = T * k, per = kThreads / kWave;
-    const dim3 grid((unsigned)((slots + per - 1) / per));
+    const int slots = T * k;
+    const dim3 grid((unsigned)slots);
     APB_BY_TYPE(k_moe_combine_backward, grid, dY, lddy, Z, ldz, slot_row, weight, slots, FastDiv((uint32_t)k), N, dZ, lddz,
                               dweight);
     APB_HIP(hipGetLastError());

@@ -139,26 +139,17 @@ __device__ __forceinline__ Eight<TYPE> load_some(const void* X, long long at, in
     return v;
 }
 
-// eight neighbours of a row, of which `have` exist
 template <int TYPE>
-__device__ __forceinline__ void load8(const void* X, long long at, int have, float (&v)[8]) {
-    if (have >= 8) {
-        const uint8_t* p = static_cast<const uint8_t*>(X) + at * (TYPE == APB_F32 ? 4 : 2);
-        const u32x4 w = load16_any(p);
-        if (TYPE == APB_F32) {
-            const u32x4 x = load16_any(p + 16);
+__device__ __forceinline__ void floats(const Eight<TYPE>& x, float (&v)[8]) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t a = w[q], b = x[q];
-                v[q] = __builtin_bit_cast(float, a);
-                v[4 + q] = __builtin_bit_cast(float, b);
-            }
-            return;
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t pair = w[q];                          // (a bit cast of w[q] itself would take w[0]'s place)
-            if (TYPE == APB_BF16) {
+    for (int q = 0; q < 4; ++q) {
+        if constexpr (TYPE == APB_F32) {
+            const uint32_t a = x.w[0][q], b = x.w[1][q];         // (a bit cast of a vector's element itself takes the first's place)
+            v[q] = __builtin_bit_cast(float, a);
+            v[4 + q] = __builtin_bit_cast(float, b);
+        } else {
+            const uint32_t pair = x.w[0][q];
+            if constexpr (TYPE == APB_BF16) {
                 v[2 * q] = __builtin_bit_cast(float, pair << 16);
                 v[2 * q + 1] = __builtin_bit_cast(float, pair & 0xffff0000u);
             } else {
@@ -167,11 +158,9 @@ __device__ __forceinline__ void load8(const void* X, long long at, int have, flo
                 v[2 * q + 1] = (float)h[1];
             }
         }
-        return;
     }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = q < have ? load_f32(X, TYPE, at + q) : 0.0f;
 }
+// eight neighbours of a row, of which `have` exist
 template <int TYPE>
 __device__ __forceinline__ void store8(void* X, long long at, int have, const float (&v)[8]) {
     if (have >= 8 && TYPE != APB_F32) {
