@@ -6,8 +6,12 @@ namespace {
 
 constexpr int kThreads = 256;                 // four waves, two by two
 
-// Every wave's loads are in LDS and every wave's reads of LDS before this point have been answered.
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All of this wave's loads but the last `Behind` are in LDS and its reads of LDS have been answered; then so are everybody's.
+template <int Behind>
+__device__ __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(Behind) : "memory");
+}
+
 // Which tile a workgroup takes: workgroups go to the eight XCDs in turn, and sixteen in a row on one XCD take a block of 4 x 4
 // tiles, which shares its operands in that XCD's cache.
 __device__ __forceinline__ void tile_of(int id, int tiles_n, int& t, int& n) {
@@ -18,20 +22,27 @@ __device__ __forceinline__ void tile_of(int id, int tiles_n, int& t, int& n) {
     n = rest >> 2;
 }
 
-// A workgroup computes a tile of 64 * F x 64 * F outputs, a wave 32 * F x 32 * F.  The rows' segments of 256 values (a line of
-// 128 bytes each) go from memory straight to LDS, one segment ahead of the one being multiplied, and from there to registers
-// one step (64 values) ahead.  In LDS the eight 16-byte chunks of a line are permuted by the row's number (by exchanging what the
-// lanes of a load ask for), so that 32 lanes reading the same chunk of 32 rows meet every bank equally often.  Lane (r, h)
-// holds 32 values of row r: step s multiplies block s (h = 0) and block 4 + s (h = 1) of the segment, so that a lane's four
-// scales are one word.  Rows of B go in the first operand: a lane then holds four neighbours of a row of Y.
+constexpr int kHalf = kMxSeg / 2;             // values that a pass sums over
+constexpr int kHalfBytes = kHalf / 2;
+constexpr int kRing = 4;                      // passes of operands in LDS
+
+// A workgroup computes a tile of 64 * F x 64 * F outputs, a wave 32 * F x 32 * F.  A pass sums over half a segment, 128 values, in
+// two steps of 64.  The rows' half segments go from memory straight to LDS, three passes ahead of the one being multiplied, and
+// from there to registers a step ahead.  What keeps the matrix cores fed is the order of the instructions: a wave issues them one
+// by one, a load or an LDS read that finds its queue full holds up the matrix instructions behind it, so every two of those are
+// followed by one read for the next step and every few by one load.  In LDS the four 16-byte chunks of a half segment are
+// permuted by the row's number (by exchanging what the lanes of a load ask for), so that 16 lanes reading the same chunk of 16
+// rows meet every bank once.  Lane (r, h) holds 32 values of row r: step s multiplies blocks s (h = 0) and 2 + s (h = 1) of the
+// half segment.  Rows of B go in the first operand: a lane then holds four neighbours of a row of Y.
 template <int F>
 __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx B, const int32_t* __restrict__ offsets, int E, int N,
                                                                        int tiles_n, int type, void* __restrict__ Y, long long ldy) {
     constexpr int kRows = 64 * F;                                // of either operand
-    constexpr int kLoads = 2 * kRows / 8 / 4;                    // instructions of a wave that fetch a segment's codes
-    constexpr int kScaleLoads = 2 * kRows / 32 / 4;              // ... its scales
-    constexpr int kStage = 2 * kRows * (kMxSegBytes + 8);
-    __shared__ __align__(16) uint8_t lds[2 * kStage];
+    constexpr int kLoads = 2 * kRows / 16 / 4;                   // instructions of a wave that fetch a pass's codes
+    constexpr int kScaleLoads = F == 4 ? 2 : 1;                  // ... its scales
+    constexpr int kPass = kLoads + kScaleLoads;
+    constexpr int kStage = 2 * kRows * (kHalfBytes + 4);
+    __shared__ __align__(16) uint8_t lds[kRing * kStage];
     int tile, nt;
     tile_of(blockIdx.x, tiles_n, tile, nt);
     const RowTile t = find_row_tile(offsets, E, A.rows, kRows, tile);
@@ -48,7 +59,6 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
         }
         return;
     }
-    const int segs = A.segs;
     f32x16 acc[F][F];
 #pragma unroll
     for (int x = 0; x < F; ++x)
@@ -65,80 +75,102 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
     const uint8_t* scales = (fetch_b ? B.scales : A.scales) + (size_t)q0 * 8;
     const size_t scale_pitch = (size_t)(fetch_b ? B.rows : A.rows) * 8;
     uint32_t at[kLoads], scale_at[kScaleLoads];
+    const int first = F == 1 ? 0 : (wave & 1) * (kRows / 2);     // (64 scales are one load: both waves fetch them)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        const int row = (wave & 1) * (kRows / 2) + 8 * i + (lane >> 3);
-        at[i] = min(row, last) * pitch + 16 * ((lane & 7) ^ (row & 7));
+        const int row = (wave & 1) * (kRows / 2) + 16 * i + (lane >> 2);
+        at[i] = min(row, last) * pitch + 16 * ((lane & 3) ^ ((row >> 2) & 3));
     }
 #pragma unroll
-    for (int i = 0; i < kScaleLoads; ++i)
-        scale_at[i] = 8 * min((wave & 1) * (kRows / 2) + 32 * i + (lane >> 1), last) + 4 * (lane & 1);
+    for (int i = 0; i < kScaleLoads; ++i) scale_at[i] = 8 * min(first + 64 * i + lane, last);
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds));
-    const uint32_t to = lds0 + wave * kLoads * 1024, scales_to = lds0 + 2 * kRows * kMxSegBytes + wave * kScaleLoads * 256;
+    const uint32_t to = lds0 + wave * kLoads * 1024;
+    const uint32_t scales_to = lds0 + 2 * kRows * kHalfBytes + (fetch_b ? 4 * kRows : 0) + 4 * first;
 
-    auto fetch = [&](int stage, int seg) {
-        const uint8_t* p = codes + (size_t)seg * kMxSegBytes;
-        const uint8_t* q = scales + (size_t)seg * scale_pitch;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load16_to_lds(to + stage + 1024 * i, p, at[i]);
-#pragma unroll
-        for (int i = 0; i < kScaleLoads; ++i) load4_to_lds(scales_to + stage + 256 * i, q, scale_at[i]);
+    // the loads of a pass into a stage, one by one
+    const uint8_t *codes_from, *scales_from;
+    uint32_t codes_to, marks_to;
+    auto aim = [&](int stage, int pass) {
+        codes_from = codes + (size_t)pass * kHalfBytes;
+        scales_from = scales + (size_t)(pass >> 1) * scale_pitch + 4 * (pass & 1);
+        codes_to = to + stage;
+        marks_to = scales_to + stage;
+    };
+    auto fetch = [&](int i) {
+        if (i < kLoads) load16_to_lds(codes_to + 1024 * i, codes_from, at[i]);
+        else load4_to_lds(marks_to + 256 * (i - kLoads), scales_from, scale_at[i - kLoads]);
     };
     u32x4 fm[2][F], fn[2][F];
-    int vm[F], vn[F], next_m[F], next_n[F];
-    const uint8_t* row_m = lds + (wm + r) * kMxSegBytes;
-    const uint8_t* row_n = lds + (kRows + wn + r) * kMxSegBytes;
-    const uint8_t* row_s = lds + 2 * kRows * kMxSegBytes + 8 * r + 4 * h;
-    auto read = [&](int from, int s, u32x4 (&m)[F], u32x4 (&n)[F]) {
-        const int at = from + 16 * ((4 * h + s) ^ (r & 7));
+    int vm[2][F], vn[2][F];
+    const uint8_t* row_m = lds + (wm + r) * kHalfBytes;
+    const uint8_t* row_n = lds + (kRows + wn + r) * kHalfBytes;
+    const uint8_t* marks = lds + 2 * kRows * kHalfBytes + 4 * r + 2 * h;
+    // the reads of a step's operands, one by one, and of a pass's scales
+    auto read = [&](int i, int stage, int s) {
+        const int at = stage + 16 * ((2 * h + s) ^ ((r >> 2) & 3));
+        if (i < F) fn[s][i] = *reinterpret_cast<const u32x4*>(row_n + 32 * i * kHalfBytes + at);
+        else fm[s][i - F] = *reinterpret_cast<const u32x4*>(row_m + 32 * (i - F) * kHalfBytes + at);
+    };
+    auto read_scales = [&](int stage, int (&m)[F], int (&n)[F]) {
 #pragma unroll
         for (int f = 0; f < F; ++f) {
-            m[f] = *reinterpret_cast<const u32x4*>(row_m + 32 * f * kMxSegBytes + at);
-            n[f] = *reinterpret_cast<const u32x4*>(row_n + 32 * f * kMxSegBytes + at);
+            n[f] = *reinterpret_cast<const uint16_t*>(marks + stage + 4 * (kRows + wn + 32 * f));
+            m[f] = *reinterpret_cast<const uint16_t*>(marks + stage + 4 * (wm + 32 * f));
         }
     };
-    auto read_scales = [&](int from, int (&m)[F], int (&n)[F]) {
+    const int passes = 2 * A.segs;
 #pragma unroll
-        for (int f = 0; f < F; ++f) {
-            m[f] = *reinterpret_cast<const int*>(row_s + from + 8 * (wm + 32 * f));
-            n[f] = *reinterpret_cast<const int*>(row_s + from + 8 * (kRows + wn + 32 * f));
-        }
-    };
-    // (reads stay ahead of the products they are hidden under)
-#define APB_MULTIPLY(S, SET)                                                                               \
-    __builtin_amdgcn_sched_barrier(0);                                                                     \
-    _Pragma("unroll") for (int x = 0; x < F; ++x) _Pragma("unroll") for (int y = 0; y < F; ++y)            \
-        acc[x][y] = mfma32<S>(fn[SET][y], fm[SET][x], acc[x][y], vn[y], vm[x]);                              \
-    __builtin_amdgcn_sched_barrier(0)
-    // A segment per pass.  The last step's operands are in registers before the barrier, behind which the segment after next takes
-    // this one's place in LDS and the next one's first operands are read, under the last step's products.  (The last segment is
-    // fetched again where there is none after it: no branch in the loop.)
-    fetch(0, 0);
-    arrived();
-    fetch(kStage, min(1, segs - 1));
-    read(0, 0, fm[0], fn[0]);
-    read_scales(0, vm, vn);
+    for (int p = 0; p < kRing - 1; ++p) {
+        aim(p * kStage, min(p, passes - 1));
+#pragma unroll
+        for (int i = 0; i < kPass; ++i) fetch(i);
+    }
+    arrived<(kRing - 2) * kPass>();
+#pragma unroll
+    for (int i = 0; i < 2 * F; ++i) read(i, 0, 0);
+    read_scales(0, vm[0], vn[0]);
+    aim((kRing - 1) * kStage, min(kRing - 1, passes - 1));
+#pragma unroll
+    for (int i = 0; i < kPass / 2; ++i) fetch(i);                // (the other half under the first step's products)
     int now = 0;
-    for (int seg = 0; seg < segs; ++seg) {
-        read(now, 1, fm[1], fn[1]);
-        APB_MULTIPLY(0, 0);
-        read(now, 2, fm[0], fn[0]);
-        APB_MULTIPLY(1, 1);
-        read(now, 3, fm[1], fn[1]);
-        APB_MULTIPLY(2, 0);
-        arrived();
-        fetch(now, min(seg + 2, segs - 1));
-        now = kStage - now;
-        read(now, 0, fm[0], fn[0]);
-        read_scales(now, next_m, next_n);
-        APB_MULTIPLY(3, 1);
+    // Passes go in pairs, which is how a segment has them.  (Beyond the last pass it is fetched again: no branch in the loop.)
+    for (int pass = 0; pass < passes; pass += 2) {
 #pragma unroll
-        for (int f = 0; f < F; ++f) {
-            vm[f] = next_m[f];
-            vn[f] = next_n[f];
+        for (int half = 0; half < 2; ++half) {
+            const int next = now == (kRing - 1) * kStage ? 0 : now + kStage;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s == 1) {
+                    // this pass's place is free and the next pass is there
+                    arrived<(kRing - 2) * kPass>();
+                    aim(now, min(pass + half + kRing, passes - 1));
+                    read_scales(next, vm[1 - half], vn[1 - half]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < F * F; ++i) {
+                    const int x = i / F, y = i % F;
+                    acc[x][y] = s == 0 ? mfma32<0>(fn[0][y], fm[0][x], acc[x][y], vn[half][y], vm[half][x])
+                                       : mfma32<1>(fn[1][y], fm[1][x], acc[x][y], vn[half][y], vm[half][x]);
+                    // F * F products of a step, 2 * F reads; from one arrived() to the next kPass loads under 2 * F * F products
+                    constexpr int kEach = F * F / (2 * F) > 0 ? F * F / (2 * F) : 1;
+                    if (i % kEach == kEach - 1) {
+#pragma unroll
+                        for (int u = 0; u < (F == 1 ? 2 : 1); ++u)
+                            if (s == 0) read(i / kEach * (F == 1 ? 2 : 1) + u, now, 1);
+                            else read(i / kEach * (F == 1 ? 2 : 1) + u, next, 0);
+                    }
+                    const int slot = (s == 1 ? 0 : F * F) + i;   // products since arrived()
+                    const int begin = slot * kPass / (2 * F * F), end = (slot + 1) * kPass / (2 * F * F);
+#pragma unroll
+                    for (int j = begin; j < end; ++j) fetch(j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            now = next;
         }
     }
-    arrived();                                                   // (nothing is under way to LDS when the workgroup ends)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // (nothing is under way to LDS when the workgroup ends)
 #pragma unroll
     for (int x = 0; x < F; ++x) {
         const int m = wm + 32 * x + r;
