@@ -269,6 +269,56 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
+// ---- from accumulators to rows -----------------------------------------------------------------------------
+
+// Bytes of LDS that a wave needs to write 32 rows of 32 * F outputs.
+template <int F>
+constexpr int kRowsLds = 32 * (32 * F * 4 + 16);
+
+// A wave's 32 rows x 32 * F columns, which its lanes hold as the matrix instruction leaves them (lane (r, h): of row r the columns
+// 32 y + 8 q + 4 h + 0..3), written to memory as rows: through LDS of the wave's own, so that a store covers whole lines of few
+// rows instead of 16 or 32 bytes of each of 32.  Row i < rows goes to out + (first + i) * ld + col; columns from `cols` on are not
+// there.
+template <int F>
+__device__ __forceinline__ void store_tile(const f32x16 (&acc)[F], uint8_t* lds, void* out, int type, long long first, long long ld,
+                                           int rows, long long col, int cols) {
+    const int lane = threadIdx.x & (kWave - 1), r = lane & 31, h = lane >> 5;
+    const int size = type == APB_F32 ? 4 : 2;
+    const int pitch = 32 * F * size + 16;                        // (rows start 4 banks apart)
+#pragma unroll
+    for (int y = 0; y < F; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v[4] = {acc[y][4 * q], acc[y][4 * q + 1], acc[y][4 * q + 2], acc[y][4 * q + 3]};
+            uint8_t* p = lds + r * pitch + (32 * y + 8 * q + 4 * h) * size;
+            if (type == APB_F32) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+            else *reinterpret_cast<u32x2*>(p) = u32x2{pack2(type, v[0], v[1]), pack2(type, v[2], v[3])};
+        }
+    // (the wave's own writes and reads of LDS stay in this order)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const int chunks = 2 * F * size;                             // 16-byte chunks of a row: a power of two up to 64
+    const int chunk = lane & (chunks - 1), each = 16 / size, n = chunk * each;
+    const int have = cols - n;
+    if (have <= 0) return;
+    for (int i = lane / chunks; i < rows; i += kWave / chunks) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + i * pitch + 16 * chunk);
+        const long long at = (first + i) * ld + col + n;
+        if (have >= each) {
+            store16_any(static_cast<uint8_t*>(out) + at * size, v);
+        } else if (type == APB_F32) {
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+                if (q < have) static_cast<uint32_t*>(out)[at + q] = v[q];
+        } else {
+#pragma unroll
+            for (int q = 0; q < 7; ++q)
+                if (q < have) static_cast<uint16_t*>(out)[at + q] = (uint16_t)(v[q / 2] >> (16 * (q & 1)));
+        }
+    }
+}
+
 // ---- groups of rows ---------------------------------------------------------------------------------
 
 // Where a workgroup's tile of rows lies: rows row0 .. row0 + rows - 1 of group e; e == E: the rows that belong to no expert;

@@ -4,7 +4,7 @@
 // values, products of a level and a power of two, are exact in bfloat16, and the bfloat16 matrix instruction multiplies them
 // with G.  A bfloat16 G is taken as it is; a float16 G is the sum of two bfloat16 values, a float32 G of three (each part takes
 // the next 8 bits), and each part goes through the matrix cores, so no bit of G is dropped.
-#include <type_traits>
+#include <utility>
 
 #include "apb_mx4.h"
 
@@ -24,58 +24,114 @@ struct Parts {
 // successive rows meets a bank twice.
 __device__ __forceinline__ int lds_at(int row, int chunk) { return row * kStep + 8 * (chunk ^ ((row + (row >> 3)) & 7)); }
 
-// The bfloat16 parts of eight values, pairs of neighbours in a word: each takes the leading 8 significant bits of what is left
-// (cut off, so that no part is larger than the value and none overflows).  Bits below 2^-133, which bfloat16 has not, are lost.
-template <int TYPE>
-__device__ __forceinline__ void split(const Eight<TYPE>& v, u32x4 (&part)[Parts<TYPE>::n]) {
-    if (TYPE == APB_BF16) {
-        part[0] = v.w[0];
-        return;
-    }
+// N words at any address.
+template <int N>
+struct Words {
+    uint32_t w[N];
+};
+template <int N, class Pointer>
+__device__ __forceinline__ Words<N> load_words(Pointer p) {
+    typedef uint32_t Vector __attribute__((ext_vector_type(N > 4 ? 4 : N)));
+    typedef Vector Any __attribute__((aligned(1)));
+    Words<N> v;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        float x[2];
-        if (TYPE == APB_F32) {
-            const uint32_t a = v.w[TYPE == APB_F32 ? q / 2 : 0][2 * q & 3], c = v.w[TYPE == APB_F32 ? q / 2 : 0][(2 * q & 3) + 1];
-            x[0] = __builtin_bit_cast(float, a);
-            x[1] = __builtin_bit_cast(float, c);
-        } else {
-            const uint32_t pair = v.w[0][q];
-            const f16x2 p = __builtin_bit_cast(f16x2, pair);
-            x[0] = (float)p[0];
-            x[1] = (float)p[1];
+    for (int i = 0; i < N; i += 4) {
+        const Vector x = *(__attribute__((address_space(1))) const Any*)(p + 4 * i);
+#pragma unroll
+        for (int q = 0; q < (N > 4 ? 4 : N); ++q) {
+            if constexpr (N == 1) v.w[0] = __builtin_bit_cast(uint32_t, x);
+            else v.w[i + q] = x[q];
         }
+    }
+    return v;
+}
+// `count` neighbours of a row of G from element `at` on, of which `have` exist; the others are zero
+template <int TYPE, int COUNT>
+__device__ __forceinline__ Words<COUNT * (TYPE == APB_F32 ? 4 : 2) / 4> load_some_words(const void* G, long long at, int have) {
+    constexpr int kSize = TYPE == APB_F32 ? 4 : 2, N = COUNT * kSize / 4;
+    if (have >= COUNT) return load_words<N>((__attribute__((address_space(1))) const uint8_t*)G + at * kSize);
+    Words<N> v;
 #pragma unroll
-        for (int p = 0; p < Parts<TYPE>::n; ++p) {
-            uint32_t bits[2];
+    for (int q = 0; q < N; ++q) {
+        if constexpr (TYPE == APB_F32) {
+            v.w[q] = q < have ? static_cast<const uint32_t*>(G)[at + q] : 0u;
+        } else {
+            const uint16_t* p = static_cast<const uint16_t*>(G) + at + 2 * q;
+            v.w[q] = (2 * q < have ? (uint32_t)p[0] : 0u) | (2 * q + 1 < have ? (uint32_t)p[1] << 16 : 0u);
+        }
+    }
+    return v;
+}
+
+// The bfloat16 parts of 2 * N neighbours, two to a word: each part takes the leading 8 significant bits of what is left (cut off,
+// so that no part is larger than the value and none overflows).  Bits below 2^-133, which bfloat16 has not, are lost.
+template <int TYPE, int N>
+__device__ __forceinline__ void split(const Words<N * (TYPE == APB_F32 ? 2 : 1)>& v, Words<N> (&part)[Parts<TYPE>::n]) {
+    if constexpr (TYPE == APB_BF16) {
+        part[0] = v;
+    } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                bits[i] = __builtin_bit_cast(uint32_t, x[i]);
-                // an infinity is its own first part; a NaN leaves a NaN
-                x[i] = (bits[i] & 0x7fffffffu) == 0x7f800000u ? 0.0f : x[i] - __builtin_bit_cast(float, bits[i] & 0xffff0000u);
+        for (int q = 0; q < N; ++q) {
+            float x[2];
+            if constexpr (TYPE == APB_F32) {
+                x[0] = __builtin_bit_cast(float, v.w[2 * q]);
+                x[1] = __builtin_bit_cast(float, v.w[2 * q + 1]);
+            } else {
+                const f16x2 p = __builtin_bit_cast(f16x2, v.w[q]);
+                x[0] = (float)p[0];
+                x[1] = (float)p[1];
             }
-            part[p][q] = __builtin_amdgcn_perm(bits[1], bits[0], 0x07060302u);
+#pragma unroll
+            for (int p = 0; p < Parts<TYPE>::n; ++p) {
+                uint32_t bits[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    bits[i] = float_bits(x[i]);
+                    x[i] -= __builtin_bit_cast(float, bits[i] & 0xffff0000u);
+                    // an infinity is its own first part; a NaN leaves a NaN
+                    if (p == 0 && (bits[i] & 0x7fffffffu) == 0x7f800000u) x[i] = 0.0f;
+                }
+                part[p].w[q] = __builtin_amdgcn_perm(bits[1], bits[0], 0x07060302u);
+            }
         }
     }
 }
 
-// 8 x 8 transpose into LDS: in[c] holds the values of output indices row .. row+7 at summation index c, two to a word
-__device__ __forceinline__ void store_transposed(uint16_t* tile, int row, int chunk, const u32x4 (&in)[8]) {
+// f(0), f(1), ... f(N - 1), each with its number as a constant
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+
+// One row of an 8 x 2N transpose into LDS: in[c] holds the values of output indices row .. row+2N-1 at summation index c, two to a
+// word; output index row + i gets its eight.
+template <int N>
+__device__ __forceinline__ void store_transposed(uint16_t* tile, int row, int chunk, const Words<N> (&in)[8], int i) {
+    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        u32x4 w;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            w[q] = __builtin_amdgcn_perm(in[2 * q + 1][i / 2], in[2 * q][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
-        *reinterpret_cast<u32x4*>(tile + lds_at(row + i, chunk)) = w;
-    }
+    for (int q = 0; q < 4; ++q)
+        w[q] = __builtin_amdgcn_perm(in[2 * q + 1].w[i / 2], in[2 * q].w[i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+    *reinterpret_cast<u32x4*>(tile + lds_at(row + i, chunk)) = w;
 }
+
+typedef __attribute__((address_space(1))) const uint8_t* Bytes;
+// A base address that the compiler takes as it is, in scalar registers, instead of folding lane offsets into it.
+__device__ __forceinline__ Bytes opaque(Bytes p) {
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+// All of this wave's reads and writes of LDS are done; then so are everybody's.  (Loads to registers stay under way.)
+__device__ __forceinline__ void lds_ready() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // OUT[i, j] = sum_c P[i, c] Q^[c, j] over the 4-bit matrix Q's rows c.
 //   WEIGHT = false: P = G, i = row m of the group, c = n.     WEIGHT = true: P = G^T, i = n, c = row m of the group.
-// A workgroup makes a tile of 64 * F x 64 * F outputs, a wave 32 * F x 32 * F.  A pass sums over 64 indices: while the matrix
-// cores work on one buffer of LDS, the next pass's operands, loaded during the pass before, are brought into the other one as
-// rows of output indices: 8 x 8 blocks transposed in registers, 4-bit values widened to bfloat16.
+// A workgroup makes a tile of 64 * F x 64 * F outputs, a wave 32 * F x 32 * F.  A pass sums over 64 indices in four steps of 16:
+// while the matrix cores work on one buffer of LDS, the next pass's operands, loaded to registers a pass earlier, are brought into
+// the other one as rows of output indices: 8 x 8 blocks transposed in registers, 4-bit values widened to bfloat16.  That work is
+// cut into small tasks, and after every matrix instruction of the first three steps comes one of them and at most one read of the
+// next step's operands, so that nothing waits behind them; the barrier stands before the fourth step, under which the next pass's
+// first operands are read.
 template <int TYPE, bool WEIGHT, int F>
 __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q,
                                                                            const int32_t* __restrict__ offsets, int E, int M, int N,
@@ -111,14 +167,25 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int wi = (wave >> 1) * 32 * F, wj = (wave & 1) * 32 * F;
     const int r = lane & 31, h = lane >> 5;
-    // who brings in what: blocks of 8 x 8 of either operand
-    const int unit = tid & (kTile - 1);
-    const bool has_g = F == 4 || tid < kTile, has_q = F == 4 || (tid >= kTile && tid < 2 * kTile);
-    const int block = 8 * (unit & (kTile / 8 - 1)), chunk = unit / (kTile / 8);       // output indices, summation indices / 8
-    const int line = unit >> 3, part_of_line = unit & 7;                              // G of dX: rows as they lie in memory
-    const uint8_t* q_codes = Q.codes + (j0 + block) / 2;
-    const uint8_t* q_scales = Q.scales + (size_t)((j0 + block) / kMxSeg) * Q.rows * 8 + (j0 + block) % kMxSeg / kMxBlock;
+    // who brings in what: blocks of eight summation indices x W output indices of either operand, as many as there are threads;
+    // of G as it lies in memory for dX, pieces of eight summation indices of kPieces rows
+    constexpr int kSize = TYPE == APB_F32 ? 4 : 2, W = 2 * F, kPieces = 2 * F;
+    const int block = W * (tid & 31), chunk = tid >> 5;
+    const int line = tid >> 3, piece = tid & 7;
     const uint32_t q_pitch = (uint32_t)Q.segs * kMxSegBytes;
+
+    // where a thread loads from: a scalar base and an offset of its own
+    const Bytes g_base = (Bytes)G + ((long long)g_row * ldg + (WEIGHT ? i0 : 0)) * kSize;
+    const Bytes q_base = (Bytes)Q.codes + (size_t)c0 * q_pitch + j0 / 2;
+    const Bytes s_base = (Bytes)Q.scales + ((size_t)(j0 / kMxSeg) * Q.rows + c0) * 8 + j0 % kMxSeg / kMxBlock;
+    const uint32_t q_at = 8 * chunk * q_pitch + block / 2, s_at = 64 * chunk + block / kMxBlock;
+    uint32_t g_at[WEIGHT ? 1 : kPieces];
+    if constexpr (WEIGHT) {
+        g_at[0] = (8 * chunk * (uint32_t)ldg + min(block, N - W - i0)) * kSize;       // (whole blocks: what is not there is not stored)
+    } else {
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u) g_at[u] = (min(u * 32 + line, rows_i - 1) * (uint32_t)ldg + 8 * piece) * kSize;
+    }
 
     f32x16 acc[F][F];
 #pragma unroll
@@ -128,136 +195,158 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.0f;
 
-    Eight<TYPE> g[8];
+    constexpr int kGCount = WEIGHT ? 8 : kPieces, kGWords = (WEIGHT ? W : 8) * kSize / 4;
+    Words<kGWords> g[kGCount];
     uint32_t code[8], scale[8];
-    // WHOLE: the pass lies inside G and Q; otherwise what lies outside is zero
-    auto load = [&](int c, auto whole) {
-        constexpr bool WHOLE = decltype(whole)::value;
-        if (has_g) {
+    Words<W / 2> q_wide[8], g_part[NP][8];
+    // the tasks: load, widen or split, store
+    auto load_g = [&](int c, int u) {
+        const Bytes p = opaque(g_base + (WEIGHT ? (long long)(c + u) * ldg : c) * kSize);
+        g[u] = load_words<kGWords>(p + g_at[WEIGHT ? 0 : u]);
+    };
+    auto codes_at = [&](Bytes p) -> uint32_t {                   // W of them
+        if constexpr (W == 8) return *(__attribute__((address_space(1))) const uint32_t*)p;
+        else if constexpr (W == 4) return *(__attribute__((address_space(1))) const uint16_t*)p;
+        else return *p;
+    };
+    auto load_q = [&](int c, int u) {
+        const Bytes p = opaque(q_base + (size_t)(c + u) * q_pitch), t = opaque(s_base + (size_t)(c + u) * 8);
+        code[u] = codes_at(p + q_at);
+        scale[u] = t[s_at];
+    };
+    auto split_g = [&](uint16_t* buffer, int u) {
+        if constexpr (WEIGHT) {
+            Words<W / 2> v[NP];
+            split<TYPE, W / 2>(g[u], v);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                if (WEIGHT) {
-                    const int cc = c + 8 * chunk + u;
-                    const int col = WHOLE ? min(i0 + block, N - 8) : i0 + block;
-                    const long long at = (long long)(g_row + cc) * ldg + col;
-                    g[u] = WHOLE ? load_eight<TYPE>(G, at) : load_some<TYPE>(G, at, cc < rows_c ? rows_i - block : 0);
-                } else {
-                    const int row = min(u * (kTile / 8) + line, rows_i - 1);
-                    const long long at = (long long)(g_row + row) * ldg + c + 8 * part_of_line;
-                    g[u] = WHOLE ? load_eight<TYPE>(G, at) : load_some<TYPE>(G, at, rows_c - c - 8 * part_of_line);
-                }
-            }
-        }
-        if (has_q) {
+            for (int p = 0; p < NP; ++p) g_part[p][u] = v[p];
+        } else {
+            Words<4> v[NP];
+            split<TYPE, 4>(g[u], v);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int cc = c + 8 * chunk + u;
-                const bool there = WHOLE || cc < rows_c;
-                const size_t row = (size_t)c0 + (WHOLE ? cc : min(cc, rows_c - 1));
-                code[u] = *reinterpret_cast<const uint32_t*>(q_codes + row * q_pitch);
-                scale[u] = q_scales[row * 8];
-                if (!WHOLE) {
-                    code[u] = there ? code[u] : 0u;
-                    scale[u] = there ? scale[u] : 0u;
-                }
-            }
+            for (int p = 0; p < NP; ++p)
+                *reinterpret_cast<u32x4*>(buffer + p * kTile * kStep + lds_at(u * 32 + line, piece)) =
+                    u32x4{v[p].w[0], v[p].w[1], v[p].w[2], v[p].w[3]};
         }
     };
-    auto bring = [&](uint16_t* buffer) {
-        if (has_g) {
-            if (WEIGHT) {
-                u32x4 part[NP][8];
+    auto store_g = [&](uint16_t* buffer, int i) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    u32x4 v[NP];
-                    split<TYPE>(g[u], v);
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) part[p][u] = v[p];
-                }
-#pragma unroll
-                for (int p = 0; p < NP; ++p) store_transposed(buffer + p * kTile * kStep, block, chunk, part[p]);
-            } else {
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    u32x4 v[NP];
-                    split<TYPE>(g[u], v);
-#pragma unroll
-                    for (int p = 0; p < NP; ++p)
-                        *reinterpret_cast<u32x4*>(buffer + p * kTile * kStep + lds_at(u * (kTile / 8) + line, part_of_line)) = v[p];
-                }
-            }
-        }
-        if (has_q) {
-            // (the conversion takes the scale as a float's exponent: every code is right as it is, 0 and NaN's 255 too)
-            u32x4 v[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float s = __builtin_bit_cast(float, scale[u] << 23);
-                v[u][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 0));
-                v[u][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 1));
-                v[u][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 2));
-                v[u][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 3));
-            }
-            store_transposed(buffer + NP * kTile * kStep, block, chunk, v);
+        for (int p = 0; p < NP; ++p) store_transposed(buffer + p * kTile * kStep, block, chunk, g_part[p], i);
+    };
+    auto widen_q = [&](int u) {
+        // (the conversion takes the scale as a float's exponent: every code is right as it is, 0 and NaN's 255 too)
+        const float s = __builtin_bit_cast(float, scale[u] << 23);
+        q_wide[u].w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 0));
+        if constexpr (W >= 4) q_wide[u].w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 1));
+        if constexpr (W >= 8) {
+            q_wide[u].w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 2));
+            q_wide[u].w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 3));
         }
     };
-    auto multiply = [&](const uint16_t* buffer, int ks) {
-        bf16x8 b[F];
-#pragma unroll
-        for (int y = 0; y < F; ++y)
-            b[y] = *reinterpret_cast<const bf16x8*>(buffer + NP * kTile * kStep + lds_at(wj + 32 * y + r, 2 * ks + h));
-#pragma unroll
-        for (int p = 0; p < NP; ++p)
-#pragma unroll
-            for (int x = 0; x < F; ++x) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8*>(buffer + p * kTile * kStep + lds_at(wi + 32 * x + r, 2 * ks + h));
-#pragma unroll
-                for (int y = 0; y < F; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[y], a, acc[x][y], 0, 0, 0);
-            }
+    auto store_q = [&](uint16_t* buffer, int i) { store_transposed(buffer + NP * kTile * kStep, block, chunk, q_wide, i); };
+    constexpr int kTasksQ = 16 + W, kTasks = kTasksQ + 2 * kGCount + (WEIGHT ? W : 0);
+    // task k of bringing in one pass (from registers) and loading the one at c
+    auto task = [&](uint16_t* buffer, int c, auto number) {
+        constexpr int k = number.value, m = k - kTasksQ;
+        if constexpr (k < 8) widen_q(k);
+        else if constexpr (k < 16) load_q(c, k - 8);
+        else if constexpr (k < kTasksQ) store_q(buffer, k - 16);
+        else if constexpr (m < kGCount) split_g(buffer, m);
+        else if constexpr (m < kTasks - kTasksQ - kGCount) store_g(buffer, m - kGCount);
+        else load_g(c, k - (kTasks - kGCount));
     };
-    constexpr std::true_type kWhole{};
-    constexpr std::false_type kEdge{};
+
+    bf16x8 fp[2][NP * F], fq[2][F];
+    const int fq_row = wj + r, fp_row = wi + r;
+    auto read = [&](const uint16_t* buffer, int ks, int set, int i) {
+        if (i < F) fq[set][i] = *reinterpret_cast<const bf16x8*>(buffer + NP * kTile * kStep + lds_at(fq_row + 32 * i, 2 * ks + h));
+        else fp[set][i - F] = *reinterpret_cast<const bf16x8*>(buffer + (i - F) / F * kTile * kStep + lds_at(fp_row + 32 * ((i - F) % F), 2 * ks + h));
+    };
+    auto multiply = [&](int set, int i) {                        // i: part, x, y
+        const int x = i / F % F, y = i % F;
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[set][y], fp[set][i / F], acc[x][y], 0, 0, 0);
+    };
+    constexpr int kReads = F + NP * F, kProducts = NP * F * F;   // of a step
     // passes that lie inside both operands
-    const int whole = !WEIGHT || rows_i == kTile || (N % 8 == 0) ? rows_c / kStep : 0;
+    const int whole = !WEIGHT || rows_i == kTile || (N % W == 0) ? rows_c / kStep : 0;
     if (whole > 0) {
-        load(0, kWhole);
-        bring(lds);
-        load(min(1, whole - 1) * kStep, kWhole);
-        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 8; ++u) load_q(0, u);
+#pragma unroll
+        for (int u = 0; u < kGCount; ++u) load_g(0, u);
+        each<kTasks>([&](auto k) { task(lds, min(1, whole - 1) * kStep, k); });
+        lds_ready();
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) read(lds, 0, 0, i);
         for (int pass = 0; pass < whole; ++pass) {
-            const uint16_t* now = lds + (pass & 1) * kBuffer;
-            multiply(now, 0);
-            multiply(now, 1);
-            bring(lds + (1 - (pass & 1)) * kBuffer);             // (after the last pass: once more, unread)
-            load(min(pass + 2, whole - 1) * kStep, kWhole);
-            multiply(now, 2);
-            multiply(now, 3);
-            __syncthreads();
+            uint16_t* now = lds + (pass & 1) * kBuffer;
+            uint16_t* next = lds + (1 - (pass & 1)) * kBuffer;
+            const int c = min(pass + 2, whole - 1) * kStep;      // (at the end: the last pass again, unread)
+            each<kStep / 16>([&](auto step) {
+                constexpr int ks = step.value, kLast = kStep / 16 - 1;
+                if (ks == kLast) lds_ready();
+                __builtin_amdgcn_sched_barrier(0);
+                each<kProducts>([&](auto product) {
+                    constexpr int i = product.value;
+                    multiply(ks & 1, i);
+                    constexpr int r0 = i * kReads / kProducts, r1 = (i + 1) * kReads / kProducts;
+                    each<r1 - r0>([&](auto j) { read(ks == kLast ? next : now, (ks + 1) & 3, 1 - (ks & 1), r0 + j.value); });
+                    if constexpr (ks < kLast) {
+                        constexpr int slot = ks * kProducts + i, kSlots = kLast * kProducts;
+                        constexpr int t0 = slot * kTasks / kSlots, t1 = (slot + 1) * kTasks / kSlots;
+                        each<t1 - t0>([&](auto j) { task(next, c, std::integral_constant<int, t0 + decltype(j)::value>{}); });
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
         }
+        lds_ready();
     }
+    // and the rest: what lies outside G and Q is zero
     for (int c = whole * kStep; c < rows_c; c += kStep) {
-        load(c, kEdge);
-        bring(lds);
-        __syncthreads();
 #pragma unroll
-        for (int ks = 0; ks < kStep / 16; ++ks) multiply(lds, ks);
-        __syncthreads();
-    }
-    // the 4-bit matrix was the first operand: a lane holds four neighbours of an output row
-#pragma unroll
-    for (int x = 0; x < F; ++x) {
-        const int i = wi + 32 * x + r;
-        if (i >= rows_i) continue;
-        const long long row = (long long)(out_row + i) * ldo;
-#pragma unroll
-        for (int y = 0; y < F; ++y)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int j = j0 + wj + 32 * y + 8 * q + 4 * h;
-                const float v[4] = {acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
-                store4(out, type, row + j, v, K - j);
+        for (int u = 0; u < kGCount; ++u) {
+            if constexpr (WEIGHT) {
+                const int cc = c + 8 * chunk + u;
+                g[u] = load_some_words<TYPE, W>(G, (long long)(g_row + cc) * ldg + i0 + block, cc < rows_c ? rows_i - block : 0);
+            } else {
+                const int row = min(u * 32 + line, rows_i - 1);
+                g[u] = load_some_words<TYPE, 8>(G, (long long)(g_row + row) * ldg + c + 8 * piece, rows_c - c - 8 * piece);
             }
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int cc = c + 8 * chunk + u, row = min(cc, rows_c - 1);
+            code[u] = codes_at(q_base + (size_t)row * q_pitch + block / 2);
+            scale[u] = s_base[(size_t)row * 8 + block / kMxBlock];
+            if (cc >= rows_c) code[u] = scale[u] = 0u;
+        }
+#pragma unroll
+        for (int u = 0; u < kGCount; ++u) split_g(lds, u);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) widen_q(u);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (WEIGHT) store_g(lds, i);
+            store_q(lds, i);
+        }
+        lds_ready();
+#pragma unroll
+        for (int ks = 0; ks < kStep / 16; ++ks) {
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) read(lds, ks, 0, i);
+#pragma unroll
+            for (int i = 0; i < kProducts; ++i) multiply(0, i);
+        }
+        lds_ready();
     }
+    // the 4-bit matrix was the first operand: a lane holds four neighbours of an output row (and every wave is past its reads of
+    // LDS: the loops end with a barrier)
+    static_assert(4 * kRowsLds<F> <= 4 * kBuffer, "a wave's rows pass through its share of the buffers");
+#pragma unroll
+    for (int x = 0; x < F; ++x)
+        store_tile<F>(acc[x], reinterpret_cast<uint8_t*>(lds) + wave * kRowsLds<F>, out, type, out_row + wi + 32 * x, ldo,
+                      min(32, rows_i - wi - 32 * x), j0 + wj, K - j0 - wj);
 }
 
 template <int TYPE, bool WEIGHT, int F>
@@ -294,7 +383,7 @@ int check(const void* G, int g_type, long long ldg, const void* Q, const int32_t
           const void* out, long long ldo) {
     if (!G || !Q || !out) return APB_ERR_NULL;
     if (bad_type(g_type) || bad_type(type)) return APB_ERR_TYPE;
-    if (bad_product(E, M, N, K, offsets) || ldg < N || ldo < K) return APB_ERR_SHAPE;
+    if (bad_product(E, M, N, K, offsets) || ldg < N || ldg > kMxMaxK || ldo < K) return APB_ERR_SHAPE;
     if (!aligned(G, type_size(g_type)) || !aligned(Q, 16) || !aligned(out, type_size(type)) || !aligned(offsets, 4)) return APB_ERR_ALIGN;
     return APB_OK;
 }

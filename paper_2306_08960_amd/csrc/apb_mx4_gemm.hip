@@ -170,21 +170,12 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
             now = next;
         }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // (nothing is under way to LDS when the workgroup ends)
+    arrived<0>();                                                // (nothing is under way to LDS any more)
+    static_assert(4 * kRowsLds<F> <= kRing * kStage, "a wave's rows pass through its share of the ring");
 #pragma unroll
-    for (int x = 0; x < F; ++x) {
-        const int m = wm + 32 * x + r;
-        if (m >= t.rows) continue;
-        const long long row = (long long)(t.row0 + m) * ldy;
-#pragma unroll
-        for (int y = 0; y < F; ++y)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int n = n0 + wn + 32 * y + 8 * g + 4 * h;
-                const float v[4] = {acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-                store4(Y, type, row + n, v, N - n);
-            }
-    }
+    for (int x = 0; x < F; ++x)
+        store_tile<F>(acc[x], lds + wave * kRowsLds<F>, Y, type, t.row0 + wm + 32 * x, ldy, min(32, t.rows - wm - 32 * x), n0 + wn,
+                      N - n0 - wn);
 }
 
 template <int F>
