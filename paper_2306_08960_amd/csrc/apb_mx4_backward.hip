@@ -19,10 +19,14 @@ struct Parts {
     static constexpr int n = TYPE == APB_F32 ? 3 : TYPE == APB_F16 ? 2 : 1;
 };
 
-// LDS tiles: `row` (an output index) has kStep bfloat16 values, in chunks of eight.  The chunks of a row are permuted by the
-// row's number so that neither a wave that writes one chunk of every eighth row nor one that reads the same chunk of 32
-// successive rows meets a bank twice.
-__device__ __forceinline__ int lds_at(int row, int chunk) { return row * kStep + 8 * (chunk ^ ((row + (row >> 3)) & 7)); }
+// LDS tiles: `row` (an output index) has kStep bfloat16 values, 128 bytes, in chunks of eight.  The chunks of a row are permuted by
+// the row's number so that neither eight lanes that write two chunks of four rows some rows apart nor eight that read the same chunk
+// of successive rows meet a bank twice; 32 rows further the permutation is the same.
+constexpr int kRowBytes = 2 * kStep;
+__device__ __forceinline__ uint32_t lds_at(int row, int chunk) { return row * kRowBytes + 16 * (chunk ^ ((row + 2 * (row >> 3)) & 7)); }
+template <class T>
+__device__ __forceinline__ T lds_load(uint32_t at) { return *(__attribute__((address_space(3))) const T*)(uintptr_t)at; }
+__device__ __forceinline__ void lds_store(uint32_t at, const u32x4& v) { *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = v; }
 
 // N words at any address.
 template <int N>
@@ -103,15 +107,15 @@ __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>)
 template <int N, class F>
 __device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
-// One row of an 8 x 2N transpose into LDS: in[c] holds the values of output indices row .. row+2N-1 at summation index c, two to a
-// word; output index row + i gets its eight.
+// One row of an 8 x 2N transpose: in[c] holds the values of 2N output indices at summation index c, two to a word; this is output
+// index i's eight.
 template <int N>
-__device__ __forceinline__ void store_transposed(uint16_t* tile, int row, int chunk, const Words<N> (&in)[8], int i) {
+__device__ __forceinline__ u32x4 transposed(const Words<N> (&in)[8], int i) {
     u32x4 w;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         w[q] = __builtin_amdgcn_perm(in[2 * q + 1].w[i / 2], in[2 * q].w[i / 2], i & 1 ? 0x07060302u : 0x05040100u);
-    *reinterpret_cast<u32x4*>(tile + lds_at(row + i, chunk)) = w;
+    return w;
 }
 
 typedef __attribute__((address_space(1))) const uint8_t* Bytes;
@@ -138,8 +142,8 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
                                                                            int K, int type, void* __restrict__ out, long long ldo) {
     constexpr int NP = Parts<TYPE>::n;
     constexpr int kTile = 64 * F;
-    constexpr int kBuffer = (NP + 1) * kTile * kStep;
-    __shared__ __align__(16) uint16_t lds[2 * kBuffer];
+    constexpr int kPart = kTile * kRowBytes, kBuffer = (NP + 1) * kPart;      // parts of P, then Q
+    __shared__ __align__(16) uint8_t lds[2 * kBuffer];
     const int j0 = blockIdx.y * kTile;
     int i0, rows_i, c0, rows_c, out_row;                         // outputs, summation range (rows of Q from c0 on)
     int g_row;                                                   // row of G that belongs to i0 (or to c0, WEIGHT)
@@ -170,7 +174,7 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
     // who brings in what: blocks of eight summation indices x W output indices of either operand, as many as there are threads;
     // of G as it lies in memory for dX, pieces of eight summation indices of kPieces rows
     constexpr int kSize = TYPE == APB_F32 ? 4 : 2, W = 2 * F, kPieces = 2 * F;
-    const int block = W * (tid & 31), chunk = tid >> 5;
+    const int block = W * ((tid & 3) | (tid >> 1 & 28)), chunk = (tid >> 2 & 1) | tid >> 6 << 1;
     const int line = tid >> 3, piece = tid & 7;
     const uint32_t q_pitch = (uint32_t)Q.segs * kMxSegBytes;
 
@@ -179,12 +183,23 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
     const Bytes q_base = (Bytes)Q.codes + (size_t)c0 * q_pitch + j0 / 2;
     const Bytes s_base = (Bytes)Q.scales + ((size_t)(j0 / kMxSeg) * Q.rows + c0) * 8 + j0 % kMxSeg / kMxBlock;
     const uint32_t q_at = 8 * chunk * q_pitch + block / 2, s_at = 64 * chunk + block / kMxBlock;
+    const uint32_t g_pitch = (uint32_t)ldg * kSize;
     uint32_t g_at[WEIGHT ? 1 : kPieces];
     if constexpr (WEIGHT) {
-        g_at[0] = (8 * chunk * (uint32_t)ldg + min(block, N - W - i0)) * kSize;       // (whole blocks: what is not there is not stored)
+        g_at[0] = 8 * chunk * g_pitch + min(block, N - W - i0) * kSize;               // (whole blocks: what is not there is not stored)
     } else {
 #pragma unroll
-        for (int u = 0; u < kPieces; ++u) g_at[u] = (min(u * 32 + line, rows_i - 1) * (uint32_t)ldg + 8 * piece) * kSize;
+        for (int u = 0; u < kPieces; ++u) g_at[u] = min(u * 32 + line, rows_i - 1) * g_pitch + 8 * piece * kSize;
+    }
+    // where it writes in LDS, and where it reads the operands of a step: in the first buffer, then by turns in either
+    const uint32_t lds0 = lds_address(lds);
+    uint32_t to[W], g_to = lds0 + lds_at(line, piece), p_from[kStep / 16], q_from[kStep / 16];
+#pragma unroll
+    for (int i = 0; i < W; ++i) to[i] = lds0 + lds_at(block + i, chunk);
+#pragma unroll
+    for (int ks = 0; ks < kStep / 16; ++ks) {
+        p_from[ks] = lds0 + lds_at(wi + r, 2 * ks + h);
+        q_from[ks] = lds0 + NP * kPart + lds_at(wj + r, 2 * ks + h);
     }
 
     f32x16 acc[F][F];
@@ -200,21 +215,27 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
     uint32_t code[8], scale[8];
     Words<W / 2> q_wide[8], g_part[NP][8];
     // the tasks: load, widen or split, store
-    auto load_g = [&](int c, int u) {
-        const Bytes p = opaque(g_base + (WEIGHT ? (long long)(c + u) * ldg : c) * kSize);
-        g[u] = load_words<kGWords>(p + g_at[WEIGHT ? 0 : u]);
+    Bytes g_next, q_next, s_next;                                // of the pass to load
+    auto aim = [&](int c) {
+        g_next = g_base + (WEIGHT ? (size_t)c * g_pitch : (size_t)c * kSize);
+        q_next = q_base + (size_t)c * q_pitch;
+        s_next = s_base + (size_t)c * 8;
+    };
+    auto load_g = [&](int u) {
+        g[u] = load_words<kGWords>(opaque(g_next) + g_at[WEIGHT ? 0 : u]);
+        if constexpr (WEIGHT) g_next += g_pitch;
     };
     auto codes_at = [&](Bytes p) -> uint32_t {                   // W of them
         if constexpr (W == 8) return *(__attribute__((address_space(1))) const uint32_t*)p;
         else if constexpr (W == 4) return *(__attribute__((address_space(1))) const uint16_t*)p;
         else return *p;
     };
-    auto load_q = [&](int c, int u) {
-        const Bytes p = opaque(q_base + (size_t)(c + u) * q_pitch), t = opaque(s_base + (size_t)(c + u) * 8);
-        code[u] = codes_at(p + q_at);
-        scale[u] = t[s_at];
+    auto load_q = [&](int u) {
+        code[u] = codes_at(opaque(q_next) + q_at);
+        scale[u] = (opaque(s_next) + s_at)[8 * u];
+        q_next += q_pitch;
     };
-    auto split_g = [&](uint16_t* buffer, int u) {
+    auto split_g = [&](int u) {
         if constexpr (WEIGHT) {
             Words<W / 2> v[NP];
             split<TYPE, W / 2>(g[u], v);
@@ -225,13 +246,12 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
             split<TYPE, 4>(g[u], v);
 #pragma unroll
             for (int p = 0; p < NP; ++p)
-                *reinterpret_cast<u32x4*>(buffer + p * kTile * kStep + lds_at(u * 32 + line, piece)) =
-                    u32x4{v[p].w[0], v[p].w[1], v[p].w[2], v[p].w[3]};
+                lds_store(g_to + p * kPart + u * 32 * kRowBytes, u32x4{v[p].w[0], v[p].w[1], v[p].w[2], v[p].w[3]});
         }
     };
-    auto store_g = [&](uint16_t* buffer, int i) {
+    auto store_g = [&](int i) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p) store_transposed(buffer + p * kTile * kStep, block, chunk, g_part[p], i);
+        for (int p = 0; p < NP; ++p) lds_store(to[i] + p * kPart, transposed(g_part[p], i));
     };
     auto widen_q = [&](int u) {
         // (the conversion takes the scale as a float's exponent: every code is right as it is, 0 and NaN's 255 too)
@@ -243,67 +263,102 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
             q_wide[u].w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 3));
         }
     };
-    auto store_q = [&](uint16_t* buffer, int i) { store_transposed(buffer + NP * kTile * kStep, block, chunk, q_wide, i); };
+    auto store_q = [&](int i) { lds_store(to[i] + NP * kPart, transposed(q_wide, i)); };
     constexpr int kTasksQ = 16 + W, kTasks = kTasksQ + 2 * kGCount + (WEIGHT ? W : 0);
-    // task k of bringing in one pass (from registers) and loading the one at c
-    auto task = [&](uint16_t* buffer, int c, auto number) {
+    // task k of bringing in one pass (from registers) and loading the one aimed at
+    auto task = [&](auto number) {
         constexpr int k = number.value, m = k - kTasksQ;
         if constexpr (k < 8) widen_q(k);
-        else if constexpr (k < 16) load_q(c, k - 8);
-        else if constexpr (k < kTasksQ) store_q(buffer, k - 16);
-        else if constexpr (m < kGCount) split_g(buffer, m);
-        else if constexpr (m < kTasks - kTasksQ - kGCount) store_g(buffer, m - kGCount);
-        else load_g(c, k - (kTasks - kGCount));
+        else if constexpr (k < 16) load_q(k - 8);
+        else if constexpr (k < kTasksQ) store_q(k - 16);
+        else if constexpr (m < kGCount) split_g(m);
+        else if constexpr (m < kTasks - kTasksQ - kGCount) store_g(m - kGCount);
+        else load_g(k - (kTasks - kGCount));
+    };
+    // what a pass in registers has of its first `skip` summation indices becomes zero
+    auto leave_out = [&](int skip) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (8 * chunk + u < skip) code[u] = scale[u] = 0u;
+#pragma unroll
+        for (int u = 0; u < kGCount; ++u)
+#pragma unroll
+            for (int q = 0; q < kGWords; ++q) {
+                if constexpr (WEIGHT) {
+                    if (8 * chunk + u < skip) g[u].w[q] = 0u;
+                } else if constexpr (TYPE == APB_F32) {
+                    if (8 * piece + q < skip) g[u].w[q] = 0u;
+                } else {
+                    if (8 * piece + 2 * q < skip) g[u].w[q] &= 0xffff0000u;
+                    if (8 * piece + 2 * q + 1 < skip) g[u].w[q] = 0u;
+                }
+            }
     };
 
     bf16x8 fp[2][NP * F], fq[2][F];
-    const int fq_row = wj + r, fp_row = wi + r;
-    auto read = [&](const uint16_t* buffer, int ks, int set, int i) {
-        if (i < F) fq[set][i] = *reinterpret_cast<const bf16x8*>(buffer + NP * kTile * kStep + lds_at(fq_row + 32 * i, 2 * ks + h));
-        else fp[set][i - F] = *reinterpret_cast<const bf16x8*>(buffer + (i - F) / F * kTile * kStep + lds_at(fp_row + 32 * ((i - F) % F), 2 * ks + h));
+    auto read = [&](int ks, int set, int i) {
+        if (i < F) fq[set][i] = lds_load<bf16x8>(q_from[ks] + 32 * i * kRowBytes);
+        else fp[set][i - F] = lds_load<bf16x8>(p_from[ks] + (i - F) / F * kPart + (i - F) % F * 32 * kRowBytes);
     };
     auto multiply = [&](int set, int i) {                        // i: part, x, y
         const int x = i / F % F, y = i % F;
         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[set][y], fp[set][i / F], acc[x][y], 0, 0, 0);
     };
     constexpr int kReads = F + NP * F, kProducts = NP * F * F;   // of a step
-    // passes that lie inside both operands
-    const int whole = !WEIGHT || rows_i == kTile || (N % W == 0) ? rows_c / kStep : 0;
-    if (whole > 0) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) load_q(0, u);
-#pragma unroll
-        for (int u = 0; u < kGCount; ++u) load_g(0, u);
-        each<kTasks>([&](auto k) { task(lds, min(1, whole - 1) * kStep, k); });
+    constexpr int kLast = kStep / 16 - 1;
+    // Loads without checks need whole passes and whole blocks of G.  The last pass is the last 64 indices: of those that it shares
+    // with the one before it takes none.
+    if (rows_c >= kStep && (!WEIGHT || rows_i == kTile || N % W == 0)) {
+        const int passes = (rows_c + kStep - 1) / kStep, skip = passes * kStep - rows_c;
+        aim(0);
+        each<8>([&](auto u) { load_q(u.value); });
+        each<kGCount>([&](auto u) { load_g(u.value); });
+        aim(min(kStep, rows_c - kStep));
+        each<kTasks>([&](auto k) { task(k); });
         lds_ready();
+        each<kReads>([&](auto i) { read(0, 0, i.value); });
+        int turn = kBuffer;                                      // from one buffer to the other: writes are one ahead of reads
 #pragma unroll
-        for (int i = 0; i < kReads; ++i) read(lds, 0, 0, i);
-        for (int pass = 0; pass < whole; ++pass) {
-            uint16_t* now = lds + (pass & 1) * kBuffer;
-            uint16_t* next = lds + (1 - (pass & 1)) * kBuffer;
-            const int c = min(pass + 2, whole - 1) * kStep;      // (at the end: the last pass again, unread)
+        for (int i = 0; i < W; ++i) to[i] += turn;
+        g_to += turn;
+        for (int pass = 0; pass < passes; ++pass) {
+            if (pass + 2 == passes && skip > 0) leave_out(skip);
+            aim(min((pass + 2) * kStep, rows_c - kStep));        // (beyond the last pass: that again, unread)
             each<kStep / 16>([&](auto step) {
-                constexpr int ks = step.value, kLast = kStep / 16 - 1;
-                if (ks == kLast) lds_ready();
+                constexpr int ks = step.value;
+                if constexpr (ks == kLast) {
+                    lds_ready();
+                    p_from[0] += turn;
+                    q_from[0] += turn;
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 each<kProducts>([&](auto product) {
                     constexpr int i = product.value;
                     multiply(ks & 1, i);
                     constexpr int r0 = i * kReads / kProducts, r1 = (i + 1) * kReads / kProducts;
-                    each<r1 - r0>([&](auto j) { read(ks == kLast ? next : now, (ks + 1) & 3, 1 - (ks & 1), r0 + j.value); });
+                    each<r1 - r0>([&](auto j) { read((ks + 1) & kLast, 1 - (ks & 1), r0 + j.value); });
                     if constexpr (ks < kLast) {
                         constexpr int slot = ks * kProducts + i, kSlots = kLast * kProducts;
                         constexpr int t0 = slot * kTasks / kSlots, t1 = (slot + 1) * kTasks / kSlots;
-                        each<t1 - t0>([&](auto j) { task(next, c, std::integral_constant<int, t0 + decltype(j)::value>{}); });
+                        each<t1 - t0>([&](auto j) { task(std::integral_constant<int, t0 + decltype(j)::value>{}); });
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 });
             });
+#pragma unroll
+            for (int ks = 1; ks < kStep / 16; ++ks) {
+                p_from[ks] += turn;
+                q_from[ks] += turn;
+            }
+            turn = -turn;
+#pragma unroll
+            for (int i = 0; i < W; ++i) to[i] += turn;
+            g_to += turn;
         }
-        lds_ready();
+        rows_c = 0;
     }
-    // and the rest: what lies outside G and Q is zero
-    for (int c = whole * kStep; c < rows_c; c += kStep) {
+    // few summation indices, or blocks of G that N cuts: what lies outside G and Q is zero
+    for (int c = 0; c < rows_c; c += kStep) {
 #pragma unroll
         for (int u = 0; u < kGCount; ++u) {
             if constexpr (WEIGHT) {
@@ -321,31 +376,28 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
             scale[u] = s_base[(size_t)row * 8 + block / kMxBlock];
             if (cc >= rows_c) code[u] = scale[u] = 0u;
         }
-#pragma unroll
-        for (int u = 0; u < kGCount; ++u) split_g(lds, u);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) widen_q(u);
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if constexpr (WEIGHT) store_g(lds, i);
-            store_q(lds, i);
-        }
+        each<kGCount>([&](auto u) { split_g(u.value); });
+        each<8>([&](auto u) { widen_q(u.value); });
+        each<W>([&](auto i) {
+            if constexpr (WEIGHT) store_g(i.value);
+            store_q(i.value);
+        });
         lds_ready();
 #pragma unroll
         for (int ks = 0; ks < kStep / 16; ++ks) {
 #pragma unroll
-            for (int i = 0; i < kReads; ++i) read(lds, ks, 0, i);
+            for (int i = 0; i < kReads; ++i) read(ks, 0, i);
 #pragma unroll
             for (int i = 0; i < kProducts; ++i) multiply(0, i);
         }
         lds_ready();
     }
-    // the 4-bit matrix was the first operand: a lane holds four neighbours of an output row (and every wave is past its reads of
-    // LDS: the loops end with a barrier)
-    static_assert(4 * kRowsLds<F> <= 4 * kBuffer, "a wave's rows pass through its share of the buffers");
+    lds_ready();
+    // the 4-bit matrix was the first operand: a lane holds four neighbours of an output row
+    static_assert(4 * kRowsLds<F> <= 2 * kBuffer, "a wave's rows pass through its share of the buffers");
 #pragma unroll
     for (int x = 0; x < F; ++x)
-        store_tile<F>(acc[x], reinterpret_cast<uint8_t*>(lds) + wave * kRowsLds<F>, out, type, out_row + wi + 32 * x, ldo,
+        store_tile<F>(acc[x], lds + wave * kRowsLds<F>, out, type, out_row + wi + 32 * x, ldo,
                       min(32, rows_i - wi - 32 * x), j0 + wj, K - j0 - wj);
 }
 
