@@ -149,7 +149,7 @@ def _check(code: int, what: str) -> None:
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     if stream is None:                                   # (the handle alone: a Stream object takes 2.6 us to make)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return int(stream.cuda_stream)
 
 
