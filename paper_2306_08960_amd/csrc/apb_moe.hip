@@ -24,17 +24,28 @@ __device__ __forceinline__ float key_value(uint32_t key) {
     return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
-// Over the lanes of a wave, in six steps of lane-permuted operands; lanes without a partner take 0.
+// Lane permutations of an operand; lanes without a partner take 0.
 template <int CTRL>
 __device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false); }
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-    v = max(v, (uint32_t)from_lane<0x111>((int)v));              // from the lane 1, 2, 4, 8 below, in rows of 16
-    v = max(v, (uint32_t)from_lane<0x112>((int)v));
-    v = max(v, (uint32_t)from_lane<0x114>((int)v));
-    v = max(v, (uint32_t)from_lane<0x118>((int)v));
-    v = max(v, (uint32_t)from_lane<0x142>((int)v));              // from the last lane of the row before
-    v = max(v, (uint32_t)from_lane<0x143>((int)v));              // from lane 31
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, kWave - 1);
+
+// The best of a group of lanes, 16 (a row of the wave) or all 64, in every one of them: rotations within a row, then exchanges.
+template <int LANES, class Best>
+__device__ __forceinline__ uint32_t best_of(uint32_t v, Best best) {
+    v = best(v, (uint32_t)from_lane<0x128>((int)v));             // by 8, 4, 2, 1
+    v = best(v, (uint32_t)from_lane<0x124>((int)v));
+    v = best(v, (uint32_t)from_lane<0x122>((int)v));
+    v = best(v, (uint32_t)from_lane<0x121>((int)v));
+    if (LANES == kWave) {
+        v = best(v, (uint32_t)__shfl_xor((int)v, 16, kWave));
+        v = best(v, (uint32_t)__shfl_xor((int)v, 32, kWave));
+    }
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor(v, d, LANES);
+    return v;
 }
 // sum over this lane and those below
 __device__ __forceinline__ int wave_prefix(int v) {
@@ -52,45 +63,48 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// One wave: the choices of token t.  Lane j gets choice j (-1: none) and its weight; lanes hold EPL experts each, expert
-// 64 * r + lane.
-template <int EPL>
-__device__ __forceinline__ int choose(const void* logits, int type, long long at, int E, int k, float& weight) {
-    const int lane = threadIdx.x & (kWave - 1);
-    uint32_t key[EPL];
+// A group of lanes: the choices of a token.  A lane holds EPL experts, expert LANES * r + lane, and gets the choices lane,
+// lane + LANES ... (-1: none) and their weights.  Every choice is two reductions, the largest key and the lowest index that has it.
+template <int LANES, int EPL>
+__device__ __forceinline__ void choose(const void* logits, int type, long long at, int E, int k, bool there,
+                                       int (&mine)[APB_MOE_MAX_K / LANES + 1], float (&weight)[APB_MOE_MAX_K / LANES + 1]) {
+    constexpr int kSlots = APB_MOE_MAX_K / LANES + 1;
+    const int lane = threadIdx.x & (LANES - 1);
+    uint32_t key[EPL], mine_key[kSlots];
 #pragma unroll
     for (int r = 0; r < EPL; ++r) {
-        const int e = r * kWave + lane;
-        key[r] = e < E ? order_key(load_f32(logits, type, at + e)) : 0u;
+        const int e = r * LANES + lane;
+        key[r] = there && e < E ? order_key(load_f32(logits, type, at + e)) : 0u;
     }
-    int mine = -1;
-    uint32_t mine_key = 0, top = 0;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) mine[i] = -1, mine_key[i] = 0u;
+    uint32_t top = 0;
     for (int j = 0; j < k; ++j) {
         uint32_t best = key[0];
 #pragma unroll
         for (int r = 1; r < EPL; ++r) best = max(best, key[r]);
-        best = wave_max(best);
-        if (best == 0u) break;
-        if (j == 0) top = best;
-        bool found = false;
+        best = best_of<LANES>(best, [](uint32_t a, uint32_t b) { return max(a, b); });
+        uint32_t not_r = 0;                                      // ~expert, so that the lowest is the largest
 #pragma unroll
-        for (int r = 0; r < EPL; ++r) {
-            const unsigned long long hit = __ballot(key[r] == best);
-            if (!found && hit) {
-                const int src = __ffsll((long long)hit) - 1;
-                found = true;
-                if (lane == j) {
-                    mine = r * kWave + src;
-                    mine_key = best;
-                }
-                if (lane == src) key[r] = 0u;
-            }
-        }
+        for (int r = EPL - 1; r >= 0; --r) not_r = key[r] == best ? ~(uint32_t)(r * LANES + lane) : not_r;
+        const uint32_t e = ~best_of<LANES>(not_r, [](uint32_t a, uint32_t b) { return max(a, b); });
+#pragma unroll
+        for (int r = 0; r < EPL; ++r)
+            if (e == (uint32_t)(r * LANES + lane)) key[r] = 0u;
+        if (j == 0) top = best;
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i)
+            if (lane + i * LANES == j && best != 0u) mine[i] = (int)e, mine_key[i] = best;
     }
-    const float p = mine >= 0 ? expf(key_value(mine_key) - key_value(top)) : 0.0f;
-    const float sum = wave_sum(p);
-    weight = mine >= 0 ? p / sum : 0.0f;
-    return mine;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+        weight[i] = mine[i] >= 0 ? expf(key_value(mine_key[i]) - key_value(top)) : 0.0f;
+        sum += weight[i];
+    }
+    sum = group_sum<LANES>(sum);
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) weight[i] = mine[i] >= 0 ? weight[i] / sum : 0.0f;
 }
 
 // What a workgroup knows of its 64 tokens: mask[e], which of them took expert e; drop[t], how many choices of token t there
@@ -126,7 +140,7 @@ __device__ __forceinline__ int start_of(int n, int lane, int& before) {
 
 // ALONE: one workgroup has all tokens and does everything.  Otherwise count[e][workgroup] is written (e == E: slots without
 // an expert) and the scan and placement kernels follow.
-template <int EPL, bool ALONE>
+template <int LANES, int EPL, bool ALONE>
 __global__ __launch_bounds__(kChooseThreads) void k_moe_choose(const void* __restrict__ logits, int type, long long ld, int T, int E,
                                                                int k, int32_t* __restrict__ expert, float* __restrict__ weight,
                                                                int32_t* __restrict__ offsets, int32_t* __restrict__ row_token,
@@ -137,13 +151,20 @@ __global__ __launch_bounds__(kChooseThreads) void k_moe_choose(const void* __res
     __syncthreads();
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int t0 = blockIdx.x * kTokens;
-    for (int i = wave; i < kTokens && t0 + i < T; i += blockDim.x / kWave) {
-        float w;
-        const int e = choose<EPL>(logits, type, (long long)(t0 + i) * ld, E, k, w);
-        if (lane < k) {
-            expert[(t0 + i) * k + lane] = e;
-            weight[(t0 + i) * k + lane] = w;
-            note(b, i, e);
+    for (int first = 0; first < kTokens && t0 + first < T; first += blockDim.x / LANES) {
+        const int i = first + threadIdx.x / LANES, t = t0 + i, l = threadIdx.x & (LANES - 1);
+        const bool there = i < kTokens && t < T;
+        int e[APB_MOE_MAX_K / LANES + 1];
+        float w[APB_MOE_MAX_K / LANES + 1];
+        choose<LANES, EPL>(logits, type, (long long)t * ld, E, k, there, e, w);
+#pragma unroll
+        for (int u = 0; u <= APB_MOE_MAX_K / LANES; ++u) {
+            const int j = l + u * LANES;
+            if (there && j < k) {
+                expert[t * k + j] = e[u];
+                weight[t * k + j] = w[u];
+                note(b, i, e[u]);
+            }
         }
     }
     __syncthreads();
@@ -337,15 +358,15 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* _
     }
 }
 
-template <int EPL>
+template <int LANES, int EPL>
 void launch_choose(int blocks, hipStream_t s, const void* logits, int type, long long ld, int T, int E, int k, int32_t* expert,
                    float* weight, int32_t* offsets, int32_t* row_token, int32_t* slot_row, int32_t* count) {
-    const dim3 threads(std::min(kChooseThreads, kWave * T));
+    const dim3 threads(std::min(kChooseThreads, (LANES * T + kWave - 1) / kWave * kWave));
     if (blocks == 1)
-        hipLaunchKernelGGL((k_moe_choose<EPL, true>), dim3(blocks), threads, 0, s, logits, type, ld, T, E, k, expert, weight, offsets,
+        hipLaunchKernelGGL((k_moe_choose<LANES, EPL, true>), dim3(blocks), threads, 0, s, logits, type, ld, T, E, k, expert, weight, offsets,
                            row_token, slot_row, count);
     else
-        hipLaunchKernelGGL((k_moe_choose<EPL, false>), dim3(blocks), threads, 0, s, logits, type, ld, T, E, k, expert, weight, offsets,
+        hipLaunchKernelGGL((k_moe_choose<LANES, EPL, false>), dim3(blocks), threads, 0, s, logits, type, ld, T, E, k, expert, weight, offsets,
                            row_token, slot_row, count);
 }
 
@@ -377,10 +398,10 @@ int apb_moe_route(const void* logits, int type, long long ld, int T, int E, int 
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const int blocks = route_blocks(T);
     int32_t* count = static_cast<int32_t*>(workspace);
-    if (E <= 64) launch_choose<1>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
-    else if (E <= 128) launch_choose<2>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
-    else if (E <= 256) launch_choose<4>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
-    else launch_choose<16>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    if (E <= 64) launch_choose<16, 4>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else if (E <= 128) launch_choose<16, 8>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else if (E <= 256) launch_choose<16, 16>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
+    else launch_choose<64, 16>(blocks, s, logits, type, ld, T, E, k, expert, weight, offsets, row_token, slot_row, count);
     if (blocks > 1) {
         int32_t* total = count + (size_t)blocks * (E + 1);
         hipLaunchKernelGGL(k_moe_scan, dim3(E + 1), dim3(kWave), 0, s, count, blocks, total);
