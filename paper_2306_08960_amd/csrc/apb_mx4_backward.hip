@@ -11,7 +11,7 @@
 namespace apb {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kGroup = 256;                   // threads that make a tile: four waves
 constexpr int kStep = 64;                     // summed over per pass: a line of 128 bytes of bfloat16 in LDS
 
 template <int TYPE>
@@ -136,14 +136,16 @@ __device__ __forceinline__ void lds_ready() { asm volatile("s_waitcnt lgkmcnt(0)
 // cut into small tasks, and after every matrix instruction of the first three steps comes one of them and at most one read of the
 // next step's operands, so that nothing waits behind them; the barrier stands before the fourth step, under which the next pass's
 // first operands are read.
-template <int TYPE, bool WEIGHT, int F>
-__global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q,
+// Where there are few tiles, GROUPS = 2 groups of four waves work on one, each with buffers of its own and every second pass, and
+// add up at the end, the first group's sums first.
+template <int TYPE, bool WEIGHT, int F, int GROUPS>
+__global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS == 2 ? 2 : 1) void k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q,
                                                                            const int32_t* __restrict__ offsets, int E, int M, int N,
                                                                            int K, int type, void* __restrict__ out, long long ldo) {
     constexpr int NP = Parts<TYPE>::n;
     constexpr int kTile = 64 * F;
     constexpr int kPart = kTile * kRowBytes, kBuffer = (NP + 1) * kPart;      // parts of P, then Q
-    __shared__ __align__(16) uint8_t lds[2 * kBuffer];
+    __shared__ __align__(16) uint8_t shared[GROUPS * 2 * kBuffer];
     const int j0 = blockIdx.y * kTile;
     int i0, rows_i, c0, rows_c, out_row;                         // outputs, summation range (rows of Q from c0 on)
     int g_row;                                                   // row of G that belongs to i0 (or to c0, WEIGHT)
@@ -168,7 +170,9 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
         rows_c = t.e < E ? N : 0;
         out_row = g_row = t.row0;
     }
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kGroup);
+    const int tid = threadIdx.x & (kGroup - 1), lane = tid & (kWave - 1), wave = tid / kWave;
+    uint8_t* lds = shared + group * 2 * kBuffer;
     const int wi = (wave >> 1) * 32 * F, wj = (wave & 1) * 32 * F;
     const int r = lane & 31, h = lane >> 5;
     // who brings in what: blocks of eight summation indices x W output indices of either operand, as many as there are threads;
@@ -192,7 +196,7 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
         for (int u = 0; u < kPieces; ++u) g_at[u] = min(u * 32 + line, rows_i - 1) * g_pitch + 8 * piece * kSize;
     }
     // where it writes in LDS, and where it reads the operands of a step: in the first buffer, then by turns in either
-    const uint32_t lds0 = lds_address(lds);
+    const uint32_t lds0 = lds_address(shared) + group * 2 * kBuffer;
     uint32_t to[W], g_to = lds0 + lds_at(line, piece), p_from[kStep / 16], q_from[kStep / 16];
 #pragma unroll
     for (int i = 0; i < W; ++i) to[i] = lds0 + lds_at(block + i, chunk);
@@ -202,17 +206,25 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
         q_from[ks] = lds0 + NP * kPart + lds_at(wj + r, 2 * ks + h);
     }
 
-    f32x16 acc[F][F];
+    // A matrix instruction waits for the one before it on the same sums: a lone tile of 32 x 32 has several, one for each part of G
+    // or for every second step.
+    constexpr int kSums = F > 1 ? 1 : NP > 1 ? NP : 2;
+    f32x16 sums[kSums][F][F];
 #pragma unroll
-    for (int x = 0; x < F; ++x)
+    for (int n = 0; n < kSums; ++n)
 #pragma unroll
-        for (int y = 0; y < F; ++y)
+        for (int x = 0; x < F; ++x)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.0f;
+            for (int y = 0; y < F; ++y)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) sums[n][x][y][q] = 0.0f;
+    f32x16(&acc)[F][F] = sums[0];
 
     constexpr int kGCount = WEIGHT ? 8 : kPieces, kGWords = (WEIGHT ? W : 8) * kSize / 4;
-    Words<kGWords> g[kGCount];
-    uint32_t code[8], scale[8];
+    // The smallest tiles' passes are shorter than the way from memory: they are loaded one further ahead.
+    constexpr int kSets = F == 1 ? 2 : 1;
+    Words<kGWords> g[kSets][kGCount];
+    uint32_t code[kSets][8], scale[kSets][8];
     Words<W / 2> q_wide[8], g_part[NP][8];
     // the tasks: load, widen or split, store
     Bytes g_next, q_next, s_next;                                // of the pass to load
@@ -221,8 +233,8 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
         q_next = q_base + (size_t)c * q_pitch;
         s_next = s_base + (size_t)c * 8;
     };
-    auto load_g = [&](int u) {
-        g[u] = load_words<kGWords>(opaque(g_next) + g_at[WEIGHT ? 0 : u]);
+    auto load_g = [&](int set, int u) {
+        g[set][u] = load_words<kGWords>(opaque(g_next) + g_at[WEIGHT ? 0 : u]);
         if constexpr (WEIGHT) g_next += g_pitch;
     };
     auto codes_at = [&](Bytes p) -> uint32_t {                   // W of them
@@ -230,20 +242,20 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
         else if constexpr (W == 4) return *(__attribute__((address_space(1))) const uint16_t*)p;
         else return *p;
     };
-    auto load_q = [&](int u) {
-        code[u] = codes_at(opaque(q_next) + q_at);
-        scale[u] = (opaque(s_next) + s_at)[8 * u];
+    auto load_q = [&](int set, int u) {
+        code[set][u] = codes_at(opaque(q_next) + q_at);
+        scale[set][u] = (opaque(s_next) + s_at)[8 * u];
         q_next += q_pitch;
     };
-    auto split_g = [&](int u) {
+    auto split_g = [&](int set, int u) {
         if constexpr (WEIGHT) {
             Words<W / 2> v[NP];
-            split<TYPE, W / 2>(g[u], v);
+            split<TYPE, W / 2>(g[set][u], v);
 #pragma unroll
             for (int p = 0; p < NP; ++p) g_part[p][u] = v[p];
         } else {
             Words<4> v[NP];
-            split<TYPE, 4>(g[u], v);
+            split<TYPE, 4>(g[set][u], v);
 #pragma unroll
             for (int p = 0; p < NP; ++p)
                 lds_store(g_to + p * kPart + u * 32 * kRowBytes, u32x4{v[p].w[0], v[p].w[1], v[p].w[2], v[p].w[3]});
@@ -253,44 +265,44 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
 #pragma unroll
         for (int p = 0; p < NP; ++p) lds_store(to[i] + p * kPart, transposed(g_part[p], i));
     };
-    auto widen_q = [&](int u) {
+    auto widen_q = [&](int set, int u) {
         // (the conversion takes the scale as a float's exponent: every code is right as it is, 0 and NaN's 255 too)
-        const float s = __builtin_bit_cast(float, scale[u] << 23);
-        q_wide[u].w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 0));
-        if constexpr (W >= 4) q_wide[u].w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 1));
+        const float s = __builtin_bit_cast(float, scale[set][u] << 23);
+        q_wide[u].w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 0));
+        if constexpr (W >= 4) q_wide[u].w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 1));
         if constexpr (W >= 8) {
-            q_wide[u].w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 2));
-            q_wide[u].w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 3));
+            q_wide[u].w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 2));
+            q_wide[u].w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 3));
         }
     };
     auto store_q = [&](int i) { lds_store(to[i] + NP * kPart, transposed(q_wide, i)); };
     constexpr int kTasksQ = 16 + W, kTasks = kTasksQ + 2 * kGCount + (WEIGHT ? W : 0);
-    // task k of bringing in one pass (from registers) and loading the one aimed at
-    auto task = [&](auto number) {
+    // task k of bringing in one pass (from a set of registers) and loading the one aimed at into it
+    auto task = [&](int set, auto number) {
         constexpr int k = number.value, m = k - kTasksQ;
-        if constexpr (k < 8) widen_q(k);
-        else if constexpr (k < 16) load_q(k - 8);
+        if constexpr (k < 8) widen_q(set, k);
+        else if constexpr (k < 16) load_q(set, k - 8);
         else if constexpr (k < kTasksQ) store_q(k - 16);
-        else if constexpr (m < kGCount) split_g(m);
+        else if constexpr (m < kGCount) split_g(set, m);
         else if constexpr (m < kTasks - kTasksQ - kGCount) store_g(m - kGCount);
-        else load_g(k - (kTasks - kGCount));
+        else load_g(set, k - (kTasks - kGCount));
     };
     // what a pass in registers has of its first `skip` summation indices becomes zero
-    auto leave_out = [&](int skip) {
+    auto leave_out = [&](int set, int skip) {
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            if (8 * chunk + u < skip) code[u] = scale[u] = 0u;
+            if (8 * chunk + u < skip) code[set][u] = scale[set][u] = 0u;
 #pragma unroll
         for (int u = 0; u < kGCount; ++u)
 #pragma unroll
             for (int q = 0; q < kGWords; ++q) {
                 if constexpr (WEIGHT) {
-                    if (8 * chunk + u < skip) g[u].w[q] = 0u;
+                    if (8 * chunk + u < skip) g[set][u].w[q] = 0u;
                 } else if constexpr (TYPE == APB_F32) {
-                    if (8 * piece + q < skip) g[u].w[q] = 0u;
+                    if (8 * piece + q < skip) g[set][u].w[q] = 0u;
                 } else {
-                    if (8 * piece + 2 * q < skip) g[u].w[q] &= 0xffff0000u;
-                    if (8 * piece + 2 * q + 1 < skip) g[u].w[q] = 0u;
+                    if (8 * piece + 2 * q < skip) g[set][u].w[q] &= 0xffff0000u;
+                    if (8 * piece + 2 * q + 1 < skip) g[set][u].w[q] = 0u;
                 }
             }
     };
@@ -300,30 +312,37 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
         if (i < F) fq[set][i] = lds_load<bf16x8>(q_from[ks] + 32 * i * kRowBytes);
         else fp[set][i - F] = lds_load<bf16x8>(p_from[ks] + (i - F) / F * kPart + (i - F) % F * 32 * kRowBytes);
     };
-    auto multiply = [&](int set, int i) {                        // i: part, x, y
-        const int x = i / F % F, y = i % F;
-        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[set][y], fp[set][i / F], acc[x][y], 0, 0, 0);
+    auto multiply = [&](int ks, int i) {                         // i: part, x, y
+        const int x = i / F % F, y = i % F, set = ks & 1, n = F > 1 ? 0 : NP > 1 ? i : ks >> 1;
+        sums[n][x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[set][y], fp[set][i / F], sums[n][x][y], 0, 0, 0);
     };
     constexpr int kReads = F + NP * F, kProducts = NP * F * F;   // of a step
     constexpr int kLast = kStep / 16 - 1;
     // Loads without checks need whole passes and whole blocks of G.  The last pass is the last 64 indices: of those that it shares
     // with the one before it takes none.
     if (rows_c >= kStep && (!WEIGHT || rows_i == kTile || N % W == 0)) {
-        const int passes = (rows_c + kStep - 1) / kStep, skip = passes * kStep - rows_c;
-        aim(0);
-        each<8>([&](auto u) { load_q(u.value); });
-        each<kGCount>([&](auto u) { load_g(u.value); });
-        aim(min(kStep, rows_c - kStep));
-        each<kTasks>([&](auto k) { task(k); });
+        const int passes = (rows_c + kStep - 1) / kStep, rounds = (passes + GROUPS - 1) / GROUPS;
+        // of this group's n-th pass: where it begins, and how many of its indices others have
+        auto begin = [&](int n) { return min((n * GROUPS + group) * kStep, rows_c - kStep); };
+        auto known = [&](int n) { return min((n * GROUPS + group) * kStep - begin(n), kStep); };
+        each<kSets>([&](auto set) {
+            aim(begin(set.value));
+            each<8>([&](auto u) { load_q(set.value, u.value); });
+            each<kGCount>([&](auto u) { load_g(set.value, u.value); });
+        });
+        if (known(0) > 0) leave_out(0, known(0));
+        aim(begin(kSets));
+        each<kTasks>([&](auto k) { task(0, k); });
         lds_ready();
         each<kReads>([&](auto i) { read(0, 0, i.value); });
         int turn = kBuffer;                                      // from one buffer to the other: writes are one ahead of reads
 #pragma unroll
         for (int i = 0; i < W; ++i) to[i] += turn;
         g_to += turn;
-        for (int pass = 0; pass < passes; ++pass) {
-            if (pass + 2 == passes && skip > 0) leave_out(skip);
-            aim(min((pass + 2) * kStep, rows_c - kStep));        // (beyond the last pass: that again, unread)
+        // multiplies the group's pass number `round`, brings in the next one and loads the one kSets further
+        auto run = [&](int round, int set) {
+            if (round + 2 == rounds && known(round + 1) > 0) leave_out(set, known(round + 1));
+            aim(begin(round + 1 + kSets));                       // (beyond the last pass: that again, unread)
             each<kStep / 16>([&](auto step) {
                 constexpr int ks = step.value;
                 if constexpr (ks == kLast) {
@@ -334,13 +353,13 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
                 __builtin_amdgcn_sched_barrier(0);
                 each<kProducts>([&](auto product) {
                     constexpr int i = product.value;
-                    multiply(ks & 1, i);
+                    multiply(ks, i);
                     constexpr int r0 = i * kReads / kProducts, r1 = (i + 1) * kReads / kProducts;
                     each<r1 - r0>([&](auto j) { read((ks + 1) & kLast, 1 - (ks & 1), r0 + j.value); });
                     if constexpr (ks < kLast) {
                         constexpr int slot = ks * kProducts + i, kSlots = kLast * kProducts;
                         constexpr int t0 = slot * kTasks / kSlots, t1 = (slot + 1) * kTasks / kSlots;
-                        each<t1 - t0>([&](auto j) { task(std::integral_constant<int, t0 + decltype(j)::value>{}); });
+                        each<t1 - t0>([&](auto j) { task(set, std::integral_constant<int, t0 + decltype(j)::value>{}); });
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 });
@@ -354,30 +373,40 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
 #pragma unroll
             for (int i = 0; i < W; ++i) to[i] += turn;
             g_to += turn;
+        };
+        if constexpr (kSets == 1) {
+            for (int round = 0; round < rounds; ++round) run(round, 0);
+        } else {
+            for (int round = 0; round < rounds; round += 2) {
+                run(round, 1);
+                if (round + 1 == rounds) break;
+                run(round + 1, 0);
+            }
         }
         rows_c = 0;
     }
     // few summation indices, or blocks of G that N cuts: what lies outside G and Q is zero
-    for (int c = 0; c < rows_c; c += kStep) {
+    for (int round = 0; round * GROUPS * kStep < rows_c; ++round) {
+        const int c = (round * GROUPS + group) * kStep;
 #pragma unroll
         for (int u = 0; u < kGCount; ++u) {
             if constexpr (WEIGHT) {
                 const int cc = c + 8 * chunk + u;
-                g[u] = load_some_words<TYPE, W>(G, (long long)(g_row + cc) * ldg + i0 + block, cc < rows_c ? rows_i - block : 0);
+                g[0][u] = load_some_words<TYPE, W>(G, (long long)(g_row + cc) * ldg + i0 + block, cc < rows_c ? rows_i - block : 0);
             } else {
                 const int row = min(u * 32 + line, rows_i - 1);
-                g[u] = load_some_words<TYPE, 8>(G, (long long)(g_row + row) * ldg + c + 8 * piece, rows_c - c - 8 * piece);
+                g[0][u] = load_some_words<TYPE, 8>(G, (long long)(g_row + row) * ldg + c + 8 * piece, rows_c - c - 8 * piece);
             }
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             const int cc = c + 8 * chunk + u, row = min(cc, rows_c - 1);
-            code[u] = codes_at(q_base + (size_t)row * q_pitch + block / 2);
-            scale[u] = s_base[(size_t)row * 8 + block / kMxBlock];
-            if (cc >= rows_c) code[u] = scale[u] = 0u;
+            code[0][u] = codes_at(q_base + (size_t)row * q_pitch + block / 2);
+            scale[0][u] = s_base[(size_t)row * 8 + block / kMxBlock];
+            if (cc >= rows_c) code[0][u] = scale[0][u] = 0u;
         }
-        each<kGCount>([&](auto u) { split_g(u.value); });
-        each<8>([&](auto u) { widen_q(u.value); });
+        each<kGCount>([&](auto u) { split_g(0, u.value); });
+        each<8>([&](auto u) { widen_q(0, u.value); });
         each<W>([&](auto i) {
             if constexpr (WEIGHT) store_g(i.value);
             store_q(i.value);
@@ -388,11 +417,35 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
 #pragma unroll
             for (int i = 0; i < kReads; ++i) read(ks, 0, i);
 #pragma unroll
-            for (int i = 0; i < kProducts; ++i) multiply(0, i);
+            for (int i = 0; i < kProducts; ++i) multiply(2 * (ks & 1), i);
         }
         lds_ready();
     }
+#pragma unroll
+    for (int n = 1; n < kSums; ++n)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[0][0][q] += sums[n][0][0][q];
     lds_ready();
+    if constexpr (GROUPS == 2) {
+        static_assert(F * F * 16 * 4 * kGroup <= 2 * kBuffer, "a group's sums fit its buffers");
+        float* theirs = reinterpret_cast<float*>(shared) + tid * 4;
+#pragma unroll
+        for (int i = 0; i < F * F * 4; ++i) {
+            const f32x16& a = acc[i / 4 / F][i / 4 % F];
+            const int q = 4 * (i & 3);
+            if (group == 1) *reinterpret_cast<f32x4*>(theirs + i * 4 * kGroup) = f32x4{a[q], a[q + 1], a[q + 2], a[q + 3]};
+        }
+        lds_ready();
+        if (group == 0)
+#pragma unroll
+            for (int i = 0; i < F * F * 4; ++i) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(theirs + i * 4 * kGroup);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[i / 4 / F][i / 4 % F][4 * (i & 3) + q] += v[q];
+            }
+        lds_ready();
+        if (group == 1) return;
+    }
     // the 4-bit matrix was the first operand: a lane holds four neighbours of an output row
     static_assert(4 * kRowsLds<F> <= 2 * kBuffer, "a wave's rows pass through its share of the buffers");
 #pragma unroll
@@ -401,24 +454,26 @@ __global__ __launch_bounds__(kThreads, F * Parts<TYPE>::n <= 2 ? 2 : 1) void k_m
                       min(32, rows_i - wi - 32 * x), j0 + wj, K - j0 - wj);
 }
 
-template <int TYPE, bool WEIGHT, int F>
+template <int TYPE, bool WEIGHT, int F, int GROUPS>
 void launch_tiles(const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type, void* out,
                   long long ldo, hipStream_t s) {
     constexpr int kTile = 64 * F;
     const unsigned tiles_i = (unsigned)(WEIGHT ? (N + kTile - 1) / kTile : max_row_tiles(M, E, offsets != nullptr, kTile));
     const dim3 grid(tiles_i, (unsigned)((K + kTile - 1) / kTile), (unsigned)(WEIGHT ? E : 1));
-    hipLaunchKernelGGL((k_mx4_backward<TYPE, WEIGHT, F>), grid, dim3(kThreads), 0, s, G, ldg, Q, offsets, E, M, N, K, type, out, ldo);
+    hipLaunchKernelGGL((k_mx4_backward<TYPE, WEIGHT, F, GROUPS>), grid, dim3(kGroup * GROUPS), 0, s, G, ldg, Q, offsets, E, M, N, K, type,
+                       out, ldo);
 }
 
 template <int TYPE, bool WEIGHT>
 void launch_type(const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type, void* out,
                  long long ldo, hipStream_t s) {
-    const long long big = ((long long)(WEIGHT ? N : M) + 255) / 256 * ((K + 255) / 256) * (WEIGHT ? E : 1);
+    auto tiles = [&](int side) { return ((long long)(WEIGHT ? N : M) + side - 1) / side * ((K + side - 1) / side) * (WEIGHT ? E : 1); };
     if constexpr (TYPE == APB_BF16) {
-        if (big >= 192) return launch_tiles<TYPE, WEIGHT, 4>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+        if (tiles(256) >= 192) return launch_tiles<TYPE, WEIGHT, 4, 1>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+        if (tiles(128) >= 192 && tiles(128) <= 256) return launch_tiles<TYPE, WEIGHT, 2, 2>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
     }
-    if (big * 4 >= 192) return launch_tiles<TYPE, WEIGHT, 2>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
-    launch_tiles<TYPE, WEIGHT, 1>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+    if (tiles(256) >= 48) return launch_tiles<TYPE, WEIGHT, 2, 1>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+    launch_tiles<TYPE, WEIGHT, 1, 2>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
 }
 
 template <bool WEIGHT>
