@@ -396,7 +396,7 @@ int apb_moe_route(const void* logits, int type, long long ld, int T, int E, int 
                   int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* workspace, void* stream);
 
 /* dlogits[t, expert[t,j]] = weight[t,j] * (dweight[t,j] - sum_i weight[t,i] * dweight[t,i]), 0 elsewhere; expert,
- * weight as apb_moe_route left them, dweight DEVICE, T*k floats.  dlogits: T rows of E elements of `type`, ld apart. */
+ * weight as apb_moe_route left them (a token's weights sum to 1), dweight DEVICE, T*k floats.  dlogits: T rows of E elements of `type`, ld apart. */
 int apb_moe_route_backward(const int32_t* expert, const float* weight, const float* dweight, int T, int E, int k, int type,
                            void* dlogits, long long ld, void* stream);
 

@@ -269,8 +269,10 @@ __global__ __launch_bounds__(kThreads) void k_moe_route_backward(const int32_t* 
         const int e = slot ? expert[t * k + lane] : -1;
         const bool there = e >= 0 && e < E;
         const float w = there ? weight[t * k + lane] : 0.0f, d = there ? dweight[t * k + lane] : 0.0f;
-        const float inner = wave_sum(w * d);
-        if (there) row[e] = w * (d - inner);
+        // d_j - sum w_i d_i = sum w_i (d_j - d_i), as the weights sum to 1: nothing is lost where one of them is nearly that
+        float inner = 0.0f;
+        for (int i = 0; i < k; ++i) inner = fmaf(__shfl(w, i, kWave), d - __shfl(d, i, kWave), inner);
+        if (there) row[e] = w * inner;
     }
     __syncthreads();
     if (t < T)
