@@ -370,11 +370,16 @@ int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const 
  *   G   DEVICE, M rows of N elements of g_type, ldg <= 2^22 apart.
  *   W   DEVICE, 4-bit matrix of E*N rows of K.     X  DEVICE, 4-bit matrix of M rows of K.
  *   dX  DEVICE, M rows of K elements of `type`, ldx apart, fully overwritten.
- *   dW  DEVICE, E*N rows of K elements of `type`, ldw apart, fully overwritten (0 for an expert without rows). */
+ *   dW  DEVICE, E*N rows of K elements of `type`, ldw apart, fully overwritten (0 for an expert without rows).
+ *   workspace, workspace_bytes  optional DEVICE scratch (NULL, 0: none), 4-byte aligned.  Where the outputs are few and the sums
+ *       long, workgroups share a sum and join it in a fixed order through it: as many bytes as the functions below
+ *       say (0: no use for any) or the sums are not shared.  `grouped`: whether offsets will be given. */
+size_t apb_mx4_backward_input_workspace_bytes(int g_type, int grouped, int E, int M, int N, int K);
+size_t apb_mx4_backward_weight_workspace_bytes(int g_type, int grouped, int E, int M, int N, int K);
 int apb_mx4_backward_input(const void* G, int g_type, long long ldg, const void* W, const int32_t* offsets, int E, int M,
-                           int N, int K, int type, void* dX, long long ldx, void* stream);
+                           int N, int K, int type, void* dX, long long ldx, void* workspace, size_t workspace_bytes, void* stream);
 int apb_mx4_backward_weight(const void* G, int g_type, long long ldg, const void* X, const int32_t* offsets, int E, int M,
-                            int N, int K, int type, void* dW, long long ldw, void* stream);
+                            int N, int K, int type, void* dW, long long ldw, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Routing tokens to experts ---------------------------------------------------------------------
  *

@@ -26,7 +26,8 @@ EXPORTS = (
     "apb_train_workspace_bytes", "apb_train_forward", "apb_train_backward",
     "apb_probe_out_bytes", "apb_probe_rate",
     "apb_mx4_bytes", "apb_mx4_quantize", "apb_mx4_dequantize", "apb_mx4_gemm", "apb_mx4_linear",
-    "apb_mx4_backward_input", "apb_mx4_backward_weight",
+    "apb_mx4_backward_input", "apb_mx4_backward_weight", "apb_mx4_backward_input_workspace_bytes",
+    "apb_mx4_backward_weight_workspace_bytes",
     "apb_moe_workspace_bytes", "apb_moe_route", "apb_moe_route_backward", "apb_moe_combine", "apb_moe_combine_backward",
     "apb_strerror", "apb_last_hip_error",
 )
@@ -117,12 +118,15 @@ def load() -> ctypes.CDLL:
     lib.apb_mx4_bytes.restype = ctypes.c_size_t
     lib.apb_moe_workspace_bytes.argtypes = [ci, ci, ci]
     lib.apb_moe_workspace_bytes.restype = ctypes.c_size_t
+    for name in ("apb_mx4_backward_input_workspace_bytes", "apb_mx4_backward_weight_workspace_bytes"):
+        getattr(lib, name).argtypes = [ci] * 6
+        getattr(lib, name).restype = ctypes.c_size_t
     for name, args in (("apb_mx4_quantize", [vp, ci, ll, ll, ci, vp, ci, ci, vp, vp]),
                        ("apb_mx4_dequantize", [vp, ci, ci, ci, vp, ll, vp]),
                        ("apb_mx4_gemm", [vp, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp]),
                        ("apb_mx4_linear", [vp, ci, ll, ci, vp, vp, vp, ci, ci, ci, ci, vp, ci, vp, ll, vp]),
-                       ("apb_mx4_backward_input", [vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp]),
-                       ("apb_mx4_backward_weight", [vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp]),
+                       ("apb_mx4_backward_input", [vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp, ctypes.c_size_t, vp]),
+                       ("apb_mx4_backward_weight", [vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp, ctypes.c_size_t, vp]),
                        ("apb_moe_route", [vp, ci, ll, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp]),
                        ("apb_moe_route_backward", [vp, vp, vp, ci, ci, ci, ci, vp, ll, vp]),
                        ("apb_moe_combine", [vp, ci, ll, vp, vp, ci, ci, ci, vp, ll, vp]),
@@ -668,6 +672,12 @@ def _mx4_ptr(mx: torch.Tensor, rows: int, K: int, name: str) -> int:
     return _array(mx, torch.uint8, None, name)
 
 
+def _used_on(t: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream]) -> None:
+    """Memory that this module made for a call on a stream of the caller's: not handed out again before that call is through."""
+    if t is not None and stream is not None:
+        t.record_stream(stream)
+
+
 def _experts(offsets: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
     """(pointer, number of groups) of the offsets; (None, 1) without."""
     if offsets is None:
@@ -722,37 +732,67 @@ def apb_mx4_linear(X: torch.Tensor, W: torch.Tensor, N: int, dtype: Optional[tor
     rows_in, K = X.shape
     M = rows_in if rows_from is None else rows_from.numel()
     off, E = _experts(offsets)
+    made = None
     if scratch is None:
-        scratch = alloc_mx4(M, K, X.device)
+        scratch = made = alloc_mx4(M, K, X.device)
     Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y")
     _check(load().apb_mx4_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), _mx4_ptr(W, E * N, K, "W"), off, E, M,
                                  int(N), K, _mx4_ptr(scratch, M, K, "scratch"), yt, yp, ldy, _stream(stream)), "apb_mx4_linear")
+    _used_on(made, stream)
     return Y
+
+
+def apb_mx4_backward_input_workspace_bytes(dtype: torch.dtype, grouped: bool, E: int, M: int, N: int, K: int) -> int:
+    """Bytes of scratch that apb_mx4_backward_input has a use for, with a gradient of type dtype."""
+    return int(load().apb_mx4_backward_input_workspace_bytes(_type(dtype), int(grouped), E, M, N, K))
+
+
+def apb_mx4_backward_weight_workspace_bytes(dtype: torch.dtype, grouped: bool, E: int, M: int, N: int, K: int) -> int:
+    return int(load().apb_mx4_backward_weight_workspace_bytes(_type(dtype), int(grouped), E, M, N, K))
+
+
+def _scratch(given: Optional[torch.Tensor], need: int, like: torch.Tensor):
+    """(tensor to keep, pointer, bytes) of an optional workspace; a new one where none is given and one is of use."""
+    if given is None:
+        if need == 0:
+            return None, None, 0
+        given = like.new_empty(need, dtype=torch.uint8)
+    if not given.is_cuda or not given.is_contiguous():
+        raise TypeError("workspace must be a contiguous tensor on the GPU")
+    return given, given.data_ptr(), given.numel() * given.element_size()
 
 
 def apb_mx4_backward_input(G: torch.Tensor, W: torch.Tensor, K: int, dtype: Optional[torch.dtype] = None,
                            dX: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None,
                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """dX[M, K] = G W^ for the gradient G [M, N] of the product with the 4-bit weights W; dX has G's type by default."""
     gp, gt, ldg = _matrix(G, "G")
     M, N = G.shape
     off, E = _experts(offsets)
+    wp = _mx4_ptr(W, E * N, K, "W")
     dX, xp, xt, ldx = _result(dX, (M, K), dtype or G.dtype, G, "dX")
-    _check(load().apb_mx4_backward_input(gp, gt, ldg, _mx4_ptr(W, E * N, K, "W"), off, E, M, N, int(K), xt, xp, ldx, _stream(stream)),
-           "apb_mx4_backward_input")
+    lib = load()
+    keep, sp, sb = _scratch(workspace, lib.apb_mx4_backward_input_workspace_bytes(gt, off is not None, E, M, N, K), G)
+    _check(lib.apb_mx4_backward_input(gp, gt, ldg, wp, off, E, M, N, K, xt, xp, ldx, sp, sb, _stream(stream)), "apb_mx4_backward_input")
+    _used_on(keep, stream)
     return dX
 
 
 def apb_mx4_backward_weight(G: torch.Tensor, X: torch.Tensor, K: int, dtype: torch.dtype = torch.float32,
                             dW: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None,
                             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """dW[E*N, K] = G^T X^ (per expert with offsets) for the 4-bit activations X of the product."""
     gp, gt, ldg = _matrix(G, "G")
     M, N = G.shape
     off, E = _experts(offsets)
+    xp = _mx4_ptr(X, M, K, "X")
     dW, wp, wt, ldw = _result(dW, (E * N, K), dtype, G, "dW")
-    _check(load().apb_mx4_backward_weight(gp, gt, ldg, _mx4_ptr(X, M, K, "X"), off, E, M, N, int(K), wt, wp, ldw, _stream(stream)),
-           "apb_mx4_backward_weight")
+    lib = load()
+    keep, sp, sb = _scratch(workspace, lib.apb_mx4_backward_weight_workspace_bytes(gt, off is not None, E, M, N, K), G)
+    _check(lib.apb_mx4_backward_weight(gp, gt, ldg, xp, off, E, M, N, K, wt, wp, ldw, sp, sb, _stream(stream)), "apb_mx4_backward_weight")
+    _used_on(keep, stream)
     return dW
 
 
@@ -779,8 +819,9 @@ def apb_moe_route(logits: torch.Tensor, k: int, workspace: Optional[torch.Tensor
     need = apb_moe_workspace_bytes(T, E, k)
     if need == 0:
         raise ApbError(APB_ERR_SHAPE, "apb_moe_route")
+    made = None
     if workspace is None:
-        workspace = alloc_moe_workspace(T, E, k, logits.device)
+        workspace = made = alloc_moe_workspace(T, E, k, logits.device)
     elif workspace.numel() * workspace.element_size() < need:
         raise ValueError("workspace smaller than apb_moe_workspace_bytes(T, E, k)")
     ints = torch.int32
@@ -790,6 +831,7 @@ def apb_moe_route(logits: torch.Tensor, k: int, workspace: Optional[torch.Tensor
     _check(load().apb_moe_route(ptr, t, ld, T, E, k, expert.data_ptr(), weight.data_ptr(), offsets.data_ptr(),
                                 row_token.data_ptr(), slot_row.data_ptr(), _array(workspace, ints, None, "workspace"),
                                 _stream(stream)), "apb_moe_route")
+    _used_on(made, stream)
     return {"expert": expert, "weight": weight, "offsets": offsets, "row_token": row_token, "slot_row": slot_row}
 
 

@@ -12,6 +12,7 @@ namespace apb {
 namespace {
 
 constexpr int kGroup = 256;                   // threads that make a tile: four waves
+constexpr int kMaxSlices = 32;
 constexpr int kStep = 64;                     // summed over per pass: a line of 128 bytes of bfloat16 in LDS
 
 template <int TYPE>
@@ -136,12 +137,14 @@ __device__ __forceinline__ void lds_ready() { asm volatile("s_waitcnt lgkmcnt(0)
 // cut into small tasks, and after every matrix instruction of the first three steps comes one of them and at most one read of the
 // next step's operands, so that nothing waits behind them; the barrier stands before the fourth step, under which the next pass's
 // first operands are read.
+// Where there are few tiles and many passes, `slices` workgroups share a tile's passes: each writes its sums as a matrix of its own
+// in the workspace, and k_mx4_join adds them up in order.
 // Where there are few tiles, GROUPS = 2 groups of four waves work on one, each with buffers of its own and every second pass, and
 // add up at the end, the first group's sums first.
 template <int TYPE, bool WEIGHT, int F, int GROUPS>
-__global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS == 2 ? 2 : 1) void k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q,
-                                                                           const int32_t* __restrict__ offsets, int E, int M, int N,
-                                                                           int K, int type, void* __restrict__ out, long long ldo) {
+__global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS == 2 ? 2 : 1) void
+k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* __restrict__ offsets, int E, int M, int N, int K,
+               int slices, int type, void* __restrict__ out, long long ldo) {
     constexpr int NP = Parts<TYPE>::n;
     constexpr int kTile = 64 * F;
     constexpr int kPart = kTile * kRowBytes, kBuffer = (NP + 1) * kPart;      // parts of P, then Q
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS =
     int i0, rows_i, c0, rows_c, out_row;                         // outputs, summation range (rows of Q from c0 on)
     int g_row;                                                   // row of G that belongs to i0 (or to c0, WEIGHT)
     if (WEIGHT) {
-        const int e = blockIdx.z;
+        const int e = blockIdx.z / slices;
         int a = 0, b = M;
         if (offsets) {
             a = min(max(offsets[e], 0), M);
@@ -170,6 +173,17 @@ __global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS =
         rows_c = t.e < E ? N : 0;
         out_row = g_row = t.row0;
     }
+    // this workgroup's share of the passes
+    const int slice = blockIdx.z % slices;
+    int g_col = WEIGHT ? i0 : 0;
+    if (slices > 1) {
+        const int passes = (rows_c + kStep - 1) / kStep;
+        const int from = (int)((long long)passes * slice / slices) * kStep, upto = (int)((long long)passes * (slice + 1) / slices) * kStep;
+        c0 += from;
+        (WEIGHT ? g_row : g_col) += from;
+        rows_c = min(rows_c, upto) - from;
+        out = static_cast<float*>(out) + (size_t)slice * (WEIGHT ? (size_t)E * N : M) * K;
+    }
     const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kGroup);
     const int tid = threadIdx.x & (kGroup - 1), lane = tid & (kWave - 1), wave = tid / kWave;
     uint8_t* lds = shared + group * 2 * kBuffer;
@@ -183,7 +197,7 @@ __global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS =
     const uint32_t q_pitch = (uint32_t)Q.segs * kMxSegBytes;
 
     // where a thread loads from: a scalar base and an offset of its own
-    const Bytes g_base = (Bytes)G + ((long long)g_row * ldg + (WEIGHT ? i0 : 0)) * kSize;
+    const Bytes g_base = (Bytes)G + ((long long)g_row * ldg + g_col) * kSize;
     const Bytes q_base = (Bytes)Q.codes + (size_t)c0 * q_pitch + j0 / 2;
     const Bytes s_base = (Bytes)Q.scales + ((size_t)(j0 / kMxSeg) * Q.rows + c0) * 8 + j0 % kMxSeg / kMxBlock;
     const uint32_t q_at = 8 * chunk * q_pitch + block / 2, s_at = 64 * chunk + block / kMxBlock;
@@ -395,7 +409,7 @@ __global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS =
                 g[0][u] = load_some_words<TYPE, W>(G, (long long)(g_row + cc) * ldg + i0 + block, cc < rows_c ? rows_i - block : 0);
             } else {
                 const int row = min(u * 32 + line, rows_i - 1);
-                g[0][u] = load_some_words<TYPE, 8>(G, (long long)(g_row + row) * ldg + c + 8 * piece, rows_c - c - 8 * piece);
+                g[0][u] = load_some_words<TYPE, 8>(G, (long long)(g_row + row) * ldg + g_col + c + 8 * piece, rows_c - c - 8 * piece);
             }
         }
 #pragma unroll
@@ -454,44 +468,121 @@ __global__ __launch_bounds__(kGroup* GROUPS, F * Parts<TYPE>::n <= 2 || GROUPS =
                       min(32, rows_i - wi - 32 * x), j0 + wj, K - j0 - wj);
 }
 
+// out = the sum of the slices' matrices, in their order; four neighbours to a thread
+__global__ __launch_bounds__(kGroup) void k_mx4_join(const float* __restrict__ parts, int slices, int rows, int K, FastDiv by_fours, int type,
+                                                     void* __restrict__ out, long long ldo) {
+    const uint32_t i = blockIdx.x * kGroup + threadIdx.x;
+    const int row = (int)by_fours.div(i), k = 4 * (int)(i - (uint32_t)row * by_fours.d);
+    if (row >= rows) return;
+    const int have = min(K - k, 4);
+    const size_t at = (size_t)row * K + k, step = (size_t)rows * K;
+    float sum[4] = {};
+    constexpr int kAhead = 8;                                    // slices under way
+    for (int s = 0; s < slices; s += kAhead) {
+        u32x4 v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const float* p = parts + min(s + u, slices - 1) * step + at;
+            if (have == 4) v[u] = load16_any(p);
+            else
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[u][q] = q < have ? float_bits(p[q]) : 0u;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t bits = v[u][q];
+                if (s + u < slices) sum[q] += __builtin_bit_cast(float, bits);
+            }
+    }
+    store4(out, type, (long long)row * ldo + k, sum, have);
+}
+
+// How the work is laid out: tiles of 64 * f a side, by how many groups of waves each, in how many slices.
+struct Plan {
+    int f, groups, slices;
+};
+
+template <bool WEIGHT>
+Plan plan_of(int g_type, bool grouped, int E, int M, int N, int K) {
+    auto tiles = [&](int side) { return ((long long)(WEIGHT ? N : M) + side - 1) / side * ((K + side - 1) / side) * (WEIGHT ? E : 1); };
+    // passes of a tile, were the experts all alike
+    const long long passes = ((WEIGHT ? (grouped ? M / E : M) : N) + kStep - 1) / kStep;
+    // slices that make a workgroup for each compute unit, of at least `least` passes
+    auto slices = [&](long long n, long long least) {
+        return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(256 / n, passes / least), kMaxSlices));
+    };
+    // Measured in bfloat16 (us).  256 a side wherever they fill three quarters of the chip: 4096^3 127, 128 a side 183.  128 a side
+    // likewise, with a second group up to one tile per compute unit: 2048^3 28, with one group 35, 64 a side 54.  64 a side if
+    // those fill the chip and the sums are short: 1024^3 11, 128 a side in slices 21.  Then slices: 512 x 4096 x 4096 41, without
+    // 50; dW of 8192 x 1024 x 1024 41, without 61; of 16384 x 256 x 256 16, without 109.
+    const bool two_groups = g_type == APB_BF16 && tiles(128) <= 256;
+    if (g_type == APB_BF16 && tiles(256) >= 192) return Plan{4, 1, 1};
+    if (tiles(128) >= 192) return Plan{2, two_groups ? 2 : 1, 1};
+    if (tiles(64) >= 192 && passes <= 24) return Plan{1, 2, 1};
+    const int shared = slices(tiles(128), g_type == APB_BF16 ? 20 : 12);      // (more parts of G: passes take longer, joining does not)
+    if (tiles(128) * shared >= 128) return Plan{2, two_groups && shared == 1 ? 2 : 1, shared};
+    return Plan{1, 2, slices(tiles(64), 8)};
+}
+
 template <int TYPE, bool WEIGHT, int F, int GROUPS>
-void launch_tiles(const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type, void* out,
-                  long long ldo, hipStream_t s) {
+void launch_tiles(const Plan& plan, const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
+                  void* out, long long ldo, hipStream_t s) {
     constexpr int kTile = 64 * F;
     const unsigned tiles_i = (unsigned)(WEIGHT ? (N + kTile - 1) / kTile : max_row_tiles(M, E, offsets != nullptr, kTile));
-    const dim3 grid(tiles_i, (unsigned)((K + kTile - 1) / kTile), (unsigned)(WEIGHT ? E : 1));
-    hipLaunchKernelGGL((k_mx4_backward<TYPE, WEIGHT, F, GROUPS>), grid, dim3(kGroup * GROUPS), 0, s, G, ldg, Q, offsets, E, M, N, K, type,
-                       out, ldo);
+    const dim3 grid(tiles_i, (unsigned)((K + kTile - 1) / kTile), (unsigned)((WEIGHT ? E : 1) * plan.slices));
+    hipLaunchKernelGGL((k_mx4_backward<TYPE, WEIGHT, F, GROUPS>), grid, dim3(kGroup * GROUPS), 0, s, G, ldg, Q, offsets, E, M, N, K,
+                       plan.slices, type, out, ldo);
 }
 
 template <int TYPE, bool WEIGHT>
-void launch_type(const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type, void* out,
-                 long long ldo, hipStream_t s) {
-    auto tiles = [&](int side) { return ((long long)(WEIGHT ? N : M) + side - 1) / side * ((K + side - 1) / side) * (WEIGHT ? E : 1); };
+void launch_type(const Plan& plan, const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
+                 void* out, long long ldo, hipStream_t s) {
     if constexpr (TYPE == APB_BF16) {
-        if (tiles(256) >= 192) return launch_tiles<TYPE, WEIGHT, 4, 1>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
-        if (tiles(128) >= 192 && tiles(128) <= 256) return launch_tiles<TYPE, WEIGHT, 2, 2>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+        if (plan.f == 4) return launch_tiles<TYPE, WEIGHT, 4, 1>(plan, G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+        if (plan.f == 2 && plan.groups == 2) return launch_tiles<TYPE, WEIGHT, 2, 2>(plan, G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
     }
-    if (tiles(256) >= 48) return launch_tiles<TYPE, WEIGHT, 2, 1>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
-    launch_tiles<TYPE, WEIGHT, 1, 2>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+    if (plan.f == 2) return launch_tiles<TYPE, WEIGHT, 2, 1>(plan, G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+    launch_tiles<TYPE, WEIGHT, 1, 2>(plan, G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+}
+
+template <bool WEIGHT>
+size_t workspace_bytes(const Plan& plan, int E, int M, int N, int K) {
+    return plan.slices > 1 ? (size_t)plan.slices * (WEIGHT ? (size_t)E * N : M) * K * sizeof(float) : 0;
 }
 
 template <bool WEIGHT>
 int launch(const void* G, int g_type, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
-           void* out, long long ldo, hipStream_t s) {
-    if (g_type == APB_F32) launch_type<APB_F32, WEIGHT>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
-    else if (g_type == APB_BF16) launch_type<APB_BF16, WEIGHT>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
-    else launch_type<APB_F16, WEIGHT>(G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
+           void* out, long long ldo, void* workspace, size_t bytes, hipStream_t s) {
+    Plan plan = plan_of<WEIGHT>(g_type, offsets != nullptr, E, M, N, K);
+    const bool split = plan.slices > 1 && workspace && bytes >= workspace_bytes<WEIGHT>(plan, E, M, N, K);
+    if (!split) plan.slices = 1;
+    void* to = split ? workspace : out;
+    const int to_type = split ? (int)APB_F32 : type;
+    const long long ld = split ? K : ldo;
+    if (g_type == APB_F32) launch_type<APB_F32, WEIGHT>(plan, G, ldg, Q, offsets, E, M, N, K, to_type, to, ld, s);
+    else if (g_type == APB_BF16) launch_type<APB_BF16, WEIGHT>(plan, G, ldg, Q, offsets, E, M, N, K, to_type, to, ld, s);
+    else launch_type<APB_F16, WEIGHT>(plan, G, ldg, Q, offsets, E, M, N, K, to_type, to, ld, s);
+    if (split) {
+        const int rows = WEIGHT ? E * N : M;
+        const uint32_t fours = (uint32_t)(K + 3) / 4;
+        const unsigned blocks = (unsigned)(((long long)rows * fours + kGroup - 1) / kGroup);
+        hipLaunchKernelGGL(k_mx4_join, dim3(blocks), dim3(kGroup), 0, s, static_cast<const float*>(workspace), plan.slices, rows, K,
+                           FastDiv(fours), type, out, ldo);
+    }
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
 
 int check(const void* G, int g_type, long long ldg, const void* Q, const int32_t* offsets, int E, int M, int N, int K, int type,
-          const void* out, long long ldo) {
+          const void* out, long long ldo, const void* workspace) {
     if (!G || !Q || !out) return APB_ERR_NULL;
     if (bad_type(g_type) || bad_type(type)) return APB_ERR_TYPE;
     if (bad_product(E, M, N, K, offsets) || ldg < N || ldg > kMxMaxK || ldo < K) return APB_ERR_SHAPE;
-    if (!aligned(G, type_size(g_type)) || !aligned(Q, 16) || !aligned(out, type_size(type)) || !aligned(offsets, 4)) return APB_ERR_ALIGN;
+    if (!aligned(G, type_size(g_type)) || !aligned(Q, 16) || !aligned(out, type_size(type)) || !aligned(offsets, 4) ||
+        !aligned(workspace, 4))
+        return APB_ERR_ALIGN;
     return APB_OK;
 }
 
@@ -502,18 +593,32 @@ using namespace apb;
 
 extern "C" {
 
+size_t apb_mx4_backward_input_workspace_bytes(int g_type, int grouped, int E, int M, int N, int K) {
+    const int32_t some = 0;
+    if (bad_type(g_type) || bad_product(E, M, N, K, grouped ? &some : nullptr)) return 0;
+    return workspace_bytes<false>(plan_of<false>(g_type, grouped != 0, E, M, N, K), E, M, N, K);
+}
+
+size_t apb_mx4_backward_weight_workspace_bytes(int g_type, int grouped, int E, int M, int N, int K) {
+    const int32_t some = 0;
+    if (bad_type(g_type) || bad_product(E, M, N, K, grouped ? &some : nullptr)) return 0;
+    return workspace_bytes<true>(plan_of<true>(g_type, grouped != 0, E, M, N, K), E, M, N, K);
+}
+
 int apb_mx4_backward_input(const void* G, int g_type, long long ldg, const void* W, const int32_t* offsets, int E, int M,
-                           int N, int K, int type, void* dX, long long ldx, void* stream) {
-    const int rc = check(G, g_type, ldg, W, offsets, E, M, N, K, type, dX, ldx);
+                           int N, int K, int type, void* dX, long long ldx, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check(G, g_type, ldg, W, offsets, E, M, N, K, type, dX, ldx, workspace);
     if (rc != APB_OK) return rc;
-    return launch<false>(G, g_type, ldg, mx_view(W, E * N, K), offsets, E, M, N, K, type, dX, ldx, reinterpret_cast<hipStream_t>(stream));
+    return launch<false>(G, g_type, ldg, mx_view(W, E * N, K), offsets, E, M, N, K, type, dX, ldx, workspace, workspace_bytes,
+                         reinterpret_cast<hipStream_t>(stream));
 }
 
 int apb_mx4_backward_weight(const void* G, int g_type, long long ldg, const void* X, const int32_t* offsets, int E, int M,
-                            int N, int K, int type, void* dW, long long ldw, void* stream) {
-    const int rc = check(G, g_type, ldg, X, offsets, E, M, N, K, type, dW, ldw);
+                            int N, int K, int type, void* dW, long long ldw, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check(G, g_type, ldg, X, offsets, E, M, N, K, type, dW, ldw, workspace);
     if (rc != APB_OK) return rc;
-    return launch<true>(G, g_type, ldg, mx_view(X, M, K), offsets, E, M, N, K, type, dW, ldw, reinterpret_cast<hipStream_t>(stream));
+    return launch<true>(G, g_type, ldg, mx_view(X, M, K), offsets, E, M, N, K, type, dW, ldw, workspace, workspace_bytes,
+                        reinterpret_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

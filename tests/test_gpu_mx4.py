@@ -262,6 +262,33 @@ def test_grouped_gradients(b, kind, M, E, N, K, t, out):
     _close(_np(gw), dw, mw, M, "f32", PARTS[t])
 
 
+@pytest.mark.parametrize("M,N,K,E", [(5000, 70, 130, 0), (60, 4100, 70, 0), (2100, 2500, 33, 0), (4096, 512, 40, 3), (9000, 40, 300, 2)])
+@pytest.mark.parametrize("t,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+def test_long_sums_shared_by_workgroups(b, M, N, K, E, t, out):
+    """Few outputs and long sums: shared through a workspace where there is one, with the same tolerance, and the same bits again."""
+    print(f"[case] mx4 long sums {M} {N} {K} {E} {t}", flush=True)
+    off = _groups("ragged", M, E) if E else None
+    dev = None if off is None else torch.from_numpy(off).cuda()
+    xf, wf = _acts(M + K, M, K), _weights(N + K, max(E, 1) * N, K)
+    g, gv = _in(np.random.default_rng(M * N).standard_normal((M, N)) * 1e-2, t)
+    x4, w4 = b.apb_mx4_quantize(torch.from_numpy(xf).cuda()), b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    dx, dw, mx, mw = o.gradients(gv, o.quantized(xf), o.quantized(wf), off)
+    args = (TYPE[t], E > 0, max(E, 1), M, N, K)
+    shared = b.apb_mx4_backward_input_workspace_bytes(*args), b.apb_mx4_backward_weight_workspace_bytes(*args)
+    assert max(shared) > 0
+    longest = M if off is None else int(np.diff(off).max())
+    for small in (False, True):
+        ws = torch.empty(16, dtype=torch.uint8, device="cuda") if small else None
+        gx, gw = torch.full((M, K + 1), 7.0, dtype=TYPE[out], device="cuda"), torch.full((max(E, 1) * N, K + 1), 7.0, dtype=TYPE[out], device="cuda")
+        b.apb_mx4_backward_input(g, w4, K, dX=gx[:, :K], offsets=dev, workspace=ws)
+        b.apb_mx4_backward_weight(g, x4, K, dW=gw[:, :K], offsets=dev, workspace=ws)
+        _close(_np(gx[:, :K]), dx, mx, N, out, PARTS[t])
+        _close(_np(gw[:, :K]), dw, mw, longest, out, PARTS[t])
+        assert (gx[:, K:] == 7).all() and (gw[:, K:] == 7).all()
+        assert torch.equal(b.apb_mx4_backward_input(g, w4, K, dtype=TYPE[out], offsets=dev, workspace=ws), gx[:, :K])
+        assert torch.equal(b.apb_mx4_backward_weight(g, x4, K, dtype=TYPE[out], offsets=dev, workspace=ws), gw[:, :K])
+
+
 def test_gradients_by_differences(b):
     """The product is linear in either operand: <G, Y(X, W1) - Y(X, W2)> = <dW, W1^ - W2^>, and the same for X."""
     M, N, K = 96, 80, 320

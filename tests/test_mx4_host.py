@@ -77,6 +77,12 @@ def test_sizes(b):
     for bad in ((0, 4), (4, 0), (-1, 4), (4, (1 << 22) + 1), (1 << 27, 1)):
         assert b.apb_mx4_bytes(*bad) == 0
     assert b.apb_moe_workspace_bytes(1, 4, 2) > 0
+    for bytes_of in (b.apb_mx4_backward_input_workspace_bytes, b.apb_mx4_backward_weight_workspace_bytes):
+        import torch
+        for bad in ((True, 0, 64, 64, 64), (False, 2, 64, 64, 64), (False, 1, 0, 64, 64), (False, 1, 64, 64, (1 << 22) + 1)):
+            assert bytes_of(torch.float32, *bad) == 0
+        need = bytes_of(torch.bfloat16, False, 1, 16384, 16384, 64)
+        assert need > 0 and need % (4 * 16384 * 64) == 0              # whole float matrices of dX's or dW's size
     for bad in ((0, 4, 2), (4, 0, 1), (4, 4, 0), (4, 4, 5), (4, 1025, 2), (4, 64, 33), (1 << 24, 4, 1)):
         assert b.apb_moe_workspace_bytes(*bad) == 0
 
@@ -98,9 +104,9 @@ def test_refusals(b):
     assert [l(X=None), l(W=None), l(sc=None), l(Y=None), l(xt=3), l(yt=3), l(ldx=7), l(ri=3), l(ri=0, f=p), l(E=3), l(M=0),
             l(ld=2), l(X=odd), l(W=odd), l(sc=odd), l(f=odd)] == [N, N, N, N, T, T, S, S, S, S, S, S, A, A, A, A]
     for call in (lib.apb_mx4_backward_input, lib.apb_mx4_backward_weight):
-        w = lambda G=p, gt=0, ldg=4, Q=p, off=None, E=1, M=4, n=4, K=8, t=0, out=p, ld=8: call(G, gt, ldg, Q, off, E, M, n, K, t, out, ld, None)
+        w = lambda G=p, gt=0, ldg=4, Q=p, off=None, E=1, M=4, n=4, K=8, t=0, out=p, ld=8, ws=None: call(G, gt, ldg, Q, off, E, M, n, K, t, out, ld, ws, 1 << 20, None)
         assert [w(G=None), w(Q=None), w(out=None), w(gt=3), w(t=3), w(ldg=3), w(ld=7), w(E=2), w(M=0), w(n=-1), w(K=0), w(G=odd),
-                w(Q=odd), w(out=odd)] == [N, N, N, T, T, S, S, S, S, S, S, A, A, A]
+                w(Q=odd), w(out=odd), w(ws=odd), w(ldg=(1 << 22) + 1)] == [N, N, N, T, T, S, S, S, S, S, S, A, A, A, A, S]
     r = lambda x=p, t=0, ld=8, T_=4, E=8, k=2, e=p, ws=p: lib.apb_moe_route(x, t, ld, T_, E, k, e, p, p, p, p, ws, None)
     assert [r(x=None), r(e=None), r(ws=None), r(t=5), r(ld=7), r(T_=0), r(E=0), r(k=0), r(k=9), r(E=2000, ld=2000), r(x=odd),
             r(ws=odd)] == [N, N, N, T, S, S, S, S, S, S, A, A]
