@@ -28,16 +28,21 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantize(const void* __restric
     if ((l & 3) == 0) scales[((size_t)seg * rows + r) * 8 + l / 4] = (uint8_t)code;
 }
 
-// Any strides: a lane takes a block of 32 values, neighbouring lanes neighbouring rows (the order of a K x M matrix).
+// Any strides: a lane takes a block of 32 values, neighbouring lanes neighbouring rows (the order of a K x M matrix), and the eight
+// waves the blocks of a segment, so that codes and scales leave as whole lines, through LDS.
+constexpr int kStridedThreads = 8 * kWave;
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void k_mx4_quantize_strided(const void* __restrict__ X, long long row_stride,
-                                                                   long long col_stride, int rows_in,
-                                                                   const int32_t* __restrict__ rows_from, int rows, int K,
-                                                                   int segs, uint8_t* __restrict__ codes,
-                                                                   uint8_t* __restrict__ scales) {
-    const int r = blockIdx.x * kWave + (threadIdx.x & (kWave - 1));
-    const int block = blockIdx.y * (kThreads / kWave) + threadIdx.x / kWave;
-    if (r >= rows || block >= segs * 8) return;
+__global__ __launch_bounds__(kStridedThreads) void k_mx4_quantize_strided(const void* __restrict__ X, long long row_stride,
+                                                                          long long col_stride, int rows_in,
+                                                                          const int32_t* __restrict__ rows_from, int rows, int K,
+                                                                          int segs, uint8_t* __restrict__ codes,
+                                                                          uint8_t* __restrict__ scales) {
+    constexpr int kPitch = kMxSegBytes + 16;                     // (rows start 4 banks apart)
+    __shared__ __align__(16) uint8_t lines[kWave * kPitch];
+    __shared__ __align__(16) uint8_t marks[kWave * 8];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int row0 = blockIdx.x * kWave, seg = blockIdx.y;
+    const int r = min(row0 + lane, rows - 1), block = seg * 8 + wave;
     const int src = rows_from ? rows_from[r] : r;
     const int have = src >= 0 && src < rows_in ? K - block * kMxBlock : 0;
     const long long at = (long long)src * row_stride + (long long)block * kMxBlock * col_stride;
@@ -61,8 +66,17 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantize_strided(const void* _
     u32x4 w;
 #pragma unroll
     for (int g = 0; g < 4; ++g) w[g] = encode8(v[g], code);
-    *reinterpret_cast<u32x4*>(codes + ((size_t)r * segs * 8 + block) * 16) = w;
-    scales[((size_t)(block / 8) * rows + r) * 8 + block % 8] = (uint8_t)code;
+    *reinterpret_cast<u32x4*>(lines + lane * kPitch + 16 * wave) = w;
+    marks[lane * 8 + wave] = (uint8_t)code;
+    __syncthreads();
+    const int there = min(kWave, rows - row0);
+    const int line = threadIdx.x >> 3, chunk = threadIdx.x & 7;
+    if (line < there)
+        *reinterpret_cast<u32x4*>(codes + ((size_t)(row0 + line) * segs + seg) * kMxSegBytes + 16 * chunk) =
+            *reinterpret_cast<const u32x4*>(lines + line * kPitch + 16 * chunk);
+    if ((int)threadIdx.x < 2 * there)
+        *reinterpret_cast<uint32_t*>(scales + ((size_t)seg * rows + row0) * 8 + 4 * threadIdx.x) =
+            *reinterpret_cast<const uint32_t*>(marks + 4 * threadIdx.x);
 }
 
 __global__ __launch_bounds__(kThreads) void k_mx4_dequantize(Mx mx, int K, FastDiv by_segs, int type, void* __restrict__ X,
@@ -100,8 +114,8 @@ void quantize_type(const void* X, long long row_stride, long long col_stride, in
                            by_segs, codes, scales);
         return;
     }
-    const dim3 grid((unsigned)((rows + kWave - 1) / kWave), (unsigned)(segs * 2));
-    hipLaunchKernelGGL((k_mx4_quantize_strided<TYPE>), grid, dim3(kThreads), 0, s, X, row_stride, col_stride, rows_in, rows_from,
+    const dim3 grid((unsigned)((rows + kWave - 1) / kWave), (unsigned)segs);
+    hipLaunchKernelGGL((k_mx4_quantize_strided<TYPE>), grid, dim3(kStridedThreads), 0, s, X, row_stride, col_stride, rows_in, rows_from,
                        rows, K, segs, codes, scales);
 }
 
