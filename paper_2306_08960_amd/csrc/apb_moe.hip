@@ -253,30 +253,45 @@ __global__ __launch_bounds__(kThreads) void k_moe_place(const int32_t* __restric
     }
 }
 
-// One wave per token; its row of dlogits is put together in LDS.
+// Sixteen tokens to a workgroup, a row of lanes each; their rows of dlogits are put together in LDS and written as one piece.
+constexpr int kRowTokens = kThreads / 16;
 __global__ __launch_bounds__(kThreads) void k_moe_route_backward(const int32_t* __restrict__ expert,
                                                                  const float* __restrict__ weight,
                                                                  const float* __restrict__ dweight, int T, int E, int k,
                                                                  int type, void* __restrict__ dlogits, long long ld) {
-    __shared__ float rows[kThreads / kWave][APB_MOE_MAX_E];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int t = blockIdx.x * (kThreads / kWave) + wave;
-    float* row = rows[wave];
-    for (int e = lane; e < E; e += kWave) row[e] = 0.0f;
+    extern __shared__ float rows[];                              // [kRowTokens][E in whole fours]
+    constexpr int kSlots = APB_MOE_MAX_K / 16;
+    const int fours = (E + 3) / 4, t0 = blockIdx.x * kRowTokens;
+    for (int i = threadIdx.x; i < kRowTokens * fours; i += kThreads) reinterpret_cast<f32x4*>(rows)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     __syncthreads();
-    if (t < T) {
-        const bool slot = lane < k;
-        const int e = slot ? expert[t * k + lane] : -1;
-        const bool there = e >= 0 && e < E;
-        const float w = there ? weight[t * k + lane] : 0.0f, d = there ? dweight[t * k + lane] : 0.0f;
-        // d_j - sum w_i d_i = sum w_i (d_j - d_i), as the weights sum to 1: nothing is lost where one of them is nearly that
-        float inner = 0.0f;
-        for (int i = 0; i < k; ++i) inner = fmaf(__shfl(w, i, kWave), d - __shfl(d, i, kWave), inner);
-        if (there) row[e] = w * inner;
+    const int l = threadIdx.x & 15, t = t0 + threadIdx.x / 16;
+    int e[kSlots];
+    float w[kSlots], d[kSlots], inner[kSlots] = {};
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) {
+        const int j = l + 16 * u;
+        const bool slot = t < T && j < k;
+        e[u] = slot ? expert[t * k + j] : -1;
+        if (e[u] >= E) e[u] = -1;
+        w[u] = e[u] >= 0 ? weight[t * k + j] : 0.0f;
+        d[u] = e[u] >= 0 ? dweight[t * k + j] : 0.0f;
     }
+    // d_j - sum w_i d_i = sum w_i (d_j - d_i), as the weights sum to 1: nothing is lost where one of them is nearly that
+    for (int i = 0; i < k; ++i) {
+        const float wi = __shfl(i < 16 ? w[0] : w[1], i & 15, 16), di = __shfl(i < 16 ? d[0] : d[1], i & 15, 16);
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) inner[u] = fmaf(wi, d[u] - di, inner[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u)
+        if (e[u] >= 0) rows[(threadIdx.x / 16) * 4 * fours + e[u]] = w[u] * inner[u];
     __syncthreads();
-    if (t < T)
-        for (int e = lane; e < E; e += kWave) store_f32(dlogits, type, (long long)t * ld + e, row[e]);
+    for (int i = threadIdx.x; i < min(kRowTokens, T - t0) * fours; i += kThreads) {
+        const int row = i / fours, first = 4 * (i - row * fours);
+        const f32x4 v = reinterpret_cast<const f32x4*>(rows)[i];
+        const float x[4] = {v[0], v[1], v[2], v[3]};
+        store4(dlogits, type, (long long)(t0 + row) * ld + first, x, E - first);
+    }
 }
 
 // A lane makes eight neighbours of a row of Y.  grid.x: tokens, grid.y: pieces of 2048 columns.
@@ -419,9 +434,9 @@ int apb_moe_route_backward(const int32_t* expert, const float* weight, const flo
     if (bad_type(type)) return APB_ERR_TYPE;
     if (bad_route(T, E, k) || ld < E) return APB_ERR_SHAPE;
     if (!aligned(expert, 4) || !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dlogits, type_size(type))) return APB_ERR_ALIGN;
-    const int per = kThreads / kWave;
-    hipLaunchKernelGGL(k_moe_route_backward, dim3((T + per - 1) / per), dim3(kThreads), 0, reinterpret_cast<hipStream_t>(stream), expert,
-                       weight, dweight, T, E, k, type, dlogits, ld);
+    const size_t lds = (size_t)kRowTokens * ((E + 3) / 4) * 16;
+    hipLaunchKernelGGL(k_moe_route_backward, dim3((T + kRowTokens - 1) / kRowTokens), dim3(kThreads), lds,
+                       reinterpret_cast<hipStream_t>(stream), expert, weight, dweight, T, E, k, type, dlogits, ld);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
