@@ -268,55 +268,115 @@ __device__ __forceinline__ void load4_to_lds(uint32_t to, const void* base, uint
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
+template <class T>
+__device__ __forceinline__ T lds_load(uint32_t at) { return *(__attribute__((address_space(3))) const T*)(uintptr_t)at; }
+template <class T>
+__device__ __forceinline__ void lds_store(uint32_t at, const T& v) { *(__attribute__((address_space(3))) T*)(uintptr_t)at = v; }
 
 // ---- from accumulators to rows -----------------------------------------------------------------------------
 
-// Bytes of LDS that a wave needs to write 32 rows of 32 * F outputs.
+// Bytes of LDS that a wave needs to write its tile of 32 * F x 32 * F outputs (256 of float32 a row: in two halves).
 template <int F>
-constexpr int kRowsLds = 32 * (32 * F * 4 + 16);
+constexpr int kTileLds = F == 4 ? 32768 : F * F * 4096;
 
-// A wave's 32 rows x 32 * F columns, which its lanes hold as the matrix instruction leaves them (lane (r, h): of row r the columns
-// 32 y + 8 q + 4 h + 0..3), written to memory as rows: through LDS of the wave's own, so that a store covers whole lines of few
-// rows instead of 16 or 32 bytes of each of 32.  Row i < rows goes to out + (first + i) * ld + col; columns from `cols` on are not
-// there.
+// Four sums of an accumulator.  With F == 4 the accumulators fill the second half of the registers and are fetched from there where
+// they are needed, and not all of them ahead of a branch.
 template <int F>
-__device__ __forceinline__ void store_tile(const f32x16 (&acc)[F], uint8_t* lds, void* out, int type, long long first, long long ld,
-                                           int rows, long long col, int cols) {
-    const int lane = threadIdx.x & (kWave - 1), r = lane & 31, h = lane >> 5;
-    const int size = type == APB_F32 ? 4 : 2;
-    const int pitch = 32 * F * size + 16;                        // (rows start 4 banks apart)
+__device__ __forceinline__ f32x4 four_sums(const f32x16& a, int i) {
+    f32x4 v;
 #pragma unroll
-    for (int y = 0; y < F; ++y)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float v[4] = {acc[y][4 * q], acc[y][4 * q + 1], acc[y][4 * q + 2], acc[y][4 * q + 3]};
-            uint8_t* p = lds + r * pitch + (32 * y + 8 * q + 4 * h) * size;
-            if (type == APB_F32) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-            else *reinterpret_cast<u32x2*>(p) = u32x2{pack2(type, v[0], v[1]), pack2(type, v[2], v[3])};
-        }
-    // (the wave's own writes and reads of LDS stay in this order)
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const int chunks = 2 * F * size;                             // 16-byte chunks of a row: a power of two up to 64
-    const int chunk = lane & (chunks - 1), each = 16 / size, n = chunk * each;
-    const int have = cols - n;
-    if (have <= 0) return;
-    for (int i = lane / chunks; i < rows; i += kWave / chunks) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + i * pitch + 16 * chunk);
-        const long long at = (first + i) * ld + col + n;
-        if (have >= each) {
-            store16_any(static_cast<uint8_t*>(out) + at * size, v);
-        } else if (type == APB_F32) {
-#pragma unroll
-            for (int q = 0; q < 3; ++q)
-                if (q < have) static_cast<uint32_t*>(out)[at + q] = v[q];
-        } else {
-#pragma unroll
-            for (int q = 0; q < 7; ++q)
-                if (q < have) static_cast<uint16_t*>(out)[at + q] = (uint16_t)(v[q / 2] >> (16 * (q & 1)));
-        }
+    for (int q = 0; q < 4; ++q) {
+        const float x = a[i + q];
+        float y = x;
+        if constexpr (F == 4) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(x));
+        v[q] = y;
     }
+    return v;
+}
+
+template <int TYPE, int F>
+__device__ __forceinline__ void store_tile_as(const f32x16 (&acc)[F][F], uint32_t lds, void* out, long long first, long long ld, int rows,
+                                              long long col, int cols) {
+    constexpr int kSize = TYPE == APB_F32 ? 4 : 2, kEach = 16 / kSize;
+    constexpr int kChunks = 2 * F * kSize, kPitch = 16 * kChunks;            // 16-byte chunks of a row
+    constexpr int kX = F * 32 * kPitch <= kTileLds<F> ? F : F / 2;                // groups of 32 rows at a time
+    constexpr int kStepRows = kWave / kChunks, kSteps = 32 * kX / kStepRows;
+    constexpr int kAhead = kSteps < 8 ? kSteps : 8;
+    // Where chunk c of a row is: the chunks are permuted by the row's number, so that lanes of many rows meet every bank once; 32
+    // rows further the permutation is the same.  (The addresses of a row's chunks differ in bits that its first one has not.)
+    auto first_of = [&](int row) {
+        constexpr int kLine = kChunks < 16 ? 16 / kChunks : 1;              // rows that share the 64 banks
+        return lds + row * kPitch + 16 * (row / kLine & (kChunks < 16 ? kChunks - 1 : 15));
+    };
+    const int lane = threadIdx.x & (kWave - 1), r = lane & 31, h = lane >> 5;
+    const int chunk = lane & (kChunks - 1), sub = lane / kChunks;
+    const int have = cols - chunk * kEach;
+    const uint32_t mine = TYPE == APB_F32 ? first_of(r) ^ 16 * h : first_of(r) + 8 * h;
+    const long long row_bytes = ld * kSize;
+    uint8_t* to = static_cast<uint8_t*>(out) + (first + sub) * row_bytes + (col + chunk * kEach) * kSize;
+#pragma unroll
+    for (int x0 = 0; x0 < F; x0 += kX) {
+#pragma unroll
+        for (int x = x0; x < x0 + kX; ++x)
+#pragma unroll
+            for (int y = 0; y < F; ++y)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 a = four_sums<F>(acc[x][y], 4 * q);
+                    const uint32_t rows_on = 32 * (x - x0) * kPitch;
+                    if constexpr (TYPE == APB_F32)
+                        lds_store((mine ^ 16 * (8 * y + 2 * q)) + rows_on, a);
+                    else
+                        lds_store((mine ^ 16 * (4 * y + q)) + rows_on,
+                                  u32x2{pack2(TYPE, a[0], a[1]), pack2(TYPE, a[2], a[3])});
+                }
+        // (the wave's own writes and reads of LDS stay in this order)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const int there = min(rows - 32 * x0, 32 * kX);
+        const long long step_bytes = kStepRows * row_bytes;
+        uint8_t* p = to;
+#pragma unroll 1
+        for (int i = 0; i < there; i += kAhead * kStepRows) {
+            u32x4 v[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v[u] = lds_load<u32x4>(first_of(i + u * kStepRows + sub) ^ 16 * chunk);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u, p += step_bytes)
+                if (i + u * kStepRows + sub < there && have >= kEach) store16_any(p, v[u]);
+        }
+        p = to;
+        if (have > 0 && have < kEach)                                        // the last columns, one by one
+#pragma unroll 1
+            for (int row = sub; row < there; row += kStepRows, p += step_bytes)
+#pragma unroll 1
+                for (int q = 0; q < have; ++q) {
+                    const uint32_t from = (first_of(row) ^ 16 * chunk) + kSize * q;
+                    if constexpr (TYPE == APB_F32) reinterpret_cast<uint32_t*>(p)[q] = lds_load<uint32_t>(from);
+                    else reinterpret_cast<uint16_t*>(p)[q] = lds_load<uint16_t>(from);
+                }
+        to += 32 * kX * row_bytes;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+}
+
+// A wave's tile of 32 * F x 32 * F outputs, which its lanes hold as the matrix instruction leaves them (acc[x][y], lane (r, h): of row
+// 32 x + r the columns 32 y + 8 q + 4 h + 0..3), written to memory as rows: through LDS of the wave's own, so that a store covers
+// whole lines of few rows instead of 16 or 32 bytes of each of 32.  Row i < rows goes to out + (first + i) * ld + col; columns from
+// `cols` on are not there.  `lds`: an address, a multiple of 512.  Few
+// instructions, each of which a tile fetches to run it once, and eight reads of LDS under way: 256 x 256 in bfloat16 take 2.3 us, in
+// a form with a branch on the type at every conversion and a read at a time 7.5.
+template <int F>
+__device__ __forceinline__ void store_tile(const f32x16 (&acc)[F][F], uint32_t lds, void* out, int type, long long first, long long ld,
+                                           int rows, long long col, int cols) {
+    // (the compiler does not see that four_sums() reads what a matrix instruction wrote: 32 cycles, for 8 passes of four)
+    if constexpr (F == 4) asm volatile("s_nop 15\n\ts_nop 15");
+    if (type == APB_F32) store_tile_as<APB_F32, F>(acc, lds, out, first, ld, rows, col, cols);
+    else if (type == APB_BF16) store_tile_as<APB_BF16, F>(acc, lds, out, first, ld, rows, col, cols);
+    else store_tile_as<APB_F16, F>(acc, lds, out, first, ld, rows, col, cols);
 }
 
 // ---- groups of rows ---------------------------------------------------------------------------------

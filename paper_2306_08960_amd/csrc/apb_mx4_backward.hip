@@ -25,9 +25,6 @@ struct Parts {
 // of successive rows meet a bank twice; 32 rows further the permutation is the same.
 constexpr int kRowBytes = 2 * kStep;
 __device__ __forceinline__ uint32_t lds_at(int row, int chunk) { return row * kRowBytes + 16 * (chunk ^ ((row + 2 * (row >> 3)) & 7)); }
-template <class T>
-__device__ __forceinline__ T lds_load(uint32_t at) { return *(__attribute__((address_space(3))) const T*)(uintptr_t)at; }
-__device__ __forceinline__ void lds_store(uint32_t at, const u32x4& v) { *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = v; }
 
 // N words at any address.
 template <int N>
@@ -148,7 +145,7 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
     constexpr int NP = Parts<TYPE>::n;
     constexpr int kTile = 64 * F;
     constexpr int kPart = kTile * kRowBytes, kBuffer = (NP + 1) * kPart;      // parts of P, then Q
-    __shared__ __align__(16) uint8_t shared[GROUPS * 2 * kBuffer];
+    __shared__ __align__(512) uint8_t shared[GROUPS * 2 * kBuffer];
     const int j0 = blockIdx.y * kTile;
     int i0, rows_i, c0, rows_c, out_row;                         // outputs, summation range (rows of Q from c0 on)
     int g_row;                                                   // row of G that belongs to i0 (or to c0, WEIGHT)
@@ -461,11 +458,8 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         if (group == 1) return;
     }
     // the 4-bit matrix was the first operand: a lane holds four neighbours of an output row
-    static_assert(4 * kRowsLds<F> <= 2 * kBuffer, "a wave's rows pass through its share of the buffers");
-#pragma unroll
-    for (int x = 0; x < F; ++x)
-        store_tile<F>(acc[x], lds + wave * kRowsLds<F>, out, type, out_row + wi + 32 * x, ldo,
-                      min(32, rows_i - wi - 32 * x), j0 + wj, K - j0 - wj);
+    static_assert(4 * kTileLds<F> <= 2 * kBuffer, "a wave's tile passes through its share of the buffers");
+    store_tile<F>(acc, lds_address(lds) + wave * kTileLds<F>, out, type, out_row + wi, ldo, min(32 * F, rows_i - wi), j0 + wj, K - j0 - wj);
 }
 
 // out = the sum of the slices' matrices, in their order; four neighbours to a thread

@@ -1,6 +1,7 @@
 // Y = Q(X) W^T for few rows, plain or grouped by expert: what bounds it is reading the weights once.  One kernel: a workgroup
 // brings its rows of X into LDS as 4-bit blocks (quantizing them on the way) while its first weights are already under way, then
 // streams weights through registers into the matrix cores.
+#include <atomic>
 #include <type_traits>
 
 #include "apb_mx4.h"
@@ -14,6 +15,7 @@ constexpr int kRing = 3;                      // segments of 16 rows of weights 
 constexpr int kSlot = 16 * kMxSegBytes + 256; // of the ring: 2 KB of codes, 16 rows' scales (twice)
 constexpr int kFourBit = 3;                   // "type" of an X that is a 4-bit matrix already
 constexpr size_t kMaxLds = 150 * 1024;
+constexpr int kMaxDevices = 64;               // devices of one process the launcher keeps state for
 constexpr int kWorkgroups = 2048;             // of a launch, at most about: two resident per compute unit, four times over
 
 struct Rows {                                 // the left operand: float rows or a 4-bit matrix
@@ -180,6 +182,17 @@ int launch(const Rows& X, const Mx& W, const int32_t* offsets, int E, int M, int
     const int groups = (tiles_n + (kWaves >> wk) - 1) / (kWaves >> wk);
     const long long per_row_tile = std::max<long long>(1, kWorkgroups / row_tiles);
     const dim3 grid((unsigned)row_tiles, (unsigned)std::min<long long>(groups, per_row_tile));
+    if (lds > 64 * 1024) {                                       // more than a launch gets without asking: once per device
+        static std::atomic<bool> asked[kMaxDevices];
+        int dev = 0;
+        APB_HIP(hipGetDevice(&dev));
+        if (dev < 0 || dev >= kMaxDevices) return APB_ERR_SHAPE;
+        if (!asked[dev].load(std::memory_order_acquire)) {
+            APB_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mx4_few<TYPE>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                        (int)kMaxLds));
+            asked[dev].store(true, std::memory_order_release);
+        }
+    }
     hipLaunchKernelGGL((k_mx4_few<TYPE>), grid, dim3(kThreads), lds, s, X, W, offsets, E, M, N, K, lds_rows, wk, type, Y, ldy);
     APB_HIP(hipGetLastError());
     return APB_OK;

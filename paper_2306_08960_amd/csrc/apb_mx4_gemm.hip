@@ -42,7 +42,7 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
     constexpr int kScaleLoads = F == 4 ? 2 : 1;                  // ... its scales
     constexpr int kPass = kLoads + kScaleLoads;
     constexpr int kStage = 2 * kRows * (kHalfBytes + 4);
-    __shared__ __align__(16) uint8_t lds[kRing * kStage];
+    __shared__ __align__(512) uint8_t lds[kRing * kStage];
     int tile, nt;
     tile_of(blockIdx.x, tiles_n, tile, nt);
     const RowTile t = find_row_tile(offsets, E, A.rows, kRows, tile);
@@ -171,11 +171,8 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
         }
     }
     arrived<0>();                                                // (nothing is under way to LDS any more)
-    static_assert(4 * kRowsLds<F> <= kRing * kStage, "a wave's rows pass through its share of the ring");
-#pragma unroll
-    for (int x = 0; x < F; ++x)
-        store_tile<F>(acc[x], lds + wave * kRowsLds<F>, Y, type, t.row0 + wm + 32 * x, ldy, min(32, t.rows - wm - 32 * x), n0 + wn,
-                      N - n0 - wn);
+    static_assert(4 * kTileLds<F> <= kRing * kStage, "a wave's tile passes through its share of the ring");
+    store_tile<F>(acc, lds0 + wave * kTileLds<F>, Y, type, t.row0 + wm, ldy, min(32 * F, t.rows - wm), n0 + wn, N - n0 - wn);
 }
 
 template <int F>

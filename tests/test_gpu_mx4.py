@@ -153,6 +153,21 @@ def test_linear(b, M, N, K, t, out):
     _close(_np(y3).T, want, mag, K, out)
 
 
+@pytest.mark.parametrize("M,N,K", [(16, 200, 4096), (12, 70, 5000), (5, 33, 13000)])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_linear_few_long_rows(b, M, N, K, t):
+    # rows that fill most of a compute unit's LDS
+    print(f"[case] mx4 linear {M} {N} {K} {t}", flush=True)
+    x, v = _in(_acts(M + N + K, M, K), t)
+    wf = _weights(N + K, N, K)
+    w4 = b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    want, mag = o.product(o.quantized(v), o.quantized(wf), N)
+    y = b.apb_mx4_linear(x, w4, N)
+    _close(_np(y), want, mag, K, t)
+    y = b.apb_mx4_gemm(b.apb_mx4_quantize(x), w4, M, N, K, dtype=TYPE[t])
+    _close(_np(y), want, mag, K, t)
+
+
 def _groups(kind, M, E, seed=0):
     g = np.random.default_rng(seed + M + E)
     if kind == "even":
