@@ -117,10 +117,11 @@ __device__ __forceinline__ u32x4 transposed(const Words<N> (&in)[8], int i) {
 }
 
 typedef __attribute__((address_space(1))) const uint8_t* Bytes;
-// A base address that the compiler takes as it is, in scalar registers, instead of folding lane offsets into it.
-__device__ __forceinline__ Bytes opaque(Bytes p) {
-    asm volatile("" : "+s"(p));
-    return p;
+// Where a lane loads from, as the load instruction has it: a base in scalar registers, which the compiler takes as it is instead of
+// folding lane offsets into it, and a 32-bit offset, which it does not widen ahead of the loop.
+__device__ __forceinline__ Bytes at_lane(Bytes& base, uint32_t& offset) {
+    asm volatile("" : "+s"(base), "+v"(offset));
+    return base + offset;
 }
 
 // All of this wave's reads and writes of LDS are done; then so are everybody's.  (Loads to registers stay under way.)
@@ -197,7 +198,7 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
     const Bytes g_base = (Bytes)G + ((long long)g_row * ldg + g_col) * kSize;
     const Bytes q_base = (Bytes)Q.codes + (size_t)c0 * q_pitch + j0 / 2;
     const Bytes s_base = (Bytes)Q.scales + ((size_t)(j0 / kMxSeg) * Q.rows + c0) * 8 + j0 % kMxSeg / kMxBlock;
-    const uint32_t q_at = 8 * chunk * q_pitch + block / 2, s_at = 64 * chunk + block / kMxBlock;
+    uint32_t q_at = 8 * chunk * q_pitch + block / 2, s_at = 64 * chunk + block / kMxBlock;
     const uint32_t g_pitch = (uint32_t)ldg * kSize;
     uint32_t g_at[WEIGHT ? 1 : kPieces];
     if constexpr (WEIGHT) {
@@ -245,7 +246,7 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         s_next = s_base + (size_t)c * 8;
     };
     auto load_g = [&](int set, int u) {
-        g[set][u] = load_words<kGWords>(opaque(g_next) + g_at[WEIGHT ? 0 : u]);
+        g[set][u] = load_words<kGWords>(at_lane(g_next, g_at[WEIGHT ? 0 : u]));
         if constexpr (WEIGHT) g_next += g_pitch;
     };
     auto codes_at = [&](Bytes p) -> uint32_t {                   // W of them
@@ -254,8 +255,8 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         else return *p;
     };
     auto load_q = [&](int set, int u) {
-        code[set][u] = codes_at(opaque(q_next) + q_at);
-        scale[set][u] = (opaque(s_next) + s_at)[8 * u];
+        code[set][u] = codes_at(at_lane(q_next, q_at));
+        scale[set][u] = at_lane(s_next, s_at)[8 * u];
         q_next += q_pitch;
     };
     auto split_g = [&](int set, int u) {
@@ -510,14 +511,17 @@ Plan plan_of(int g_type, bool grouped, int E, int M, int N, int K) {
     // Measured in bfloat16 (us).  256 a side wherever they fill three quarters of the chip: 4096^3 127, 128 a side 183.  128 a side
     // likewise, with a second group up to one tile per compute unit: 2048^3 28, with one group 35, 64 a side 54.  64 a side if
     // those fill the chip and the sums are short: 1024^3 11, 128 a side in slices 21.  Then slices: 512 x 4096 x 4096 41, without
-    // 50; dW of 8192 x 1024 x 1024 41, without 61; of 16384 x 256 x 256 16, without 109.
+    // 50; dW of 8192 x 1024 x 1024 41, without 61; of 16384 x 256 x 256 16, without 109; dX of 64 x 1000 x 64 in slices of 4 passes
+    // 7.8, of 8 9.1.
     const bool two_groups = g_type == APB_BF16 && tiles(128) <= 256;
     if (g_type == APB_BF16 && tiles(256) >= 192) return Plan{4, 1, 1};
     if (tiles(128) >= 192) return Plan{2, two_groups ? 2 : 1, 1};
     if (tiles(64) >= 192 && passes <= 24) return Plan{1, 2, 1};
     const int shared = slices(tiles(128), g_type == APB_BF16 ? 20 : 12);      // (more parts of G: passes take longer, joining does not)
     if (tiles(128) * shared >= 128) return Plan{2, two_groups && shared == 1 ? 2 : 1, shared};
-    return Plan{1, 2, slices(tiles(64), 8)};
+    // (sharing costs 3 us, a pass 0.35: two that share 8 passes lose 3 us against one, four that share 16 gain 1)
+    const int quarters = slices(tiles(64), 4);
+    return Plan{1, 2, quarters > 2 ? quarters : slices(tiles(64), 8)};
 }
 
 template <int TYPE, bool WEIGHT, int F, int GROUPS>
