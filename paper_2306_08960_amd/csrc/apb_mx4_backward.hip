@@ -500,21 +500,23 @@ struct Plan {
 };
 
 template <bool WEIGHT>
-Plan plan_of(int g_type, bool grouped, int E, int M, int N, int K) {
+Plan plan_of(int g_type, bool grouped, int E, int M, int N, int K, bool workspace = true) {
     auto tiles = [&](int side) { return ((long long)(WEIGHT ? N : M) + side - 1) / side * ((K + side - 1) / side) * (WEIGHT ? E : 1); };
     // passes of a tile, were the experts all alike
     const long long passes = ((WEIGHT ? (grouped ? M / E : M) : N) + kStep - 1) / kStep;
     // slices that make a workgroup for each compute unit, of at least `least` passes
     auto slices = [&](long long n, long long least) {
-        return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(256 / n, passes / least), kMaxSlices));
+        return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(256 / n, passes / least), workspace ? kMaxSlices : 1));
     };
-    // Measured in bfloat16 (us).  256 a side wherever they fill three quarters of the chip: 4096^3 127, 128 a side 183.  128 a side
-    // likewise, with a second group up to one tile per compute unit: 2048^3 28, with one group 35, 64 a side 54.  64 a side if
-    // those fill the chip and the sums are short: 1024^3 11, 128 a side in slices 21.  Then slices: 512 x 4096 x 4096 41, without
-    // 50; dW of 8192 x 1024 x 1024 41, without 61; of 16384 x 256 x 256 16, without 109; dX of 64 x 1000 x 64 in slices of 4 passes
-    // 7.8, of 8 9.1.
+    // Measured in bfloat16 (us).  256 a side wherever they fill more than half of the chip: 4096^3 121, 128 a side 183; dX of 2560 x
+    // 4096 x 4096 100 and 127; in two slices where they fill half of it and the sums are long: 4096 x 8192 x 2048 131, 128 a side
+    // 174.  128 a side likewise, with a second group up to one tile per compute unit: 2048^3 28, with one group 35, 64 a side 54.
+    // 64 a side if those fill the chip and the sums are short: 1024^3 11, 128 a side in slices 21.  Then slices: 512 x 4096 x 4096
+    // 37, without 45; dW of 8192 x 1024 x 1024 39, without 50; of 16384 x 256 x 256 15, without 91; dX of 64 x 1000 x 64 in slices
+    // of 4 passes 7.8, of 8 9.1.
     const bool two_groups = g_type == APB_BF16 && tiles(128) <= 256;
-    if (g_type == APB_BF16 && tiles(256) >= 192) return Plan{4, 1, 1};
+    if (g_type == APB_BF16 && tiles(256) >= 144) return Plan{4, 1, 1};
+    if (g_type == APB_BF16 && tiles(256) >= 96 && tiles(256) <= 128 && passes >= 64 && workspace) return Plan{4, 1, 2};
     if (tiles(128) >= 192) return Plan{2, two_groups ? 2 : 1, 1};
     if (tiles(64) >= 192 && passes <= 24) return Plan{1, 2, 1};
     const int shared = slices(tiles(128), g_type == APB_BF16 ? 20 : 12);      // (more parts of G: passes take longer, joining does not)
@@ -554,8 +556,8 @@ template <bool WEIGHT>
 int launch(const void* G, int g_type, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
            void* out, long long ldo, void* workspace, size_t bytes, hipStream_t s) {
     Plan plan = plan_of<WEIGHT>(g_type, offsets != nullptr, E, M, N, K);
-    const bool split = plan.slices > 1 && workspace && bytes >= workspace_bytes<WEIGHT>(plan, E, M, N, K);
-    if (!split) plan.slices = 1;
+    if (!workspace || bytes < workspace_bytes<WEIGHT>(plan, E, M, N, K)) plan = plan_of<WEIGHT>(g_type, offsets != nullptr, E, M, N, K, false);
+    const bool split = plan.slices > 1;
     void* to = split ? workspace : out;
     const int to_type = split ? (int)APB_F32 : type;
     const long long ld = split ? K : ldo;

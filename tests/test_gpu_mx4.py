@@ -304,6 +304,27 @@ def test_long_sums_shared_by_workgroups(b, M, N, K, E, t, out):
         assert torch.equal(b.apb_mx4_backward_weight(g, x4, K, dtype=TYPE[out], offsets=dev, workspace=ws), gw[:, :K])
 
 
+@pytest.mark.parametrize("M,N,K,E", [(2500, 4133, 2500, 0), (2570, 1030, 2100, 3)])
+def test_gradients_of_large_tiles(b, M, N, K, E):
+    """Tiles of 256 a side with ragged edges: whole sums, sums shared by two workgroups, and groups."""
+    print(f"[case] mx4 large gradients {M} {N} {K} {E}", flush=True)
+    off = np.array([0, 700, 700, M - 2], np.int32) if E else None
+    dev = None if off is None else torch.from_numpy(off).cuda()
+    xf, wf = _acts(M + K, M, K), _weights(N + K, max(E, 1) * N, K)
+    g, gv = _in(np.random.default_rng(M * N).standard_normal((M, N)) * 1e-2, "bf16")
+    x4, w4 = b.apb_mx4_quantize(torch.from_numpy(xf).cuda()), b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    dx, dw, mx, mw = o.gradients(gv, o.quantized(xf), o.quantized(wf), off)
+    for small in (False, True):
+        ws = torch.empty(16, dtype=torch.uint8, device="cuda") if small else None
+        gx = torch.full((M, K + 1), 7.0, dtype=torch.bfloat16, device="cuda")
+        gw = torch.full((max(E, 1) * N, K + 1), 7.0, device="cuda")
+        b.apb_mx4_backward_input(g, w4, K, dX=gx[:, :K], offsets=dev, workspace=ws)
+        b.apb_mx4_backward_weight(g, x4, K, dW=gw[:, :K], offsets=dev, workspace=ws)
+        _close(_np(gx[:, :K]), dx, mx, N, "bf16", 1)
+        _close(_np(gw[:, :K]), dw, mw, M, "f32", 1)
+        assert (gx[:, K:] == 7).all() and (gw[:, K:] == 7).all()
+
+
 def test_gradients_by_differences(b):
     """The product is linear in either operand: <G, Y(X, W1) - Y(X, W2)> = <dW, W1^ - W2^>, and the same for X."""
     M, N, K = 96, 80, 320
