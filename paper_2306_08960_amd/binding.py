@@ -629,12 +629,21 @@ def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
     return t.data_ptr(), _type(t.dtype), ld if rows > 1 else max(cols, ld)
 
 
-def _result(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dtype, like: torch.Tensor, name: str):
+def _new(like: torch.Tensor, shape, dtype: torch.dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """Memory beside `like` for a call on `stream`: that stream's own, so nothing under way on another one has it, before or after."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _result(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dtype, like: torch.Tensor, name: str,
+            stream: Optional[torch.cuda.Stream]):
     """(tensor, pointer, apb_type, row stride) of an output: `t`, or a new one beside `like`."""
     if t is None:
         if shape[0] < 0 or shape[1] < 0:
             raise ApbError(APB_ERR_SHAPE, name)
-        t = like.new_empty(shape, dtype=dtype)
+        t = _new(like, shape, dtype, stream)
         return t, t.data_ptr(), _type(dtype), shape[1]
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {list(shape)}")
@@ -665,17 +674,18 @@ def alloc_mx4(rows: int, K: int, device=None) -> torch.Tensor:
     return torch.empty(nbytes, dtype=torch.uint8, device=dev)
 
 
+def _new_mx4(like: torch.Tensor, rows: int, K: int, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    nbytes = apb_mx4_bytes(rows, K)
+    if nbytes == 0:
+        raise ApbError(APB_ERR_SHAPE, "apb_mx4_bytes")
+    return _new(like, nbytes, torch.uint8, stream)
+
+
 def _mx4_ptr(mx: torch.Tensor, rows: int, K: int, name: str) -> int:
     # (what apb_mx4_bytes says; the library refuses the sizes it has no answer for)
     if mx.numel() < rows * ((K + 255) // 256) * 136:
         raise ValueError(f"{name} smaller than apb_mx4_bytes({rows}, {K})")
     return _array(mx, torch.uint8, None, name)
-
-
-def _used_on(t: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream]) -> None:
-    """Memory that this module made for a call on a stream of the caller's: not handed out again before that call is through."""
-    if t is not None and stream is not None:
-        t.record_stream(stream)
 
 
 def _experts(offsets: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
@@ -696,7 +706,7 @@ def apb_mx4_quantize(X: torch.Tensor, mx: Optional[torch.Tensor] = None, rows_fr
     rows_in, K = X.shape
     rows = rows_in if rows_from is None else rows_from.numel()
     if mx is None:
-        mx = alloc_mx4(rows, K, X.device)
+        mx = _new_mx4(X, rows, K, stream)
     _check(load().apb_mx4_quantize(X.data_ptr(), _type(X.dtype), X.stride(0), 1 if K == 1 else X.stride(1), rows_in,
                                    _array(rows_from, torch.int32, rows, "rows_from"), rows, K, _mx4_ptr(mx, rows, K, "mx"), _stream(stream)),
            "apb_mx4_quantize")
@@ -705,7 +715,7 @@ def apb_mx4_quantize(X: torch.Tensor, mx: Optional[torch.Tensor] = None, rows_fr
 
 def apb_mx4_dequantize(mx: torch.Tensor, rows: int, K: int, dtype: torch.dtype = torch.float32,
                        X: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    X, ptr, t, ld = _result(X, (rows, K), dtype, mx, "X")
+    X, ptr, t, ld = _result(X, (rows, K), dtype, mx, "X", stream)
     _check(load().apb_mx4_dequantize(_mx4_ptr(mx, rows, K, "mx"), int(rows), int(K), t, ptr, ld, _stream(stream)),
            "apb_mx4_dequantize")
     return X
@@ -717,7 +727,7 @@ def apb_mx4_gemm(A: torch.Tensor, B: torch.Tensor, M: int, N: int, K: int, dtype
     """Y[M, N] = A^ B^T of two 4-bit matrices; with offsets (int32 [E+1]) the rows of A are grouped by expert and B holds
     E*N rows."""
     off, E = _experts(offsets)
-    Y, ptr, t, ld = _result(Y, (M, N), dtype, A, "Y")
+    Y, ptr, t, ld = _result(Y, (M, N), dtype, A, "Y", stream)
     _check(load().apb_mx4_gemm(_mx4_ptr(A, M, K, "A"), _mx4_ptr(B, E * N, K, "B"), off, E, int(M), int(N), int(K), t, ptr, ld,
                                _stream(stream)), "apb_mx4_gemm")
     return Y
@@ -732,13 +742,11 @@ def apb_mx4_linear(X: torch.Tensor, W: torch.Tensor, N: int, dtype: Optional[tor
     rows_in, K = X.shape
     M = rows_in if rows_from is None else rows_from.numel()
     off, E = _experts(offsets)
-    made = None
     if scratch is None:
-        scratch = made = alloc_mx4(M, K, X.device)
-    Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y")
+        scratch = _new_mx4(X, M, K, stream)
+    Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y", stream)
     _check(load().apb_mx4_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), _mx4_ptr(W, E * N, K, "W"), off, E, M,
                                  int(N), K, _mx4_ptr(scratch, M, K, "scratch"), yt, yp, ldy, _stream(stream)), "apb_mx4_linear")
-    _used_on(made, stream)
     return Y
 
 
@@ -751,12 +759,12 @@ def apb_mx4_backward_weight_workspace_bytes(dtype: torch.dtype, grouped: bool, E
     return int(load().apb_mx4_backward_weight_workspace_bytes(_type(dtype), int(grouped), E, M, N, K))
 
 
-def _scratch(given: Optional[torch.Tensor], need: int, like: torch.Tensor):
+def _scratch(given: Optional[torch.Tensor], need: int, like: torch.Tensor, stream: Optional[torch.cuda.Stream]):
     """(tensor to keep, pointer, bytes) of an optional workspace; a new one where none is given and one is of use."""
     if given is None:
         if need == 0:
             return None, None, 0
-        given = like.new_empty(need, dtype=torch.uint8)
+        given = _new(like, need, torch.uint8, stream)
     if not given.is_cuda or not given.is_contiguous():
         raise TypeError("workspace must be a contiguous tensor on the GPU")
     return given, given.data_ptr(), given.numel() * given.element_size()
@@ -771,11 +779,10 @@ def apb_mx4_backward_input(G: torch.Tensor, W: torch.Tensor, K: int, dtype: Opti
     M, N = G.shape
     off, E = _experts(offsets)
     wp = _mx4_ptr(W, E * N, K, "W")
-    dX, xp, xt, ldx = _result(dX, (M, K), dtype or G.dtype, G, "dX")
+    dX, xp, xt, ldx = _result(dX, (M, K), dtype or G.dtype, G, "dX", stream)
     lib = load()
-    keep, sp, sb = _scratch(workspace, lib.apb_mx4_backward_input_workspace_bytes(gt, off is not None, E, M, N, K), G)
+    keep, sp, sb = _scratch(workspace, lib.apb_mx4_backward_input_workspace_bytes(gt, off is not None, E, M, N, K), G, stream)
     _check(lib.apb_mx4_backward_input(gp, gt, ldg, wp, off, E, M, N, K, xt, xp, ldx, sp, sb, _stream(stream)), "apb_mx4_backward_input")
-    _used_on(keep, stream)
     return dX
 
 
@@ -788,11 +795,10 @@ def apb_mx4_backward_weight(G: torch.Tensor, X: torch.Tensor, K: int, dtype: tor
     M, N = G.shape
     off, E = _experts(offsets)
     xp = _mx4_ptr(X, M, K, "X")
-    dW, wp, wt, ldw = _result(dW, (E * N, K), dtype, G, "dW")
+    dW, wp, wt, ldw = _result(dW, (E * N, K), dtype, G, "dW", stream)
     lib = load()
-    keep, sp, sb = _scratch(workspace, lib.apb_mx4_backward_weight_workspace_bytes(gt, off is not None, E, M, N, K), G)
+    keep, sp, sb = _scratch(workspace, lib.apb_mx4_backward_weight_workspace_bytes(gt, off is not None, E, M, N, K), G, stream)
     _check(lib.apb_mx4_backward_weight(gp, gt, ldg, xp, off, E, M, N, K, wt, wp, ldw, sp, sb, _stream(stream)), "apb_mx4_backward_weight")
-    _used_on(keep, stream)
     return dW
 
 
@@ -819,19 +825,17 @@ def apb_moe_route(logits: torch.Tensor, k: int, workspace: Optional[torch.Tensor
     need = apb_moe_workspace_bytes(T, E, k)
     if need == 0:
         raise ApbError(APB_ERR_SHAPE, "apb_moe_route")
-    made = None
     if workspace is None:
-        workspace = made = alloc_moe_workspace(T, E, k, logits.device)
+        workspace = _new(logits, (need + 3) // 4, torch.int32, stream)
     elif workspace.numel() * workspace.element_size() < need:
         raise ValueError("workspace smaller than apb_moe_workspace_bytes(T, E, k)")
     ints = torch.int32
-    expert, weight = logits.new_empty((T, k), dtype=ints), logits.new_empty((T, k), dtype=torch.float32)
-    offsets, row_token = logits.new_empty(E + 1, dtype=ints), logits.new_empty(T * k, dtype=ints)
-    slot_row = logits.new_empty((T, k), dtype=ints)
+    expert, weight = _new(logits, (T, k), ints, stream), _new(logits, (T, k), torch.float32, stream)
+    offsets, row_token = _new(logits, E + 1, ints, stream), _new(logits, T * k, ints, stream)
+    slot_row = _new(logits, (T, k), ints, stream)
     _check(load().apb_moe_route(ptr, t, ld, T, E, k, expert.data_ptr(), weight.data_ptr(), offsets.data_ptr(),
                                 row_token.data_ptr(), slot_row.data_ptr(), _array(workspace, ints, None, "workspace"),
                                 _stream(stream)), "apb_moe_route")
-    _used_on(made, stream)
     return {"expert": expert, "weight": weight, "offsets": offsets, "row_token": row_token, "slot_row": slot_row}
 
 
@@ -841,7 +845,7 @@ def apb_moe_route_backward(expert: torch.Tensor, weight: torch.Tensor, dweight: 
     if expert.dim() != 2:
         raise ValueError("expert must be [T, k]")
     T, k = expert.shape
-    dlogits, ptr, t, ld = _result(dlogits, (T, E), dtype, expert, "dlogits")
+    dlogits, ptr, t, ld = _result(dlogits, (T, E), dtype, expert, "dlogits", stream)
     _check(load().apb_moe_route_backward(_array(expert, torch.int32, T * k, "expert"), _array(weight, torch.float32, T * k, "weight"),
                                          _array(dweight, torch.float32, T * k, "dweight"), T, int(E), k, t, ptr, ld, _stream(stream)),
            "apb_moe_route_backward")
@@ -863,7 +867,7 @@ def apb_moe_combine(Z: torch.Tensor, slot_row: torch.Tensor, weight: Optional[to
     T, k = _slots(slot_row, Z, "Z")
     zp, zt, ldz = _matrix(Z, "Z")
     N = Z.shape[1]
-    Y, yp, yt, ldy = _result(Y, (T, N), Z.dtype, Z, "Y")
+    Y, yp, yt, ldy = _result(Y, (T, N), Z.dtype, Z, "Y", stream)
     if yt != zt:
         raise TypeError("Y must have Z's type")
     _check(load().apb_moe_combine(zp, zt, ldz, _array(slot_row, torch.int32, T * k, "slot_row"), _array(weight, torch.float32, T * k, "weight"), T, k, N, yp,
@@ -885,8 +889,8 @@ def apb_moe_combine_backward(dY: torch.Tensor, Z: Optional[torch.Tensor], slot_r
         zp, zt, ldz = _matrix(Z, "Z")
         if Z.shape[1] != N or zt != gt:
             raise ValueError("Z must have dY's columns and type")
-        dweight = slot_row.new_empty((T, k), dtype=torch.float32)
-    dZ, dp, dt, lddz = _result(dZ, (T * k, N), dY.dtype, dY, "dZ")
+        dweight = _new(slot_row, (T, k), torch.float32, stream)
+    dZ, dp, dt, lddz = _result(dZ, (T * k, N), dY.dtype, dY, "dZ", stream)
     if dt != gt:
         raise TypeError("dZ must have dY's type")
     _check(load().apb_moe_combine_backward(gp, gt, ldg, zp, ldz, _array(slot_row, torch.int32, T * k, "slot_row"),

@@ -429,3 +429,25 @@ def test_binding_refusals(b):
     with pytest.raises(b.ApbError) as e:
         b.apb_mx4_quantize(x, mx=torch.empty(10000, dtype=torch.uint8, device="cuda")[1:])
     assert e.value.code == b.APB_ERR_ALIGN
+
+
+def test_new_memory_belongs_to_the_calls_stream(b):
+    """Outputs and scratch that a call makes come from its stream's memory: what another stream still works on is not in it."""
+    side = torch.cuda.Stream()
+    x, w4 = torch.randn(300, 256, device="cuda"), b.apb_mx4_quantize(torch.randn(96, 256, device="cuda"))
+    logits = torch.randn(300, 8, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    r = b.apb_moe_route(logits, 2, stream=side)
+    z = torch.zeros(600, 96, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    made = [b.apb_mx4_quantize(x, stream=side), b.apb_mx4_linear(x, w4, 96, stream=side), *r.values()]
+    made += [b.apb_mx4_dequantize(made[0], 300, 256, stream=side), b.apb_mx4_gemm(made[0], w4, 300, 96, 256, stream=side)]
+    made += [b.apb_mx4_backward_input(made[1], w4, 256, stream=side), b.apb_mx4_backward_weight(made[1], made[0], 256, stream=side)]
+    made += [b.apb_moe_combine(z, r["slot_row"], r["weight"], stream=side), *b.apb_moe_combine_backward(made[1], z, r["slot_row"], r["weight"], stream=side)]
+    made.append(b.apb_moe_route_backward(r["expert"], r["weight"], made[-1], 8, stream=side))
+    side.synchronize()
+    segments = torch.cuda.memory_snapshot()
+    for t in made:
+        home = [s for s in segments if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]]
+        assert len(home) == 1 and home[0]["stream"] == side.cuda_stream
+    assert torch.equal(made[1], b.apb_mx4_linear(x, w4, 96))
