@@ -825,17 +825,18 @@ def apb_moe_route(logits: torch.Tensor, k: int, workspace: Optional[torch.Tensor
     need = apb_moe_workspace_bytes(T, E, k)
     if need == 0:
         raise ApbError(APB_ERR_SHAPE, "apb_moe_route")
-    if workspace is None:
-        workspace = _new(logits, (need + 3) // 4, torch.int32, stream)
-    elif workspace.numel() * workspace.element_size() < need:
+    if workspace is not None and workspace.numel() * workspace.element_size() < need:
         raise ValueError("workspace smaller than apb_moe_workspace_bytes(T, E, k)")
-    ints = torch.int32
-    expert, weight = _new(logits, (T, k), ints, stream), _new(logits, (T, k), torch.float32, stream)
-    offsets, row_token = _new(logits, E + 1, ints, stream), _new(logits, T * k, ints, stream)
-    slot_row = _new(logits, (T, k), ints, stream)
+    # (one piece of memory for all whole numbers: making one takes half as long as launching a kernel)
+    ints, slots = torch.int32, T * k
+    expert, slot_row, row_token, offsets, made = _new(logits, 3 * slots + E + 1 + (need + 3) // 4, ints, stream).split_with_sizes(
+        (slots, slots, slots, E + 1, (need + 3) // 4))
+    weight = _new(logits, (T, k), torch.float32, stream)
     _check(load().apb_moe_route(ptr, t, ld, T, E, k, expert.data_ptr(), weight.data_ptr(), offsets.data_ptr(),
-                                row_token.data_ptr(), slot_row.data_ptr(), _array(workspace, ints, None, "workspace"),
+                                row_token.data_ptr(), slot_row.data_ptr(),
+                                made.data_ptr() if workspace is None else _array(workspace, ints, None, "workspace"),
                                 _stream(stream)), "apb_moe_route")
+    expert, slot_row = expert.view(T, k), slot_row.view(T, k)
     return {"expert": expert, "weight": weight, "offsets": offsets, "row_token": row_token, "slot_row": slot_row}
 
 
