@@ -105,6 +105,13 @@ def test_route_weights_by_differences(b):
         assert ((got - want).abs() <= 1e-8 + 256 * U * d.abs().sum(1).double()).all()
 
 
+@pytest.mark.parametrize("T,E,k,kind,t", [
+    (1, 128, 8, "masked", "bf16"), (2, 100, 32, "ties", "f32"), (15, 64, 4, "masked", "f16"), (16, 256, 8, "ties", "bf16"),
+    (17, 256, 8, "ties", "bf16"), (16, 512, 4, "masked", "f32"), (80, 512, 32, "ties", "bf16"), (300, 400, 8, "masked", "f32")])
+def test_route_few_tokens_and_many_experts(b, T, E, k, kind, t):
+    test_route(b, T, E, k, kind, t)
+
+
 @pytest.mark.parametrize("T,k,N,t", [(1, 1, 1, "f32"), (1, 4, 4096, "bf16"), (3, 2, 7, "f16"), (17, 8, 100, "bf16"), (40, 3, 517, "f32"),
                                      (65, 32, 40, "f16"), (9, 4, 2056, "bf16"), (5, 1, 8192, "f32"), (130, 4, 256, "bf16")])
 def test_combine(b, T, k, N, t):
