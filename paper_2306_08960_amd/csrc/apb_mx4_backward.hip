@@ -69,7 +69,10 @@ __device__ __forceinline__ Words<COUNT * (TYPE == APB_F32 ? 4 : 2) / 4> load_som
 }
 
 // The bfloat16 parts of 2 * N neighbours, two to a word: each part takes the leading 8 significant bits of what is left (cut off,
-// so that no part is larger than the value and none overflows).  Bits below 2^-133, which bfloat16 has not, are lost.
+// so that no part is larger than the value and none overflows).  Of a float32 value the second part is taken 2^7 and the third 2^15
+// times as large, no larger than the value yet, and the parts' sums are kept apart until the end: bfloat16 ends at 2^-133, the value
+// at 2^-149.  So nothing is lost of values from 2^-125 on, and less than 2^-148 of smaller ones.
+constexpr float kSecond = 128.0f, kThird = 256.0f;               // ... than the part before
 template <int TYPE, int N>
 __device__ __forceinline__ void split(const Words<N * (TYPE == APB_F32 ? 2 : 1)>& v, Words<N> (&part)[Parts<TYPE>::n]) {
     if constexpr (TYPE == APB_BF16) {
@@ -93,6 +96,7 @@ __device__ __forceinline__ void split(const Words<N * (TYPE == APB_F32 ? 2 : 1)>
                 for (int i = 0; i < 2; ++i) {
                     bits[i] = float_bits(x[i]);
                     x[i] -= __builtin_bit_cast(float, bits[i] & 0xffff0000u);
+                    if (TYPE == APB_F32) x[i] *= p == 0 ? kSecond : kThird;
                     // an infinity is its own first part; a NaN leaves a NaN
                     if (p == 0 && (bits[i] & 0x7fffffffu) == 0x7f800000u) x[i] = 0.0f;
                 }
@@ -221,9 +225,9 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         q_from[ks] = lds0 + NP * kPart + lds_at(wj + r, 2 * ks + h);
     }
 
-    // A matrix instruction waits for the one before it on the same sums: a lone tile of 32 x 32 has several, one for each part of G
-    // or for every second step.
-    constexpr int kSums = F > 1 ? 1 : NP > 1 ? NP : 2;
+    // The parts of a float32 G have sums of their own, for they are scaled.  And a matrix instruction waits for the one before it on
+    // the same sums: a lone tile of 32 x 32 has several, one for each part of G or for every second step.
+    constexpr int kSums = NP == 3 ? 3 : F > 1 ? 1 : 2;
     f32x16 sums[kSums][F][F];
 #pragma unroll
     for (int n = 0; n < kSums; ++n)
@@ -328,7 +332,7 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         else fp[set][i - F] = lds_load<bf16x8>(p_from[ks] + (i - F) / F * kPart + (i - F) % F * 32 * kRowBytes);
     };
     auto multiply = [&](int ks, int i) {                         // i: part, x, y
-        const int x = i / F % F, y = i % F, set = ks & 1, n = F > 1 ? 0 : NP > 1 ? i : ks >> 1;
+        const int x = i / F % F, y = i % F, set = ks & 1, n = kSums == 1 ? 0 : NP > 1 ? i / (F * F) : ks >> 1;
         sums[n][x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[set][y], fp[set][i / F], sums[n][x][y], 0, 0, 0);
     };
     constexpr int kReads = F + NP * F, kProducts = NP * F * F;   // of a step
@@ -439,7 +443,12 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
 #pragma unroll
     for (int n = 1; n < kSums; ++n)
 #pragma unroll
-        for (int q = 0; q < 16; ++q) acc[0][0][q] += sums[n][0][0][q];
+        for (int x = 0; x < F; ++x)
+#pragma unroll
+            for (int y = 0; y < F; ++y)
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    acc[x][y][q] = fmaf(sums[n][x][y][q], NP < 3 ? 1.0f : n == 1 ? 1.0f / kSecond : 1.0f / (kSecond * kThird), acc[x][y][q]);
     lds_ready();
     if constexpr (GROUPS == 2) {
         static_assert(F * F * 16 * 4 * kGroup <= 2 * kBuffer, "a group's sums fit its buffers");

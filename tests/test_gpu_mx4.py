@@ -356,6 +356,23 @@ def test_every_bit_of_the_gradient_counts(b, t):
     assert torch.equal(got.cpu(), g.float())
 
 
+def test_gradients_near_the_ends_of_float32(b):
+    """A float32 gradient from the largest values to the smallest: finite where the result is, exact from 2^-125 on."""
+    w = torch.zeros(64, 64)
+    w[torch.arange(64), torch.arange(64)] = torch.where(torch.arange(64) % 2 == 0, 1.5, 1.0)
+    w4 = b.apb_mx4_quantize(w.cuda())
+    rows = torch.tensor([127, 126, 100, -90, -109, -111, -118, -120, -124, -125])
+    g = torch.ldexp(1 + torch.randint(0, 2 ** 23, (10, 64), generator=torch.Generator().manual_seed(1)).double() * 2.0 ** -23, rows[:, None].double())
+    g[0] = 2.0 ** 127 * (1 + 2.0 ** -7 - 2.0 ** -23)                          # (its last 16 bits are as large as they can be)
+    got = b.apb_mx4_backward_input(g.float().cuda(), w4, 64, dtype=torch.float32).cpu()
+    assert torch.isfinite(got).all()
+    assert torch.equal(got[:, 1::2], g[:, 1::2].float())
+    assert ((got.double() - g * w.diagonal().double()).abs() <= 2.0 ** -22 * g.abs()).all()
+    small = torch.randint(0, 2 ** 24, (64, 64), generator=torch.Generator().manual_seed(2)).double() * 2.0 ** -149
+    got = b.apb_mx4_backward_input(small.float().cuda(), w4, 64, dtype=torch.float32).cpu()
+    assert ((got.double() - small)[:, 1::2].abs() <= 2.0 ** -148).all()
+
+
 def test_gradient_infinities_and_nan(b):
     for t in ("f32", "bf16", "f16"):
         g = torch.ones(40, 64, dtype=TYPE[t])
