@@ -357,7 +357,9 @@ int apb_mx4_gemm(const void* A, const void* B, const int32_t* offsets, int E, in
 /* apb_mx4_quantize of the activations and apb_mx4_gemm as one call, with the same Y.  Few rows (per expert, on
  * average) run as a single kernel that quantizes in registers and streams the weights once: the form for
  * single tokens.  X, x_type, ldx, rows_in, rows_from: as in apb_mx4_quantize with col_stride 1.
- *   scratch  DEVICE, apb_mx4_bytes(M, K) bytes; contents unspecified afterwards. */
+ *   scratch  DEVICE, apb_mx4_linear_scratch_bytes() bytes: apb_mx4_bytes(M, K), or 0 for the single kernel, which does
+ *            not touch it (but it must not be NULL); contents unspecified afterwards.  `grouped`: whether offsets will be given. */
+size_t apb_mx4_linear_scratch_bytes(int grouped, int E, int M, int N, int K);
 int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const void* W,
                    const int32_t* offsets, int E, int M, int N, int K, void* scratch, int y_type, void* Y, long long ldy,
                    void* stream);

@@ -25,7 +25,7 @@ EXPORTS = (
     "apb_w2_pack", "apb_w2_export", "apb_w2_free", "apb_gemm_2_2_int", "apb_gemm_2_2",
     "apb_train_workspace_bytes", "apb_train_forward", "apb_train_backward",
     "apb_probe_out_bytes", "apb_probe_rate",
-    "apb_mx4_bytes", "apb_mx4_quantize", "apb_mx4_dequantize", "apb_mx4_gemm", "apb_mx4_linear",
+    "apb_mx4_bytes", "apb_mx4_quantize", "apb_mx4_dequantize", "apb_mx4_gemm", "apb_mx4_linear", "apb_mx4_linear_scratch_bytes",
     "apb_mx4_backward_input", "apb_mx4_backward_weight", "apb_mx4_backward_input_workspace_bytes",
     "apb_mx4_backward_weight_workspace_bytes",
     "apb_moe_workspace_bytes", "apb_moe_route", "apb_moe_route_backward", "apb_moe_combine", "apb_moe_combine_backward",
@@ -118,6 +118,8 @@ def load() -> ctypes.CDLL:
     lib.apb_mx4_bytes.restype = ctypes.c_size_t
     lib.apb_moe_workspace_bytes.argtypes = [ci, ci, ci]
     lib.apb_moe_workspace_bytes.restype = ctypes.c_size_t
+    lib.apb_mx4_linear_scratch_bytes.argtypes = [ci] * 5
+    lib.apb_mx4_linear_scratch_bytes.restype = ctypes.c_size_t
     for name in ("apb_mx4_backward_input_workspace_bytes", "apb_mx4_backward_weight_workspace_bytes"):
         getattr(lib, name).argtypes = [ci] * 6
         getattr(lib, name).restype = ctypes.c_size_t
@@ -733,6 +735,11 @@ def apb_mx4_gemm(A: torch.Tensor, B: torch.Tensor, M: int, N: int, K: int, dtype
     return Y
 
 
+def apb_mx4_linear_scratch_bytes(grouped: bool, E: int, M: int, N: int, K: int) -> int:
+    """Bytes of scratch that apb_mx4_linear uses: 0 where it runs as one kernel."""
+    return int(load().apb_mx4_linear_scratch_bytes(int(grouped), E, M, N, K))
+
+
 def apb_mx4_linear(X: torch.Tensor, W: torch.Tensor, N: int, dtype: Optional[torch.dtype] = None,
                    Y: Optional[torch.Tensor] = None, rows_from: Optional[torch.Tensor] = None,
                    offsets: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None,
@@ -742,11 +749,16 @@ def apb_mx4_linear(X: torch.Tensor, W: torch.Tensor, N: int, dtype: Optional[tor
     rows_in, K = X.shape
     M = rows_in if rows_from is None else rows_from.numel()
     off, E = _experts(offsets)
-    if scratch is None:
-        scratch = _new_mx4(X, M, K, stream)
+    lib, wp = load(), _mx4_ptr(W, E * N, K, "W")
+    if scratch is not None:
+        sp = _mx4_ptr(scratch, M, K, "scratch")
+    else:
+        need = lib.apb_mx4_linear_scratch_bytes(off is not None, E, M, N, K)
+        scratch = _new(X, need, torch.uint8, stream) if need else None
+        sp = scratch.data_ptr() if need else wp                       # (none needed: not touched, but not NULL)
     Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y", stream)
-    _check(load().apb_mx4_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), _mx4_ptr(W, E * N, K, "W"), off, E, M,
-                                 int(N), K, _mx4_ptr(scratch, M, K, "scratch"), yt, yp, ldy, _stream(stream)), "apb_mx4_linear")
+    _check(lib.apb_mx4_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), wp, off, E, M, int(N), K, sp, yt, yp,
+                              ldy, _stream(stream)), "apb_mx4_linear")
     return Y
 
 

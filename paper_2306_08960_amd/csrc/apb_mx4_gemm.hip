@@ -219,6 +219,12 @@ int apb_mx4_gemm(const void* A, const void* B, const int32_t* offsets, int E, in
     return launch_mx4_gemm(a, b, offsets, E, M, N, type, Y, ldy, s);
 }
 
+size_t apb_mx4_linear_scratch_bytes(int grouped, int E, int M, int N, int K) {
+    const int32_t some = 0, *offsets = grouped ? &some : nullptr;
+    if (bad_product(E, M, N, K, offsets) || mx4_few_applies(offsets, E, M, K)) return 0;
+    return apb_mx4_bytes(M, K);
+}
+
 int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const void* W,
                    const int32_t* offsets, int E, int M, int N, int K, void* scratch, int y_type, void* Y, long long ldy,
                    void* stream) {

@@ -468,3 +468,12 @@ def test_new_memory_belongs_to_the_calls_stream(b):
         home = [s for s in segments if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]]
         assert len(home) == 1 and home[0]["stream"] == side.cuda_stream
     assert torch.equal(made[1], b.apb_mx4_linear(x, w4, 96))
+
+
+def test_no_scratch_is_touched_where_none_is_needed(b):
+    """The weights stand in for the scratch of the single kernel: they and the result stay what they are."""
+    x, w4 = torch.randn(3, 512, device="cuda"), b.apb_mx4_quantize(torch.randn(70, 512, device="cuda"))
+    assert b.apb_mx4_linear_scratch_bytes(False, 1, 3, 70, 512) == 0
+    before, scratch = w4.clone(), torch.full((b.apb_mx4_bytes(3, 512),), 0xa5, dtype=torch.uint8, device="cuda")
+    assert torch.equal(b.apb_mx4_linear(x, w4, 70), b.apb_mx4_linear(x, w4, 70, scratch=scratch))
+    assert torch.equal(w4, before) and (scratch == 0xa5).all()

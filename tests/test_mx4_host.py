@@ -88,6 +88,15 @@ def test_sizes(b):
 
 
 @built
+def test_scratch_of_the_product_with_quantization(b):
+    assert b.apb_mx4_linear_scratch_bytes(False, 1, 4096, 64, 1000) == b.apb_mx4_bytes(4096, 1000)
+    assert b.apb_mx4_linear_scratch_bytes(True, 16, 4096, 64, 1000) == b.apb_mx4_bytes(4096, 1000)
+    assert b.apb_mx4_linear_scratch_bytes(False, 1, 1, 4096, 4096) == b.apb_mx4_linear_scratch_bytes(True, 64, 64, 2048, 2048) == 0
+    for bad in ((True, 0, 64, 64, 64), (False, 2, 64, 64, 64), (False, 1, 0, 64, 64), (False, 1, 64, 0, 64), (False, 1, 64, 64, 0)):
+        assert b.apb_mx4_linear_scratch_bytes(*bad) == 0
+
+
+@built
 def test_refusals(b):
     lib, p, odd = b.load(), ctypes.c_void_p(4096), ctypes.c_void_p(4098)     # never dereferenced
     S, N, T, A = b.APB_ERR_SHAPE, b.APB_ERR_NULL, b.APB_ERR_TYPE, b.APB_ERR_ALIGN
