@@ -240,10 +240,8 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
     f32x16(&acc)[F][F] = sums[0];
 
     constexpr int kGCount = WEIGHT ? 8 : kPieces, kGWords = (WEIGHT ? W : 8) * kSize / 4;
-    // The smallest tiles' passes are shorter than the way from memory: they are loaded one further ahead.
-    constexpr int kSets = F == 1 ? 2 : 1;
-    Words<kGWords> g[kSets][kGCount];
-    uint32_t code[kSets][8], scale[kSets][8];
+    Words<kGWords> g[kGCount];
+    uint32_t code[8], scale[8];
     Words<W / 2> q_wide[8], g_part[NP][8];
     // the tasks: load, widen or split, store
     Bytes g_next, q_next, s_next;                                // of the pass to load
@@ -252,8 +250,8 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         q_next = q_base + (size_t)c * q_pitch;
         s_next = s_base + (size_t)c * 8;
     };
-    auto load_g = [&](int set, int u) {
-        g[set][u] = load_words<kGWords>(at_lane(g_next, g_at[WEIGHT ? 0 : u]));
+    auto load_g = [&](int u) {
+        g[u] = load_words<kGWords>(at_lane(g_next, g_at[WEIGHT ? 0 : u]));
         if constexpr (WEIGHT) g_next += g_pitch;
     };
     auto codes_at = [&](Bytes p) -> uint32_t {                   // W of them
@@ -261,20 +259,20 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         else if constexpr (W == 4) return *(__attribute__((address_space(1))) const uint16_t*)p;
         else return *p;
     };
-    auto load_q = [&](int set, int u) {
-        code[set][u] = codes_at(at_lane(q_next, q_at));
-        scale[set][u] = at_lane(s_next, s_at)[8 * u];
+    auto load_q = [&](int u) {
+        code[u] = codes_at(at_lane(q_next, q_at));
+        scale[u] = at_lane(s_next, s_at)[8 * u];
         q_next += q_pitch;
     };
-    auto split_g = [&](int set, int u) {
+    auto split_g = [&](int u) {
         if constexpr (WEIGHT) {
             Words<W / 2> v[NP];
-            split<TYPE, W / 2>(g[set][u], v);
+            split<TYPE, W / 2>(g[u], v);
 #pragma unroll
             for (int p = 0; p < NP; ++p) g_part[p][u] = v[p];
         } else {
             Words<4> v[NP];
-            split<TYPE, 4>(g[set][u], v);
+            split<TYPE, 4>(g[u], v);
 #pragma unroll
             for (int p = 0; p < NP; ++p)
                 lds_store(g_to + p * kPart + u * 32 * kRowBytes, u32x4{v[p].w[0], v[p].w[1], v[p].w[2], v[p].w[3]});
@@ -284,44 +282,44 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
 #pragma unroll
         for (int p = 0; p < NP; ++p) lds_store(to[i] + p * kPart, transposed(g_part[p], i));
     };
-    auto widen_q = [&](int set, int u) {
+    auto widen_q = [&](int u) {
         // (the conversion takes the scale as a float's exponent: every code is right as it is, 0 and NaN's 255 too)
-        const float s = __builtin_bit_cast(float, scale[set][u] << 23);
-        q_wide[u].w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 0));
-        if constexpr (W >= 4) q_wide[u].w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 1));
+        const float s = __builtin_bit_cast(float, scale[u] << 23);
+        q_wide[u].w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 0));
+        if constexpr (W >= 4) q_wide[u].w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 1));
         if constexpr (W >= 8) {
-            q_wide[u].w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 2));
-            q_wide[u].w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[set][u], s, 3));
+            q_wide[u].w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 2));
+            q_wide[u].w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], s, 3));
         }
     };
     auto store_q = [&](int i) { lds_store(to[i] + NP * kPart, transposed(q_wide, i)); };
     constexpr int kTasksQ = 16 + W, kTasks = kTasksQ + 2 * kGCount + (WEIGHT ? W : 0);
-    // task k of bringing in one pass (from a set of registers) and loading the one aimed at into it
-    auto task = [&](int set, auto number) {
+    // task k of bringing in one pass and loading the one aimed at into its registers
+    auto task = [&](auto number) {
         constexpr int k = number.value, m = k - kTasksQ;
-        if constexpr (k < 8) widen_q(set, k);
-        else if constexpr (k < 16) load_q(set, k - 8);
+        if constexpr (k < 8) widen_q(k);
+        else if constexpr (k < 16) load_q(k - 8);
         else if constexpr (k < kTasksQ) store_q(k - 16);
-        else if constexpr (m < kGCount) split_g(set, m);
+        else if constexpr (m < kGCount) split_g(m);
         else if constexpr (m < kTasks - kTasksQ - kGCount) store_g(m - kGCount);
-        else load_g(set, k - (kTasks - kGCount));
+        else load_g(k - (kTasks - kGCount));
     };
     // what a pass in registers has of its first `skip` summation indices becomes zero
-    auto leave_out = [&](int set, int skip) {
+    auto leave_out = [&](int skip) {
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            if (8 * chunk + u < skip) code[set][u] = scale[set][u] = 0u;
+            if (8 * chunk + u < skip) code[u] = scale[u] = 0u;
 #pragma unroll
         for (int u = 0; u < kGCount; ++u)
 #pragma unroll
             for (int q = 0; q < kGWords; ++q) {
                 if constexpr (WEIGHT) {
-                    if (8 * chunk + u < skip) g[set][u].w[q] = 0u;
+                    if (8 * chunk + u < skip) g[u].w[q] = 0u;
                 } else if constexpr (TYPE == APB_F32) {
-                    if (8 * piece + q < skip) g[set][u].w[q] = 0u;
+                    if (8 * piece + q < skip) g[u].w[q] = 0u;
                 } else {
-                    if (8 * piece + 2 * q < skip) g[set][u].w[q] &= 0xffff0000u;
-                    if (8 * piece + 2 * q + 1 < skip) g[set][u].w[q] = 0u;
+                    if (8 * piece + 2 * q < skip) g[u].w[q] &= 0xffff0000u;
+                    if (8 * piece + 2 * q + 1 < skip) g[u].w[q] = 0u;
                 }
             }
     };
@@ -344,24 +342,24 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         // of this group's n-th pass: where it begins, and how many of its indices others have
         auto begin = [&](int n) { return min((n * GROUPS + group) * kStep, rows_c - kStep); };
         auto known = [&](int n) { return min((n * GROUPS + group) * kStep - begin(n), kStep); };
-        each<kSets>([&](auto set) {
-            aim(begin(set.value));
-            each<8>([&](auto u) { load_q(set.value, u.value); });
-            each<kGCount>([&](auto u) { load_g(set.value, u.value); });
-        });
-        if (known(0) > 0) leave_out(0, known(0));
-        aim(begin(kSets));
-        each<kTasks>([&](auto k) { task(0, k); });
+        aim(begin(0));
+        each<8>([&](auto u) { load_q(u.value); });
+        each<kGCount>([&](auto u) { load_g(u.value); });
+        if (known(0) > 0) leave_out(known(0));
+        aim(begin(1));
+        each<kTasks>([&](auto k) { task(k); });
         lds_ready();
         each<kReads>([&](auto i) { read(0, 0, i.value); });
         int turn = kBuffer;                                      // from one buffer to the other: writes are one ahead of reads
 #pragma unroll
         for (int i = 0; i < W; ++i) to[i] += turn;
         g_to += turn;
-        // multiplies the group's pass number `round`, brings in the next one and loads the one kSets further
-        auto run = [&](int round, int set) {
-            if (round + 2 == rounds && known(round + 1) > 0) leave_out(set, known(round + 1));
-            aim(begin(round + 1 + kSets));                       // (beyond the last pass: that again, unread)
+        // A round multiplies one pass of the group's, brings in the next one and loads the one behind it.  (Two passes ahead in registers,
+        // by turns in two copies of this loop, cost more in fetching instructions than they saved in waiting: 333 x 1000 x 517 24.2 us
+        // instead of 22.5.)
+        for (int round = 0; round < rounds; ++round) {
+            if (round + 2 == rounds && known(round + 1) > 0) leave_out(known(round + 1));
+            aim(begin(round + 2));                               // (beyond the last pass: that again, unread)
             each<kStep / 16>([&](auto step) {
                 constexpr int ks = step.value;
                 if constexpr (ks == kLast) {
@@ -378,7 +376,7 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
                     if constexpr (ks < kLast) {
                         constexpr int slot = ks * kProducts + i, kSlots = kLast * kProducts;
                         constexpr int t0 = slot * kTasks / kSlots, t1 = (slot + 1) * kTasks / kSlots;
-                        each<t1 - t0>([&](auto j) { task(set, std::integral_constant<int, t0 + decltype(j)::value>{}); });
+                        each<t1 - t0>([&](auto j) { task(std::integral_constant<int, t0 + decltype(j)::value>{}); });
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 });
@@ -392,15 +390,6 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
 #pragma unroll
             for (int i = 0; i < W; ++i) to[i] += turn;
             g_to += turn;
-        };
-        if constexpr (kSets == 1) {
-            for (int round = 0; round < rounds; ++round) run(round, 0);
-        } else {
-            for (int round = 0; round < rounds; round += 2) {
-                run(round, 1);
-                if (round + 1 == rounds) break;
-                run(round + 1, 0);
-            }
         }
         rows_c = 0;
     }
@@ -411,21 +400,21 @@ k_mx4_backward(const void* __restrict__ G, long long ldg, Mx Q, const int32_t* _
         for (int u = 0; u < kGCount; ++u) {
             if constexpr (WEIGHT) {
                 const int cc = c + 8 * chunk + u;
-                g[0][u] = load_some_words<TYPE, W>(G, (long long)(g_row + cc) * ldg + i0 + block, cc < rows_c ? rows_i - block : 0);
+                g[u] = load_some_words<TYPE, W>(G, (long long)(g_row + cc) * ldg + i0 + block, cc < rows_c ? rows_i - block : 0);
             } else {
                 const int row = min(u * 32 + line, rows_i - 1);
-                g[0][u] = load_some_words<TYPE, 8>(G, (long long)(g_row + row) * ldg + g_col + c + 8 * piece, rows_c - c - 8 * piece);
+                g[u] = load_some_words<TYPE, 8>(G, (long long)(g_row + row) * ldg + g_col + c + 8 * piece, rows_c - c - 8 * piece);
             }
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             const int cc = c + 8 * chunk + u, row = min(cc, rows_c - 1);
-            code[0][u] = codes_at(q_base + (size_t)row * q_pitch + block / 2);
-            scale[0][u] = s_base[(size_t)row * 8 + block / kMxBlock];
-            if (cc >= rows_c) code[0][u] = scale[0][u] = 0u;
+            code[u] = codes_at(q_base + (size_t)row * q_pitch + block / 2);
+            scale[u] = s_base[(size_t)row * 8 + block / kMxBlock];
+            if (cc >= rows_c) code[u] = scale[u] = 0u;
         }
-        each<kGCount>([&](auto u) { split_g(0, u.value); });
-        each<8>([&](auto u) { widen_q(0, u.value); });
+        each<kGCount>([&](auto u) { split_g(u.value); });
+        each<8>([&](auto u) { widen_q(u.value); });
         each<W>([&](auto i) {
             if constexpr (WEIGHT) store_g(i.value);
             store_q(i.value);
