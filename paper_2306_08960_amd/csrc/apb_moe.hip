@@ -2,8 +2,8 @@
 // joining the experts' results; and both gradients.
 //
 // Routing is a few short kernels, each bound by its launch and a chain of dependent steps: 16384 tokens, 8 of 128 experts: choosing
-// 9.4 us, the two steps of the order 2.2 and 5.4, the logits' gradient 4.9; one token 3.4 as one kernel, and 1.8.  Joining is bound
-// by memory: 8192 tokens, 4 rows of 4096 bfloat16 values each, 336 MB: 77 us; its gradients, 604 MB, 118 us, as fast as a copy.
+// 9 us, the two steps of the order 2 and 6, the logits' gradient 5; one token 3 as one kernel, and 1.8.  Joining is bound by memory:
+// 8192 tokens, 4 rows of 4096 bfloat16 values each, 336 MB: 59 us (5.7 TB/s); its gradients, 604 MB, 118 us (5.1), as fast as a copy.
 //
 // The order is that of a stable counting sort by expert.  A token takes an expert once at most, so the slots of an expert
 // among 64 tokens are a 64-bit mask, the rank of one the number of mask bits below it, and nothing depends on the order in
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_route_backward(const int32_t* 
 }
 
 // A lane makes eight neighbours of a row of Y.  grid.x: tokens, grid.y: pieces of 2048 columns.
-template <int TYPE>
+template <int TYPE, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_moe_combine(const void* __restrict__ Z, long long ldz,
                                                           const int32_t* __restrict__ slot_row,
                                                           const float* __restrict__ weight, int T, int k, int N,
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine(const void* __restrict
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (w[u] != 0.0f) v[u] = load_some<TYPE>(Z, (long long)row[u] * ldz + n, N - n);
+            if (w[u] != 0.0f) v[u] = load_some<TYPE, ONCE>(Z, (long long)row[u] * ldz + n, N - n);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (w[u] == 0.0f) continue;
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine(const void* __restrict
 }
 
 // One workgroup per slot: its row of dZ and its dweight.
-template <int TYPE>
+template <int TYPE, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* __restrict__ dY, long long lddy,
                                                                    const void* __restrict__ Z, long long ldz,
                                                                    const int32_t* __restrict__ slot_row,
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_combine_backward(const void* _
         const Eight<TYPE> a = load_some<TYPE>(dY, (long long)t * lddy + n, N - n);
         float g[8], d[8];
         if (dweight) {
-            const Eight<TYPE> b = load_some<TYPE>(Z, (long long)row * ldz + n, N - n);
+            const Eight<TYPE> b = load_some<TYPE, ONCE>(Z, (long long)row * ldz + n, N - n);
             float z[8];
             floats(a, g);
             floats(b, z);
@@ -407,6 +407,10 @@ void launch_by_experts(int E, int T, int blocks, hipStream_t s, Args... args) {
 bool bad_route(int T, int E, int k) {
     return T <= 0 || E <= 0 || k <= 0 || k > E || E > APB_MOE_MAX_E || k > APB_MOE_MAX_K || (long long)T * k >= kMaxSlots;
 }
+// Rows that the last cache (256 MB) would not keep for who reads them next beside what else is in use are read past it.  Measured
+// with and without, the join, its gradients, one behind the other (us): 268 MB 59 and 66, 118 and 121, 175 and 196; 134 MB 35 and
+// 35, 62 and 62, 96 and 101; 34 MB 9 and 9, 19 and 18, 29 and 26.
+bool beyond_caches(int T, int k, int N, int type) { return (long long)T * k * N * type_size(type) >= 128LL << 20; }
 int route_blocks(int T) { return (T + kTokens - 1) / kTokens; }
 
 }  // namespace
@@ -457,11 +461,16 @@ int apb_moe_route_backward(const int32_t* expert, const float* weight, const flo
     return APB_OK;
 }
 
-#define APB_BY_TYPE(kernel, grid, ...)                                                                         \
-    do {                                                                                                       \
-        if (type == APB_F32) hipLaunchKernelGGL((kernel<APB_F32>), grid, dim3(kThreads), 0, s, __VA_ARGS__);   \
-        else if (type == APB_BF16) hipLaunchKernelGGL((kernel<APB_BF16>), grid, dim3(kThreads), 0, s, __VA_ARGS__); \
-        else hipLaunchKernelGGL((kernel<APB_F16>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                   \
+#define APB_LAUNCH(kernel, type, once, grid, ...)                                                                          \
+    do {                                                                                                                   \
+        if (once) hipLaunchKernelGGL((kernel<type, true>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                       \
+        else hipLaunchKernelGGL((kernel<type, false>), grid, dim3(kThreads), 0, s, __VA_ARGS__);                           \
+    } while (0)
+#define APB_BY_TYPE(kernel, once, grid, ...)                                                                               \
+    do {                                                                                                                   \
+        if (type == APB_F32) APB_LAUNCH(kernel, APB_F32, once, grid, __VA_ARGS__);                                         \
+        else if (type == APB_BF16) APB_LAUNCH(kernel, APB_BF16, once, grid, __VA_ARGS__);                                  \
+        else APB_LAUNCH(kernel, APB_F16, once, grid, __VA_ARGS__);                                                         \
     } while (0)
 
 int apb_moe_combine(const void* Z, int type, long long ldz, const int32_t* slot_row, const float* weight, int T, int k,
@@ -472,7 +481,7 @@ int apb_moe_combine(const void* Z, int type, long long ldz, const int32_t* slot_
     if (!aligned(Z, type_size(type)) || !aligned(Y, type_size(type)) || !aligned(slot_row, 4) || !aligned(weight, 4)) return APB_ERR_ALIGN;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)T, (unsigned)((N + kThreads * 8 - 1) / (kThreads * 8)));
-    APB_BY_TYPE(k_moe_combine, grid, Z, ldz, slot_row, weight, T, k, N, Y, ldy);
+    APB_BY_TYPE(k_moe_combine, beyond_caches(T, k, N, type), grid, Z, ldz, slot_row, weight, T, k, N, Y, ldy);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
@@ -490,8 +499,8 @@ int apb_moe_combine_backward(const void* dY, int type, long long lddy, const voi
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const int slots = T * k;
     const dim3 grid((unsigned)slots);
-    APB_BY_TYPE(k_moe_combine_backward, grid, dY, lddy, Z, ldz, slot_row, weight, slots, FastDiv((uint32_t)k), N, dZ, lddz,
-                              dweight);
+    APB_BY_TYPE(k_moe_combine_backward, beyond_caches(T, k, N, type), grid, dY, lddy, Z, ldz, slot_row, weight, slots, FastDiv((uint32_t)k), N,
+                dZ, lddz, dweight);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }

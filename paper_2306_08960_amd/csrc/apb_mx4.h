@@ -88,6 +88,7 @@ __device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
 typedef u32x4 u32x4_any __attribute__((aligned(1)));
 typedef u32x2 u32x2_any __attribute__((aligned(1)));
 __device__ __forceinline__ u32x4 load16_any(const void* p) { return *static_cast<const u32x4_any*>(p); }
+__device__ __forceinline__ u32x4 load16_once(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4_any*>(p)); }
 __device__ __forceinline__ void store16_any(void* p, const u32x4& v) { *static_cast<u32x4_any*>(p) = v; }
 __device__ __forceinline__ void store8_any(void* p, const u32x2& v) { *static_cast<u32x2_any*>(p) = v; }
 
@@ -113,18 +114,18 @@ struct Eight {
     u32x4 w[TYPE == APB_F32 ? 2 : 1];
 };
 
-template <int TYPE>
+template <int TYPE, bool ONCE = false>
 __device__ __forceinline__ Eight<TYPE> load_eight(const void* X, long long at) {
     Eight<TYPE> v;
     const uint8_t* p = static_cast<const uint8_t*>(X) + at * (TYPE == APB_F32 ? 4 : 2);
-    v.w[0] = load16_any(p);
-    if constexpr (TYPE == APB_F32) v.w[1] = load16_any(p + 16);
+    v.w[0] = ONCE ? load16_once(p) : load16_any(p);
+    if constexpr (TYPE == APB_F32) v.w[1] = ONCE ? load16_once(p + 16) : load16_any(p + 16);
     return v;
 }
-// ... of which `have` exist; the others are zero
-template <int TYPE>
+// ... of which `have` exist; the others are zero.  ONCE: memory that is read once passes by the caches' other lines.
+template <int TYPE, bool ONCE = false>
 __device__ __forceinline__ Eight<TYPE> load_some(const void* X, long long at, int have) {
-    if (have >= 8) return load_eight<TYPE>(X, at);
+    if (have >= 8) return load_eight<TYPE, ONCE>(X, at);
     Eight<TYPE> v;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {

@@ -141,6 +141,23 @@ def test_combine(b, T, k, N, t):
         assert none is None and torch.equal(only, gz[:, :N].contiguous())
 
 
+@pytest.mark.parametrize("N,t", [(8192, "bf16"), (8190, "f16"), (4099, "f32")])
+def test_combine_beyond_the_caches(b, N, t):
+    """Rows larger than the caches are read another way: to the bit what their quarters give, which are not."""
+    print(f"[case] large combine {N} {t}", flush=True)
+    T, k, q = 2100, 4, 525
+    z, dy = torch.randn(T * k, N, device="cuda").to(TYPE[t]), torch.randn(T, N, device="cuda").to(TYPE[t])
+    row = torch.cat([torch.randperm(q * k, device="cuda").int().view(q, k) for _ in range(4)])        # within its quarter's rows
+    far = row + torch.arange(4, device="cuda", dtype=torch.int32).repeat_interleave(q)[:, None] * (q * k)
+    w = torch.rand(T, k, device="cuda")
+    y, (dz, dw) = b.apb_moe_combine(z, far, w), b.apb_moe_combine_backward(dy, z, far, w)
+    for c in range(4):
+        rows, tokens = slice(c * q * k, (c + 1) * q * k), slice(c * q, (c + 1) * q)
+        assert torch.equal(y[tokens], b.apb_moe_combine(z[rows], row[tokens], w[tokens]))
+        dz_c, dw_c = b.apb_moe_combine_backward(dy[tokens], z[rows], row[tokens], w[tokens])
+        assert torch.equal(dz[rows], dz_c) and torch.equal(dw[tokens], dw_c)
+
+
 def test_slots_of_weight_zero_add_nothing(b):
     z = torch.ones(6, 40, device="cuda")
     z[2], z[5] = float("nan"), float("inf")
