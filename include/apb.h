@@ -367,8 +367,9 @@ int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const 
 /* The gradients at the quantized operands (straight-through, as apb_train_backward has it):
  *      dX[m, k]     = sum_n G[m, n] * W^[n, k]                (grouped: W^ of the row's expert)
  *      dW[e][n, k]  = sum over the rows m of expert e of G[m, n] * X^[m, k]
- * G keeps every bit of its type: the matrix cores multiply bfloat16, in which 4-bit values are exact, and a
- * G of APB_F16 or APB_F32 goes through them as two or three bfloat16 parts whose sum it is.
+ * G keeps the bits of its type: the matrix cores multiply bfloat16, in which 4-bit values are exact, and a
+ * G of APB_F16 or APB_F32 goes through them as two or three bfloat16 parts whose sum it is
+ * (APB_F32 below 2^-125: to within 2^-148).
  *   G   DEVICE, M rows of N elements of g_type, ldg <= 2^22 apart.
  *   W   DEVICE, 4-bit matrix of E*N rows of K.     X  DEVICE, 4-bit matrix of M rows of K.
  *   dX  DEVICE, M rows of K elements of `type`, ldx apart, fully overwritten.
