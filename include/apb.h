@@ -334,7 +334,7 @@ int apb_train_backward(const float* W, const float* G, long long n, float alpha,
  * Sums are float32.  Everything only enqueues on `stream`, allocates nothing and records no memset. */
 enum apb_type { APB_F32 = 0, APB_BF16 = 1, APB_F16 = 2 };
 
-/* Bytes of a 4-bit matrix; 0 on bad arguments (rows or K <= 0, K > 2^22, or rows * ceil(K/256) >= 2^27). */
+/* Bytes of a 4-bit matrix; 0 on bad arguments (rows or K <= 0, K > 2^22, or rows * ceil(K/256) > 2^27 - 8). */
 size_t apb_mx4_bytes(int rows, int K);
 
 /*   X           DEVICE, element (r, k) at X[r * row_stride + k * col_stride]; strides of any sign or order.

@@ -30,9 +30,10 @@ struct Mx {
 
 inline int mx_segs(int K) { return (int)(((long long)K + kMxSeg - 1) / kMxSeg); }
 constexpr int kMxMaxK = 1 << 22;
-// rows * segs < 2^27 (34 G values): eight segments to a workgroup of 256 lanes, the lanes of a launch fit 32 bits
+constexpr long long kMxMaxSegs = (1LL << 27) - 8;   // of a matrix (34 G values): eight go to a workgroup of 256 lanes, and a launch has
+                                                    // fewer than 2^32 lanes
 inline bool bad_shape_mx(long long rows, int K) {
-    return rows <= 0 || K <= 0 || K > kMxMaxK || rows * mx_segs(K) >= (1LL << 27);
+    return rows <= 0 || K <= 0 || K > kMxMaxK || rows * mx_segs(K) > kMxMaxSegs;
 }
 inline Mx mx_view(const void* p, int rows, int K) {
     const int segs = mx_segs(K);

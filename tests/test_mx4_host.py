@@ -130,3 +130,17 @@ def test_refusals(b):
             cb(dw=odd)] == [N, N, N, N, T, S, S, S, S, A, A]
     for code in (b.APB_ERR_TYPE, b.APB_ERR_ALIGN):
         assert "unknown" not in b.strerror(code)
+
+
+@built
+def test_no_size_is_accepted_that_a_launch_cannot_have(b):
+    """Eight segments of 256 values go to a workgroup of 256 lanes, and a launch has fewer than 2^32 lanes."""
+    most = (1 << 27) - 8
+    assert (most + 7) // 8 * 256 < 1 << 32 <= (most + 8) // 8 * 256
+    p = ctypes.c_void_p(4096)                                         # never dereferenced
+    assert b.apb_mx4_bytes(most, 1) == most * 136 and b.apb_mx4_bytes(most // 2, 257) == most * 136
+    for rows, K in ((most + 1, 1), (most + 7, 200), (most // 2 + 1, 257)):
+        assert b.apb_mx4_bytes(rows, K) == 0
+        assert b.load().apb_mx4_quantize(p, 0, K, 1, rows, None, rows, K, p, None) == b.APB_ERR_SHAPE
+        assert b.load().apb_mx4_dequantize(p, rows, K, 0, p, K, None) == b.APB_ERR_SHAPE
+        assert b.load().apb_mx4_gemm(p, p, None, 1, rows, 4, K, 0, p, 4, None) == b.APB_ERR_SHAPE
