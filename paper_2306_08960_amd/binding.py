@@ -751,11 +751,15 @@ def apb_mx4_linear(X: torch.Tensor, W: torch.Tensor, N: int, dtype: Optional[tor
     off, E = _experts(offsets)
     lib, wp = load(), _mx4_ptr(W, E * N, K, "W")
     if scratch is not None:
-        sp = _mx4_ptr(scratch, M, K, "scratch")
+        sp = _array(scratch, torch.uint8, None, "scratch")
+        if scratch.numel() < M * ((K + 255) // 256) * 136:            # (whole 4-bit matrices are always enough: nothing is asked)
+            if scratch.numel() < lib.apb_mx4_linear_scratch_bytes(off is not None, E, M, N, K):
+                raise ValueError("scratch smaller than apb_mx4_linear_scratch_bytes(...)")
+            sp = wp                                                   # (none needed: not touched, but not NULL)
     else:
         need = lib.apb_mx4_linear_scratch_bytes(off is not None, E, M, N, K)
         scratch = _new(X, need, torch.uint8, stream) if need else None
-        sp = scratch.data_ptr() if need else wp                       # (none needed: not touched, but not NULL)
+        sp = scratch.data_ptr() if need else wp
     Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y", stream)
     _check(lib.apb_mx4_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), wp, off, E, M, int(N), K, sp, yt, yp,
                               ldy, _stream(stream)), "apb_mx4_linear")

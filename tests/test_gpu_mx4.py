@@ -477,3 +477,19 @@ def test_no_scratch_is_touched_where_none_is_needed(b):
     before, scratch = w4.clone(), torch.full((b.apb_mx4_bytes(3, 512),), 0xa5, dtype=torch.uint8, device="cuda")
     assert torch.equal(b.apb_mx4_linear(x, w4, 70), b.apb_mx4_linear(x, w4, 70, scratch=scratch))
     assert torch.equal(w4, before) and (scratch == 0xa5).all()
+
+
+def test_scratch_of_the_published_size_is_enough(b):
+    """As many bytes as apb_mx4_linear_scratch_bytes says: none, or what the 4-bit form takes; one byte less is refused."""
+    w4 = b.apb_mx4_quantize(torch.from_numpy(_weights(3, 70, 512)).cuda())
+    for M in (3, 200):
+        x = torch.from_numpy(_acts(M, M, 512)).cuda()
+        need = b.apb_mx4_linear_scratch_bytes(False, 1, M, 70, 512)
+        assert (need == 0) == (M == 3)
+        want = b.apb_mx4_linear(x, w4, 70)
+        assert torch.equal(b.apb_mx4_linear(x, w4, 70, scratch=torch.empty(need, dtype=torch.uint8, device="cuda")), want)
+        if need:
+            with pytest.raises(ValueError):
+                b.apb_mx4_linear(x, w4, 70, scratch=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+        with pytest.raises(TypeError):
+            b.apb_mx4_linear(x, w4, 70, scratch=torch.empty(need, device="cuda"))
