@@ -259,13 +259,14 @@ __device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f3
 // ---- loads to LDS --------------------------------------------------------------------------------------
 
 // A load of 16 (4) bytes per lane that goes to LDS, to 16 (4) bytes per lane from `to` on, without passing through registers.  Written
-// out because several segments can be under way: the compiler would wait for all of them before each read of LDS.  Whoever
-// reads what arrived waits for it first (s_waitcnt vmcnt).
+// out because several segments can be under way: the compiler would wait for all of them before each read of LDS.  `to` is asked for in
+// m0, where the instruction looks for it, so the compiler knows what m0 holds.  Whoever reads what arrived waits for it first
+// (s_waitcnt vmcnt).
 __device__ __forceinline__ void load16_to_lds(uint32_t to, const void* base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base));
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(offset), "s"(base));
 }
 __device__ __forceinline__ void load4_to_lds(uint32_t to, const void* base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base));
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(to), "v"(offset), "s"(base));
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;

@@ -2,6 +2,9 @@
 library's checks of arguments, each of which answers before anything is launched."""
 import ctypes
 import os
+import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -144,3 +147,36 @@ def test_no_size_is_accepted_that_a_launch_cannot_have(b):
         assert b.load().apb_mx4_quantize(p, 0, K, 1, rows, None, rows, K, p, None) == b.APB_ERR_SHAPE
         assert b.load().apb_mx4_dequantize(p, rows, K, 0, p, K, None) == b.APB_ERR_SHAPE
         assert b.load().apb_mx4_gemm(p, p, None, 1, rows, 4, K, 0, p, 4, None) == b.APB_ERR_SHAPE
+
+
+HOLDS_M0 = r"""
+#include "apb_mx4.h"
+using namespace apb;
+typedef __attribute__((address_space(3))) uint32_t* Lds;
+typedef __attribute__((address_space(1))) uint32_t* Global;
+// two loads to the same place of LDS, for which the compiler sets m0, and the library's own between them
+__global__ void between(const uint32_t* a, const uint32_t* b, uint32_t* out) {
+    __shared__ uint32_t lds[256];
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(lds));
+    __builtin_amdgcn_global_load_lds((Global)(a + threadIdx.x), (Lds)lds, 4, 0, 0);
+    LOAD(at + 512, b, 4 * threadIdx.x);
+    __builtin_amdgcn_global_load_lds((Global)(a + 64 + threadIdx.x), (Lds)lds, 4, 256, 0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    out[threadIdx.x] = lds[threadIdx.x] + lds[64 + threadIdx.x] + lds[128 + threadIdx.x];
+}
+"""
+
+
+@pytest.mark.parametrize("load", ["load4_to_lds", "load16_to_lds"])
+def test_loads_to_lds_say_that_they_change_m0(tmp_path, load):
+    """Compiled, not run: the compiler sets m0 again for a load of its own behind one of the library's."""
+    hipcc = os.environ.get("HIPCC") or shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    if not os.path.exists(hipcc):
+        pytest.skip("hipcc not found")
+    src, asm = tmp_path / "m0.hip", tmp_path / "m0.s"
+    src.write_text(HOLDS_M0)
+    subprocess.run([hipcc, "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+                    f"-DLOAD={load}", "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2306_08960_amd", "csrc"),
+                    "--cuda-device-only", "-S", str(src), "-o", str(asm)], check=True, stderr=subprocess.DEVNULL)
+    order = re.findall(r"^\s+(s_\w+ m0,|global_load_lds)", asm.read_text(), re.M)
+    assert [i.startswith("global") for i in order] == [False, True] * 3
