@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "apb_internal.h"
+#include "apb_mx4_shape.h"
 
 namespace apb {
 
@@ -16,11 +17,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kMxBlock = 32;                  // values that share a scale
-constexpr int kMxSeg = 256;                   // a row is padded to whole segments of 256 values: one 128-byte line of
-                                              // codes, 8 scale bytes
-constexpr int kMxSegBytes = kMxSeg / 2;
-
 // A 4-bit matrix in memory (the layout of apb.h).
 struct Mx {
     const uint8_t* codes;                     // [rows][segs * 128]
@@ -28,13 +24,6 @@ struct Mx {
     int rows, segs;
 };
 
-inline int mx_segs(int K) { return (int)(((long long)K + kMxSeg - 1) / kMxSeg); }
-constexpr int kMxMaxK = 1 << 22;
-constexpr long long kMxMaxSegs = (1LL << 27) - 8;   // of a matrix (34 G values): eight go to a workgroup of 256 lanes, and a launch has
-                                                    // fewer than 2^32 lanes
-inline bool bad_shape_mx(long long rows, int K) {
-    return rows <= 0 || K <= 0 || K > kMxMaxK || rows * mx_segs(K) > kMxMaxSegs;
-}
 inline Mx mx_view(const void* p, int rows, int K) {
     const int segs = mx_segs(K);
     const uint8_t* b = static_cast<const uint8_t*>(p);
@@ -389,12 +378,6 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[F][F], uint32_t l
 struct RowTile {
     int e, row0, rows;
 };
-
-// Tiles of `tile` rows that R rows in E groups (and the rows behind them) take at most.
-inline long long max_row_tiles(int R, int E, bool grouped, int tile) {
-    const long long whole = ((long long)R + tile - 1) / tile;
-    return grouped ? whole + std::min<long long>((long long)E + 1, R) : whole;
-}
 
 // The t-th tile of `tile` rows.  Called by whole waves, all lanes with the same t; each lane takes a group, a prefix sum over
 // the lanes counts tiles, 64 groups at a time.

@@ -15,8 +15,7 @@ namespace apb {
 namespace {
 
 constexpr int kGroup = 256;                   // threads that make a tile: four waves
-constexpr int kMaxSlices = 32;
-constexpr int kStep = 64;                     // summed over per pass: a line of 128 bytes of bfloat16 in LDS
+constexpr int kStep = kMx4Pass;               // summed over per pass: a line of 128 bytes of bfloat16 in LDS
 
 template <int TYPE>
 struct Parts {
@@ -495,40 +494,8 @@ __global__ __launch_bounds__(kGroup) void k_mx4_join(const float* __restrict__ p
     store4(out, type, (long long)row * ldo + k, sum, have);
 }
 
-// How the work is laid out: tiles of 64 * f a side, by how many groups of waves each, in how many slices.
-struct Plan {
-    int f, groups, slices;
-};
-
-template <bool WEIGHT>
-Plan plan_of(int g_type, bool grouped, int E, int M, int N, int K, bool workspace = true) {
-    auto tiles = [&](int side) { return ((long long)(WEIGHT ? N : M) + side - 1) / side * ((K + side - 1) / side) * (WEIGHT ? E : 1); };
-    // passes of a tile, were the experts all alike
-    const long long passes = ((WEIGHT ? (grouped ? M / E : M) : N) + kStep - 1) / kStep;
-    // slices that make a workgroup for each compute unit, of at least `least` passes
-    auto slices = [&](long long n, long long least) {
-        return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(256 / n, passes / least), workspace ? kMaxSlices : 1));
-    };
-    // Measured in bfloat16 (us).  256 a side wherever they fill more than half of the chip: 4096^3 121, 128 a side 183; dX of 2560 x
-    // 4096 x 4096 100 and 127; in two slices where they fill half of it and the sums are long: 4096 x 8192 x 2048 131, 128 a side
-    // 174.  128 a side likewise, with a second group up to one tile per compute unit: 2048^3 28, with one group 35, 64 a side 54.
-    // 64 a side if those fill the chip and the sums are short: 1024^3 11, 128 a side in slices 21.  Then slices: 512 x 4096 x 4096
-    // 37, without 45; dW of 8192 x 1024 x 1024 39, without 50; of 16384 x 256 x 256 15, without 91; dX of 64 x 1000 x 64 in slices
-    // of 4 passes 7.8, of 8 9.1.
-    const bool two_groups = g_type == APB_BF16 && tiles(128) <= 256;
-    if (g_type == APB_BF16 && tiles(256) >= 144) return Plan{4, 1, 1};
-    if (g_type == APB_BF16 && tiles(256) >= 96 && tiles(256) <= 128 && passes >= 64 && workspace) return Plan{4, 1, 2};
-    if (tiles(128) >= 192) return Plan{2, two_groups ? 2 : 1, 1};
-    if (tiles(64) >= 192 && passes <= 24) return Plan{1, 2, 1};
-    const int shared = slices(tiles(128), g_type == APB_BF16 ? 20 : 12);      // (more parts of G: passes take longer, joining does not)
-    if (tiles(128) * shared >= 128) return Plan{2, two_groups && shared == 1 ? 2 : 1, shared};
-    // (sharing costs 3 us, a pass 0.35: two that share 8 passes lose 3 us against one, four that share 16 gain 1)
-    const int quarters = slices(tiles(64), 4);
-    return Plan{1, 2, quarters > 2 ? quarters : slices(tiles(64), 8)};
-}
-
 template <int TYPE, bool WEIGHT, int F, int GROUPS>
-void launch_tiles(const Plan& plan, const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
+void launch_tiles(const Mx4Plan& plan, const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
                   void* out, long long ldo, hipStream_t s) {
     constexpr int kTile = 64 * F;
     const unsigned tiles_i = (unsigned)(WEIGHT ? (N + kTile - 1) / kTile : max_row_tiles(M, E, offsets != nullptr, kTile));
@@ -538,7 +505,7 @@ void launch_tiles(const Plan& plan, const void* G, long long ldg, const Mx& Q, c
 }
 
 template <int TYPE, bool WEIGHT>
-void launch_type(const Plan& plan, const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
+void launch_type(const Mx4Plan& plan, const void* G, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
                  void* out, long long ldo, hipStream_t s) {
     if constexpr (TYPE == APB_BF16) {
         if (plan.f == 4) return launch_tiles<TYPE, WEIGHT, 4, 1>(plan, G, ldg, Q, offsets, E, M, N, K, type, out, ldo, s);
@@ -549,15 +516,15 @@ void launch_type(const Plan& plan, const void* G, long long ldg, const Mx& Q, co
 }
 
 template <bool WEIGHT>
-size_t workspace_bytes(const Plan& plan, int E, int M, int N, int K) {
+size_t workspace_bytes(const Mx4Plan& plan, int E, int M, int N, int K) {
     return plan.slices > 1 ? (size_t)plan.slices * (WEIGHT ? (size_t)E * N : M) * K * sizeof(float) : 0;
 }
 
 template <bool WEIGHT>
 int launch(const void* G, int g_type, long long ldg, const Mx& Q, const int32_t* offsets, int E, int M, int N, int K, int type,
            void* out, long long ldo, void* workspace, size_t bytes, hipStream_t s) {
-    Plan plan = plan_of<WEIGHT>(g_type, offsets != nullptr, E, M, N, K);
-    if (!workspace || bytes < workspace_bytes<WEIGHT>(plan, E, M, N, K)) plan = plan_of<WEIGHT>(g_type, offsets != nullptr, E, M, N, K, false);
+    Mx4Plan plan = mx4_gradient_plan<WEIGHT>(g_type, offsets != nullptr, E, M, N, K);
+    if (!workspace || bytes < workspace_bytes<WEIGHT>(plan, E, M, N, K)) plan = mx4_gradient_plan<WEIGHT>(g_type, offsets != nullptr, E, M, N, K, false);
     const bool split = plan.slices > 1;
     void* to = split ? workspace : out;
     const int to_type = split ? (int)APB_F32 : type;
@@ -597,13 +564,13 @@ extern "C" {
 size_t apb_mx4_backward_input_workspace_bytes(int g_type, int grouped, int E, int M, int N, int K) {
     const int32_t some = 0;
     if (bad_type(g_type) || bad_product(E, M, N, K, grouped ? &some : nullptr)) return 0;
-    return workspace_bytes<false>(plan_of<false>(g_type, grouped != 0, E, M, N, K), E, M, N, K);
+    return workspace_bytes<false>(mx4_gradient_plan<false>(g_type, grouped != 0, E, M, N, K), E, M, N, K);
 }
 
 size_t apb_mx4_backward_weight_workspace_bytes(int g_type, int grouped, int E, int M, int N, int K) {
     const int32_t some = 0;
     if (bad_type(g_type) || bad_product(E, M, N, K, grouped ? &some : nullptr)) return 0;
-    return workspace_bytes<true>(plan_of<true>(g_type, grouped != 0, E, M, N, K), E, M, N, K);
+    return workspace_bytes<true>(mx4_gradient_plan<true>(g_type, grouped != 0, E, M, N, K), E, M, N, K);
 }
 
 int apb_mx4_backward_input(const void* G, int g_type, long long ldg, const void* W, const int32_t* offsets, int E, int M,

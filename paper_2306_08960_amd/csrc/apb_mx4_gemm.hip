@@ -190,12 +190,9 @@ void launch_tiles(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M
 
 int launch_mx4_gemm(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy,
                     hipStream_t s) {
-    // Tiles of 256 a side load least per product, and there is one to a compute unit; smaller ones fill the chip sooner.  Measured
-    // with 256, 128 and 64 a side (us): 4096^3 42, 52, 84; 1500 x 8192 x 4096 (192 tiles of 256) 36, 41, 66; 2560 x 2560 x 4096
-    // (100) 31, 27, 39; 1024 x 4096 x 4096 (64) 31, 15, 23; 512 x 4096 x 4096 (32) 27, 12, 12; 1024 x 1024 x 4096 (16) 28, 12, 9.
-    const long long big = ((long long)M + 255) / 256 * ((N + 255) / 256);
-    if (big >= 192) launch_tiles<4>(A, B, offsets, E, M, N, type, Y, ldy, s);
-    else if (big * 4 >= 192) launch_tiles<2>(A, B, offsets, E, M, N, type, Y, ldy, s);
+    const int side = mx4_product_side(M, N);
+    if (side == 256) launch_tiles<4>(A, B, offsets, E, M, N, type, Y, ldy, s);
+    else if (side == 128) launch_tiles<2>(A, B, offsets, E, M, N, type, Y, ldy, s);
     else launch_tiles<1>(A, B, offsets, E, M, N, type, Y, ldy, s);
     APB_HIP(hipGetLastError());
     return APB_OK;

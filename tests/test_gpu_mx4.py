@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+import mx4_tile_cases as cases
 from oracle import mx4_oracle as o
 
 pytestmark = pytest.mark.gpu
@@ -493,3 +494,54 @@ def test_scratch_of_the_published_size_is_enough(b):
                 b.apb_mx4_linear(x, w4, 70, scratch=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
         with pytest.raises(TypeError):
             b.apb_mx4_linear(x, w4, 70, scratch=torch.empty(need, device="cuda"))
+
+
+# ------------------------------------------------------------------------------------------ every tile size
+
+@pytest.mark.parametrize("M,N,K,E,side", cases.PRODUCTS)
+def test_products_of_every_tile_size(b, M, N, K, E, side):
+    """Ragged products by tiles of 64, 128 and 256 a side, plain and in groups, into every type; what lies around Y stays."""
+    print(f"[case] mx4 tiles {M} {N} {K} {E} {side}", flush=True)
+    off = cases.offsets(M, E)
+    dev = None if off is None else torch.from_numpy(off).cuda()
+    xf, wf = _acts(M + N + K, M, K), _weights(N + K, max(E, 1) * N, K)
+    x4, w4 = b.apb_mx4_quantize(torch.from_numpy(xf).cuda()), b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    want, mag = o.product(o.quantized(xf), o.quantized(wf), N, off)
+    for out in ("f32", "bf16", "f16"):
+        guard = torch.full((M + 2, N + 5), 7.0, dtype=TYPE[out], device="cuda")
+        y = guard[1:M + 1, 2:N + 2]
+        b.apb_mx4_gemm(x4, w4, M, N, K, Y=y, offsets=dev)
+        _close(_np(y), want, mag, K, out)
+        assert E == 0 or (y[int(off[-1]):] == 0).all()
+        y.fill_(7.0)
+        assert (guard == 7).all()
+        again = b.apb_mx4_linear(torch.from_numpy(xf).cuda(), w4, N, dtype=TYPE[out], offsets=dev)
+        assert torch.equal(again, b.apb_mx4_gemm(x4, w4, M, N, K, dtype=TYPE[out], offsets=dev))
+
+
+@pytest.mark.parametrize("M,N,K,E,side", cases.PRODUCTS)
+def test_nan_stays_in_its_row_and_column_for_every_tile_size(b, M, N, K, E, side):
+    """A block of NaN or of an infinity on either side makes its row or column of Y NaN and changes no bit of another."""
+    print(f"[case] mx4 tiles with nan {M} {N} {K} {E} {side}", flush=True)
+    off = cases.offsets(M, E)
+    dev = None if off is None else torch.from_numpy(off).cuda()
+    last = M if off is None else int(off[-1])
+    x, w = torch.from_numpy(_acts(M + N, M, K)).cuda(), torch.from_numpy(_weights(N, max(E, 1) * N, K)).cuda()
+    y = b.apb_mx4_linear(x, b.apb_mx4_quantize(w), N, offsets=dev)
+    rows, cols = [0, last // 2, last - 1], [0, 3, N - 1]
+    x[rows[0], 0], x[rows[1], K - 1], x[rows[2], K // 2] = float("nan"), float("inf"), float("-inf")
+    got = b.apb_mx4_linear(x, b.apb_mx4_quantize(w), N, offsets=dev)
+    assert torch.isnan(got[rows]).all()
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep[rows] = False
+    assert torch.equal(got[keep], y[keep]) and torch.isfinite(y).all()
+    e = max(E, 1) - 1                                                # (the last expert: it has rows)
+    first = 0 if off is None else int(off[e])
+    for i, n in enumerate(cols):
+        w[e * N + n, i * (K - 1) // 2] = (float("nan"), float("inf"), float("nan"))[i]
+    got = b.apb_mx4_linear(x, b.apb_mx4_quantize(w), N, offsets=dev)
+    assert torch.isnan(got[first:last][:, cols]).all()
+    keep_cols = torch.ones(N, dtype=torch.bool, device="cuda")
+    keep_cols[cols] = False
+    assert torch.equal(got[keep][:, keep_cols], y[keep][:, keep_cols])
+    assert torch.equal(got[:first][keep[:first]], y[:first][keep[:first]]) and (got[last:] == 0).all()
