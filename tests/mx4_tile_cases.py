@@ -1,5 +1,5 @@
-"""Sizes by which the products of 4-bit matrices reach every tile size, and the offsets of their groups.  The host
-test checks that the rules send them there, the GPU tests what comes out."""
+"""Sizes by which the products of 4-bit matrices and their gradients reach every tile size, and the offsets of their groups.  The
+host test checks that the rules send them there, the GPU tests what comes out."""
 import numpy as np
 
 # M, N, K, E (0: no groups), side of the product's tiles.  Ragged in every direction; a K of one segment is fewer passes than the
@@ -8,6 +8,24 @@ PRODUCTS = [
     (130, 300, 520, 0, 64),
     (1700, 2050, 300, 0, 128), (1540, 1801, 40, 0, 128), (1700, 2050, 1300, 5, 128),
     (3400, 3601, 520, 0, 256), (3330, 3650, 33, 0, 256), (3400, 3601, 777, 4, 256),
+]
+
+# M, N, K, E, type of the gradient, then for dX and dW: tiles of 64 * f a side, groups of waves, slices.  Sums of odd and even numbers
+# of passes of 64, the last one never whole; an N of whole blocks (1032, 2500) and others.
+GRADIENTS = [
+    (2000, 2050, 1900, 0, "bf16", (2, 2, 1), (2, 2, 1)), (2000, 2050, 1900, 0, "f32", (2, 1, 1), (2, 1, 1)),
+    (2000, 2050, 1900, 0, "f16", (2, 1, 1), (2, 1, 1)),
+    (2500, 2050, 2500, 0, "bf16", (2, 1, 1), (2, 1, 1)),
+    (510, 4100, 4000, 0, "bf16", (2, 1, 2), (4, 1, 1)), (510, 4100, 4000, 0, "f32", (2, 1, 2), (2, 1, 1)),
+    (510, 4100, 4000, 0, "f16", (2, 1, 2), (2, 1, 1)),
+    (8200, 1030, 1000, 0, "bf16", (2, 1, 1), (2, 1, 3)), (8200, 1030, 1000, 0, "f32", (2, 1, 1), (2, 1, 3)),
+    (8200, 1030, 1000, 0, "f16", (2, 1, 1), (2, 1, 3)),
+    (4133, 2500, 2500, 0, "bf16", (4, 1, 1), (4, 1, 2)),
+    (2500, 4133, 2500, 0, "bf16", (4, 1, 2), (4, 1, 1)),
+    (3400, 1032, 2600, 4, "bf16", (4, 1, 1), (4, 1, 1)),
+    (2000, 1026, 1900, 3, "bf16", (2, 2, 1), (2, 1, 1)), (2000, 1026, 1900, 3, "f32", (2, 1, 1), (2, 1, 1)),
+    (500, 4100, 2000, 2, "bf16", (2, 1, 3), (4, 1, 1)), (500, 4100, 2000, 2, "f16", (2, 1, 4), (2, 1, 1)),
+    (8200, 1030, 520, 2, "bf16", (2, 1, 1), (2, 1, 2)), (8200, 1030, 520, 2, "f32", (2, 1, 1), (2, 1, 2)),
 ]
 
 

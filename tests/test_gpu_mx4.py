@@ -545,3 +545,27 @@ def test_nan_stays_in_its_row_and_column_for_every_tile_size(b, M, N, K, E, side
     keep_cols[cols] = False
     assert torch.equal(got[keep][:, keep_cols], y[keep][:, keep_cols])
     assert torch.equal(got[:first][keep[:first]], y[:first][keep[:first]]) and (got[last:] == 0).all()
+
+
+@pytest.mark.parametrize("M,N,K,E,t,plan_x,plan_w", cases.GRADIENTS)
+def test_gradients_of_every_tile_size(b, M, N, K, E, t, plan_x, plan_w):
+    """Sums of many passes, by every kernel there is; with a workspace and without."""
+    print(f"[case] mx4 gradients by tiles {M} {N} {K} {E} {t} {plan_x} {plan_w}", flush=True)
+    off = cases.offsets(M, E)
+    dev = None if off is None else torch.from_numpy(off).cuda()
+    xf, wf = _acts(M + K, M, K), _weights(N + K, max(E, 1) * N, K)
+    g, gv = _in(np.random.default_rng(M * N).standard_normal((M, N)) * 1e-2, t)
+    x4, w4 = b.apb_mx4_quantize(torch.from_numpy(xf).cuda()), b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    dx, dw, mx, mw = o.gradients(gv, o.quantized(xf), o.quantized(wf), off)
+    longest = M if off is None else int(np.diff(off).max())
+    for small in (False, True):
+        ws = torch.empty(16, dtype=torch.uint8, device="cuda") if small else None
+        gx = torch.full((M + 1, K + 3), 7.0, dtype=TYPE[t], device="cuda")
+        gw = torch.full((max(E, 1) * N + 1, K + 3), 7.0, device="cuda")
+        b.apb_mx4_backward_input(g, w4, K, dX=gx[:M, 1:K + 1], offsets=dev, workspace=ws)
+        b.apb_mx4_backward_weight(g, x4, K, dW=gw[:-1, 1:K + 1], offsets=dev, workspace=ws)
+        _close(_np(gx[:M, 1:K + 1]), dx, mx, N, t, PARTS[t])
+        _close(_np(gw[:-1, 1:K + 1]), dw, mw, longest, "f32", PARTS[t])
+        for guard, rows in ((gx, M), (gw, max(E, 1) * N)):
+            guard[:rows, 1:K + 1] = 7.0
+            assert (guard == 7).all()

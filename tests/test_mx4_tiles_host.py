@@ -1,4 +1,4 @@
-"""The tile rules of the 4-bit products (apb_mx4_shape.h), compiled with the host compiler: the sizes that the GPU
+"""The tile rules of the 4-bit products and their gradients (apb_mx4_shape.h), compiled with the host compiler: the sizes that the GPU
 tests take reach the kernels that they are there for."""
 import os
 import subprocess
@@ -55,3 +55,14 @@ def test_products_reach_every_tile_size(ask):
     assert all(M > 16 * max(E, 1) for M, _, _, E, _ in cases.PRODUCTS)
     for plain in (True, False):
         assert {128, 256} <= {side for *_, E, side in cases.PRODUCTS if (E == 0) == plain}
+
+
+def test_gradients_reach_every_kernel(ask):
+    for i, what in ((5, "x"), (6, "w")):
+        got = ask([(what, TYPE[t], E, M, N, K) for M, N, K, E, t, *_ in cases.GRADIENTS])
+        assert got == [c[i] for c in cases.GRADIENTS]
+        # what there is by type of the gradient: tiles of 256 and two groups of waves on one of 128 in bfloat16 alone; with and without
+        # slices
+        reached = {(c[4], *c[i][:2], c[i][2] > 1) for c in cases.GRADIENTS}
+        assert reached >= {("bf16", 4, 1, False), ("bf16", 4, 1, True), ("bf16", 2, 2, False)}
+        assert reached >= {(t, 2, 1, shared) for t in TYPE for shared in (False, True)}
