@@ -28,6 +28,18 @@ GRADIENTS = [
     (8200, 1030, 520, 2, "bf16", (2, 1, 1), (2, 1, 2)), (8200, 1030, 520, 2, "f32", (2, 1, 1), (2, 1, 2)),
 ]
 
+# The same for a 4-bit matrix with blocks of NaN and of the smallest and largest scales: each tile size with whole passes of 64 and with
+# sums shorter than that.
+SPECIAL = [
+    (40, 50, 300, "bf16", (1, 2, 1), (1, 2, 1)), (40, 50, 300, "f32", (1, 2, 1), (1, 2, 1)),
+    (200, 300, 520, "bf16", (1, 2, 1), (1, 2, 1)), (200, 300, 520, "f16", (1, 2, 1), (1, 2, 1)), (200, 300, 520, "f32", (1, 2, 1), (1, 2, 1)),
+    (2050, 40, 1900, "bf16", (2, 2, 1), (1, 2, 8)), (40, 2050, 1900, "f32", (1, 2, 8), (2, 1, 1)),
+    (1700, 130, 1900, "bf16", (2, 2, 1), (1, 2, 2)), (1700, 130, 1900, "f16", (2, 1, 1), (1, 2, 2)), (1700, 130, 1900, "f32", (2, 1, 1), (1, 2, 2)),
+    (130, 1700, 1900, "bf16", (1, 2, 2), (2, 2, 1)), (130, 1700, 1900, "f32", (1, 2, 2), (2, 1, 1)),
+    (3400, 130, 2600, "bf16", (4, 1, 1), (1, 2, 2)), (130, 3400, 2600, "bf16", (1, 2, 2), (4, 1, 1)),
+    (3400, 40, 2600, "bf16", (4, 1, 1), (1, 2, 6)), (40, 3400, 2600, "bf16", (1, 2, 6), (4, 1, 1)),
+]
+
 
 def offsets(M, E):
     """An expert of 3/5 of the rows, one without any, one of 30, the others alike; ten rows belong to none."""

@@ -569,3 +569,40 @@ def test_gradients_of_every_tile_size(b, M, N, K, E, t, plan_x, plan_w):
         for guard, rows in ((gx, M), (gw, max(E, 1) * N)):
             guard[:rows, 1:K + 1] = 7.0
             assert (guard == 7).all()
+
+
+def _special_blocks(seed, rows, K):
+    """Rows with a block of NaN, of an infinity, of values below 2^-126 (scale code 0) and of the largest (252)."""
+    x = _weights(seed, rows, K)
+    x[rows // 3, 5], x[rows - 1, 40] = np.nan, -np.inf
+    x[rows // 2, 64:96] = np.random.default_rng(seed).choice([-1, 1], 32) * np.float32(2.0) ** -126 * np.linspace(0.01, 0.99, 32, dtype=np.float32)
+    x[1, 128:160] = np.random.default_rng(seed).choice([-1, 1], 32) * np.float32(3e38) * np.linspace(0.01, 1, 32, dtype=np.float32)
+    scales = o.quantize(x)[1]
+    assert scales[rows // 3, 0] == scales[rows - 1, 1] == 255 and scales[rows // 2, 2] == 0 and scales[1, 4] == 252
+    return x
+
+
+@pytest.mark.parametrize("M,N,K,t,plan_x,plan_w", cases.SPECIAL)
+def test_gradients_of_special_blocks(b, M, N, K, t, plan_x, plan_w):
+    """4-bit matrices with blocks of NaN and of the smallest and largest scales: a sum that meets a NaN is NaN, also where it meets it
+    with a zero, and no other.  Sums of values near the end of float32 are rounded to a multiple of 2^-149 in each addition."""
+    print(f"[case] mx4 gradients of special blocks {M} {N} {K} {t} {plan_x} {plan_w}", flush=True)
+    xf, wf = _special_blocks(M + K, M, K), _special_blocks(N + K, N, K)
+    # (the small blocks' columns hold nothing else, so that they are what the sums are made of)
+    for a in (xf, wf):
+        a[np.arange(len(a)) != len(a) // 2, 64:96] = 0
+    raw = np.random.default_rng(M * N).standard_normal((M, N)) * 2.0 ** -6
+    raw[0] = 0
+    raw[:, 0] = 0
+    g, gv = _in(raw, t)
+    x4, w4 = b.apb_mx4_quantize(torch.from_numpy(xf).cuda()), b.apb_mx4_quantize(torch.from_numpy(wf).cuda())
+    with np.errstate(invalid="ignore"):
+        dx, dw, mx, mw = o.gradients(gv, o.quantized(xf), o.quantized(wf))
+    got = (_np(b.apb_mx4_backward_input(g, w4, K, dtype=torch.float32)), _np(b.apb_mx4_backward_weight(g, x4, K)))
+    for have, want, mag, terms in zip(got, (dx, dw), (mx, mw), (N, M)):
+        nan = np.isnan(want)
+        assert nan[:, :64].all() and not nan[:, 64:].any()
+        assert np.array_equal(np.isnan(have), nan)
+        err, tol = np.abs(have - want)[:, 64:], (PARTS[t] * terms / 16 + 64) * (2.0 ** -23 * mag[:, 64:] + 2.0 ** -149)
+        assert (err <= tol).all(), (np.unravel_index(np.argmax(err - tol), err.shape), err.max())
+        assert np.abs(want[:, 64:96]).max() > 2.0 ** -136 and np.abs(want[:, 128:160]).max() > 2.0 ** 115

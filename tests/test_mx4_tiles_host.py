@@ -66,3 +66,11 @@ def test_gradients_reach_every_kernel(ask):
         reached = {(c[4], *c[i][:2], c[i][2] > 1) for c in cases.GRADIENTS}
         assert reached >= {("bf16", 4, 1, False), ("bf16", 4, 1, True), ("bf16", 2, 2, False)}
         assert reached >= {(t, 2, 1, shared) for t in TYPE for shared in (False, True)}
+
+
+def test_special_blocks_reach_every_tile_size(ask):
+    for i, what in ((4, "x"), (5, "w")):
+        assert ask([(what, TYPE[t], 0, M, N, K) for M, N, K, t, *_ in cases.SPECIAL]) == [c[i] for c in cases.SPECIAL]
+        for f in (1, 2, 4):                                          # sums of whole passes and shorter ones
+            long = {c[1 if what == "x" else 0] >= 64 for c in cases.SPECIAL if c[i][0] == f}
+            assert long == {True, False}
