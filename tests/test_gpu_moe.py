@@ -225,3 +225,32 @@ def test_refusals(b):
         b.apb_moe_combine(torch.zeros(8, 8, device="cuda"), row.long())
     with pytest.raises(ValueError):
         b.apb_moe_combine(torch.zeros(8, 8, device="cuda"), row, torch.ones(4, device="cuda"))
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 9, 3), (40, 24, 4), (70, 300, 8)])
+def test_route_gradient_by_differences_of_its_own_weights(b, T, E, k):
+    """Central differences of apb_moe_route's weights, s = 1/8 and 1/16 combined so that their s^2 terms cancel.  In one logit a weight
+    is a logistic function, the others what it leaves, and the fifth derivative of that function is 1/4 at most: s^4 / 480 * 1/4 * 2 max|d|
+    is left.  Weights are within 64 * 2^-24 of themselves, so a difference is within 64 * 2^-24 / s and the two combined within three
+    times that, of the sum of |d|; the gradient itself is within 128 * 2^-24 of twice that sum.  The logits lie 1/4 apart: no step
+    changes their order, and all of them are exact."""
+    g, s = np.random.default_rng(T + E), 2.0 ** -3
+    z = torch.from_numpy(np.stack([g.permutation(E) for _ in range(T)]).astype(np.float32) / 4).cuda()
+    d = torch.from_numpy(g.standard_normal((T, k)).astype(np.float32)).cuda()
+    r = b.apb_moe_route(z, k)
+    grad = b.apb_moe_route_backward(r["expert"], r["weight"], d, E).double()
+
+    def loss(j, step):
+        moved = z.scatter_add(1, r["expert"][:, j:j + 1].long(), torch.full((T, 1), step, device="cuda"))
+        at = b.apb_moe_route(moved, k)
+        assert torch.equal(at["expert"], r["expert"])
+        return (at["weight"].double() * d.double()).sum(1)
+
+    size = d.double().abs()
+    tol = (3 * 64 / s + 256) * U * size.sum(1) + s ** 4 / 480 / 4 * 2 * size.amax(1)
+    for j in range(k):
+        diff = [(loss(j, h) - loss(j, -h)) / (2 * h) for h in (s, s / 2)]
+        want = (4 * diff[1] - diff[0]) / 3
+        got = grad.gather(1, r["expert"][:, j:j + 1].long())[:, 0]
+        assert ((got - want).abs() <= tol).all()
+    assert tol.max() < 0.01 * grad.abs().max()                       # (the tolerance says something)
