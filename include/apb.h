@@ -325,9 +325,10 @@ int apb_train_backward(const float* W, const float* G, long long n, float alpha,
  *
  * Groups: `offsets` (DEVICE, E+1 int32, ascending, offsets[0] = 0) gives every expert e the rows
  * offsets[e] .. offsets[e+1]-1 of the left operand; the right operand then is E <= APB_MOE_MAX_E matrices of
- * N rows each (one 4-bit matrix of E*N rows).  Experts may have no rows.  Rows from offsets[E] on belong to no expert and
- * their results are 0.  offsets == NULL: one matrix, E must be 1.  The offsets are read on the device; values
- * that are not ascending or leave 0 .. M give unspecified results, never an access out of bounds.
+ * N rows each (one 4-bit matrix of E*N rows; N <= 128 * 65535, with groups and without).  Experts may have no rows.
+ * Rows from offsets[E] on belong to no expert and their results are 0.  offsets == NULL: one matrix, E must be 1.
+ * The offsets are read on the device; values that are not ascending or leave 0 .. M give unspecified results, never
+ * an access out of bounds.
  *
  * Element types of the float matrices: apb_type.  Row strides (ld...) count elements and may be any number
  * >= the row length; any alignment that suits the elements is taken.
@@ -404,13 +405,15 @@ int apb_moe_route(const void* logits, int type, long long ld, int T, int E, int 
                   int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* workspace, void* stream);
 
 /* dlogits[t, expert[t,j]] = weight[t,j] * (dweight[t,j] - sum_i weight[t,i] * dweight[t,i]), 0 elsewhere; expert,
- * weight as apb_moe_route left them (a token's weights sum to 1), dweight DEVICE, T*k floats.  dlogits: T rows of E elements of `type`, ld apart. */
+ * weight as apb_moe_route left them (a token's weights sum to 1), dweight DEVICE, T*k floats.  dlogits: T rows of E
+ * elements of `type`, ld apart.  T, E, k as in apb_moe_route. */
 int apb_moe_route_backward(const int32_t* expert, const float* weight, const float* dweight, int T, int E, int k, int type,
                            void* dlogits, long long ld, void* stream);
 
 /* Y[t] = sum_j weight[t,j] * Z[slot_row[t,j]], and its gradients dZ[slot_row[t,j]] = weight[t,j] * dY[t] and
  * dweight[t,j] = <dY[t], Z[slot_row[t,j]]>.  weight == NULL: all 1 (the gradient of the gather that rows_from is).
  * A slot of weight 0 adds nothing, whatever its row holds, and its dZ is 0.  Sums over j in the order of j.
+ *   k <= APB_MOE_MAX_K, T * k < 2^24, N <= 2^22.
  *   Z, dZ  DEVICE, T*k rows of N elements, ldz / lddz apart.   Y, dY  DEVICE, T rows of N elements, ldy / lddy apart.
  *   An entry of slot_row outside 0 .. T*k-1 is a row of zeros and its dZ is not written.
  *   dZ is fully overwritten if slot_row is a permutation.  dweight: T*k floats, or NULL. */

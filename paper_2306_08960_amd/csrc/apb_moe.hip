@@ -2,8 +2,9 @@
 // joining the experts' results; and both gradients.
 //
 // Routing is a few short kernels, each bound by its launch and a chain of dependent steps: 16384 tokens, 8 of 128 experts: choosing
-// 9 us, the two steps of the order 2 and 6, the logits' gradient 5; one token 3 as one kernel, and 1.8.  Joining is bound by memory:
-// 8192 tokens, 4 rows of 4096 bfloat16 values each, 336 MB: 59 us (5.7 TB/s); its gradients, 604 MB, 118 us (5.1), as fast as a copy.
+// 9.6 us, the two steps of the order 2.7 and 6.4, the logits' gradient 5.1; one token 3.1 as one kernel, and 1.8.  Joining is bound by
+// memory: 8192 tokens, 4 rows of 4096 bfloat16 values each, 336 MB: 65 us (5.2 TB/s); its gradients, 604 MB, 124 us (4.9); a large copy
+// runs at 5.1.
 //
 // The order is that of a stable counting sort by expert.  A token takes an expert once at most, so the slots of an expert
 // among 64 tokens are a 64-bit mask, the rank of one the number of mask bits below it, and nothing depends on the order in

@@ -40,8 +40,9 @@ inline bool bad_type(int t) { return t != APB_F32 && t != APB_BF16 && t != APB_F
 inline int type_size(int t) { return t == APB_F32 ? 4 : 2; }
 inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// n / d for any 32-bit n without a division: m = ceil(2^(32+s) / d) with 2^s >= d is less than 1 above 2^(32+s) / d, so n * m
-// is less than 2^(32+s) / d above n * 2^(32+s) / d: too little to reach the next whole quotient.
+// n / d for any 32-bit n without a division (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994):
+// m = ceil(2^(32+s) / d) with 2^s >= d is less than 1 above 2^(32+s) / d, so n * m is less than 2^(32+s) / d above n * 2^(32+s) / d:
+// too little to reach the next whole quotient.
 struct FastDiv {
     uint32_t mul, shift, d;
     __host__ explicit FastDiv(uint32_t div) : d(div) {

@@ -4,9 +4,10 @@
 // values, products of a level and a power of two, are exact in bfloat16, and the bfloat16 matrix instruction multiplies them
 // with G.  A bfloat16 G is taken as it is; a float16 G is the sum of two bfloat16 values, a float32 G of three (each part takes
 // the next 8 bits), and each part goes through the matrix cores, so no bit of G is dropped.
-// Bound by the matrix cores and their power: 8192^3 in bfloat16 takes 857 us for either gradient (1283 TFLOP/s; a large bfloat16
-// product of the library reaches 1400), 4096^3 121 and 123 us.  With nothing but the first pass's operands, from the caches, the
-// former is 3 % faster, so memory is not what it waits for.
+// Bound by the matrix cores and their power: dX and dW of 8192^3 in bfloat16, one call behind another, take 896 and 914 us (1230 and
+// 1200 TFLOP/s; a large bfloat16 product of the library reaches 1400), of 4096^3 123 and 132.  With nothing but the first pass's
+// operands, from the caches, the former is 3 % faster, so memory is not what it waits for.  Of 4096^3 with a float32 G 537 and 509 us,
+// a float16 G 342 and 375: three and two times the products, a split that every tile repeats, tiles of 128 a side.
 #include <utility>
 
 #include "apb_mx4.h"

@@ -1,7 +1,7 @@
 // Y = Q(X) W^T for few rows, plain or grouped by expert: what bounds it is reading the weights once.  One kernel: a workgroup
 // brings its rows of X into LDS as 4-bit blocks (quantizing them on the way) while its first weights are already under way, then
 // streams weights through a ring of its own in LDS into the matrix cores.  One row of 4096 through 4096 x 4096 weights, 8.9 MB:
-// 4.9 us, of which an empty launch has 2; 16 tokens at 4 of 64 experts of 2048 x 2048, 92 MB of weights: 19.5 us, 4.7 TB/s.
+// 5.1 us, of which an empty launch has 2; 16 tokens at 4 of 64 experts of 2048 x 2048, 92 MB of weights: 21 us, 4.3 TB/s.
 #include <atomic>
 #include <type_traits>
 
@@ -204,7 +204,7 @@ int launch(const Rows& X, const Mx& W, const int32_t* offsets, int E, int M, int
 // A workgroup quantizes every row it multiplies with, so the rows must be few and short.  Measured against quantization and
 // tiles (us): 4096 x 4096, 1 row 5.0 : 11.7, 16 rows 10.4 : 12.2, 32 rows 16.9 : 12.4; 8192 x 8192, 4 rows 12.2 : 19.9, 16 rows
 // 20.5 : 20.0; 64 experts of 2048 x 2048, a row each 20.5 : 26.1, 4 rows 33.9 : 36.1, 8 rows 38.4 : 36.8; 16 experts of
-// 2048 x 4096, 8 rows each 28.4 : 17.2.
+// 2048 x 4096, 8 rows each 28.4 : 17.2.  Not measured: experts of K above 8192, which go to tiles with a row each.
 bool mx4_few_applies(const int32_t* offsets, int E, int M, int K) {
     const int mean = offsets ? (M + E - 1) / E : M;              // rows of an expert, were they all alike
     return mean <= 16 && (long long)mean * K <= (offsets ? 8192 : 65536) && lds_bytes(std::min(M, 16), mx_segs(K)) <= kMaxLds;

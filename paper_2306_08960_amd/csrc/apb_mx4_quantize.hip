@@ -2,7 +2,7 @@
 // e = floor(log2(max |x|)) - 2, so that the largest magnitude lies in [4, 8) * 2^e, and each value becomes the nearest of
 // +-{0, .5, 1, 1.5, 2, 3, 4, 6} * 2^e (ties to the even index, beyond 6: 6).  The conversion instruction scales and rounds
 // once, so the codes are defined to the bit.  Both directions are one pass over memory and bound by it: 16384 x 4096 bfloat16
-// values, 134 MB and 36 MB of codes and scales, take 36 us there (4.7 TB/s; a large copy runs at 5.1) and 27 us back.
+// values, 134 MB and 36 MB of codes and scales, take 39 us there (4.4 TB/s; a large copy runs at 5.1) and 27 us back.
 #include "apb_mx4.h"
 
 namespace apb {

@@ -54,12 +54,12 @@ inline Mx4Plan mx4_gradient_plan(int g_type, bool grouped, int E, int M, int N, 
     auto slices = [&](long long n, long long least) {
         return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(256 / n, passes / least), workspace ? kMx4MaxSlices : 1));
     };
-    // Measured in bfloat16 on plain products (us).  256 a side wherever they fill more than half of the chip: 4096^3 121, 128 a side 183; dX of 2560 x
-    // 4096 x 4096 100 and 127; in two slices where they fill half of it and the sums are long: 4096 x 8192 x 2048 131, 128 a side
-    // 174.  128 a side likewise, with a second group up to one tile per compute unit: 2048^3 28, with one group 35, 64 a side 54.
-    // 64 a side if those fill the chip and the sums are short: 1024^3 11, 128 a side in slices 21.  Then slices: 512 x 4096 x 4096
-    // 37, without 45; dW of 8192 x 1024 x 1024 39, without 50; of 16384 x 256 x 256 15, without 91; dX of 64 x 1000 x 64 in slices
-    // of 4 passes 7.8, of 8 9.1.
+    // Measured in bfloat16 on plain products (us).  256 a side wherever they fill more than half of the chip: 4096^3 121, 128 a side 183;
+    // dX of 2560 x 4096 x 4096 100 and 127; in two slices where they fill half of it and the sums are long: 4096 x 8192 x 2048 131, 128
+    // a side 174.  128 a side likewise, with a second group up to one tile per compute unit: 2048^3 28, with one group 35, 64 a side 54.
+    // 64 a side if those fill the chip and the sums are short: 1024^3 11, 128 a side in slices 21.  Then slices: 512 x 4096 x 4096 37,
+    // without 45; dW of 8192 x 1024 x 1024 39, without 50; of 16384 x 256 x 256 15, without 91; dX of 64 x 1000 x 64 in slices of 4 passes
+    // 7.8, of 8 9.1.  dX counts the rows of all experts as one matrix: a tile may be taller than what an expert has.
     const bool two_groups = g_type == APB_BF16 && tiles(128) <= 256;
     if (g_type == APB_BF16 && tiles(256) >= 144) return Mx4Plan{4, 1, 1};
     if (g_type == APB_BF16 && tiles(256) >= 96 && tiles(256) <= 128 && passes >= 64 && workspace) return Mx4Plan{4, 1, 2};
