@@ -61,12 +61,12 @@ typedef enum apb_status {
     APB_ERR_NULL = -1,     /* a required pointer is NULL                                   */
     APB_ERR_SHAPE = -2,    /* N, K or M <= 0, or too large (N*K >= 2^31, 3*K >= 2^31, ...)  */
     APB_ERR_BITS = -3,     /* bits is not 1 or 2                                           */
-    APB_ERR_VALUE = -4,    /* delta is NaN; alpha negative or infinite; step not finite or <= 0 */
+    APB_ERR_VALUE = -4,    /* delta is NaN; alpha negative or infinite; step not finite or <= 0; no such activation */
     APB_ERR_NOMEM = -5,    /* host or device allocation failed                             */
     APB_ERR_HIP = -6,      /* a HIP call failed; see apb_last_hip_error()                  */
     APB_ERR_SCRATCH = -7,  /* apb_quantize_forward_static: sizes beyond the static scratch array */
     APB_ERR_TYPE = -8,     /* an element type is not one of apb_type                       */
-    APB_ERR_ALIGN = -9     /* a 4-bit matrix is not 16-byte aligned, or an array not aligned to its elements */
+    APB_ERR_ALIGN = -9     /* a 4- or 8-bit matrix is not 16-byte aligned, or an array not aligned to its elements */
 } apb_status;
 
 /* Opaque compressed layer.  Holds, in device memory: the sign words, the CSR of
@@ -422,6 +422,116 @@ int apb_moe_combine(const void* Z, int type, long long ldz, const int32_t* slot_
 int apb_moe_combine_backward(const void* dY, int type, long long lddy, const void* Z, long long ldz, const int32_t* slot_row,
                              const float* weight, int T, int k, int N, void* dZ, long long lddz, float* dweight,
                              void* stream);
+
+/* ---- 8-bit activation checkpoints -------------------------------------------------------------------
+ *
+ * What a training step keeps of its activations for the backward pass, in 8 bits.  Rows are cut into blocks of 32
+ * neighbours; a block has one scale 2^e (8 bits) and each value is a whole number:
+ *      e  = clamp(floor(log2(max |x|)) - 6, -127, 121)      (-127 for a block of zeros)
+ *      i  = clamp(x * 2^-e rounded to the nearest, midway to the even one, -127, 127),      x^ = i * 2^e
+ * so a value is off by at most 2^-7 of its block's largest magnitude (2^-134 in a block of the smallest scale).  A block
+ * that holds a NaN or an infinity gets the scale code of NaN: all its values read as NaN.  Defined to the bit.
+ *
+ * Layout of an 8-bit matrix of `rows` x K, with Kp = 32 * ceil(K / 32); 16-byte aligned:
+ *   int8  codes[rows][Kp]            values k >= K are 0
+ *   uint8 scales[rows][Kp/32]        e + 127, or 255 for NaN
+ * Plain device memory without a record of its sizes, like a 4-bit matrix. */
+enum { APB_MX8 = 3 };   /* beside apb_type, where a function says so: an 8-bit matrix */
+
+/* Bytes of an 8-bit matrix; 0 on bad arguments (rows or K <= 0, K > 2^22, or rows * ceil(K/32) > 2^30 - 64). */
+size_t apb_mx8_bytes(int rows, int K);
+/*   X  DEVICE, `rows` rows of K elements of `type`, ldx >= K apart.    mx8  DEVICE, apb_mx8_bytes(rows, K) bytes. */
+int apb_mx8_quantize(const void* X, int type, long long ldx, int rows, int K, void* mx8, void* stream);
+/* The values an 8-bit matrix stands for, rounded once to `type` (exact in APB_F32). */
+int apb_mx8_dequantize(const void* mx8, int rows, int K, int type, void* X, long long ldx, void* stream);
+
+/* ---- Gated feed-forward blocks ------------------------------------------------------------------------
+ *
+ *      Y[m, n] = act(G[m, n]) * U[m, n],      G = X Wg^T,  U = X Wu^T
+ * with act(x) one of
+ *      APB_SILU   x * s(x)                                            s(z) = 1 / (1 + e^-z)
+ *      APB_GELU   x * s(2 sqrt(2/pi) (x + 0.044715 x^3))              (the same as x/2 (1 + tanh(sqrt(2/pi) (x + ...))))
+ *      APB_RELU   max(x, 0)
+ * in float32; at the infinities their limits, NaN for NaN.  An s below 2^-126 counts as 0.
+ *
+ * A gated layer has ONE 4-bit matrix of weights, for every expert first the N rows of the gate, then the N rows of the up
+ * projection (E * 2N rows of K): what the gradients of the 4-bit products take with 2N in the place of N, and [dG | dU]
+ * (M rows of 2N) as their G.
+ *
+ * `saved` (optional, NULL: none) receives G and U for the backward pass as an 8-bit matrix of 2M rows of N: G's rows,
+ * then U's; apb_mx8_bytes(2M, N) bytes. */
+enum apb_activation { APB_SILU = 0, APB_GELU = 1, APB_RELU = 2 };
+
+/* Both projections of a 4-bit A (M rows of K), the activation and the product as one kernel.  offsets, E, Y as in
+ * apb_mx4_gemm; W: 4-bit matrix of E*2N rows; E*2N and M as apb_mx4_gemm has N and M.  Rows that belong to no expert: Y = 0
+ * and zeros in `saved`. */
+int apb_mx4_gated_gemm(const void* A, const void* W, const int32_t* offsets, int E, int M, int N, int K, int activation,
+                       int type, void* Y, long long ldy, void* saved, void* stream);
+/* The same from float activations, quantized within the call: as apb_mx4_linear is to apb_mx4_gemm, with few rows as a single
+ * kernel unless `saved` is asked for.  scratch: apb_mx4_gated_linear_scratch_bytes() bytes, 0 for the single kernel (not
+ * touched, but not NULL). */
+size_t apb_mx4_gated_linear_scratch_bytes(int grouped, int E, int M, int N, int K, int with_saved);
+int apb_mx4_gated_linear(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const void* W,
+                         const int32_t* offsets, int E, int M, int N, int K, int activation, void* scratch, int y_type,
+                         void* Y, long long ldy, void* saved, void* stream);
+
+/* From G and U at hand (M rows of 2N elements, [G | U], ldgu >= 2N apart), as a program has them that adds something to the
+ * projections first, such as adapters.  Y and GU are of `type`. */
+int apb_gated_forward(const void* GU, int type, long long ldgu, int M, int N, int activation, void* Y, long long ldy,
+                      void* saved, void* stream);
+/*      dG = dY * U * act'(G),  dU = dY * act(G)             (act'(0) = 0 for APB_RELU)
+ *   GU      DEVICE: gu_type APB_MX8: what `saved` holds (ldgu is not looked at); an apb_type: M rows of 2N elements.
+ *   dY      DEVICE, M rows of N elements of `type`.
+ *   dGU     DEVICE, M rows of 2N elements of `type`, [dG | dU], lddgu >= 2N apart, fully overwritten.
+ *   Y       NULL, or DEVICE, M rows of N elements of `type`: act(G) * U over again, so that a program need not keep it.
+ *   The outputs overlap nothing that is read, but dGU may be GU itself if it has the same type and row stride. */
+int apb_gated_backward(const void* GU, int gu_type, long long ldgu, const void* dY, int type, long long lddy, int M, int N,
+                       int activation, void* dGU, long long lddgu, void* Y, long long ldy, void* stream);
+
+/* ---- Low-rank adapters of many requests ---------------------------------------------------------------
+ *
+ * Beside a projection that all rows share, every request (or training sequence) has a low-rank matrix of its own:
+ *      T[m, :]  = scale[a] * X[m, :] A[a]^T          A[a]: r x K
+ *      Y[m, :]  = Y0[m, :] + T[m, :] B[a]            B[a]: r x N
+ * where a is the adapter of row m.  Both factors are held with their long side contiguous, A as [L][r][K] and B as
+ * [L][r][N], so the backward pass is the same operators with the factors exchanged:
+ *      dT[m, :] = scale[a] * dY[m, :] B[a]^T         apb_adapter_down(dY, B)
+ *      dX[m, :] = dX0[m, :] + dT[m, :] A[a]          apb_adapter_up(dT, A)
+ *      dB[a]    = sum over the rows m of a of  T[m, :]^T dY[m, :]         apb_adapter_gradient(T, dY)
+ *      dA[a]    = sum over the rows m of a of dT[m, :]^T  X[m, :]         apb_adapter_gradient(dT, X)
+ * Adapters of different ranks share a call with the largest one's r, the missing rows of A and B zero.
+ *
+ * Segments: offsets (DEVICE, S+1 int32, ascending, offsets[0] = 0) gives segment s the rows offsets[s] .. offsets[s+1]-1, and
+ * adapter[s] (DEVICE, S int32) its adapter; any number of segments may have the same one, and one outside 0 .. L-1 is none.
+ * adapter == NULL: segment s has adapter s (S == L).  offsets == NULL: one segment of all M rows (S == 1).  Rows without an
+ * adapter, and rows behind the last segment, have T = 0 and Y = Y0.  Offsets that are not ascending or leave 0 .. M give
+ * unspecified results, never an access out of bounds.
+ *
+ * T is float32, as `parts` sums whose total it is ([parts][M][r], parts = apb_adapter_parts(), fixed by the sizes): where rows
+ * are few, workgroups share a row's sum, and whoever reads T adds the parts up, in order.  Repeating a call repeats its
+ * bits.  X, A, Y0, Y are of one `type`; products are exact or float32, sums float32; Y is rounded once.
+ *   r <= APB_ADAPTER_MAX_R, S <= APB_ADAPTER_MAX_S, L <= APB_ADAPTER_MAX_L, K, N <= 2^22, M <= 2^24. */
+#define APB_ADAPTER_MAX_R 256
+#define APB_ADAPTER_MAX_S 4096
+#define APB_ADAPTER_MAX_L 4096
+int apb_adapter_parts(int S, int M, int K, int r);   /* 0 on bad arguments */
+/*   X  DEVICE, M rows of K elements, ldx >= K apart.   A  DEVICE, [L][r][K].   scale  DEVICE, L floats, or NULL: all 1.
+ *   T  DEVICE, apb_adapter_parts(S, M, K, r) * M * r floats, fully overwritten. */
+int apb_adapter_down(const void* X, int type, long long ldx, const void* A, const int32_t* offsets, const int32_t* adapter,
+                     const float* scale, int S, int L, int M, int K, int r, float* T, void* stream);
+/*   T   as apb_adapter_down left it, `parts` sums of it.   B  DEVICE, [L][r][N].
+ *   Y0  DEVICE, M rows of N elements, or NULL: zeros.      Y  DEVICE, the same, fully overwritten; may be Y0 itself
+ *       (with the same row stride), then rows without an adapter are not touched.  Otherwise the two do not overlap. */
+int apb_adapter_up(const float* T, int parts, const void* B, int type, const int32_t* offsets, const int32_t* adapter, int S,
+                   int L, int M, int N, int r, const void* Y0, long long ldy0, void* Y, long long ldy, void* stream);
+/*   X   DEVICE, M rows of K elements of x_type, ldx >= K apart; or x_type APB_MX8: an 8-bit matrix of M rows of K.
+ *   dA  DEVICE, [L][r][K] floats, fully overwritten (0 for an adapter without rows).
+ *   workspace, workspace_bytes  optional DEVICE scratch (NULL, 0: none), 4-byte aligned: with as many bytes as the function says
+ *       (0: no use for any), workgroups share the sum over many rows and join it in a fixed order. */
+size_t apb_adapter_gradient_workspace_bytes(int L, int M, int K, int r);
+int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, long long ldx, const int32_t* offsets,
+                         const int32_t* adapter, int S, int L, int M, int K, int r, float* dA, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /* ---- Measurement support: instruction-rate probes ---------------------------------------------
  *

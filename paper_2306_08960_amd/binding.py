@@ -29,6 +29,9 @@ EXPORTS = (
     "apb_mx4_backward_input", "apb_mx4_backward_weight", "apb_mx4_backward_input_workspace_bytes",
     "apb_mx4_backward_weight_workspace_bytes",
     "apb_moe_workspace_bytes", "apb_moe_route", "apb_moe_route_backward", "apb_moe_combine", "apb_moe_combine_backward",
+    "apb_mx8_bytes", "apb_mx8_quantize", "apb_mx8_dequantize", "apb_mx4_gated_gemm", "apb_mx4_gated_linear",
+    "apb_mx4_gated_linear_scratch_bytes", "apb_gated_forward", "apb_gated_backward",
+    "apb_adapter_parts", "apb_adapter_down", "apb_adapter_up", "apb_adapter_gradient", "apb_adapter_gradient_workspace_bytes",
     "apb_strerror", "apb_last_hip_error",
 )
 
@@ -132,9 +135,22 @@ def load() -> ctypes.CDLL:
                        ("apb_moe_route", [vp, ci, ll, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp]),
                        ("apb_moe_route_backward", [vp, vp, vp, ci, ci, ci, ci, vp, ll, vp]),
                        ("apb_moe_combine", [vp, ci, ll, vp, vp, ci, ci, ci, vp, ll, vp]),
-                       ("apb_moe_combine_backward", [vp, ci, ll, vp, ll, vp, vp, ci, ci, ci, vp, ll, vp, vp])):
+                       ("apb_moe_combine_backward", [vp, ci, ll, vp, ll, vp, vp, ci, ci, ci, vp, ll, vp, vp]),
+                       ("apb_mx8_quantize", [vp, ci, ll, ci, ci, vp, vp]),
+                       ("apb_mx8_dequantize", [vp, ci, ci, ci, vp, ll, vp]),
+                       ("apb_mx4_gated_gemm", [vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, ll, vp, vp]),
+                       ("apb_mx4_gated_linear", [vp, ci, ll, ci, vp, vp, vp, ci, ci, ci, ci, ci, vp, ci, vp, ll, vp, vp]),
+                       ("apb_gated_forward", [vp, ci, ll, ci, ci, ci, vp, ll, vp, vp]),
+                       ("apb_gated_backward", [vp, ci, ll, vp, ci, ll, ci, ci, ci, vp, ll, vp, ll, vp]),
+                       ("apb_adapter_parts", [ci] * 4),
+                       ("apb_adapter_down", [vp, ci, ll, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp]),
+                       ("apb_adapter_up", [vp, ci, vp, ci, vp, vp, ci, ci, ci, ci, ci, vp, ll, vp, ll, vp]),
+                       ("apb_adapter_gradient", [vp, ci, vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, vp, ctypes.c_size_t, vp])):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = ci
+    for name, sizes in (("apb_mx8_bytes", 2), ("apb_mx4_gated_linear_scratch_bytes", 6), ("apb_adapter_gradient_workspace_bytes", 4)):
+        getattr(lib, name).argtypes = [ci] * sizes
+        getattr(lib, name).restype = ctypes.c_size_t
     lib.apb_strerror.argtypes = [ci]
     lib.apb_strerror.restype = ctypes.c_char_p
     lib.apb_last_hip_error.argtypes = []
@@ -915,3 +931,256 @@ def apb_moe_combine_backward(dY: torch.Tensor, Z: Optional[torch.Tensor], slot_r
                                            None if dweight is None else dweight.data_ptr(), _stream(stream)),
            "apb_moe_combine_backward")
     return dZ, dweight
+
+
+# ----------------------------------------------------------------------------- 8-bit activation checkpoints
+
+_MX8 = 3                                                              # APB_MX8
+
+
+def apb_mx8_bytes(rows: int, K: int) -> int:
+    return int(load().apb_mx8_bytes(int(rows), int(K)))
+
+
+def alloc_mx8(rows: int, K: int, device=None) -> torch.Tensor:
+    """Memory for an 8-bit matrix of `rows` rows of K values (uint8, see the header for the layout)."""
+    nbytes = apb_mx8_bytes(rows, K)
+    if nbytes == 0:
+        raise ApbError(APB_ERR_SHAPE, "apb_mx8_bytes")
+    dev = device if device is not None else torch.device("cuda", torch.cuda.current_device())
+    return torch.empty(nbytes, dtype=torch.uint8, device=dev)
+
+
+def _mx8_ptr(mx8: Optional[torch.Tensor], rows: int, K: int, name: str) -> Optional[int]:
+    if mx8 is None:
+        return None
+    if mx8.numel() < rows * ((K + 31) // 32) * 33:                    # (as _mx4_ptr)
+        raise ValueError(f"{name} smaller than apb_mx8_bytes({rows}, {K})")
+    return _array(mx8, torch.uint8, None, name)
+
+
+def apb_mx8_quantize(X: torch.Tensor, mx8: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """X [rows, K] -> its 8-bit form."""
+    ptr, t, ld = _matrix(X, "X")
+    rows, K = X.shape
+    if mx8 is None:
+        nbytes = apb_mx8_bytes(rows, K)
+        if nbytes == 0:
+            raise ApbError(APB_ERR_SHAPE, "apb_mx8_bytes")
+        mx8 = _new(X, nbytes, torch.uint8, stream)
+    _check(load().apb_mx8_quantize(ptr, t, ld, rows, K, _mx8_ptr(mx8, rows, K, "mx8"), _stream(stream)), "apb_mx8_quantize")
+    return mx8
+
+
+def apb_mx8_dequantize(mx8: torch.Tensor, rows: int, K: int, dtype: torch.dtype = torch.float32,
+                       X: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    X, ptr, t, ld = _result(X, (rows, K), dtype, mx8, "X", stream)
+    _check(load().apb_mx8_dequantize(_mx8_ptr(mx8, rows, K, "mx8"), int(rows), int(K), t, ptr, ld, _stream(stream)),
+           "apb_mx8_dequantize")
+    return X
+
+
+# ----------------------------------------------------------------------------- gated feed-forward blocks
+
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}                      # apb_activation
+
+
+def _activation(name: str) -> int:
+    a = _ACTIVATIONS.get(name)
+    if a is None:
+        raise ValueError("activation must be 'silu', 'gelu' or 'relu'")
+    return a
+
+
+def apb_mx4_gated_gemm(A: torch.Tensor, W: torch.Tensor, M: int, N: int, K: int, activation: str = "silu",
+                       dtype: torch.dtype = torch.float32, Y: Optional[torch.Tensor] = None,
+                       offsets: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y[M, N] = act(A^ Wg^T) * (A^ Wu^T); W: for every expert N rows of the gate, then N of the up projection.  saved: memory from
+    alloc_mx8(2 * M, N) that receives both projections in 8 bits for apb_gated_backward."""
+    off, E = _experts(offsets)
+    act = _activation(activation)
+    Y, ptr, t, ld = _result(Y, (M, N), dtype, A, "Y", stream)
+    _check(load().apb_mx4_gated_gemm(_mx4_ptr(A, M, K, "A"), _mx4_ptr(W, E * 2 * N, K, "W"), off, E, int(M), int(N), int(K), act, t, ptr,
+                                     ld, _mx8_ptr(saved, 2 * M, N, "saved"), _stream(stream)), "apb_mx4_gated_gemm")
+    return Y
+
+
+def apb_mx4_gated_linear_scratch_bytes(grouped: bool, E: int, M: int, N: int, K: int, with_saved: bool = False) -> int:
+    """Bytes of scratch that apb_mx4_gated_linear uses: 0 where it runs as one kernel."""
+    return int(load().apb_mx4_gated_linear_scratch_bytes(int(grouped), E, M, N, K, int(with_saved)))
+
+
+def apb_mx4_gated_linear(X: torch.Tensor, W: torch.Tensor, N: int, activation: str = "silu", dtype: Optional[torch.dtype] = None,
+                         Y: Optional[torch.Tensor] = None, rows_from: Optional[torch.Tensor] = None,
+                         offsets: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None,
+                         saved: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """apb_mx4_quantize of X [rows_in, K] + apb_mx4_gated_gemm with the 4-bit weights W in one call; Y has X's type by default."""
+    xp, xt, ldx = _matrix(X, "X")
+    rows_in, K = X.shape
+    M = rows_in if rows_from is None else rows_from.numel()
+    off, E = _experts(offsets)
+    act = _activation(activation)
+    lib, wp = load(), _mx4_ptr(W, E * 2 * N, K, "W")
+    need = lib.apb_mx4_gated_linear_scratch_bytes(off is not None, E, M, N, K, saved is not None)
+    if scratch is not None:
+        sp = _array(scratch, torch.uint8, None, "scratch")
+        if scratch.numel() < need:
+            raise ValueError("scratch smaller than apb_mx4_gated_linear_scratch_bytes(...)")
+    else:
+        scratch = _new(X, need, torch.uint8, stream) if need else None
+        sp = scratch.data_ptr() if need else wp                       # (none needed: not touched, but not NULL)
+    Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y", stream)
+    _check(lib.apb_mx4_gated_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), wp, off, E, M, int(N), K, act,
+                                    sp if need else wp, yt, yp, ldy, _mx8_ptr(saved, 2 * M, N, "saved"), _stream(stream)),
+           "apb_mx4_gated_linear")
+    return Y
+
+
+def apb_gated_forward(GU: torch.Tensor, activation: str = "silu", Y: Optional[torch.Tensor] = None,
+                      saved: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y[M, N] = act(G) * U from [G | U] = GU [M, 2N], in GU's type.  saved: as in apb_mx4_gated_gemm."""
+    gp, gt, ldg = _matrix(GU, "GU")
+    M, N = GU.shape[0], GU.shape[1] // 2
+    if GU.shape[1] % 2:
+        raise ValueError("GU must have an even number of columns")
+    act = _activation(activation)
+    Y, yp, yt, ldy = _result(Y, (M, N), GU.dtype, GU, "Y", stream)
+    if yt != gt:
+        raise TypeError("Y must have GU's type")
+    _check(load().apb_gated_forward(gp, gt, ldg, M, N, act, yp, ldy, _mx8_ptr(saved, 2 * M, N, "saved"), _stream(stream)), "apb_gated_forward")
+    return Y
+
+
+def apb_gated_backward(GU: torch.Tensor, dY: torch.Tensor, activation: str = "silu", dGU: Optional[torch.Tensor] = None,
+                       Y: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """dGU [M, 2N] = [dG | dU] in dY's type, from dY [M, N] and GU: what `saved` has received (uint8), or a matrix [G | U].
+    Y: if given, receives act(G) * U over again."""
+    dp, dt, ldd = _matrix(dY, "dY")
+    M, N = dY.shape
+    act = _activation(activation)
+    if GU.dtype == torch.uint8:
+        gp, gt, ldg = _mx8_ptr(GU, 2 * M, N, "GU"), _MX8, 2 * N
+    else:
+        gp, gt, ldg = _matrix(GU, "GU")
+        if tuple(GU.shape) != (M, 2 * N):
+            raise ValueError("GU must be [M, 2N]")
+    dGU, op, ot, ldo = _result(dGU, (M, 2 * N), dY.dtype, dY, "dGU", stream)
+    yp, yt, ldy = None, dt, N
+    if Y is not None:
+        Y, yp, yt, ldy = _result(Y, (M, N), dY.dtype, dY, "Y", stream)
+    if ot != dt or yt != dt:
+        raise TypeError("dGU and Y must have dY's type")
+    _check(load().apb_gated_backward(gp, gt, ldg, dp, dt, ldd, M, N, act, op, ldo, yp, ldy, _stream(stream)), "apb_gated_backward")
+    return dGU
+
+
+# ----------------------------------------------------------------------------- low-rank adapters
+
+def _factors(F: torch.Tensor, type_: torch.dtype, name: str) -> Tuple[int, int, int, int]:
+    """(pointer, L, r, long side) of an adapters' factor."""
+    if F.dim() != 3:
+        raise ValueError(f"{name} must be [L, r, long side]")
+    return (_array(F, type_, None, name), *F.shape)
+
+
+def _segments(offsets: Optional[torch.Tensor], adapter: Optional[torch.Tensor]):
+    """(pointer of offsets, pointer of adapter, number of segments)."""
+    off, S = _experts(offsets)
+    return off, _array(adapter, torch.int32, S, "adapter"), S
+
+
+def _low_rank(T: torch.Tensor, M: int) -> Tuple[int, int, int]:
+    """(pointer, parts, r) of what apb_adapter_down returned."""
+    if T.dim() != 3 or T.shape[1] != M:
+        raise ValueError("T must be [parts, M, r]")
+    return _array(T, torch.float32, None, "T"), T.shape[0], T.shape[2]
+
+
+def apb_adapter_parts(S: int, M: int, K: int, r: int) -> int:
+    return int(load().apb_adapter_parts(int(S), int(M), int(K), int(r)))
+
+
+def apb_adapter_down(X: torch.Tensor, A: torch.Tensor, offsets: Optional[torch.Tensor] = None, adapter: Optional[torch.Tensor] = None,
+                     scale: Optional[torch.Tensor] = None, T: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """T = scale[a] X A[a]^T for X [M, K] and A [L, r, K], a the adapter of the row's segment (offsets int32 [S+1], adapter int32 [S]):
+    float32 [parts, M, r], whose sum over the parts it is."""
+    xp, xt, ldx = _matrix(X, "X")
+    M, K = X.shape
+    ap, L, r, k = _factors(A, X.dtype, "A")
+    if k != K:
+        raise ValueError("A must be [L, r, K]")
+    off, adp, S = _segments(offsets, adapter)
+    lib = load()
+    parts = lib.apb_adapter_parts(S, M, K, r)
+    if T is None:
+        if parts == 0:
+            raise ApbError(APB_ERR_SHAPE, "apb_adapter_down")
+        T = _new(X, (parts, M, r), torch.float32, stream)
+    elif tuple(T.shape) != (parts, M, r):
+        raise ValueError(f"T must be [{parts}, {M}, {r}]")
+    _check(lib.apb_adapter_down(xp, xt, ldx, ap, off, adp, _array(scale, torch.float32, L, "scale"), S, L, M, K, r,
+                                _array(T, torch.float32, None, "T"), _stream(stream)), "apb_adapter_down")
+    return T
+
+
+def apb_adapter_up(T: torch.Tensor, B: torch.Tensor, Y0: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                   offsets: Optional[torch.Tensor] = None, adapter: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y = Y0 + T B[a] for B [L, r, N], in B's type (Y0 None: zeros).  Y may be Y0: rows without an adapter are then not touched."""
+    if T.dim() != 3:
+        raise ValueError("T must be [parts, M, r]")
+    M = T.shape[1]
+    tp, parts, r = _low_rank(T, M)
+    bp, L, rb, N = _factors(B, B.dtype, "B")
+    if rb != r:
+        raise ValueError("B must be [L, r, N]")
+    off, adp, S = _segments(offsets, adapter)
+    p0, ld0 = None, N
+    if Y0 is not None:
+        if tuple(Y0.shape) != (M, N) or Y0.dtype != B.dtype:
+            raise ValueError("Y0 must be [M, N] in B's type")
+        p0, _, ld0 = _matrix(Y0, "Y0")
+    Y, yp, yt, ldy = _result(Y, (M, N), B.dtype, B, "Y", stream)
+    if Y.dtype != B.dtype:
+        raise TypeError("Y must have B's type")
+    _check(load().apb_adapter_up(tp, parts, bp, yt, off, adp, S, L, M, N, r, p0, ld0, yp, ldy, _stream(stream)), "apb_adapter_up")
+    return Y
+
+
+def apb_adapter_gradient_workspace_bytes(L: int, M: int, K: int, r: int) -> int:
+    """Bytes of scratch that apb_adapter_gradient has a use for."""
+    return int(load().apb_adapter_gradient_workspace_bytes(int(L), int(M), int(K), int(r)))
+
+
+def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[int] = None, offsets: Optional[torch.Tensor] = None,
+                         adapter: Optional[torch.Tensor] = None, dA: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """dA[a] = sum over a's rows of T^T X, float32 [L, r, K].  X: [M, K], or its 8-bit form (uint8) with K given."""
+    if T.dim() != 3:
+        raise ValueError("T must be [parts, M, r]")
+    M = T.shape[1]
+    tp, parts, r = _low_rank(T, M)
+    if X.dtype == torch.uint8:
+        if K is None:
+            raise ValueError("K must be given for an 8-bit X")
+        xp, xt, ldx = _mx8_ptr(X, M, K, "X"), _MX8, K
+    else:
+        xp, xt, ldx = _matrix(X, "X")
+        if X.shape[0] != M or K not in (None, X.shape[1]):
+            raise ValueError("X must be [M, K]")
+        K = X.shape[1]
+    off, adp, S = _segments(offsets, adapter)
+    lib = load()
+    if dA is None:
+        if L <= 0:
+            raise ApbError(APB_ERR_SHAPE, "apb_adapter_gradient")
+        dA = _new(T, (L, r, K), torch.float32, stream)
+    elif tuple(dA.shape) != (L, r, K):
+        raise ValueError(f"dA must be [{L}, {r}, {K}]")
+    keep, sp, sb = _scratch(workspace, lib.apb_adapter_gradient_workspace_bytes(L, M, K, r), T, stream)
+    _check(lib.apb_adapter_gradient(tp, parts, xp, xt, ldx, off, adp, S, int(L), M, int(K), r, _array(dA, torch.float32, None, "dA"), sp, sb,
+                                    _stream(stream)), "apb_adapter_gradient")
+    return dA

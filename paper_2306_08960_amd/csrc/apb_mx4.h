@@ -287,11 +287,19 @@ __device__ __forceinline__ f32x4 four_sums(const f32x16& a, int i) {
     return v;
 }
 
-template <int TYPE, int F>
-__device__ __forceinline__ void store_tile_as(const f32x16 (&acc)[F][F], uint32_t lds, void* out, long long first, long long ld, int rows,
+// Before the first of them: the compiler does not see that four_sums() reads what a matrix instruction wrote (32 cycles, for 8 passes
+// of four).
+template <int F>
+__device__ __forceinline__ void settled() {
+    if constexpr (F == 4) asm volatile("s_nop 15\n\ts_nop 15");
+}
+
+// SUMS(x, y, q): the lane's four outputs of row 32 x + r, columns 32 y + 8 q + 4 h + 0..3.  HALF: the tile has 16 * F columns.
+template <int TYPE, int F, bool HALF, class SUMS>
+__device__ __forceinline__ void store_tile_as(const SUMS& sums, uint32_t lds, void* out, long long first, long long ld, int rows,
                                               long long col, int cols) {
     constexpr int kSize = TYPE == APB_F32 ? 4 : 2, kEach = 16 / kSize;
-    constexpr int kChunks = 2 * F * kSize, kPitch = 16 * kChunks;            // 16-byte chunks of a row
+    constexpr int kChunks = (HALF ? 1 : 2) * F * kSize, kPitch = 16 * kChunks;            // 16-byte chunks of a row
     constexpr int kX = F * 32 * kPitch <= kTileLds<F> ? F : F / 2;                // groups of 32 rows at a time
     constexpr int kStepRows = kWave / kChunks, kSteps = 32 * kX / kStepRows;
     constexpr int kAhead = kSteps < 8 ? kSteps : 8;
@@ -312,10 +320,10 @@ __device__ __forceinline__ void store_tile_as(const f32x16 (&acc)[F][F], uint32_
 #pragma unroll
         for (int x = x0; x < x0 + kX; ++x)
 #pragma unroll
-            for (int y = 0; y < F; ++y)
+            for (int y = 0; y < (HALF ? (F + 1) / 2 : F); ++y)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const f32x4 a = four_sums<F>(acc[x][y], 4 * q);
+                for (int q = 0; q < (HALF && F == 1 ? 2 : 4); ++q) {
+                    const f32x4 a = sums(x, y, q);
                     const uint32_t rows_on = 32 * (x - x0) * kPitch;
                     if constexpr (TYPE == APB_F32)
                         lds_store((mine ^ 16 * (8 * y + 2 * q)) + rows_on, a);
@@ -365,11 +373,11 @@ __device__ __forceinline__ void store_tile_as(const f32x16 (&acc)[F][F], uint32_
 template <int F>
 __device__ __forceinline__ void store_tile(const f32x16 (&acc)[F][F], uint32_t lds, void* out, int type, long long first, long long ld,
                                            int rows, long long col, int cols) {
-    // (the compiler does not see that four_sums() reads what a matrix instruction wrote: 32 cycles, for 8 passes of four)
-    if constexpr (F == 4) asm volatile("s_nop 15\n\ts_nop 15");
-    if (type == APB_F32) store_tile_as<APB_F32, F>(acc, lds, out, first, ld, rows, col, cols);
-    else if (type == APB_BF16) store_tile_as<APB_BF16, F>(acc, lds, out, first, ld, rows, col, cols);
-    else store_tile_as<APB_F16, F>(acc, lds, out, first, ld, rows, col, cols);
+    settled<F>();
+    auto sums = [&](int x, int y, int q) { return four_sums<F>(acc[x][y], 4 * q); };
+    if (type == APB_F32) store_tile_as<APB_F32, F, false>(sums, lds, out, first, ld, rows, col, cols);
+    else if (type == APB_BF16) store_tile_as<APB_BF16, F, false>(sums, lds, out, first, ld, rows, col, cols);
+    else store_tile_as<APB_F16, F, false>(sums, lds, out, first, ld, rows, col, cols);
 }
 
 // ---- groups of rows ---------------------------------------------------------------------------------
@@ -422,10 +430,17 @@ int launch_mx4_quantize(const void* X, int type, long long row_stride, long long
                         const int32_t* rows_from, int rows, int K, void* mx, hipStream_t s);
 // Few rows: may it run as the one kernel that streams the weights (apb_mx4_few.hip)?
 bool mx4_few_applies(const int32_t* offsets, int E, int M, int K);
+bool mx4_few_gated_applies(const int32_t* offsets, int E, int M, int K);
 int launch_mx4_few(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const Mx& W, const int32_t* offsets,
                    int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s);
 int launch_mx4_few(const Mx& A, const Mx& W, const int32_t* offsets, int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s);
 int launch_mx4_gemm(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy,
                     hipStream_t s);
+// The same two with both projections of a gated block and its activation (N: of either projection).
+int launch_mx4_few_gated(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const Mx& W,
+                         const int32_t* offsets, int E, int M, int N, int K, int activation, int type, void* Y, long long ldy,
+                         hipStream_t s);
+int launch_mx4_few_gated(const Mx& A, const Mx& W, const int32_t* offsets, int E, int M, int N, int K, int activation, int type, void* Y,
+                         long long ldy, hipStream_t s);
 
 }  // namespace apb

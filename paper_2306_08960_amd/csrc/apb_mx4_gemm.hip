@@ -3,7 +3,7 @@
 // Bound by the matrix cores, and for long products by the power they may draw: 8192^3 with a bfloat16 result, one call behind another,
 // takes 262 us (4200 TFLOP/s) on random values and 191 on zeros, with the same instructions.  4096^3: 42 us (3260), 1024 x 4096 x
 // 4096: 15 us.
-#include "apb_mx4.h"
+#include "apb_mx8.h"
 
 namespace apb {
 namespace {
@@ -30,6 +30,87 @@ constexpr int kHalf = kMxSeg / 2;             // values that a pass sums over
 constexpr int kHalfBytes = kHalf / 2;
 constexpr int kRing = 4;                      // passes of operands in LDS
 
+// The two halves of a gated wave's sums: four of G and the four of U beside them.
+template <int F>
+__device__ __forceinline__ f32x4 four_gate(const f32x16 (&acc)[F][F], int x, int y, int q) { return four_sums<F>(acc[x][y], 4 * q); }
+template <int F>
+__device__ __forceinline__ f32x4 four_up(const f32x16 (&acc)[F][F], int x, int y, int q) {
+    if constexpr (F == 1) return four_sums<F>(acc[x][y], 8 + 4 * q);
+    else return four_sums<F>(acc[x][y + F / 2], 4 * q);
+}
+
+// G or U of a wave's tile in 8 bits.  A block of 32 columns of a row lies in the lanes (r, 0) and (r, 1); with F == 1, in two waves,
+// which exchange their maxima through LDS (`tops`, 64 rows x 2).
+template <int F, class SUMS>
+__device__ __forceinline__ void save_tile(const SUMS& sums, uint32_t* tops, const Mx8& to, long long first, int rows, int col, int cols) {
+    constexpr int kBlocks = (F + 1) / 2, kFours = F == 1 ? 2 : 4;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, r = lane & 31, h = lane >> 5;
+    uint32_t top[F][kBlocks];
+#pragma unroll
+    for (int x = 0; x < F; ++x)
+#pragma unroll
+        for (int y = 0; y < kBlocks; ++y) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int q = 0; q < kFours; ++q) {
+                const f32x4 v = sums(x, y, q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)                      // (columns that are not there have another row's sums)
+                    most = max(most, 32 * y + 8 * q + 4 * h + i < cols ? float_bits(v[i]) & 0x7fffffffu : 0u);
+            }
+            top[x][y] = max(most, (uint32_t)__shfl_xor((int)most, 32, kWave));
+        }
+    if constexpr (F == 1) {
+        tops[wave * 32 + r] = top[0][0];
+        __syncthreads();
+        top[0][0] = max(top[0][0], tops[(wave ^ 1) * 32 + r]);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int x = 0; x < F; ++x)
+#pragma unroll
+        for (int y = 0; y < kBlocks; ++y) {
+            const uint32_t code = scale8_code(top[x][y]);
+            const float inverse = scale8_inverse(code);
+            const int k = col + 32 * y;                          // (a multiple of 32, or of 16 with F == 1)
+            const long long at = (first + 32 * x + r) * to.blocks + k / kMx8Block;
+            const bool there = 32 * x + r < rows && k / kMx8Block < to.blocks;
+#pragma unroll
+            for (int q = 0; q < kFours; ++q) {
+                const f32x4 v = sums(x, y, q);
+                float w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = 32 * y + 8 * q + 4 * h + i < cols ? v[i] : 0.0f;
+                if (there)
+                    *reinterpret_cast<uint32_t*>(to.codes + at * kMx8Block + k % kMx8Block + 8 * q + 4 * h) =
+                        encode8_four(w, inverse, code == 255u);
+            }
+            if (there && h == 0 && k % kMx8Block == 0) to.scales[at] = (uint8_t)code;
+        }
+}
+
+// A gated wave's tile of 32 * F x 16 * F outputs.  `all`: the workgroup's LDS, which nobody else needs any more.
+template <int F>
+__device__ __forceinline__ void store_gated(const f32x16 (&acc)[F][F], uint32_t lds, uint8_t* all, void* out, int type, long long first,
+                                            long long ld, int rows, int col, int cols, const Act& act, const Mx8& saved, int M) {
+    settled<F>();
+    if (saved.codes) {
+        uint32_t* tops = reinterpret_cast<uint32_t*>(all);
+        save_tile<F>([&](int x, int y, int q) { return four_gate<F>(acc, x, y, q); }, tops, saved, first, rows, col, cols);
+        save_tile<F>([&](int x, int y, int q) { return four_up<F>(acc, x, y, q); }, tops, saved, M + first, rows, col, cols);
+    }
+    auto sums = [&](int x, int y, int q) {
+        const f32x4 g = four_gate<F>(acc, x, y, q), u = four_up<F>(acc, x, y, q);
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_value(act, g[i]) * u[i];
+        return v;
+    };
+    if (type == APB_F32) store_tile_as<APB_F32, F, true>(sums, lds, out, first, ld, rows, col, cols);
+    else if (type == APB_BF16) store_tile_as<APB_BF16, F, true>(sums, lds, out, first, ld, rows, col, cols);
+    else store_tile_as<APB_F16, F, true>(sums, lds, out, first, ld, rows, col, cols);
+}
+
 // A workgroup computes a tile of 64 * F x 64 * F outputs, a wave 32 * F x 32 * F.  A pass sums over half a segment, 128 values, in
 // two steps of 64.  The rows' half segments go from memory straight to LDS, three passes ahead of the one being multiplied, and
 // from there to registers a step ahead.  What keeps the matrix cores fed is the order of the instructions: a wave issues them one
@@ -38,10 +119,16 @@ constexpr int kRing = 4;                      // passes of operands in LDS
 // permuted by the row's number (by exchanging what the lanes of a load ask for), so that 16 lanes reading the same chunk of 16
 // rows meet every bank once.  Lane (r, h) holds 32 values of row r: step s multiplies blocks s (h = 0) and 2 + s (h = 1) of the
 // half segment.  Rows of B go in the first operand: a lane then holds four neighbours of a row of Y.
-template <int F>
+//
+// GATED: both projections of a gated block.  Of the 32 * F rows of B that a wave multiplies, the first half are the gate's, the second
+// the up projection's for the same 16 * F columns of Y, so a lane holds both factors of each of its outputs; N counts the columns
+// of Y, the tile has 32 * F of them.  `saved`: where G and U go in 8 bits, if anywhere.
+template <int F, bool GATED>
 __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx B, const int32_t* __restrict__ offsets, int E, int N,
-                                                                       int tiles_n, int type, void* __restrict__ Y, long long ldy) {
+                                                                       int tiles_n, int type, void* __restrict__ Y, long long ldy,
+                                                                       Act act, Mx8 saved) {
     constexpr int kRows = 64 * F;                                // of either operand
+    constexpr int kCols = GATED ? kRows / 2 : kRows;             // of the tile
     constexpr int kLoads = 2 * kRows / 16 / 4;                   // instructions of a wave that fetch a pass's codes
     constexpr int kScaleLoads = F == 4 ? 2 : 1;                  // ... its scales
     constexpr int kPass = kLoads + kScaleLoads;
@@ -51,15 +138,21 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
     tile_of(blockIdx.x, tiles_n, tile, nt);
     const RowTile t = find_row_tile(offsets, E, A.rows, kRows, tile);
     if (t.rows <= 0) return;
-    const int n0 = nt * kRows;
+    const int n0 = nt * kCols;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane & 31, h = lane >> 5;
     const int wm = (wave >> 1) * 32 * F, wn = (wave & 1) * 32 * F;
     if (t.e >= E) {
         const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int i = threadIdx.x; i < t.rows * (kRows / 4); i += kThreads) {
-            const int n = n0 + i % (kRows / 4) * 4;
-            store4(Y, type, (long long)(t.row0 + i / (kRows / 4)) * ldy + n, zero, N - n);
+        for (int i = threadIdx.x; i < t.rows * (kCols / 4); i += kThreads) {
+            const int row = t.row0 + i / (kCols / 4), n = n0 + i % (kCols / 4) * 4;
+            store4(Y, type, (long long)row * ldy + n, zero, N - n);
+            if (GATED && saved.codes && n < saved.blocks * kMx8Block)
+                for (int u = 0; u < 2; ++u) {
+                    const long long at = ((long long)(u ? A.rows : 0) + row) * saved.blocks + n / kMx8Block;
+                    *reinterpret_cast<uint32_t*>(saved.codes + at * kMx8Block + n % kMx8Block) = 0u;
+                    if (n % kMx8Block == 0) saved.scales[at] = 0;
+                }
         }
         return;
     }
@@ -73,8 +166,12 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
 
     // waves 0 and 1 fetch A's rows, 2 and 3 B's; rows beyond the tile's repeat its last one
     const bool fetch_b = wave >= 2;
-    const int q0 = fetch_b ? t.e * N + n0 : t.row0, last = fetch_b ? N - 1 - n0 : t.rows - 1;
+    const int q0 = fetch_b ? (GATED ? 2 : 1) * t.e * N + n0 : t.row0, last = fetch_b ? N - 1 - n0 : t.rows - 1;
+    // the row that takes place `row` of an operand in LDS, relative to q0, and whether it is one of the up projection's, N rows further
+    auto row_at = [&](int row) { return min(GATED && fetch_b ? row / (32 * F) * 16 * F + (row & (16 * F - 1)) : row, last); };
+    auto is_up = [&](int row) { return GATED && fetch_b && (row & (32 * F - 1)) >= 16 * F; };
     const uint32_t pitch = (uint32_t)A.segs * kMxSegBytes;
+    const size_t up = GATED && fetch_b ? (size_t)N * pitch : 0;
     const uint8_t* codes = (fetch_b ? B.codes : A.codes) + (size_t)q0 * pitch;
     const uint8_t* scales = (fetch_b ? B.scales : A.scales) + (size_t)q0 * 8;
     const size_t scale_pitch = (size_t)(fetch_b ? B.rows : A.rows) * 8;
@@ -83,10 +180,13 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
         const int row = (wave & 1) * (kRows / 2) + 16 * i + (lane >> 2);
-        at[i] = min(row, last) * pitch + 16 * ((lane & 3) ^ ((row >> 2) & 3));
+        at[i] = row_at(row) * pitch + 16 * ((lane & 3) ^ ((row >> 2) & 3));
     }
 #pragma unroll
-    for (int i = 0; i < kScaleLoads; ++i) scale_at[i] = 8 * min(first + 64 * i + lane, last);
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int row = first + 64 * i + lane;
+        scale_at[i] = 8 * (row_at(row) + (is_up(row) ? N : 0));
+    }
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds));
     const uint32_t to = lds0 + wave * kLoads * 1024;
     const uint32_t scales_to = lds0 + 2 * kRows * kHalfBytes + (fetch_b ? 4 * kRows : 0) + 4 * first;
@@ -101,7 +201,8 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
         marks_to = scales_to + stage;
     };
     auto fetch = [&](int i) {
-        if (i < kLoads) load16_to_lds(codes_to + 1024 * i, codes_from, at[i]);
+        // (of B's rows the second half of the loads are the up projection's)
+        if (i < kLoads) load16_to_lds(codes_to + 1024 * i, GATED && i >= kLoads / 2 ? codes_from + up : codes_from, at[i]);
         else load4_to_lds(marks_to + 256 * (i - kLoads), scales_from, scale_at[i - kLoads]);
     };
     u32x4 fm[2][F], fn[2][F];
@@ -176,15 +277,39 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
     }
     arrived<0>();                                                // (nothing is under way to LDS any more)
     static_assert(4 * kTileLds<F> <= kRing * kStage, "a wave's tile passes through its share of the ring");
-    store_tile<F>(acc, lds0 + wave * kTileLds<F>, Y, type, t.row0 + wm, ldy, min(32 * F, t.rows - wm), n0 + wn, N - n0 - wn);
+    if constexpr (GATED) {
+        store_gated<F>(acc, lds0 + wave * kTileLds<F>, lds, Y, type, t.row0 + wm, ldy, min(32 * F, t.rows - wm), n0 + wn / 2, N - n0 - wn / 2,
+                       act, saved, A.rows);
+    } else {
+        store_tile<F>(acc, lds0 + wave * kTileLds<F>, Y, type, t.row0 + wm, ldy, min(32 * F, t.rows - wm), n0 + wn, N - n0 - wn);
+    }
 }
 
-template <int F>
-void launch_tiles(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy, hipStream_t s) {
+template <int F, bool GATED>
+void launch_tiles(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy, const Act& act,
+                  const Mx8& saved, hipStream_t s) {
+    constexpr int kCols = GATED ? 32 * F : 64 * F;
     const long long tiles_m = (max_row_tiles(M, E, offsets != nullptr, 64 * F) + 3) / 4 * 4;
-    const int tiles_n = (N + 64 * F - 1) / (64 * F);
+    const int tiles_n = (N + kCols - 1) / kCols;
     const unsigned blocks = (unsigned)((tiles_m * tiles_n + 127) / 128 * 128);
-    hipLaunchKernelGGL((k_mx4_gemm<F>), dim3(blocks), dim3(kThreads), 0, s, A, B, offsets, E, N, tiles_n, type, Y, ldy);
+    hipLaunchKernelGGL((k_mx4_gemm<F, GATED>), dim3(blocks), dim3(kThreads), 0, s, A, B, offsets, E, N, tiles_n, type, Y, ldy, act, saved);
+}
+
+int launch_mx4_gated(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int activation, int type, void* Y,
+                     long long ldy, void* saved, hipStream_t s) {
+    const int side = mx4_product_side(M, 2 * N);
+    const Act act = act_of(activation);
+    const Mx8 keep = mx8_view(saved, 2LL * M, N);
+    if (side == 256) launch_tiles<4, true>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
+    else if (side == 128) launch_tiles<2, true>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
+    else launch_tiles<1, true>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
+    APB_HIP(hipGetLastError());
+    return APB_OK;
+}
+
+// The sizes of a gated product; N counts the columns of Y.
+bool bad_gated(int E, int M, int N, int K, const int32_t* offsets) {
+    return N <= 0 || N > kMxMaxK || bad_product(E, M, 2 * N, K, offsets) || bad_shape_mx8(2LL * M, N);
 }
 
 }  // namespace
@@ -192,9 +317,11 @@ void launch_tiles(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M
 int launch_mx4_gemm(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy,
                     hipStream_t s) {
     const int side = mx4_product_side(M, N);
-    if (side == 256) launch_tiles<4>(A, B, offsets, E, M, N, type, Y, ldy, s);
-    else if (side == 128) launch_tiles<2>(A, B, offsets, E, M, N, type, Y, ldy, s);
-    else launch_tiles<1>(A, B, offsets, E, M, N, type, Y, ldy, s);
+    const Act none = {};
+    const Mx8 nowhere = {};
+    if (side == 256) launch_tiles<4, false>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
+    else if (side == 128) launch_tiles<2, false>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
+    else launch_tiles<1, false>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
@@ -238,6 +365,44 @@ int apb_mx4_linear(const void* X, int x_type, long long ldx, int rows_in, const 
     const int rc = launch_mx4_quantize(X, x_type, ldx, 1, rows_in, rows_from, M, K, scratch, s);
     if (rc != APB_OK) return rc;
     return launch_mx4_gemm(mx_view(scratch, M, K), mx_view(W, E * N, K), offsets, E, M, N, y_type, Y, ldy, s);
+}
+
+int apb_mx4_gated_gemm(const void* A, const void* W, const int32_t* offsets, int E, int M, int N, int K, int activation, int type,
+                       void* Y, long long ldy, void* saved, void* stream) {
+    if (!A || !W || !Y) return APB_ERR_NULL;
+    if (bad_type(type)) return APB_ERR_TYPE;
+    if (bad_activation(activation)) return APB_ERR_VALUE;
+    if (bad_gated(E, M, N, K, offsets) || ldy < N) return APB_ERR_SHAPE;
+    if (!aligned(A, 16) || !aligned(W, 16) || !aligned(Y, type_size(type)) || !aligned(offsets, 4) || !aligned(saved, 16)) return APB_ERR_ALIGN;
+    const Mx a = mx_view(A, M, K), w = mx_view(W, E * 2 * N, K);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (!saved && mx4_few_gated_applies(offsets, E, M, K)) return launch_mx4_few_gated(a, w, offsets, E, M, N, K, activation, type, Y, ldy, s);
+    return launch_mx4_gated(a, w, offsets, E, M, N, activation, type, Y, ldy, saved, s);
+}
+
+size_t apb_mx4_gated_linear_scratch_bytes(int grouped, int E, int M, int N, int K, int with_saved) {
+    const int32_t some = 0, *offsets = grouped ? &some : nullptr;
+    if (bad_gated(E, M, N, K, offsets) || (!with_saved && mx4_few_gated_applies(offsets, E, M, K))) return 0;
+    return apb_mx4_bytes(M, K);
+}
+
+int apb_mx4_gated_linear(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const void* W,
+                         const int32_t* offsets, int E, int M, int N, int K, int activation, void* scratch, int y_type, void* Y,
+                         long long ldy, void* saved, void* stream) {
+    if (!X || !W || !scratch || !Y) return APB_ERR_NULL;
+    if (bad_type(x_type) || bad_type(y_type)) return APB_ERR_TYPE;
+    if (bad_activation(activation)) return APB_ERR_VALUE;
+    if (bad_gated(E, M, N, K, offsets) || ldy < N || ldx < K || rows_in <= 0 || (!rows_from && rows_in != M)) return APB_ERR_SHAPE;
+    if (!aligned(X, type_size(x_type)) || !aligned(W, 16) || !aligned(scratch, 16) || !aligned(Y, type_size(y_type)) ||
+        !aligned(offsets, 4) || !aligned(rows_from, 4) || !aligned(saved, 16))
+        return APB_ERR_ALIGN;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const Mx w = mx_view(W, E * 2 * N, K);
+    if (!saved && mx4_few_gated_applies(offsets, E, M, K))
+        return launch_mx4_few_gated(X, x_type, ldx, rows_in, rows_from, w, offsets, E, M, N, K, activation, y_type, Y, ldy, s);
+    const int rc = launch_mx4_quantize(X, x_type, ldx, 1, rows_in, rows_from, M, K, scratch, s);
+    if (rc != APB_OK) return rc;
+    return launch_mx4_gated(mx_view(scratch, M, K), w, offsets, E, M, N, activation, y_type, Y, ldy, saved, s);
 }
 
 }  // extern "C"
