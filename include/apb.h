@@ -508,23 +508,27 @@ int apb_gated_backward(const void* GU, int gu_type, long long ldgu, const void* 
  * unspecified results, never an access out of bounds.
  *
  * T is float32, as `parts` sums whose total it is ([parts][M][r], parts = apb_adapter_parts(), fixed by the sizes): where rows
- * are few, workgroups share a row's sum, and whoever reads T adds the parts up, in order.  Repeating a call repeats its
- * bits.  X, A, Y0, Y are of one `type`; products are exact or float32, sums float32; Y is rounded once.
+ * are few, workgroups share a row's sum, and whoever reads T adds the parts up, in order.  X, A, Y0, Y are of one `type`;
+ * products are exact or float32, sums float32 in a fixed order (repeating a call repeats its bits); Y is rounded once.  With a 16-bit `type`, T enters Y as two 16-bit parts, which is off by 2^-16 of each
+ * term (and for APB_F16 by up to 2^-39 of the largest |T| of the row), and the gradients as three (2^-24).  Rows and factors that
+ * a result does not depend on do not reach it, whatever they hold; an infinity among those it depends on may come out as a NaN.
  *   r <= APB_ADAPTER_MAX_R, S <= APB_ADAPTER_MAX_S, L <= APB_ADAPTER_MAX_L, K, N <= 2^22, M <= 2^24. */
 #define APB_ADAPTER_MAX_R 256
 #define APB_ADAPTER_MAX_S 4096
 #define APB_ADAPTER_MAX_L 4096
+#define APB_ADAPTER_MAX_PARTS 8
 int apb_adapter_parts(int S, int M, int K, int r);   /* 0 on bad arguments */
 /*   X  DEVICE, M rows of K elements, ldx >= K apart.   A  DEVICE, [L][r][K].   scale  DEVICE, L floats, or NULL: all 1.
  *   T  DEVICE, apb_adapter_parts(S, M, K, r) * M * r floats, fully overwritten. */
 int apb_adapter_down(const void* X, int type, long long ldx, const void* A, const int32_t* offsets, const int32_t* adapter,
                      const float* scale, int S, int L, int M, int K, int r, float* T, void* stream);
-/*   T   as apb_adapter_down left it, `parts` sums of it.   B  DEVICE, [L][r][N].
+/*   T   as apb_adapter_down left it, or any `parts` sums of M rows of r floats.   B  DEVICE, [L][r][N].
  *   Y0  DEVICE, M rows of N elements, or NULL: zeros.      Y  DEVICE, the same, fully overwritten; may be Y0 itself
  *       (with the same row stride), then rows without an adapter are not touched.  Otherwise the two do not overlap. */
 int apb_adapter_up(const float* T, int parts, const void* B, int type, const int32_t* offsets, const int32_t* adapter, int S,
                    int L, int M, int N, int r, const void* Y0, long long ldy0, void* Y, long long ldy, void* stream);
-/*   X   DEVICE, M rows of K elements of x_type, ldx >= K apart; or x_type APB_MX8: an 8-bit matrix of M rows of K.
+/*   T   as in apb_adapter_up.
+ *   X   DEVICE, M rows of K elements of x_type, ldx >= K apart; or x_type APB_MX8: an 8-bit matrix of M rows of K.
  *   dA  DEVICE, [L][r][K] floats, fully overwritten (0 for an adapter without rows).
  *   workspace, workspace_bytes  optional DEVICE scratch (NULL, 0: none), 4-byte aligned: with as many bytes as the function says
  *       (0: no use for any), workgroups share the sum over many rows and join it in a fixed order. */

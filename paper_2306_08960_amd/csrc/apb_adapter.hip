@@ -1,15 +1,19 @@
 // Low-rank adapters of many requests: T = scale X A^T (down), Y = Y0 + T B (up), dA = sum T^T X (gradient), every row with the factors of
 // its segment's adapter.  A and B have their long side contiguous, so that each of them and each of the gradients' operands is read
 // in whole lines and all directions are these three kernels.
+#include <type_traits>
+
 #include "apb_mx8.h"
+#include <type_traits>
+
 
 namespace apb {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kMaxParts = 32;
-constexpr int kMaxSlices = 32;
+constexpr int kUpRows = 64;                    // of a workgroup that streams them past B, at most
+constexpr int kMaxParts = APB_ADAPTER_MAX_PARTS;
 constexpr int kCols = 128;                    // of a wave, in up and gradient: eight to a lane
 constexpr int kStage = 64;                    // ranks of T that are in LDS at a time
 
@@ -20,10 +24,52 @@ struct Segments {
     int S, L, M;
 };
 
-__device__ __forceinline__ int adapter_of(const Segments& g, int s) {
-    if (s >= g.S) return -1;
-    const int a = g.adapter ? g.adapter[s] : s;
-    return a < g.L ? a : -1;
+// Segment s's adapter, -1 for none; first row and number of rows.  (Loads that do not wait for one another.)
+__device__ __forceinline__ int rows_of(const Segments& seg, int s, int& first, int& count) {
+    const int at = min(s, seg.S - 1);
+    const int a = seg.adapter ? seg.adapter[at] : at;
+    first = seg.offsets ? min(max(seg.offsets[at], 0), seg.M) : 0;
+    count = (seg.offsets ? max(first, min(seg.offsets[at + 1], seg.M)) : seg.M) - first;
+    if (s >= seg.S) count = 0;
+    return s < seg.S && a >= 0 && a < seg.L ? a : -1;
+}
+
+// The t-th tile of `tile` rows: its rows, none of two segments, and their adapter.  Called by whole waves, like find_row_tile; the rows
+// behind the last segment are tiles as well.
+struct SegmentTile {
+    int a, row0, rows;
+};
+__device__ __forceinline__ SegmentTile find_tile(const Segments& seg, int tile, int t) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int before = 0, behind = 0;
+    for (int base = 0; base <= seg.S; base += kWave) {
+        const int s = base + lane;
+        int first, count;
+        const int a = rows_of(seg, s, first, count);
+        const int last = __shfl(first + count, min(seg.S - 1 - base, kWave - 1), kWave);      // (of segments so far)
+        if (s == seg.S) {
+            first = base == seg.S ? behind : last;
+            count = seg.M - first;
+        }
+        behind = last;
+        const int tiles = (count + tile - 1) / tile;
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int v = __shfl_up(upto, d, kWave);
+            if (lane >= d) upto += v;
+        }
+        const unsigned long long hit = __ballot(t < before + upto);
+        if (hit) {
+            const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
+            const int from = __builtin_amdgcn_readlane(before + upto - tiles, src);
+            const int row0 = __builtin_amdgcn_readlane(first, src) + (t - from) * tile;
+            const int end = __builtin_amdgcn_readlane(first + count, src);
+            return SegmentTile{__builtin_amdgcn_readlane(a, src), row0, min(tile, end - row0)};
+        }
+        before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    return SegmentTile{-1, 0, 0};
 }
 
 // d[i, n] += sum over eight values of each of the four lanes of a row: a's row i in lanes i, i + 16, ..., b's row n likewise.
@@ -43,65 +89,151 @@ __device__ __forceinline__ f32x4 multiply8(const Eight<TYPE>& a, const Eight<TYP
     }
 }
 
-// A workgroup takes 16 * RT rows of a segment, 16 * JT ranks and one part of K; its waves take chunks of 128 bytes of the rows in turn,
-// straight from memory in the order of the operands (a row's four lanes read a whole line), and join their sums in LDS.
-template <int TYPE, int RT, int JT>
-__global__ __launch_bounds__(kThreads) void k_adapter_down(const void* __restrict__ X, long long ldx, const void* __restrict__ A, Segments seg,
-                                                           const float* __restrict__ scale, int K, int r, int chunks_each,
-                                                           float* __restrict__ T) {
-    constexpr int kChunk = TYPE == APB_F32 ? 32 : 64, kEach = kChunk / 4;        // values of a row: in a chunk, of a lane
-    __shared__ f32x4 sums[kWaves][RT * JT][kWave];
-    const RowTile t = find_row_tile(seg.offsets, seg.S, seg.M, 16 * RT, blockIdx.x);
+// A workgroup takes 16 * RT rows of a segment, 16 * JT ranks and one part of K; its waves take lines of 128 bytes of all those rows in
+// turn and join their sums in LDS.  A line is loaded by eight neighbouring lanes and goes through LDS of the wave's own: in the order
+// of the operands, sixteen neighbouring lanes would ask for sixteen lines, and a compute unit would be brought 17 bytes a cycle.  The
+// next lines are under way while these are multiplied.  In LDS the eight 16-byte pieces of a line are permuted by the row's number, so
+// that eight lanes reading the same piece of eight rows meet every bank once.
+template <int RT, int JT>
+constexpr int kDownWaves = RT + JT <= 2 ? 16 : RT + JT <= 4 ? 8 : 4;
+template <int TYPE, int RT, int JT, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) void k_adapter_down(const void* __restrict__ X, long long ldx, const void* __restrict__ A,
+                                                                Segments seg, const float* __restrict__ scale, int K, int r, int lines_each,
+                                                                float* __restrict__ T) {
+    constexpr int kW = WAVES, kPiece = TYPE == APB_F32 ? 4 : 8, kLine = 8 * kPiece;       // values of 16 and of 128 bytes
+    constexpr int kLoads = 2 * (RT + JT);                        // of a wave for a line of all rows, eight rows each
+    __shared__ union {
+        uint8_t lines[kW][kLoads * 1024];
+        f32x4 sums[kW][RT * JT][kWave];
+    } lds;
+    const SegmentTile t = find_tile(seg, 16 * RT, blockIdx.x);
     if (t.rows <= 0) return;
-    const int j0 = blockIdx.z * 16 * JT, ranks = min(16 * JT, r - j0);
-    float* out = T + ((size_t)blockIdx.y * seg.M + t.row0) * r + j0;
-    const int a = adapter_of(seg, t.e);
+    const int j0 = blockIdx.y * 16 * JT, ranks = min(16 * JT, r - j0);
+    float* out = T + ((size_t)blockIdx.z * seg.M + t.row0) * r + j0;
+    const int a = t.a;
     if (a < 0) {
-        for (int i = threadIdx.x; i < t.rows * ranks; i += kThreads) out[(size_t)(i / ranks) * r + i % ranks] = 0.0f;
+        for (int i = threadIdx.x; i < t.rows * ranks; i += kW * kWave) out[(size_t)(i / ranks) * r + i % ranks] = 0.0f;
         return;
     }
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, i = lane & 15, g = lane >> 4;
-    long long x_at[RT], a_at[JT];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
+    const int sub = lane >> 3, piece = lane & 7;
+    // (rows and ranks that are not there repeat the last ones)
+    const uint8_t* at[kLoads];
 #pragma unroll
-    for (int x = 0; x < RT; ++x) x_at[x] = (t.row0 + min(16 * x + i, t.rows - 1)) * ldx;
+    for (int n = 0; n < kLoads; ++n) {
+        const int row = 8 * n + sub;
+        const long long first = n < 2 * RT ? (t.row0 + min(row, t.rows - 1)) * ldx : ((long long)a * r + j0 + min(row - 16 * RT, ranks - 1)) * K;
+        at[n] = static_cast<const uint8_t*>(n < 2 * RT ? X : A) + first * (TYPE == APB_F32 ? 4 : 2) + 16 * piece;
+    }
+    u32x4 v[kLoads];
+    auto fetch = [&](int line) {
+        const int have = K - line * kLine - kPiece * piece;
+        if ((line + 1) * kLine <= K) {
 #pragma unroll
-    for (int j = 0; j < JT; ++j) a_at[j] = ((long long)a * r + min(j0 + 16 * j + i, r - 1)) * K;
+            for (int n = 0; n < kLoads; ++n) v[n] = load16_any(at[n] + 128LL * line);
+        } else {
+#pragma unroll 1
+            for (int n = 0; n < kLoads; ++n) {
+                u32x4 w;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if constexpr (TYPE == APB_F32) {
+                        w[q] = q < have ? reinterpret_cast<const uint32_t*>(at[n] + 128LL * line)[q] : 0u;
+                    } else {
+                        const uint16_t* p = reinterpret_cast<const uint16_t*>(at[n] + 128LL * line) + 2 * q;
+                        w[q] = (2 * q < have ? (uint32_t)p[0] : 0u) | (2 * q + 1 < have ? (uint32_t)p[1] << 16 : 0u);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kLoads; ++u)
+                    if (u == n) v[u] = w;
+            }
+        }
+    };
     f32x4 acc[RT][JT];
 #pragma unroll
     for (int x = 0; x < RT; ++x)
 #pragma unroll
         for (int j = 0; j < JT; ++j) acc[x][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int last = min((int)(blockIdx.y + 1) * chunks_each, (K + kChunk - 1) / kChunk);
-    for (int c = blockIdx.y * chunks_each + wave; c < last; c += kWaves) {
+    uint8_t* mine = lds.lines[wave];
+    auto operand = [&](int row, int h) { return *reinterpret_cast<const u32x4*>(mine + row * 128 + 16 * ((4 * h + g) ^ (row & 7))); };
+    const int last = min((int)(blockIdx.z + 1) * lines_each, (K + kLine - 1) / kLine);
+    int line = blockIdx.z * lines_each + wave;
+    if (line < last) fetch(line);
+    for (; line < last; line += kW) {
 #pragma unroll
-        for (int h = 0; h < kEach / 8; ++h) {
-            const int k = c * kChunk + kEach * g + 8 * h;
-            Eight<TYPE> xv[RT], av[JT];
+        for (int n = 0; n < kLoads; ++n) *reinterpret_cast<u32x4*>(mine + (8 * n + sub) * 128 + 16 * (piece ^ sub)) = v[n];
+        if (line + kW < last) fetch(line + kW);
+        // (the wave's own writes and reads of LDS stay in this order)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        Eight<TYPE> xv[TYPE == APB_F32 ? 1 : 2][RT], av[TYPE == APB_F32 ? 1 : 2][JT];
 #pragma unroll
-            for (int x = 0; x < RT; ++x) xv[x] = load_some<TYPE>(X, x_at[x] + k, K - k);
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int j = 0; j < JT; ++j) av[j] = load_some<TYPE>(A, a_at[j] + k, K - k);
+            for (int x = 0; x < RT; ++x) xv[TYPE == APB_F32 ? 0 : h][x].w[TYPE == APB_F32 ? h : 0] = operand(16 * x + i, h);
+#pragma unroll
+            for (int j = 0; j < JT; ++j) av[TYPE == APB_F32 ? 0 : h][j].w[TYPE == APB_F32 ? h : 0] = operand(16 * (RT + j) + i, h);
+        }
+#pragma unroll
+        for (int h = 0; h < (TYPE == APB_F32 ? 1 : 2); ++h)
 #pragma unroll
             for (int x = 0; x < RT; ++x)
 #pragma unroll
-                for (int j = 0; j < JT; ++j) acc[x][j] = multiply8<TYPE>(av[j], xv[x], acc[x][j]);
-        }
+                for (int j = 0; j < JT; ++j) acc[x][j] = multiply8<TYPE>(av[h][j], xv[h][x], acc[x][j]);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
+    __syncthreads();
 #pragma unroll
     for (int x = 0; x < RT; ++x)
 #pragma unroll
-        for (int j = 0; j < JT; ++j) sums[wave][x * JT + j][lane] = acc[x][j];
+        for (int j = 0; j < JT; ++j) lds.sums[wave][x * JT + j][lane] = acc[x][j];
     __syncthreads();
     const float by = scale ? scale[a] : 1.0f;
-    for (int n = wave; n < RT * JT; n += kWaves) {
-        f32x4 v = sums[0][n][lane];
+    for (int n = wave; n < RT * JT; n += kW) {
+        f32x4 v = lds.sums[0][n][lane];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += sums[w][n][lane];
+        for (int w = 1; w < kW; ++w) v += lds.sums[w][n][lane];
         const int row = 16 * (n / JT) + i, j = 16 * (n % JT) + 4 * g;
         if (row < t.rows)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 if (j + q < ranks) out[(size_t)row * r + j + q] = v[q] * by;
+    }
+}
+
+// N values of T from `from` on, `step` apart, its parts added up in order: loads that do not wait for one another.
+template <int N>
+__device__ __forceinline__ void sum_parts(const float* __restrict__ from, const int (&at)[N], int parts, size_t pitch, float (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = from[at[e]];
+    for (int p = 1; p < parts; p += 2) {
+        float w[2][N];
+        const float* one = from + p * pitch;
+        const float* two = from + min(p + 1, parts - 1) * pitch;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            w[0][e] = one[at[e]];
+            w[1][e] = two[at[e]];
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            v[e] += w[0][e];
+            if (p + 1 < parts) v[e] += w[1][e];
+        }
+    }
+}
+
+// Rows without an adapter: Y = Y0, or zeros.
+template <int TYPE>
+__device__ __forceinline__ void copy_rows(const void* Y0, long long ldy0, void* Y, long long ldy, const SegmentTile& t, int c, int have, int g) {
+    for (int row = g; row < t.rows; row += 4) {
+        float v[8] = {};
+        if (Y0) floats(load_some<TYPE>(Y0, (t.row0 + row) * ldy0 + c, have), v);
+        store8<TYPE>(Y, (t.row0 + row) * ldy + c, have, v);
     }
 }
 
@@ -113,18 +245,13 @@ __global__ __launch_bounds__(kThreads) void k_adapter_up(const float* __restrict
                                                          int N, int r, const void* Y0, long long ldy0, void* Y, long long ldy) {
     constexpr int kPitch = kStage + 1;
     __shared__ float lds[16 * RT * kPitch];
-    const RowTile t = find_row_tile(seg.offsets, seg.S, seg.M, 16 * RT, blockIdx.x);
+    const SegmentTile t = find_tile(seg, 16 * RT, blockIdx.x);
     if (t.rows <= 0) return;
-    const int a = adapter_of(seg, t.e);
+    const int a = t.a;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, i = lane & 15, g = lane >> 4;
     const int c = (blockIdx.y * kWaves + wave) * kCols + 8 * i, have = N - c;
     if (a < 0) {
-        if (Y0 == Y) return;
-        for (int row = g; row < t.rows; row += 4) {
-            float v[8] = {};
-            if (Y0) floats(load_some<TYPE>(Y0, (t.row0 + row) * ldy0 + c, have), v);
-            store8<TYPE>(Y, (t.row0 + row) * ldy + c, have, v);
-        }
+        if (Y0 != Y) copy_rows<TYPE>(Y0, ldy0, Y, ldy, t, c, have, g);
         return;
     }
     f32x4 acc[RT][8];
@@ -136,10 +263,9 @@ __global__ __launch_bounds__(kThreads) void k_adapter_up(const float* __restrict
         const int ranks = min(kStage, r - j0);
         for (int n = threadIdx.x; n < 16 * RT * kStage; n += kThreads) {
             const int row = n / kStage, j = n % kStage;
-            float v = 0.0f;
-            if (row < t.rows && j < ranks)
-                for (int p = 0; p < parts; ++p) v += T[((size_t)p * seg.M + t.row0 + row) * r + j0 + j];
-            lds[row * kPitch + j] = v;
+            float v[1];
+            sum_parts<1>(T + (size_t)t.row0 * r + j0, {min(row, t.rows - 1) * r + min(j, ranks - 1)}, parts, (size_t)seg.M * r, v);
+            lds[row * kPitch + j] = row < t.rows && j < ranks ? v[0] : 0.0f;
         }
         __syncthreads();
         for (int j = g; j - g < ranks; j += 4) {
@@ -168,83 +294,474 @@ __global__ __launch_bounds__(kThreads) void k_adapter_up(const float* __restrict
         }
 }
 
-// Eight neighbours of a row of X as float32; XT: an apb_type or APB_MX8.
-template <int XT>
-__device__ __forceinline__ void row_values(const void* X, long long ldx, const Mx8& x8, long long row, int c, int have, float (&v)[8]) {
-    if constexpr (XT == APB_MX8) {
-        if (have <= 0) {
+// ---- 16-bit factors: T as a sum of 16-bit parts ---------------------------------------------------------------------------------
+
+// Eight floats to `PARTS` bfloat16 operands whose sum they are, to 2^-8 of each part's last: two parts 2^-16, three 2^-24.  A part stays
+// finite, so that an infinity is left to the last one.
+template <int PARTS>
+__device__ __forceinline__ void bf16_parts(float (&t)[8], Eight<APB_BF16> (&out)[PARTS]) {
+    constexpr float kMost = 3.3895314e38f;                       // the largest bfloat16
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = 0.0f;
-            return;
+    for (int p = 0; p < PARTS; ++p) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float& x = t[2 * q + e];
+                v[e] = x;
+                if (p + 1 < PARTS) {
+                    v[e] = fminf(fmaxf((float)(__bf16)x, -kMost), kMost);
+                    x -= v[e];
+                }
+            }
+            out[p].w[0][q] = pack2(APB_BF16, v[0], v[1]);
         }
-        const u32x2 w = *reinterpret_cast<const u32x2*>(x8.codes + row * x8.blocks * kMx8Block + c);
-        const float scale = scale_value(x8.scales[row * x8.blocks + c / kMx8Block]);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = decode8(w[q / 4], q & 3, scale);
-    } else {
-        floats(load_some<XT>(X, row * ldx + c, have), v);
     }
 }
 
-// Segment s's rows if its adapter is a: first row and number.
-__device__ __forceinline__ void rows_of(const Segments& seg, int s, int a, int& first, int& count) {
-    first = count = 0;
-    if (s >= seg.S || adapter_of(seg, s) != a) return;
-    first = seg.offsets ? min(max(seg.offsets[s], 0), seg.M) : 0;
-    count = (seg.offsets ? max(first, min(seg.offsets[s + 1], seg.M)) : seg.M) - first;
+// Eight rows of eight 16-bit neighbours -> eight columns of eight.
+__device__ __forceinline__ void transpose8(const u32x4 (&row)[8], u32x4 (&col)[8]) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+            col[n][d] = __builtin_amdgcn_perm(row[2 * d + 1][n / 2], row[2 * d][n / 2], n & 1 ? 0x07060302u : 0x05040100u);
 }
 
-// A workgroup takes one adapter, 16 * JT ranks, kCols columns a wave, and a slice of the adapter's rows, counted through all of its
-// segments.
+// ---- eight neighbours of a row of n, from element c on, by loads without a branch ---------------------------------------------------
+//
+// A branch around a load makes the compiler wait for the loads before it.  So a wave asks once whether all of its lanes have eight
+// elements (WHOLE) and runs one of two copies of its loop; in the other one a lane loads the row's last eight and, when it uses
+// them, moves those that are its own to the front.  What stands behind them is unspecified, and so is everything from c >= n on.
+template <int TYPE, bool WHOLE>
+__device__ __forceinline__ Eight<TYPE> load_row(const void* X, long long row, int c, int n) {
+    return load_eight<TYPE>(X, row + (WHOLE ? c : min(c, n - 8)));
+}
+template <int TYPE, bool WHOLE>
+__device__ __forceinline__ Eight<TYPE> settle(const Eight<TYPE>& x, int c, int n) {
+    if constexpr (WHOLE) return x;
+    const int by = n < 8 ? 0 : max(c - (n - 8), 0) & 7;          // elements to move by
+    Eight<TYPE> v = x;
+    if constexpr (TYPE == APB_F32) {
+#pragma unroll
+        for (int d = 4; d >= 1; d >>= 1)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const uint32_t from = q + d < 8 ? v.w[(q + d) / 4 & 1][(q + d) & 3] : 0u;
+                v.w[q / 4][q & 3] = by & d ? from : v.w[q / 4][q & 3];
+            }
+    } else {
+#pragma unroll
+        for (int d = 2; d >= 1; d >>= 1)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t from = q + d < 4 ? v.w[0][(q + d) & 3] : 0u;
+                v.w[0][q] = by & (2 * d) ? from : v.w[0][q];
+            }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t next = q < 3 ? v.w[0][(q + 1) & 3] : 0u;
+            v.w[0][q] = by & 1 ? v.w[0][q] >> 16 | next << 16 : v.w[0][q];
+        }
+    }
+    return v;
+}
+
+// Two operands to eight ranks of a row of T.  float16 has few exponents, so the row is scaled by the power of two that takes its largest
+// value (`top`, as bits) to 2^13 .. 2^14, and `back` takes the sums back: off by 2^-22 of a value or 2^-39 of the row's largest,
+// whichever is more.  bfloat16: 2^-16 of a value.
+template <int TYPE>
+__device__ __forceinline__ void split(float (&t)[8], uint32_t top, u32x4& hi, u32x4& lo, float& back) {
+    back = 1.0f;
+    if constexpr (TYPE == APB_BF16) {
+        Eight<APB_BF16> part[2];
+        bf16_parts<2>(t, part);
+        hi = part[0].w[0];
+        lo = part[1].w[0];
+    } else {
+        // (exponents 14 .. 254 have a scale and its inverse among the normal numbers; below, T * 2^126 is small enough as it is)
+        const uint32_t ex = top >> 23, up = ex == 255u ? 127u : 267u - max(ex, 14u);
+        const float scale = __builtin_bit_cast(float, up << 23);
+        back = __builtin_bit_cast(float, (254u - up) << 23);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            f16x2 h, l;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float x = t[2 * q + e] * scale;
+                h[e] = (_Float16)fminf(fmaxf(x, -65504.0f), 65504.0f);
+                l[e] = (_Float16)(x - (float)h[e]);
+            }
+            hi[q] = __builtin_bit_cast(uint32_t, h);
+            lo[q] = __builtin_bit_cast(uint32_t, l);
+        }
+    }
+}
+
+// Y = Y0 + T B with factors of 16 bits, for N >= 8 and ranks up to 32 * CH, or up to 16 with CH == 0.  A workgroup puts the T of its
+// rows into LDS as two operands of 16 bits; a wave keeps its 128 columns of B in registers, eight columns to a lane, as operands that
+// sum over 32 ranks, and streams Y0 past them, 16 rows at a time, the next ones under way.  Up to 16 ranks, both operands of T fit
+// into one product, over the same B twice.
+template <int TYPE, int CH>
+__global__ __launch_bounds__(kThreads) void k_adapter_up16(const float* __restrict__ T, int parts, const void* __restrict__ B, Segments seg,
+                                                           int tile, int N, int r, const void* Y0, long long ldy0, void* Y,
+                                                           long long ldy) {
+    constexpr int kSteps = CH == 0 ? 1 : CH, kOctets = CH == 0 ? 2 : 4 * CH;
+    constexpr int kPitch = 32 * kOctets + 16;
+    __shared__ __align__(16) uint8_t lds[kUpRows * kPitch];
+    __shared__ float backs[kUpRows];
+    const SegmentTile t = find_tile(seg, tile, blockIdx.z * gridDim.y + blockIdx.y);
+    if (t.rows <= 0) return;
+    const int a = t.a;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
+    const int c0 = (blockIdx.x * kWaves + wave) * kCols, c = c0 + 8 * i, have = N - c;
+    if (a < 0) {
+        if (Y0 != Y) copy_rows<TYPE>(Y0, ldy0, Y, ldy, t, c, have, g);
+        return;
+    }
+    const bool whole = c0 + kCols <= N;                          // (the same answer for the whole wave)
+    Eight<TYPE> row[kSteps][8], y0[4] = {};
+    auto fetch_b = [&](auto whole) {
+#pragma unroll
+        for (int h = 0; h < kSteps; ++h)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = CH == 0 ? 8 * (g & 1) + e : 32 * h + 8 * g + e;
+                row[h][e] = load_row<TYPE, decltype(whole)::value>(B, ((long long)a * r + min(j, r - 1)) * N, c, N);
+            }
+    };
+    auto fetch = [&](int x, auto whole) {
+        if (Y0)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y0[q] = load_row<TYPE, decltype(whole)::value>(Y0, (t.row0 + min(x + 4 * g + q, t.rows - 1)) * ldy0, c, N);
+    };
+    if (whole) {
+        fetch_b(std::true_type{});
+        fetch(0, std::true_type{});
+    } else if (c0 < N) {
+        fetch_b(std::false_type{});
+        fetch(0, std::false_type{});
+    }
+    for (int n = threadIdx.x; n < (t.rows + 15) / 16 * 16 * kOctets; n += kThreads) {
+        const int row = n / kOctets, octet = n % kOctets;
+        float v[8];
+        int at[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) at[q] = min(row, t.rows - 1) * r + min(8 * octet + q, r - 1);
+        sum_parts<8>(T + (size_t)t.row0 * r, at, parts, (size_t)seg.M * r, v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = row < t.rows && 8 * octet + q < r ? v[q] : 0.0f;
+        uint32_t top = 0;
+        if constexpr (TYPE == APB_F16) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) top = max(top, float_bits(v[q]) & 0x7fffffffu);
+#pragma unroll
+            for (int d = 1; d < kOctets; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, kWave));
+        }
+        u32x4 hi, lo;
+        float back;
+        split<TYPE>(v, top, hi, lo, back);
+        *reinterpret_cast<u32x4*>(lds + row * kPitch + 16 * octet) = hi;
+        *reinterpret_cast<u32x4*>(lds + row * kPitch + 16 * (kOctets + octet)) = lo;
+        if (TYPE == APB_F16 && octet == 0) backs[row] = back;
+    }
+    __syncthreads();
+    if (c0 >= N) return;
+    auto stream = [&](auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
+        u32x4 b[kSteps][8];
+#pragma unroll
+        for (int h = 0; h < kSteps; ++h) {
+            u32x4 rows[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool there = (CH == 0 ? 8 * (g & 1) : 32 * h + 8 * g) + e < r;
+                const u32x4 v = settle<TYPE, kWhole>(row[h][e], c, N).w[0];
+                rows[e] = there ? v : u32x4{0u, 0u, 0u, 0u};
+            }
+            transpose8(rows, b[h]);
+        }
+        for (int x = 0; x < t.rows; x += 16) {
+            Eight<TYPE> was[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) was[q] = settle<TYPE, kWhole>(y0[q], c, N);
+            if (x + 16 < t.rows) fetch(x + 16, whole);
+            f32x4 acc[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            const uint8_t* from = lds + (x + i) * kPitch + 16 * g;   // (with CH == 0 the four octets of both operands)
+#pragma unroll
+            for (int h = 0; h < kSteps; ++h) {
+                Eight<TYPE> hi, lo, bn;
+                hi.w[0] = *reinterpret_cast<const u32x4*>(from + 64 * h);
+                if (CH > 0) lo.w[0] = *reinterpret_cast<const u32x4*>(from + 64 * (kSteps + h));
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    bn.w[0] = b[h][n];
+                    if (CH > 0) acc[n] = multiply8<TYPE>(lo, bn, acc[n]);
+                    acc[n] = multiply8<TYPE>(hi, bn, acc[n]);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int row = x + 4 * g + q;
+                const float back = TYPE == APB_F16 ? backs[row] : 1.0f;
+                float v[8];
+                floats(was[q], v);
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const float sum = TYPE == APB_F16 ? acc[n][q] * back : acc[n][q];
+                    v[n] += sum;
+                }
+                if (row < t.rows) store8<TYPE>(Y, (t.row0 + row) * ldy + c, kWhole ? 8 : have, v);
+            }
+        }
+    };
+    if (whole) stream(std::true_type{});
+    else stream(std::false_type{});
+}
+
+// ---- gradients --------------------------------------------------------------------------------------------------------------
+
+// The rows of adapter a, and of all adapters before it.
+struct Span {
+    int rows, before;
+};
+// its, first, count: the last segment that the lane has looked at.
+__device__ __forceinline__ Span span_of(const Segments& seg, int a, int& its, int& first, int& count) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int rows = 0, before = 0;
+    for (int base = 0; base < seg.S; base += kWave) {
+        its = rows_of(seg, base + lane, first, count);
+        rows += its == a ? count : 0;
+        before += its >= 0 && its < a ? count : 0;
+    }
+    // (together they are no more than M; of offsets that do not ascend, that much is kept)
+    rows = min(rows, seg.M);
+    before = min(before, seg.M);
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        rows += __shfl_xor(rows, d, kWave);
+        before += __shfl_xor(before, d, kWave);
+    }
+    rows = min(__builtin_amdgcn_readfirstlane(rows), seg.M);
+    return Span{rows, min(__builtin_amdgcn_readfirstlane(before), seg.M - rows)};
+}
+// Where slice z of an adapter of more than `each` rows leaves its sum: slices of different adapters never meet, as n rows have
+// ceil(n / each) <= floor(2 n / each) slices, and there are at most 2 M / each places.
+__device__ __forceinline__ int place_of_slice(const Span& s, int each, int z) { return (int)(2LL * s.before / each) + z; }
+
+// Rows of X as they are loaded: what a lane has of 32 of them.  16 bits: eight columns of eight rows 8 g ..; float32: eight columns
+// of rows g, g + 4, ...; 8 bits: as 16 bits, and each row's scale.
+template <int XT>
+struct Rows32 {
+    Eight<XT == APB_F32 ? APB_F32 : APB_BF16> v[8];
+};
+template <>
+struct Rows32<APB_MX8> {
+    u32x2 v[8];
+    uint8_t scale[8];
+};
+// (fewer than eight columns: one by one)
+template <int XT, bool WHOLE>
+__device__ __forceinline__ void load_rows(Rows32<XT>& x, const void* X, long long ldx, const Mx8& x8, int m, int end, int g, int c, int K) {
+    auto row = [&](int e) { return (long long)min(m + (XT == APB_F32 ? 4 * e + g : 8 * g + e), end - 1); };
+    if constexpr (XT == APB_MX8) {
+        const int at = min(c, x8.blocks * kMx8Block - 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x.v[e] = *reinterpret_cast<const u32x2*>(x8.codes + row(e) * x8.blocks * kMx8Block + at);
+            x.scale[e] = x8.scales[row(e) * x8.blocks + at / kMx8Block];
+        }
+    } else {
+        constexpr int kAs = XT == APB_F32 ? APB_F32 : APB_BF16;
+        if (WHOLE || K >= 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x.v[e] = load_row<kAs, WHOLE>(X, row(e) * ldx, c, K);
+        } else {
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+                const Eight<kAs> v = load_some<kAs>(X, row(e) * ldx + c, K - c);
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (u == e) x.v[u] = v;
+            }
+        }
+    }
+}
+// Rows that are not there as zeros (they repeat the last one, and zero times infinity is not zero).
+template <int XT>
+__device__ __forceinline__ void clear_rows(Rows32<XT>& x, int rows, int g) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if ((XT == APB_F32 ? 4 * e + g : 8 * g + e) >= rows) {
+            if constexpr (XT == APB_MX8) {
+                x.v[e] = u32x2{0u, 0u};
+                x.scale[e] = 0;
+            } else {
+                x.v[e].w[0] = u32x4{0u, 0u, 0u, 0u};
+                if constexpr (XT == APB_F32) x.v[e].w[1] = u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+}
+// Column n of the lane's eight as bfloat16 operands of eight rows: 16-bit floats in one or two parts, 8-bit values in one.
+template <int XT>
+constexpr int kXParts = XT == APB_F16 ? 2 : 1;
+template <int XT>
+__device__ __forceinline__ void column(const Rows32<XT>& x, int n, Eight<APB_BF16> (&out)[kXParts<XT>]) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        if constexpr (XT == APB_BF16) {
+            out[0].w[0][d] = __builtin_amdgcn_perm(x.v[2 * d + 1].w[0][n / 2], x.v[2 * d].w[0][n / 2], n & 1 ? 0x07060302u : 0x05040100u);
+        } else if constexpr (XT == APB_MX8) {
+            out[0].w[0][d] = pack2(APB_BF16, decode8(x.v[2 * d][n / 4], n & 3, scale_value(x.scale[2 * d])),
+                                   decode8(x.v[2 * d + 1][n / 4], n & 3, scale_value(x.scale[2 * d + 1])));
+        } else {
+            const uint32_t w = __builtin_amdgcn_perm(x.v[2 * d + 1].w[0][n / 2], x.v[2 * d].w[0][n / 2], n & 1 ? 0x07060302u : 0x05040100u);
+            const f16x2 h = __builtin_bit_cast(f16x2, w);
+            const uint32_t hi = pack2(APB_BF16, (float)h[0], (float)h[1]);
+            out[0].w[0][d] = hi;
+            out[1].w[0][d] = pack2(APB_BF16, (float)h[0] - __builtin_bit_cast(float, hi << 16),
+                                   (float)h[1] - __builtin_bit_cast(float, hi & 0xffff0000u));
+        }
+    }
+}
+
+// A workgroup takes one adapter, 16 * JT ranks, kCols columns a wave, and `each` of the adapter's rows, counted through all of its
+// segments, 32 rows of a segment at a time: while one such chunk is multiplied, the next one's X comes to registers, where it is
+// transposed, and T, its parts added up, on its way to LDS, where it is in three bfloat16 operands of eight rows, or in float32 for
+// an X of float32.
 template <int XT, int JT>
 __global__ __launch_bounds__(kThreads) void k_adapter_gradient(const float* __restrict__ T, int parts, const void* __restrict__ X,
-                                                               long long ldx, Mx8 x8, Segments seg, int K, int r, int rank_tiles,
-                                                               float* __restrict__ out) {
-    const int a = blockIdx.y / rank_tiles, j0 = blockIdx.y % rank_tiles * 16 * JT;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, i = lane & 15, g = lane >> 4;
-    const int c = (blockIdx.x * kWaves + wave) * kCols + 8 * i;
-    int total = 0;
-    for (int base = 0; base < seg.S; base += kWave) {
-        int first, count;
-        rows_of(seg, base + lane, a, first, count);
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) count += __shfl_xor(count, d, kWave);
-        total += count;
-    }
-    const int each = ((total + (int)gridDim.z - 1) / (int)gridDim.z + 3) / 4 * 4;
-    const int lo = blockIdx.z * each, hi = min(lo + each, total);
+                                                               long long ldx, Mx8 x8, Segments seg, int K, int r, int rank_tiles, int each,
+                                                               float* __restrict__ dA, float* __restrict__ shared) {
+    constexpr bool kWide = XT == APB_F32;
+    constexpr int kRanks = 16 * JT, kChunk = 32;
+    constexpr int kPitch = kWide ? 4 * (kRanks + 1) : 2 * kChunk + 16;            // of a row of T; of a rank
+    constexpr int kStageBytes = ((kWide ? kChunk * kPitch : 3 * kRanks * kPitch) + 15) / 16 * 16;
+    static_assert(kRanks * kChunk / 8 <= kThreads, "a thread brings eight values of T");
+    __shared__ __align__(16) uint8_t lds[2 * kStageBytes];
+    const int a = blockIdx.y / rank_tiles, j0 = blockIdx.y % rank_tiles * kRanks;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
+    const int c0 = (blockIdx.x * kWaves + wave) * kCols, c = c0 + 8 * i;
+    const bool whole = c0 + kCols <= K, there = c0 < K;
+    int its, first, count;
+    const Span span = span_of(seg, a, its, first, count);
+    const int lo = blockIdx.z * each, hi = min(lo + each, span.rows);
+    if (blockIdx.z > 0 && lo >= hi) return;
     f32x4 acc[JT][8];
 #pragma unroll
     for (int j = 0; j < JT; ++j)
 #pragma unroll
         for (int q = 0; q < 8; ++q) acc[j][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    int before = 0;
-    for (int base = 0; base < seg.S && before < hi; base += kWave) {
-        int first, count;
-        rows_of(seg, base + lane, a, first, count);
-        for (unsigned long long left = __ballot(count > 0); left; left &= left - 1) {
+
+    // the chunks, one after another: rows m .. min(m + 32, end) - 1
+    int base = -kWave, before = 0, m = 0, end = 0;
+    unsigned long long left = 0;
+    auto advance = [&]() {
+        m += kChunk;
+        while (m >= end) {
+            while (!left) {
+                base += kWave;
+                if (base >= seg.S || before >= hi) return false;
+                if (seg.S > kWave) its = rows_of(seg, base + lane, first, count);
+                left = __ballot(its == a && count > 0);
+            }
             const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)left) - 1);
             const int from = __builtin_amdgcn_readlane(first, src), rows = __builtin_amdgcn_readlane(count, src);
-            const int end = from + min(rows, hi - before);
-            for (int m = from + max(lo - before, 0); m < end; m += 4) {
-                const int row = m + g;
-                float v[8], tv[JT];
-                row_values<XT>(X, ldx, x8, row, c, row < end ? K - c : 0, v);
+            left &= left - 1;
+            m = from + max(lo - before, 0);
+            end = from + min(rows, hi - before);
+            before += rows;
+        }
+        return true;
+    };
+    const int tj = threadIdx.x % kRanks, octet = threadIdx.x / kRanks;
+    const bool brings = octet < kChunk / 8;
+    Rows32<XT> x;
+    float tv[8];
+    auto fetch = [&](auto all) {
+        if (there) load_rows<XT, decltype(all)::value>(x, X, ldx, x8, m, end, g, c, K);
+        if (brings) {
+            // (rows and ranks that are not there repeat the last ones, and are cleared)
+            int at[8];
 #pragma unroll
-                for (int j = 0; j < JT; ++j) {
-                    tv[j] = 0.0f;
-                    if (row < end && j0 + 16 * j + i < r)
-                        for (int p = 0; p < parts; ++p) tv[j] += T[((size_t)p * seg.M + row) * r + j0 + 16 * j + i];
+            for (int e = 0; e < 8; ++e) at[e] = min(8 * octet + e, end - 1 - m) * r + min(j0 + tj, r - 1);
+            sum_parts<8>(T + (size_t)m * r, at, parts, (size_t)seg.M * r, tv);
+        }
+    };
+    auto multiply = [&](auto all) {
+        bool more = advance();
+        if (more) fetch(all);
+        uint32_t stage = 0;
+        while (more) {
+            const int rows = min(end - m, kChunk);
+            uint8_t* to = lds + stage;
+            stage = kStageBytes - stage;
+            if (brings) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) tv[e] = 8 * octet + e < rows && j0 + tj < r ? tv[e] : 0.0f;
+                if constexpr (kWide) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) *reinterpret_cast<float*>(to + (8 * octet + e) * kPitch + 4 * tj) = tv[e];
+                } else {
+                    Eight<APB_BF16> part[3];
+                    bf16_parts<3>(tv, part);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(to + (p * kRanks + tj) * kPitch + 16 * octet) = part[p].w[0];
                 }
+            }
+            Rows32<XT> now = x;
+            more = advance();
+            if (more) fetch(all);
+            __syncthreads();                                         // (of the other stage, everybody has read by the time they are here)
+            if (!there) continue;
+            if constexpr (XT != APB_MX8)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) now.v[e] = settle<XT == APB_F32 ? APB_F32 : APB_BF16, decltype(all)::value>(now.v[e], c, K);
+            if (rows < kChunk) clear_rows<XT>(now, rows, g);
+            if constexpr (kWide) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float v[8];
+                    floats(now.v[e], v);
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) {
+                        const float t = *reinterpret_cast<const float*>(to + (4 * e + g) * kPitch + 4 * (16 * j + i));
+#pragma unroll
+                        for (int n = 0; n < 8; ++n) acc[j][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(t, v[n], acc[j][n], 0, 0, 0);
+                    }
+                }
+            } else {
+                Eight<APB_BF16> t[JT][3];
 #pragma unroll
                 for (int j = 0; j < JT; ++j)
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) acc[j][q] = __builtin_amdgcn_mfma_f32_16x16x4f32(tv[j], v[q], acc[j][q], 0, 0, 0);
+                    for (int p = 0; p < 3; ++p)
+                        t[j][p].w[0] = *reinterpret_cast<const u32x4*>(to + (p * kRanks + 16 * j + i) * kPitch + 16 * g);
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    Eight<APB_BF16> xv[kXParts<XT>];
+                    column<XT>(now, n, xv);
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) {
+                        // (the smallest first; the third part of T times the second of X is below 2^-24)
+                        if constexpr (kXParts<XT> == 2) {
+                            acc[j][n] = multiply8<APB_BF16>(t[j][1], xv[1], acc[j][n]);
+                            acc[j][n] = multiply8<APB_BF16>(t[j][0], xv[1], acc[j][n]);
+                        }
+#pragma unroll
+                        for (int p = 2; p >= 0; --p) acc[j][n] = multiply8<APB_BF16>(t[j][p], xv[0], acc[j][n]);
+                    }
+                }
             }
-            before += rows;
         }
-    }
-    out += ((size_t)blockIdx.z * seg.L + a) * r * K;
+    };
+    if (whole) multiply(std::true_type{});
+    else multiply(std::false_type{});
+    if (!there) return;
+    float* out = span.rows > each ? shared + (size_t)place_of_slice(span, each, blockIdx.z) * r * K : dA + (size_t)a * r * K;
 #pragma unroll
     for (int j = 0; j < JT; ++j)
 #pragma unroll
@@ -258,12 +775,49 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gradient(const float* __re
         }
 }
 
-// The slices' sums added up in order.
-__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ parts, int slices, long long n, float* __restrict__ out) {
-    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kThreads) {
-        float v = parts[i];
-        for (int s = 1; s < slices; ++s) v += parts[s * n + i];
-        out[i] = v;
+// The slices of the adapters that have several, added up in order.
+__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int each, long long n,
+                                                           float* __restrict__ dA) {
+    const int a = blockIdx.y;
+    int its, first, count;
+    const Span span = span_of(seg, a, its, first, count);
+    if (span.rows <= each) return;
+    const int slices = (span.rows + each - 1) / each;
+    const float* from = shared + (size_t)place_of_slice(span, each, 0) * n;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    __shared__ f32x4 sums[kWaves][kWave];
+    // four neighbours to a lane; a wave takes every fourth slice, eight at a time
+    for (long long k0 = (long long)blockIdx.x * 4 * kWave; k0 < n; k0 += (long long)gridDim.x * 4 * kWave) {
+        const long long k = k0 + 4 * lane;
+        const int have = (int)std::min<long long>(n - k, 4);
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int z = wave; z < slices; z += 8 * kWaves) {
+            u32x4 w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float* at = from + min(z + u * kWaves, slices - 1) * n + k;
+                if (have >= 4) w[u] = load16_any(at);
+                else
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) w[u][q] = q < have ? float_bits(at[q]) : 0u;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t bits = w[u][q];
+                    if (z + u * kWaves < slices) v[q] += __builtin_bit_cast(float, bits);
+                }
+        }
+        sums[wave][lane] = v;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v += sums[w][lane];
+            const float all[4] = {v[0], v[1], v[2], v[3]};
+            store4(dA, APB_F32, a * n + k, all, have);
+        }
+        __syncthreads();
     }
 }
 
@@ -272,44 +826,69 @@ bool bad_adapter(int S, int L, int M, int K, int r, const int32_t* offsets, cons
            r > APB_ADAPTER_MAX_R || (!offsets && S != 1) || (!adapter && S != L);
 }
 
-// Groups of 16 rows that a workgroup takes: four where segments have them on average.
-int row_groups(int S, int M) { return (M + S - 1) / S > 32 ? 4 : 1; }
 int rank_groups(int r) { return r <= 16 ? 1 : r <= 32 ? 2 : 4; }
 
-int down_parts(int S, int M, int K, int r) {
-    const int rows = 16 * row_groups(S, M), ranks = 16 * rank_groups(r);
-    const long long tiles = std::max<long long>((M + rows - 1) / rows, std::min(S, M)) * ((r + ranks - 1) / ranks);
-    // two chunks to a wave at least
-    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(512 / tiles, K / 512), kMaxParts));
+// Rows to a workgroup that streams them past its share of B.
+int up_rows(int S, int M, int N) {
+    const long long columns = (N + kCols * kWaves - 1) / (kCols * kWaves);
+    int rows = 16;
+    while (rows < kUpRows && rows < (M + S - 1) / S && M / (2 * rows) * columns >= 1024) rows *= 2;
+    return rows;
 }
 
-int gradient_slices(int L, int M, int K, int r) {
+// Rows of an adapter to a workgroup of its gradient: as many workgroups as fill the chip twice, were the rows spread evenly, but no
+// more than 16384 that may find none.
+int gradient_rows(int L, int M, int K, int r) {
     const int ranks = 16 * rank_groups(r);
-    const long long tiles = (long long)((K + kCols * kWaves - 1) / (kCols * kWaves)) * L * ((r + ranks - 1) / ranks);
-    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(512 / tiles, M / L / 32), kMaxSlices));
+    const long long columns = (long long)((K + kCols * kWaves - 1) / (kCols * kWaves)) * ((r + ranks - 1) / ranks);
+    const long long rows = std::max<long long>(M * columns / 256, M * columns * L / 16384);
+    return (int)std::min<long long>(1 << 24, std::max<long long>(128, (rows + 63) / 64 * 64));
+}
+
+// Groups of rows and of ranks to a workgroup of down, and parts of K.
+struct DownPlan {
+    int rt, jt, parts;
+};
+DownPlan down_plan(int S, int M, int K, int r) {
+    DownPlan best{1, 1, 1};
+    double least = 1e30;
+    for (int rt = 1; rt <= 4; rt *= 2)
+        for (int jt = 1; jt <= rank_groups(r); jt *= 2)
+            for (int parts = 1; parts <= kMaxParts; parts *= 2) {
+                if (parts > 1 && ((long long)parts * M > 8192 || K < 512 * parts)) continue;
+                const long long tiles = std::max<long long>((M + 16 * rt - 1) / (16 * rt), std::min(S, M)) * ((r + 16 * jt - 1) / (16 * jt));
+                const long long rounds = (tiles * parts + 255) / 256;
+                const double cost = (double)rounds * (rt + jt) / parts * K * 32 / 40e3 + 0.25 * parts;
+                if (cost < least) {
+                    least = cost;
+                    best = DownPlan{rt, jt, parts};
+                }
+            }
+    return best;
 }
 
 template <int TYPE, int RT, int JT>
 void down_tiles(const void* X, long long ldx, const void* A, const Segments& seg, const float* scale, int K, int r, int parts, float* T,
                 hipStream_t s) {
-    constexpr int kChunk = TYPE == APB_F32 ? 32 : 64;
-    const int chunks = (K + kChunk - 1) / kChunk, each = (chunks + parts - 1) / parts;
-    const dim3 grid((unsigned)max_row_tiles(seg.M, seg.S, seg.offsets != nullptr, 16 * RT), (unsigned)parts, (unsigned)((r + 16 * JT - 1) / (16 * JT)));
-    hipLaunchKernelGGL((k_adapter_down<TYPE, RT, JT>), grid, dim3(kThreads), 0, s, X, ldx, A, seg, scale, K, r, each, T);
-}
-template <int TYPE, int RT>
-void down_ranks(const void* X, long long ldx, const void* A, const Segments& seg, const float* scale, int K, int r, int parts, float* T,
-                hipStream_t s) {
-    const int j = rank_groups(r);
-    if (j == 1) down_tiles<TYPE, RT, 1>(X, ldx, A, seg, scale, K, r, parts, T, s);
-    else if (j == 2) down_tiles<TYPE, RT, 2>(X, ldx, A, seg, scale, K, r, parts, T, s);
-    else down_tiles<TYPE, RT, 4>(X, ldx, A, seg, scale, K, r, parts, T, s);
+    constexpr int kLine = TYPE == APB_F32 ? 32 : 64, kW = kDownWaves<RT, JT>;
+    const int lines = (K + kLine - 1) / kLine, each = (lines + parts - 1) / parts;
+    const dim3 grid((unsigned)max_row_tiles(seg.M, seg.S, seg.offsets != nullptr, 16 * RT), (unsigned)((r + 16 * JT - 1) / (16 * JT)), (unsigned)parts);
+    hipLaunchKernelGGL((k_adapter_down<TYPE, RT, JT, kW>), grid, dim3(kW * kWave), 0, s, X, ldx, A, seg, scale, K, r, each, T);
 }
 template <int TYPE>
 void down(const void* X, long long ldx, const void* A, const Segments& seg, const float* scale, int K, int r, float* T, hipStream_t s) {
-    const int parts = down_parts(seg.S, seg.M, K, r);
-    if (row_groups(seg.S, seg.M) == 4) down_ranks<TYPE, 4>(X, ldx, A, seg, scale, K, r, parts, T, s);
-    else down_ranks<TYPE, 1>(X, ldx, A, seg, scale, K, r, parts, T, s);
+    const DownPlan p = down_plan(seg.S, seg.M, K, r);
+    auto with = [&](auto rt, auto jt) {
+        down_tiles<TYPE, decltype(rt)::value, decltype(jt)::value>(X, ldx, A, seg, scale, K, r, p.parts, T, s);
+    };
+    auto with_rows = [&](auto rt) {
+        if (p.jt == 1) with(rt, std::integral_constant<int, 1>{});
+        else if (p.jt == 2) with(rt, std::integral_constant<int, 2>{});
+        else with(rt, std::integral_constant<int, 4>{});
+    };
+    if (p.rt == 1) with_rows(std::integral_constant<int, 1>{});
+    else if (p.rt == 2) with_rows(std::integral_constant<int, 2>{});
+    else with_rows(std::integral_constant<int, 4>{});
 }
 
 template <int TYPE, int RT>
@@ -318,27 +897,42 @@ void up_tiles(const float* T, int parts, const void* B, const Segments& seg, int
     const dim3 grid((unsigned)max_row_tiles(seg.M, seg.S, seg.offsets != nullptr, 16 * RT), (unsigned)((N + kCols * kWaves - 1) / (kCols * kWaves)));
     hipLaunchKernelGGL((k_adapter_up<TYPE, RT>), grid, dim3(kThreads), 0, s, T, parts, B, seg, N, r, Y0, ldy0, Y, ldy);
 }
+template <int TYPE, int CH>
+void up16_tiles(const float* T, int parts, const void* B, const Segments& seg, int N, int r, const void* Y0, long long ldy0, void* Y,
+                long long ldy, hipStream_t s) {
+    const int tile = up_rows(seg.S, seg.M, N);
+    // neighbouring workgroups take neighbouring columns
+    const unsigned tiles = (unsigned)max_row_tiles(seg.M, seg.S, seg.offsets != nullptr, tile), most = 32768;
+    const dim3 grid((unsigned)((N + kCols * kWaves - 1) / (kCols * kWaves)), std::min(tiles, most), (tiles + most - 1) / most);
+    hipLaunchKernelGGL((k_adapter_up16<TYPE, CH>), grid, dim3(kThreads), 0, s, T, parts, B, seg, tile, N, r, Y0, ldy0, Y, ldy);
+}
 template <int TYPE>
 void up(const float* T, int parts, const void* B, const Segments& seg, int N, int r, const void* Y0, long long ldy0, void* Y, long long ldy,
         hipStream_t s) {
-    if (row_groups(seg.S, seg.M) == 4) up_tiles<TYPE, 4>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
+    if constexpr (TYPE != APB_F32) if (N >= 8) {
+        if (r <= 16) return up16_tiles<TYPE, 0>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
+        if (r <= 32) return up16_tiles<TYPE, 1>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
+        if (r <= 64) return up16_tiles<TYPE, 2>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
+        if (r <= 128) return up16_tiles<TYPE, 4>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
+    }
+    if (up_rows(seg.S, seg.M, N) == kUpRows) up_tiles<TYPE, 4>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
     else up_tiles<TYPE, 1>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
 }
 
 template <int XT, int JT>
-void gradient_tiles(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int slices,
-                    float* out, hipStream_t s) {
+void gradient_tiles(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int each,
+                    float* dA, float* shared, hipStream_t s) {
     const int rank_tiles = (r + 16 * JT - 1) / (16 * JT);
-    const dim3 grid((unsigned)((K + kCols * kWaves - 1) / (kCols * kWaves)), (unsigned)(seg.L * rank_tiles), (unsigned)slices);
-    hipLaunchKernelGGL((k_adapter_gradient<XT, JT>), grid, dim3(kThreads), 0, s, T, parts, X, ldx, x8, seg, K, r, rank_tiles, out);
+    const dim3 grid((unsigned)((K + kCols * kWaves - 1) / (kCols * kWaves)), (unsigned)(seg.L * rank_tiles), (unsigned)((seg.M + each - 1) / each));
+    hipLaunchKernelGGL((k_adapter_gradient<XT, JT>), grid, dim3(kThreads), 0, s, T, parts, X, ldx, x8, seg, K, r, rank_tiles, each, dA, shared);
 }
 template <int XT>
-void gradient(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int slices,
-              float* out, hipStream_t s) {
+void gradient(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int each,
+              float* dA, float* shared, hipStream_t s) {
     const int j = rank_groups(r);
-    if (j == 1) gradient_tiles<XT, 1>(T, parts, X, ldx, x8, seg, K, r, slices, out, s);
-    else if (j == 2) gradient_tiles<XT, 2>(T, parts, X, ldx, x8, seg, K, r, slices, out, s);
-    else gradient_tiles<XT, 4>(T, parts, X, ldx, x8, seg, K, r, slices, out, s);
+    if (j == 1) gradient_tiles<XT, 1>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+    else if (j == 2) gradient_tiles<XT, 2>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+    else gradient_tiles<XT, 4>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
 }
 
 }  // namespace
@@ -350,7 +944,7 @@ extern "C" {
 
 int apb_adapter_parts(int S, int M, int K, int r) {
     static const int32_t some = 0;
-    return bad_adapter(S, 1, M, K, r, &some, &some) ? 0 : down_parts(S, M, K, r);
+    return bad_adapter(S, 1, M, K, r, &some, &some) ? 0 : down_plan(S, M, K, r).parts;
 }
 
 int apb_adapter_down(const void* X, int type, long long ldx, const void* A, const int32_t* offsets, const int32_t* adapter,
@@ -391,8 +985,8 @@ int apb_adapter_up(const float* T, int parts, const void* B, int type, const int
 size_t apb_adapter_gradient_workspace_bytes(int L, int M, int K, int r) {
     static const int32_t some = 0;
     if (bad_adapter(1, L, M, K, r, &some, &some)) return 0;
-    const int slices = gradient_slices(L, M, K, r);
-    return slices > 1 ? (size_t)slices * L * r * K * sizeof(float) : 0;
+    const int each = gradient_rows(L, M, K, r);
+    return M > each ? (size_t)(2LL * M / each + 1) * r * K * sizeof(float) : 0;
 }
 
 int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, long long ldx, const int32_t* offsets,
@@ -409,19 +1003,19 @@ int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, l
     const Segments seg{offsets, adapter, S, L, M};
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const size_t need = apb_adapter_gradient_workspace_bytes(L, M, K, r);
-    const bool shared = need != 0 && workspace != nullptr && workspace_bytes >= need;
-    const int slices = shared ? gradient_slices(L, M, K, r) : 1;
-    float* out = shared ? static_cast<float*>(workspace) : dA;
+    const bool join = need != 0 && workspace != nullptr && workspace_bytes >= need;
+    const int each = join ? gradient_rows(L, M, K, r) : M;
+    float* shared = static_cast<float*>(workspace);
     const Mx8 x8 = mx8_view(X, M, K);
-    if (x_type == APB_F32) gradient<APB_F32>(T, parts, X, ldx, x8, seg, K, r, slices, out, s);
-    else if (x_type == APB_BF16) gradient<APB_BF16>(T, parts, X, ldx, x8, seg, K, r, slices, out, s);
-    else if (x_type == APB_F16) gradient<APB_F16>(T, parts, X, ldx, x8, seg, K, r, slices, out, s);
-    else gradient<APB_MX8>(T, parts, X, ldx, x8, seg, K, r, slices, out, s);
+    if (x_type == APB_F32) gradient<APB_F32>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+    else if (x_type == APB_BF16) gradient<APB_BF16>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+    else if (x_type == APB_F16) gradient<APB_F16>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+    else gradient<APB_MX8>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
     APB_HIP(hipGetLastError());
-    if (shared) {
-        const long long n = (long long)L * r * K;
-        const unsigned blocks = (unsigned)std::min<long long>((n + kThreads - 1) / kThreads, 4096);
-        hipLaunchKernelGGL(k_adapter_join, dim3(blocks), dim3(kThreads), 0, s, static_cast<const float*>(workspace), slices, n, dA);
+    if (join) {
+        const long long n = (long long)r * K;
+        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096), (unsigned)L);
+        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, each, n, dA);
         APB_HIP(hipGetLastError());
     }
     return APB_OK;

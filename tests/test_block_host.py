@@ -189,7 +189,7 @@ def test_adapter_refusals(b):
         assert f(off=odd1) == b.APB_ERR_ALIGN and f(ad=odd1) == b.APB_ERR_ALIGN
     assert down(t=3) == b.APB_ERR_TYPE and up(t=3) == b.APB_ERR_TYPE and down(scale=ODD) == b.APB_ERR_ALIGN
     for f in (up, gradient):
-        assert f(parts=0) == b.APB_ERR_SHAPE and f(parts=33) == b.APB_ERR_SHAPE
+        assert f(parts=0) == b.APB_ERR_SHAPE and f(parts=9) == b.APB_ERR_SHAPE
     assert up(Y0=P, ld0=63) == b.APB_ERR_SHAPE and up(Y0=P, ld0=65, X=P) == b.APB_ERR_SHAPE
     assert gradient(t=3, X=ODD) == b.APB_ERR_ALIGN and gradient(A=ODD) == b.APB_ERR_ALIGN and gradient(ws=ODD) == b.APB_ERR_ALIGN
     assert b.apb_adapter_parts(0, 4, 4, 4) == 0 and b.apb_adapter_parts(1, 1, 1, 1) == 1 and b.apb_adapter_parts(1, 1, 1, 257) == 0
