@@ -3,6 +3,8 @@
 // Bound by the matrix cores, and for long products by the power they may draw: 8192^3 with a bfloat16 result, one call behind another,
 // takes 262 us (4200 TFLOP/s) on random values and 191 on zeros, with the same instructions.  4096^3: 42 us (3260), 1024 x 4096 x
 // 4096: 15 us.
+#include <type_traits>
+
 #include "apb_mx8.h"
 
 namespace apb {
@@ -39,71 +41,86 @@ __device__ __forceinline__ f32x4 four_up(const f32x16 (&acc)[F][F], int x, int y
     else return four_sums<F>(acc[x][y + F / 2], 4 * q);
 }
 
-// G or U of a wave's tile in 8 bits.  A block of 32 columns of a row lies in the lanes (r, 0) and (r, 1); with F == 1, in two waves,
-// which exchange their maxima through LDS (`tops`, 64 rows x 2).
-template <int F, class SUMS>
+// What two lanes, 32 apart, have of two words: the lower lane's a and the upper one's a, or their b's.
+__device__ __forceinline__ u32x2 exchange(uint32_t a, uint32_t b) {
+    const auto v = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    return u32x2{v[0], v[1]};
+}
+
+// G or U of a wave's tile in 8 bits.  A block of 32 columns of a row lies in the lanes (r, 0) and (r, 1), which exchange fours until
+// each has 16 neighbours; with F == 1 it lies in two waves, which exchange their maxima through LDS (`tops`, 64 rows x 2).  WHOLE:
+// every column of the tile is there.
+template <int F, bool WHOLE, class SUMS>
 __device__ __forceinline__ void save_tile(const SUMS& sums, uint32_t* tops, const Mx8& to, long long first, int rows, int col, int cols) {
     constexpr int kBlocks = (F + 1) / 2, kFours = F == 1 ? 2 : 4;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, r = lane & 31, h = lane >> 5;
-    uint32_t top[F][kBlocks];
 #pragma unroll
     for (int x = 0; x < F; ++x)
 #pragma unroll
         for (int y = 0; y < kBlocks; ++y) {
+            float v[kFours][4];
             uint32_t most = 0;
 #pragma unroll
             for (int q = 0; q < kFours; ++q) {
-                const f32x4 v = sums(x, y, q);
+                const f32x4 s = sums(x, y, q);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)                      // (columns that are not there have another row's sums)
-                    most = max(most, 32 * y + 8 * q + 4 * h + i < cols ? float_bits(v[i]) & 0x7fffffffu : 0u);
+                for (int i = 0; i < 4; ++i) {                    // (columns that are not there have another row's sums)
+                    v[q][i] = WHOLE || 32 * y + 8 * q + 4 * h + i < cols ? s[i] : 0.0f;
+                    most = max(most, float_bits(v[q][i]) & 0x7fffffffu);
+                }
             }
-            top[x][y] = max(most, (uint32_t)__shfl_xor((int)most, 32, kWave));
-        }
-    if constexpr (F == 1) {
-        tops[wave * 32 + r] = top[0][0];
-        __syncthreads();
-        top[0][0] = max(top[0][0], tops[(wave ^ 1) * 32 + r]);
-        __syncthreads();
-    }
-#pragma unroll
-    for (int x = 0; x < F; ++x)
-#pragma unroll
-        for (int y = 0; y < kBlocks; ++y) {
-            const uint32_t code = scale8_code(top[x][y]);
+            const u32x2 both = exchange(most, most);
+            most = max(both[0], both[1]);
+            if constexpr (F == 1) {
+                tops[wave * 32 + r] = most;
+                __syncthreads();
+                most = max(most, tops[(wave ^ 1) * 32 + r]);
+                __syncthreads();
+            }
+            const uint32_t code = scale8_code(most);
             const float inverse = scale8_inverse(code);
+            uint32_t w[kFours];
+#pragma unroll
+            for (int q = 0; q < kFours; ++q) w[q] = encode8_four(v[q], inverse, code == 255u);
             const int k = col + 32 * y;                          // (a multiple of 32, or of 16 with F == 1)
             const long long at = (first + 32 * x + r) * to.blocks + k / kMx8Block;
-            const bool there = 32 * x + r < rows && k / kMx8Block < to.blocks;
-#pragma unroll
-            for (int q = 0; q < kFours; ++q) {
-                const f32x4 v = sums(x, y, q);
-                float w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = 32 * y + 8 * q + 4 * h + i < cols ? v[i] : 0.0f;
-                if (there)
-                    *reinterpret_cast<uint32_t*>(to.codes + at * kMx8Block + k % kMx8Block + 8 * q + 4 * h) =
-                        encode8_four(w, inverse, code == 255u);
+            uint8_t* p = to.codes + at * kMx8Block + k % kMx8Block;
+            const bool there = 32 * x + r < rows && (WHOLE || k / kMx8Block < to.blocks);
+            if constexpr (F == 1) {
+                const u32x2 eight = exchange(w[0], w[1]);
+                if (there) *reinterpret_cast<u32x2*>(p + 8 * h) = eight;
+            } else {
+                const u32x2 a = exchange(w[0], w[kFours / 2]), b = exchange(w[1], w[kFours - 1]);
+                if (there) *reinterpret_cast<u32x4*>(p + 16 * h) = u32x4{a[0], a[1], b[0], b[1]};
             }
             if (there && h == 0 && k % kMx8Block == 0) to.scales[at] = (uint8_t)code;
         }
 }
 
 // A gated wave's tile of 32 * F x 16 * F outputs.  `all`: the workgroup's LDS, which nobody else needs any more.
-template <int F>
+template <int F, int ACT>
 __device__ __forceinline__ void store_gated(const f32x16 (&acc)[F][F], uint32_t lds, uint8_t* all, void* out, int type, long long first,
                                             long long ld, int rows, int col, int cols, const Act& act, const Mx8& saved, int M) {
     settled<F>();
+    auto gate = [&](int x, int y, int q) { return four_gate<F>(acc, x, y, q); };
+    auto up = [&](int x, int y, int q) { return four_up<F>(acc, x, y, q); };
     if (saved.codes) {
         uint32_t* tops = reinterpret_cast<uint32_t*>(all);
-        save_tile<F>([&](int x, int y, int q) { return four_gate<F>(acc, x, y, q); }, tops, saved, first, rows, col, cols);
-        save_tile<F>([&](int x, int y, int q) { return four_up<F>(acc, x, y, q); }, tops, saved, M + first, rows, col, cols);
+        // (with F == 1 a wave's 16 columns may be all there and its neighbour's not: both take the same branch, for the barriers)
+        const int left = F == 1 ? cols + (col & 16) - 16 : cols;
+        if (left >= 16 * F) {
+            save_tile<F, true>(gate, tops, saved, first, rows, col, cols);
+            save_tile<F, true>(up, tops, saved, M + first, rows, col, cols);
+        } else {
+            save_tile<F, false>(gate, tops, saved, first, rows, col, cols);
+            save_tile<F, false>(up, tops, saved, M + first, rows, col, cols);
+        }
     }
     auto sums = [&](int x, int y, int q) {
-        const f32x4 g = four_gate<F>(acc, x, y, q), u = four_up<F>(acc, x, y, q);
+        const f32x4 g = gate(x, y, q), u = up(x, y, q);
         f32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act_value(act, g[i]) * u[i];
+        for (int i = 0; i < 4; ++i) v[i] = act_value<ACT>(act, g[i]) * u[i];
         return v;
     };
     if (type == APB_F32) store_tile_as<APB_F32, F, true>(sums, lds, out, first, ld, rows, col, cols);
@@ -120,13 +137,14 @@ __device__ __forceinline__ void store_gated(const f32x16 (&acc)[F][F], uint32_t 
 // rows meet every bank once.  Lane (r, h) holds 32 values of row r: step s multiplies blocks s (h = 0) and 2 + s (h = 1) of the
 // half segment.  Rows of B go in the first operand: a lane then holds four neighbours of a row of Y.
 //
-// GATED: both projections of a gated block.  Of the 32 * F rows of B that a wave multiplies, the first half are the gate's, the second
+// ACT, if not -1, is an apb_activation: both projections of a gated block.  Of the 32 * F rows of B that a wave multiplies, the first half are the gate's, the second
 // the up projection's for the same 16 * F columns of Y, so a lane holds both factors of each of its outputs; N counts the columns
 // of Y, the tile has 32 * F of them.  `saved`: where G and U go in 8 bits, if anywhere.
-template <int F, bool GATED>
+template <int F, int ACT>
 __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx B, const int32_t* __restrict__ offsets, int E, int N,
                                                                        int tiles_n, int type, void* __restrict__ Y, long long ldy,
                                                                        Act act, Mx8 saved) {
+    constexpr bool GATED = ACT >= 0;
     constexpr int kRows = 64 * F;                                // of either operand
     constexpr int kCols = GATED ? kRows / 2 : kRows;             // of the tile
     constexpr int kLoads = 2 * kRows / 16 / 4;                   // instructions of a wave that fetch a pass's codes
@@ -278,21 +296,21 @@ __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx 
     arrived<0>();                                                // (nothing is under way to LDS any more)
     static_assert(4 * kTileLds<F> <= kRing * kStage, "a wave's tile passes through its share of the ring");
     if constexpr (GATED) {
-        store_gated<F>(acc, lds0 + wave * kTileLds<F>, lds, Y, type, t.row0 + wm, ldy, min(32 * F, t.rows - wm), n0 + wn / 2, N - n0 - wn / 2,
+        store_gated<F, ACT>(acc, lds0 + wave * kTileLds<F>, lds, Y, type, t.row0 + wm, ldy, min(32 * F, t.rows - wm), n0 + wn / 2, N - n0 - wn / 2,
                        act, saved, A.rows);
     } else {
         store_tile<F>(acc, lds0 + wave * kTileLds<F>, Y, type, t.row0 + wm, ldy, min(32 * F, t.rows - wm), n0 + wn, N - n0 - wn);
     }
 }
 
-template <int F, bool GATED>
+template <int F, int ACT>
 void launch_tiles(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int type, void* Y, long long ldy, const Act& act,
                   const Mx8& saved, hipStream_t s) {
-    constexpr int kCols = GATED ? 32 * F : 64 * F;
+    constexpr int kCols = ACT >= 0 ? 32 * F : 64 * F;
     const long long tiles_m = (max_row_tiles(M, E, offsets != nullptr, 64 * F) + 3) / 4 * 4;
     const int tiles_n = (N + kCols - 1) / kCols;
     const unsigned blocks = (unsigned)((tiles_m * tiles_n + 127) / 128 * 128);
-    hipLaunchKernelGGL((k_mx4_gemm<F, GATED>), dim3(blocks), dim3(kThreads), 0, s, A, B, offsets, E, N, tiles_n, type, Y, ldy, act, saved);
+    hipLaunchKernelGGL((k_mx4_gemm<F, ACT>), dim3(blocks), dim3(kThreads), 0, s, A, B, offsets, E, N, tiles_n, type, Y, ldy, act, saved);
 }
 
 int launch_mx4_gated(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int activation, int type, void* Y,
@@ -300,9 +318,15 @@ int launch_mx4_gated(const Mx& A, const Mx& B, const int32_t* offsets, int E, in
     const int side = mx4_product_side(M, 2 * N);
     const Act act = act_of(activation);
     const Mx8 keep = mx8_view(saved, 2LL * M, N);
-    if (side == 256) launch_tiles<4, true>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
-    else if (side == 128) launch_tiles<2, true>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
-    else launch_tiles<1, true>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
+    auto with = [&](auto kind) {
+        constexpr int kAct = decltype(kind)::value;
+        if (side == 256) launch_tiles<4, kAct>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
+        else if (side == 128) launch_tiles<2, kAct>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
+        else launch_tiles<1, kAct>(A, B, offsets, E, M, N, type, Y, ldy, act, keep, s);
+    };
+    if (activation == APB_SILU) with(std::integral_constant<int, APB_SILU>{});
+    else if (activation == APB_GELU) with(std::integral_constant<int, APB_GELU>{});
+    else with(std::integral_constant<int, APB_RELU>{});
     APB_HIP(hipGetLastError());
     return APB_OK;
 }
@@ -319,9 +343,9 @@ int launch_mx4_gemm(const Mx& A, const Mx& B, const int32_t* offsets, int E, int
     const int side = mx4_product_side(M, N);
     const Act none = {};
     const Mx8 nowhere = {};
-    if (side == 256) launch_tiles<4, false>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
-    else if (side == 128) launch_tiles<2, false>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
-    else launch_tiles<1, false>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
+    if (side == 256) launch_tiles<4, -1>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
+    else if (side == 128) launch_tiles<2, -1>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
+    else launch_tiles<1, -1>(A, B, offsets, E, M, N, type, Y, ldy, none, nowhere, s);
     APB_HIP(hipGetLastError());
     return APB_OK;
 }

@@ -34,15 +34,16 @@ __device__ __forceinline__ uint32_t scale8_code(uint32_t top) {
 // 2^-e (a normal number for every code that is not NaN's: 0 .. 248)
 __device__ __forceinline__ float scale8_inverse(uint32_t code) { return __builtin_bit_cast(float, (254u - code) << 23); }
 
-// Four values to four whole numbers in a word.  Multiplying by 2^-e is exact where the product is not far below 1/2.
+// Four values to four whole numbers in a word.  x * 2^-e, exact unless it is far below 1/2, is rounded once, to nearest even, where
+// it is added to 3 * 2^22; the whole number then is in the low bits.
 __device__ __forceinline__ uint32_t encode8_four(const float* v, float inverse, bool nan) {
-    uint32_t w = 0;
+    constexpr float kWhole = 12582912.0f;
+    uint32_t i[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int i = (int)fminf(fmaxf(__builtin_rintf(v[q] * inverse), -127.0f), 127.0f);
-        w |= ((uint32_t)i & 255u) << (8 * q);
-    }
-    return nan ? 0u : w;
+    for (int q = 0; q < 4; ++q)
+        i[q] = float_bits(__builtin_amdgcn_fmed3f(__builtin_fmaf(v[q], inverse, kWhole), kWhole - 127.0f, kWhole + 127.0f));
+    const uint32_t lo = __builtin_amdgcn_perm(i[1], i[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(i[3], i[2], 0x04000c0cu);
+    return nan ? 0u : lo | hi;
 }
 __device__ __forceinline__ float decode8(uint32_t w, int q, float scale) { return (float)(int8_t)(w >> (8 * q)) * scale; }
 
@@ -61,24 +62,33 @@ inline Act act_of(int a) {
     return Act{(float)log2e, 0.0f, a == APB_RELU};
 }
 
+// KIND: an apb_activation, or -1 for whichever `k` says.
 // (x^2 is kept finite, for 0 * x^2; a NaN comes back in through x)
 __device__ __forceinline__ float act_square(float x) { return fminf(x * x, 1e37f); }
+template <int KIND = -1>
 __device__ __forceinline__ float act_sigmoid(const Act& k, float x, float square) {
-    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x * __builtin_fmaf(k.c1, square, k.c0)));
+    const float z = KIND == APB_SILU ? k.c0 : __builtin_fmaf(k.c1, square, k.c0);
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x * z));
 }
+// (the limit at -infinity: a finite value times s = 0)
+__device__ __forceinline__ float act_times(float x, float s) { return fmaxf(x, -3.4028235e38f) * s; }
+template <int KIND = -1>
 __device__ __forceinline__ float act_value(const Act& k, float x) {
-    const float s = act_sigmoid(k, x, act_square(x));
-    const float v = s == 0.0f ? 0.0f : x * s;                    // (the limit at -infinity)
-    return k.relu ? (x < 0.0f ? 0.0f : x) : v;
+    const float relu = x < 0.0f ? 0.0f : x;
+    if (KIND == APB_RELU || (KIND < 0 && k.relu)) return relu;
+    return act_times(x, act_sigmoid<KIND>(k, x, KIND == APB_SILU ? 0.0f : act_square(x)));
 }
 __device__ __forceinline__ void act_both(const Act& k, float x, float& value, float& slope) {
+    if (k.relu) {
+        value = x < 0.0f ? 0.0f : x;
+        slope = x > 0.0f ? 1.0f : 0.0f;
+        return;
+    }
     const float sq = act_square(x), s = act_sigmoid(k, x, sq);
-    const float v = s == 0.0f ? 0.0f : x * s;
     // s' = s (1 - s) z'; where s (1 - s) is 0, x may be infinite.  ln(2): the constants are to base 2
     const float p = s * (1.0f - s);
-    const float d = p == 0.0f ? s : __builtin_fmaf(x * p, 0.69314718f * __builtin_fmaf(3.0f * k.c1, sq, k.c0), s);
-    value = k.relu ? (x < 0.0f ? 0.0f : x) : v;
-    slope = k.relu ? (x > 0.0f ? 1.0f : 0.0f) : d;
+    value = act_times(x, s);
+    slope = p == 0.0f ? s : __builtin_fmaf(x * p, 0.69314718f * __builtin_fmaf(3.0f * k.c1, sq, k.c0), s);
 }
 
 }  // namespace apb
