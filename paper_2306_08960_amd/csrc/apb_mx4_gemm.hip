@@ -315,7 +315,7 @@ void launch_tiles(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M
 
 int launch_mx4_gated(const Mx& A, const Mx& B, const int32_t* offsets, int E, int M, int N, int activation, int type, void* Y,
                      long long ldy, void* saved, hipStream_t s) {
-    const int side = mx4_product_side(M, 2 * N);
+    const int side = mx4_gated_side(M, N, E, offsets != nullptr);
     const Act act = act_of(activation);
     const Mx8 keep = mx8_view(saved, 2LL * M, N);
     auto with = [&](auto kind) {

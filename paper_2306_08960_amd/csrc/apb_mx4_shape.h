@@ -37,6 +37,14 @@ inline int mx4_product_side(int M, int N) {
     return big >= 192 ? 256 : big * 4 >= 192 ? 128 : 64;
 }
 
+// The same for both projections of a gated block (N columns of each).  Experts of fewer than 512 rows on average take no tiles of 256:
+// 16 experts of 256 rows, 2 x 2048 x 2048, 37 us with 128 a side and 44 with 256; 64 of 64, 2 x 1024 x 2048, 32 and 47; 64 of 256, rows
+// spread unevenly, 70 and 88; of 512 rows, 2 x 2048 x 2048 on 4 experts, 23 and 22, 2 x 4096 x 2048 on 16 unevenly, 128 and 120.
+inline int mx4_gated_side(int M, int N, int E, bool grouped) {
+    const int side = mx4_product_side(M, 2 * N);
+    return grouped && M / E < 512 ? std::min(side, 128) : side;
+}
+
 constexpr int kMx4Pass = 64;                  // rows of the 4-bit matrix that a pass of the gradients sums over
 constexpr int kMx4MaxSlices = 32;
 
