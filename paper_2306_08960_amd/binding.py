@@ -947,8 +947,7 @@ def alloc_mx8(rows: int, K: int, device=None) -> torch.Tensor:
     nbytes = apb_mx8_bytes(rows, K)
     if nbytes == 0:
         raise ApbError(APB_ERR_SHAPE, "apb_mx8_bytes")
-    dev = device if device is not None else torch.device("cuda", torch.cuda.current_device())
-    return torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda" if device is None else device)
 
 
 def _mx8_ptr(mx8: Optional[torch.Tensor], rows: int, K: int, name: str) -> Optional[int]:

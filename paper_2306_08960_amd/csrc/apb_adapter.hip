@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
+constexpr int kList = 1024;                    // rows of an adapter whose numbers a workgroup of the gradient holds at a time
 constexpr int kUpRows = 64;                    // of a workgroup that streams them past B, at most
 constexpr int kMaxParts = APB_ADAPTER_MAX_PARTS;
 constexpr int kCols = 128;                    // of a wave, in up and gradient: eight to a lane
@@ -206,8 +207,8 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_down(const void* __re
 }
 
 // N values of T from `from` on, `step` apart, its parts added up in order: loads that do not wait for one another.
-template <int N>
-__device__ __forceinline__ void sum_parts(const float* __restrict__ from, const int (&at)[N], int parts, size_t pitch, float (&v)[N]) {
+template <int N, class INDEX>
+__device__ __forceinline__ void sum_parts(const float* __restrict__ from, const INDEX (&at)[N], int parts, size_t pitch, float (&v)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = from[at[e]];
     for (int p = 1; p < parts; p += 2) {
@@ -563,30 +564,27 @@ struct Rows32<APB_MX8> {
     u32x2 v[8];
     uint8_t scale[8];
 };
-// (fewer than eight columns: one by one)
+// `rows`: the numbers of the 32 rows.  (Fewer than eight columns: one by one.)
 template <int XT, bool WHOLE>
-__device__ __forceinline__ void load_rows(Rows32<XT>& x, const void* X, long long ldx, const Mx8& x8, int m, int end, int g, int c, int K) {
-    auto row = [&](int e) { return (long long)min(m + (XT == APB_F32 ? 4 * e + g : 8 * g + e), end - 1); };
+__device__ __forceinline__ void load_rows(Rows32<XT>& x, const void* X, long long ldx, const Mx8& x8, const int* rows, int g, int c, int K) {
+    long long row[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) row[e] = rows[XT == APB_F32 ? 4 * e + g : 8 * g + e];
     if constexpr (XT == APB_MX8) {
         const int at = min(c, x8.blocks * kMx8Block - 8);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            x.v[e] = *reinterpret_cast<const u32x2*>(x8.codes + row(e) * x8.blocks * kMx8Block + at);
-            x.scale[e] = x8.scales[row(e) * x8.blocks + at / kMx8Block];
+            x.v[e] = *reinterpret_cast<const u32x2*>(x8.codes + row[e] * x8.blocks * kMx8Block + at);
+            x.scale[e] = x8.scales[row[e] * x8.blocks + at / kMx8Block];
         }
     } else {
         constexpr int kAs = XT == APB_F32 ? APB_F32 : APB_BF16;
         if (WHOLE || K >= 8) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x.v[e] = load_row<kAs, WHOLE>(X, row(e) * ldx, c, K);
+            for (int e = 0; e < 8; ++e) x.v[e] = load_row<kAs, WHOLE>(X, row[e] * ldx, c, K);
         } else {
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-                const Eight<kAs> v = load_some<kAs>(X, row(e) * ldx + c, K - c);
 #pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    if (u == e) x.v[u] = v;
-            }
+            for (int e = 0; e < 8; ++e) x.v[e] = load_some<kAs>(X, row[e] * ldx + c, K - c);
         }
     }
 }
@@ -629,7 +627,7 @@ __device__ __forceinline__ void column(const Rows32<XT>& x, int n, Eight<APB_BF1
 }
 
 // A workgroup takes one adapter, 16 * JT ranks, kCols columns a wave, and `each` of the adapter's rows, counted through all of its
-// segments, 32 rows of a segment at a time: while one such chunk is multiplied, the next one's X comes to registers, where it is
+// segments, whose numbers it lists in LDS, and of these 32 at a time: while one such chunk is multiplied, the next one's X comes to registers, where it is
 // transposed, and T, its parts added up, on its way to LDS, where it is in three bfloat16 operands of eight rows, or in float32 for
 // an X of float32.
 template <int XT, int JT>
@@ -642,6 +640,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gradient(const float* __re
     constexpr int kStageBytes = ((kWide ? kChunk * kPitch : 3 * kRanks * kPitch) + 15) / 16 * 16;
     static_assert(kRanks * kChunk / 8 <= kThreads, "a thread brings eight values of T");
     __shared__ __align__(16) uint8_t lds[2 * kStageBytes];
+    __shared__ int list[kList + kChunk];
     const int a = blockIdx.y / rank_tiles, j0 = blockIdx.y % rank_tiles * kRanks;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
     const int c0 = (blockIdx.x * kWaves + wave) * kCols, c = c0 + 8 * i;
@@ -656,106 +655,107 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gradient(const float* __re
 #pragma unroll
         for (int q = 0; q < 8; ++q) acc[j][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // the chunks, one after another: rows m .. min(m + 32, end) - 1
-    int base = -kWave, before = 0, m = 0, end = 0;
-    unsigned long long left = 0;
-    auto advance = [&]() {
-        m += kChunk;
-        while (m >= end) {
-            while (!left) {
-                base += kWave;
-                if (base >= seg.S || before >= hi) return false;
+    // the numbers of the adapter's rows start .. start + count - 1; behind them the last one again, up to a whole chunk
+    auto list_rows = [&](int start, int rows) {
+        if (wave == 0) {
+            int before = 0;
+            for (int base = 0; base < seg.S && before < start + rows; base += kWave) {
                 if (seg.S > kWave) its = rows_of(seg, base + lane, first, count);
-                left = __ballot(its == a && count > 0);
+                for (unsigned long long left = __ballot(its == a && count > 0); left; left &= left - 1) {
+                    const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)left) - 1);
+                    const int from = __builtin_amdgcn_readlane(first, src), n = __builtin_amdgcn_readlane(count, src);
+                    const int skip = max(start - before, 0), end = min(n, start + rows - before);
+                    for (int k = skip + lane; k < end; k += kWave) list[before + k - start] = from + k;
+                    if (before + n >= start + rows && lane < kChunk && end > skip) list[rows + lane] = from + end - 1;
+                    before += n;
+                    if (before >= start + rows) break;
+                }
             }
-            const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)left) - 1);
-            const int from = __builtin_amdgcn_readlane(first, src), rows = __builtin_amdgcn_readlane(count, src);
-            left &= left - 1;
-            m = from + max(lo - before, 0);
-            end = from + min(rows, hi - before);
-            before += rows;
         }
-        return true;
+        __syncthreads();
     };
     const int tj = threadIdx.x % kRanks, octet = threadIdx.x / kRanks;
     const bool brings = octet < kChunk / 8;
     Rows32<XT> x;
     float tv[8];
-    auto fetch = [&](auto all) {
-        if (there) load_rows<XT, decltype(all)::value>(x, X, ldx, x8, m, end, g, c, K);
+    auto fetch = [&](int m, auto all) {
+        if (there) load_rows<XT, decltype(all)::value>(x, X, ldx, x8, list + m, g, c, K);
         if (brings) {
             // (rows and ranks that are not there repeat the last ones, and are cleared)
-            int at[8];
+            size_t at[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) at[e] = min(8 * octet + e, end - 1 - m) * r + min(j0 + tj, r - 1);
-            sum_parts<8>(T + (size_t)m * r, at, parts, (size_t)seg.M * r, tv);
+            for (int e = 0; e < 8; ++e) at[e] = (size_t)list[m + 8 * octet + e] * r + min(j0 + tj, r - 1);
+            sum_parts<8>(T, at, parts, (size_t)seg.M * r, tv);
         }
     };
     auto multiply = [&](auto all) {
-        bool more = advance();
-        if (more) fetch(all);
         uint32_t stage = 0;
-        while (more) {
-            const int rows = min(end - m, kChunk);
-            uint8_t* to = lds + stage;
-            stage = kStageBytes - stage;
-            if (brings) {
+        for (int start = lo; start < hi; start += kList) {
+            const int rows_listed = min(hi - start, kList);
+            list_rows(start, rows_listed);
+            fetch(0, all);
+            for (int m = 0; m < rows_listed; m += kChunk) {
+                const int rows = min(rows_listed - m, kChunk);
+                uint8_t* to = lds + stage;
+                stage = kStageBytes - stage;
+                if (brings) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) tv[e] = 8 * octet + e < rows && j0 + tj < r ? tv[e] : 0.0f;
+                    for (int e = 0; e < 8; ++e) tv[e] = 8 * octet + e < rows && j0 + tj < r ? tv[e] : 0.0f;
+                    if constexpr (kWide) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) *reinterpret_cast<float*>(to + (8 * octet + e) * kPitch + 4 * tj) = tv[e];
+                    } else {
+                        Eight<APB_BF16> part[3];
+                        bf16_parts<3>(tv, part);
+#pragma unroll
+                        for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(to + (p * kRanks + tj) * kPitch + 16 * octet) = part[p].w[0];
+                    }
+                }
+                Rows32<XT> now = x;
+                if (m + kChunk < rows_listed) fetch(m + kChunk, all);
+                __syncthreads();                                         // (of the other stage, everybody has read by the time they are here)
+                if (!there) continue;
+                if constexpr (XT != APB_MX8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) now.v[e] = settle<XT == APB_F32 ? APB_F32 : APB_BF16, decltype(all)::value>(now.v[e], c, K);
+                if (rows < kChunk) clear_rows<XT>(now, rows, g);
                 if constexpr (kWide) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) *reinterpret_cast<float*>(to + (8 * octet + e) * kPitch + 4 * tj) = tv[e];
-                } else {
-                    Eight<APB_BF16> part[3];
-                    bf16_parts<3>(tv, part);
+                    for (int e = 0; e < 8; ++e) {
+                        float v[8];
+                        floats(now.v[e], v);
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(to + (p * kRanks + tj) * kPitch + 16 * octet) = part[p].w[0];
-                }
-            }
-            Rows32<XT> now = x;
-            more = advance();
-            if (more) fetch(all);
-            __syncthreads();                                         // (of the other stage, everybody has read by the time they are here)
-            if (!there) continue;
-            if constexpr (XT != APB_MX8)
+                        for (int j = 0; j < JT; ++j) {
+                            const float t = *reinterpret_cast<const float*>(to + (4 * e + g) * kPitch + 4 * (16 * j + i));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) now.v[e] = settle<XT == APB_F32 ? APB_F32 : APB_BF16, decltype(all)::value>(now.v[e], c, K);
-            if (rows < kChunk) clear_rows<XT>(now, rows, g);
-            if constexpr (kWide) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float v[8];
-                    floats(now.v[e], v);
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) {
-                        const float t = *reinterpret_cast<const float*>(to + (4 * e + g) * kPitch + 4 * (16 * j + i));
-#pragma unroll
-                        for (int n = 0; n < 8; ++n) acc[j][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(t, v[n], acc[j][n], 0, 0, 0);
-                    }
-                }
-            } else {
-                Eight<APB_BF16> t[JT][3];
-#pragma unroll
-                for (int j = 0; j < JT; ++j)
-#pragma unroll
-                    for (int p = 0; p < 3; ++p)
-                        t[j][p].w[0] = *reinterpret_cast<const u32x4*>(to + (p * kRanks + 16 * j + i) * kPitch + 16 * g);
-#pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    Eight<APB_BF16> xv[kXParts<XT>];
-                    column<XT>(now, n, xv);
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) {
-                        // (the smallest first; the third part of T times the second of X is below 2^-24)
-                        if constexpr (kXParts<XT> == 2) {
-                            acc[j][n] = multiply8<APB_BF16>(t[j][1], xv[1], acc[j][n]);
-                            acc[j][n] = multiply8<APB_BF16>(t[j][0], xv[1], acc[j][n]);
+                            for (int n = 0; n < 8; ++n) acc[j][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(t, v[n], acc[j][n], 0, 0, 0);
                         }
+                    }
+                } else {
+                    Eight<APB_BF16> t[JT][3];
 #pragma unroll
-                        for (int p = 2; p >= 0; --p) acc[j][n] = multiply8<APB_BF16>(t[j][p], xv[0], acc[j][n]);
+                    for (int j = 0; j < JT; ++j)
+#pragma unroll
+                        for (int p = 0; p < 3; ++p)
+                            t[j][p].w[0] = *reinterpret_cast<const u32x4*>(to + (p * kRanks + 16 * j + i) * kPitch + 16 * g);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        Eight<APB_BF16> xv[kXParts<XT>];
+                        column<XT>(now, n, xv);
+#pragma unroll
+                        for (int j = 0; j < JT; ++j) {
+                            // (the smallest first; the third part of T times the second of X is below 2^-24)
+                            if constexpr (kXParts<XT> == 2) {
+                                acc[j][n] = multiply8<APB_BF16>(t[j][1], xv[1], acc[j][n]);
+                                acc[j][n] = multiply8<APB_BF16>(t[j][0], xv[1], acc[j][n]);
+                            }
+#pragma unroll
+                            for (int p = 2; p >= 0; --p) acc[j][n] = multiply8<APB_BF16>(t[j][p], xv[0], acc[j][n]);
+                        }
                     }
                 }
             }
+            if (start + kList < hi) __syncthreads();                     // (the list has been read)
         }
     };
     if (whole) multiply(std::true_type{});

@@ -73,6 +73,7 @@ CASES = [
     (1, 1, 1, 1, 1, "all"), (1, 4096, 4096, 16, 3, "all"), (1, 1000, 517, 5, 2, "tokens"), (64, 4096, 600, 16, 8, "tokens"),
     (33, 517, 1000, 3, 2, "mixed"), (100, 300, 130, 17, 4, "mixed"), (40, 64, 512, 33, 5, "own"), (16, 70, 31, 64, 2, "mixed"),
     (333, 517, 1000, 16, 2, "mixed"), (900, 1000, 515, 8, 3, "own"), (700, 2048, 1100, 32, 1, "all"), (1500, 300, 260, 64, 3, "mixed"),
+    (2600, 40, 24, 4, 1, "all"), (4096, 16, 40, 3, 7, "tokens"), (3000, 5, 6, 18, 2, "mixed"),
     (400, 200, 140, 100, 2, "mixed"), (300, 96, 520, 256, 2, "all"), (2000, 130, 70, 20, 9, "many"), (8, 9000, 100, 130, 4, "tokens"),
 ]
 
