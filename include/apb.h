@@ -476,7 +476,7 @@ int apb_mx4_gated_linear(const void* X, int x_type, long long ldx, int rows_in, 
                          void* Y, long long ldy, void* saved, void* stream);
 
 /* From G and U at hand (M rows of 2N elements, [G | U], ldgu >= 2N apart), as a program has them that adds something to the
- * projections first, such as adapters.  Y and GU are of `type`. */
+ * projections first, such as adapters.  Y and GU are of `type` and do not overlap. */
 int apb_gated_forward(const void* GU, int type, long long ldgu, int M, int N, int activation, void* Y, long long ldy,
                       void* saved, void* stream);
 /*      dG = dY * U * act'(G),  dU = dY * act(G)             (act'(0) = 0 for APB_RELU)
@@ -484,7 +484,8 @@ int apb_gated_forward(const void* GU, int type, long long ldgu, int M, int N, in
  *   dY      DEVICE, M rows of N elements of `type`.
  *   dGU     DEVICE, M rows of 2N elements of `type`, [dG | dU], lddgu >= 2N apart, fully overwritten.
  *   Y       NULL, or DEVICE, M rows of N elements of `type`: act(G) * U over again, so that a program need not keep it.
- *   The outputs overlap nothing that is read, but dGU may be GU itself if it has the same type and row stride. */
+ *   dGU may be GU itself if it has the same type and row stride (APB_ERR_SHAPE if not); otherwise the outputs overlap nothing
+ *   that is read. */
 int apb_gated_backward(const void* GU, int gu_type, long long ldgu, const void* dY, int type, long long lddy, int M, int N,
                        int activation, void* dGU, long long lddgu, void* Y, long long ldy, void* stream);
 

@@ -186,7 +186,9 @@ int apb_gated_backward(const void* GU, int gu_type, long long ldgu, const void* 
     if (!GU || !dY || !dGU) return APB_ERR_NULL;
     if ((bad_type(gu_type) && gu_type != APB_MX8) || bad_type(type)) return APB_ERR_TYPE;
     if (bad_activation(activation)) return APB_ERR_VALUE;
-    if (bad_shape_mx8(2LL * M, N) || (gu_type != APB_MX8 && ldgu < 2LL * N) || lddy < N || lddgu < 2LL * N || (Y && ldy < N)) return APB_ERR_SHAPE;
+    if (bad_shape_mx8(2LL * M, N) || (gu_type != APB_MX8 && ldgu < 2LL * N) || lddy < N || lddgu < 2LL * N || (Y && ldy < N) ||
+        (GU == dGU && (gu_type != type || ldgu != lddgu)))
+        return APB_ERR_SHAPE;
     if (!aligned(GU, gu_type == APB_MX8 ? 16 : type_size(gu_type)) || !aligned(dY, type_size(type)) || !aligned(dGU, type_size(type)) ||
         !aligned(Y, type_size(type)))
         return APB_ERR_ALIGN;

@@ -90,7 +90,7 @@ def b():
     return binding
 
 
-P, ODD = ctypes.c_void_p(1 << 20), ctypes.c_void_p((1 << 20) + 2)     # never followed: every call fails before
+P, Q, ODD = ctypes.c_void_p(1 << 20), ctypes.c_void_p(1 << 21), ctypes.c_void_p((1 << 20) + 2)     # never followed: every call fails before
 
 
 def test_mx8_bytes(b):
@@ -149,7 +149,7 @@ def test_gated_activation_refusals(b):
     def forward(GU=P, t=1, ldgu=80, M=8, N=40, act=0, Y=P, ld=40, saved=None):
         return lib.apb_gated_forward(GU, t, ldgu, M, N, act, Y, ld, saved, None)
 
-    def backward(GU=P, gt=1, ldgu=80, dY=P, t=1, lddy=40, M=8, N=40, act=0, dGU=P, lddgu=80, Y=None, ld=40):
+    def backward(GU=P, gt=1, ldgu=80, dY=P, t=1, lddy=40, M=8, N=40, act=0, dGU=Q, lddgu=80, Y=None, ld=40):
         return lib.apb_gated_backward(GU, gt, ldgu, dY, t, lddy, M, N, act, dGU, lddgu, Y, ld, None)
 
     for f in (forward, backward):
@@ -161,6 +161,8 @@ def test_gated_activation_refusals(b):
     assert backward(dY=None) == b.APB_ERR_NULL and backward(dGU=None) == b.APB_ERR_NULL and backward(gt=4) == b.APB_ERR_TYPE
     assert backward(lddy=39) == b.APB_ERR_SHAPE and backward(lddgu=79) == b.APB_ERR_SHAPE
     assert backward(GU=ODD, gt=3) == b.APB_ERR_ALIGN and backward(GU=ODD, gt=0) == b.APB_ERR_ALIGN
+    assert backward(dGU=P, gt=3) == b.APB_ERR_SHAPE and backward(dGU=P, gt=2) == b.APB_ERR_SHAPE      # (GU itself)
+    assert backward(dGU=P, lddgu=96) == b.APB_ERR_SHAPE
     assert backward(dY=ODD, t=0) == b.APB_ERR_ALIGN and backward(dGU=ODD, t=0) == b.APB_ERR_ALIGN
 
 

@@ -189,6 +189,31 @@ def test_values_outside_stay_outside(b):
     assert rows.nonzero().flatten().tolist() == [3]
 
 
+def test_rows_beyond_32_bits(b):
+    """X and Y of more than 2^32 bytes and 2^31 elements: the last segment, its gradients too, against the oracle."""
+    M, K, r, L, tail = 70000, 32000, 8, 2, 300
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    x[:1000] = 1.0
+    x[M - tail:] = torch.randn(tail, K, generator=g, device="cuda").bfloat16()
+    A = (torch.randn(L, r, K, generator=g, device="cuda") * K ** -0.5).bfloat16()
+    seg = dict(offsets=torch.tensor([0, M - tail, M], dtype=torch.int32).cuda(), adapter=torch.tensor([0, 1], dtype=torch.int32).cuda())
+    T = b.apb_adapter_down(x, A, **seg)
+    xv, Av = _np(x[M - tail:]), _np(A)
+    which = np.ones(tail, int)
+    want, mag = o.down(xv, Av, which)
+    _check(_np(T).sum(0)[M - tail:], want, _sum(K) * mag, "f32")
+    Tv = _np(T).sum(0)[M - tail:]
+    y = b.apb_adapter_up(T, A, Y0=x, **seg)
+    _check(_np(y[M - tail:]), xv + o.up(Tv, Av, which), (_sum(r) + PARTS["bf16"]) * o.up(np.abs(Tv), np.abs(Av), which) + 2.0 ** -23 * np.abs(xv), "bf16")
+    del y
+    dA = b.apb_adapter_gradient(T, x, L, **seg)
+    x8 = b.apb_mx8_quantize(x)
+    d8 = b.apb_adapter_gradient(T, x8, L, K=K, **seg)
+    for got, v in ((dA, xv), (d8, o.values8(*o.quantize8(xv.astype(np.float32)), K))):
+        _check(_np(got[1]), o.gradient(Tv, v, which, L)[1], _sum(tail) * o.gradient(np.abs(Tv), np.abs(v), which, L)[1], "f32")
+
+
 def test_odd_offsets_are_survived(b):
     """Offsets that the documentation leaves without a result: nothing is read or written out of range."""
     M, K, N, r, L = 64, 96, 80, 4, 2

@@ -219,7 +219,7 @@ def _check_saved(saved, gu, mag, K, M, N, inside):
 
 
 # few rows (16 and fewer, short K), every tile size plain and in groups, ragged in every direction; the sides are the product's for 2N
-PRODUCTS = [(1, 1, 1, 0), (1, 17, 300, 0), (16, 33, 256, 0), (16, 4100, 4096, 0), (7, 1000, 9000, 0), (17, 15, 31, 0), (130, 150, 520, 0),
+PRODUCTS = [(1, 1, 1, 0), (16, 130, 8193, 0), (1, 17, 300, 0), (16, 33, 256, 0), (16, 4100, 4096, 0), (7, 1000, 9000, 0), (17, 15, 31, 0), (130, 150, 520, 0),
             (64, 32, 257, 0), (200, 47, 1300, 3), (1700, 1025, 300, 0), (1540, 901, 40, 0), (1700, 1025, 1300, 5),
             (3400, 1801, 520, 0), (3330, 1825, 33, 0), (3400, 1801, 777, 4)]
 
@@ -292,6 +292,27 @@ def test_gated_blocks_of_nan_and_zero(b):
     assert np.isnan(back[M:, :32]).all()
     few = b.apb_mx4_gated_linear(torch.from_numpy(x[:10]).cuda(), w4, N).cpu().numpy()
     assert np.array_equal(np.isnan(few), want[:10])
+
+
+def test_rows_beyond_32_bits(b):
+    """Matrices of more than 2^32 bytes and 2^31 elements: their last rows against the same rows by themselves, to the bit."""
+    M, N = 70000, 16000
+    gu = torch.empty(M, 2 * N, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for at in range(0, M, 10000):
+        gu[at:at + 10000] = torch.randn(10000, 2 * N, generator=g, device="cuda").bfloat16()
+    dy = gu[:, :N].contiguous()
+    saved = b.alloc_mx8(2 * M, N)
+    y = b.apb_gated_forward(gu, "silu", saved=saved)
+    dgu = b.apb_gated_backward(saved, dy, "silu")
+    tail = slice(M - 50, M)
+    few = b.alloc_mx8(100, N)
+    assert torch.equal(y[tail], b.apb_gated_forward(gu[tail], "silu", saved=few))
+    assert torch.equal(dgu[tail], b.apb_gated_backward(few, dy[tail], "silu"))
+    del y, dgu, dy
+    x8 = b.apb_mx8_quantize(gu)
+    back = b.apb_mx8_dequantize(x8, M, 2 * N, torch.bfloat16)
+    assert torch.equal(back[tail], b.apb_mx8_dequantize(b.apb_mx8_quantize(gu[tail]), 50, 2 * N, torch.bfloat16))
 
 
 def test_gated_refusals(b):
