@@ -96,7 +96,7 @@ __device__ __forceinline__ f32x4 multiply8(const Eight<TYPE>& a, const Eight<TYP
 // next lines are under way while these are multiplied.  In LDS the eight 16-byte pieces of a line are permuted by the row's number, so
 // that eight lanes reading the same piece of eight rows meet every bank once.
 template <int RT, int JT>
-constexpr int kDownWaves = RT + JT <= 2 ? 16 : RT + JT <= 4 ? 8 : 4;
+constexpr int kDownWaves = RT + JT <= 4 ? 16 : 8;
 template <int TYPE, int RT, int JT, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void k_adapter_down(const void* __restrict__ X, long long ldx, const void* __restrict__ A,
                                                                 Segments seg, const float* __restrict__ scale, int K, int r, int lines_each,
