@@ -836,16 +836,20 @@ int up_rows(int S, int M, int N) {
     return rows;
 }
 
-// Rows of an adapter to a workgroup of its gradient: as many workgroups as fill the chip twice, were the rows spread evenly, but no
-// more than 16384 that may find none.
+// Rows of an adapter to a workgroup of its gradient: so many that a workgroup comes to each compute unit, were they spread evenly, but at
+// least 128, and no more than 16384 workgroups that may find none.  4100 rows of 4096, rank 16, four adapters (us): 512 workgroups 21.5,
+// 256 16.0, 128 18.9; 8196 rows, rank 64: 55, 43, 48.  Up to 256 rows are never shared: joining takes 4 us and another launch.
 int gradient_rows(int L, int M, int K, int r) {
     const int ranks = 16 * rank_groups(r);
     const long long columns = (long long)((K + kCols * kWaves - 1) / (kCols * kWaves)) * ((r + ranks - 1) / ranks);
     const long long rows = std::max<long long>(M * columns / 256, M * columns * L / 16384);
-    return (int)std::min<long long>(1 << 24, std::max<long long>(128, (rows + 63) / 64 * 64));
+    return M <= 256 ? 256 : (int)std::min<long long>(1 << 24, std::max<long long>(128, (rows + 63) / 64 * 64));
 }
 
-// Groups of rows and of ranks to a workgroup of down, and parts of K.
+// Groups of rows and of ranks to a workgroup of down, and parts of K: what takes least by a count of the bytes that the busiest compute
+// unit brings (40 GB/s each), a quarter of a microsecond for each part that the readers of T will add up, and parts only where T stays
+// small.  Measured (us; groups of rows, of ranks, parts): one row of 4096, rank 16: 1 1 1 5.8, 1 1 4 4.3, 1 1 8 4.1; 512 rows, rank 16:
+// 1 1 1 10.0, 1 1 4 4.7; 4100 rows, rank 16: 1 1 1 12.2, 2 1 1 11.6; 8196 rows, rank 64: 1 1 1 68, 2 2 1 34, 4 4 1 25.
 struct DownPlan {
     int rt, jt, parts;
 };
