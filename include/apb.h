@@ -463,12 +463,12 @@ int apb_mx8_dequantize(const void* mx8, int rows, int K, int type, void* X, long
 enum apb_activation { APB_SILU = 0, APB_GELU = 1, APB_RELU = 2 };
 
 /* Both projections of a 4-bit A (M rows of K), the activation and the product as one kernel.  offsets, E, Y as in
- * apb_mx4_gemm; W: 4-bit matrix of E*2N rows; E*2N and M as apb_mx4_gemm has N and M.  Rows that belong to no expert: Y = 0
- * and zeros in `saved`. */
+ * apb_mx4_gemm; W: 4-bit matrix of E*2N rows, within apb_mx4_gemm's limits for 2N columns; N <= 2^22.  Rows that belong to no
+ * expert: Y = 0 and zeros in `saved`. */
 int apb_mx4_gated_gemm(const void* A, const void* W, const int32_t* offsets, int E, int M, int N, int K, int activation,
                        int type, void* Y, long long ldy, void* saved, void* stream);
-/* The same from float activations, quantized within the call: as apb_mx4_linear is to apb_mx4_gemm, with few rows as a single
- * kernel unless `saved` is asked for.  scratch: apb_mx4_gated_linear_scratch_bytes() bytes, 0 for the single kernel (not
+/* The same from float activations, quantized within the call: as apb_mx4_linear is to apb_mx4_gemm, few rows or little work as a
+ * single kernel unless `saved` is asked for.  scratch: apb_mx4_gated_linear_scratch_bytes() bytes, 0 for the single kernel (not
  * touched, but not NULL). */
 size_t apb_mx4_gated_linear_scratch_bytes(int grouped, int E, int M, int N, int K, int with_saved);
 int apb_mx4_gated_linear(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const void* W,

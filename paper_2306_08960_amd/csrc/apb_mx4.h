@@ -430,7 +430,7 @@ int launch_mx4_quantize(const void* X, int type, long long row_stride, long long
                         const int32_t* rows_from, int rows, int K, void* mx, hipStream_t s);
 // Few rows: may it run as the one kernel that streams the weights (apb_mx4_few.hip)?
 bool mx4_few_applies(const int32_t* offsets, int E, int M, int K);
-bool mx4_few_gated_applies(const int32_t* offsets, int E, int M, int K);
+bool mx4_few_gated_applies(const int32_t* offsets, int E, int M, int N, int K);
 int launch_mx4_few(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const Mx& W, const int32_t* offsets,
                    int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s);
 int launch_mx4_few(const Mx& A, const Mx& W, const int32_t* offsets, int E, int M, int N, int K, int type, void* Y, long long ldy, hipStream_t s);

@@ -400,13 +400,13 @@ int apb_mx4_gated_gemm(const void* A, const void* W, const int32_t* offsets, int
     if (!aligned(A, 16) || !aligned(W, 16) || !aligned(Y, type_size(type)) || !aligned(offsets, 4) || !aligned(saved, 16)) return APB_ERR_ALIGN;
     const Mx a = mx_view(A, M, K), w = mx_view(W, E * 2 * N, K);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (!saved && mx4_few_gated_applies(offsets, E, M, K)) return launch_mx4_few_gated(a, w, offsets, E, M, N, K, activation, type, Y, ldy, s);
+    if (!saved && mx4_few_gated_applies(offsets, E, M, N, K)) return launch_mx4_few_gated(a, w, offsets, E, M, N, K, activation, type, Y, ldy, s);
     return launch_mx4_gated(a, w, offsets, E, M, N, activation, type, Y, ldy, saved, s);
 }
 
 size_t apb_mx4_gated_linear_scratch_bytes(int grouped, int E, int M, int N, int K, int with_saved) {
     const int32_t some = 0, *offsets = grouped ? &some : nullptr;
-    if (bad_gated(E, M, N, K, offsets) || (!with_saved && mx4_few_gated_applies(offsets, E, M, K))) return 0;
+    if (bad_gated(E, M, N, K, offsets) || (!with_saved && mx4_few_gated_applies(offsets, E, M, N, K))) return 0;
     return apb_mx4_bytes(M, K);
 }
 
@@ -422,7 +422,7 @@ int apb_mx4_gated_linear(const void* X, int x_type, long long ldx, int rows_in, 
         return APB_ERR_ALIGN;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Mx w = mx_view(W, E * 2 * N, K);
-    if (!saved && mx4_few_gated_applies(offsets, E, M, K))
+    if (!saved && mx4_few_gated_applies(offsets, E, M, N, K))
         return launch_mx4_few_gated(X, x_type, ldx, rows_in, rows_from, w, offsets, E, M, N, K, activation, y_type, Y, ldy, s);
     const int rc = launch_mx4_quantize(X, x_type, ldx, 1, rows_in, rows_from, M, K, scratch, s);
     if (rc != APB_OK) return rc;

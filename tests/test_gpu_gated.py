@@ -218,8 +218,8 @@ def _check_saved(saved, gu, mag, K, M, N, inside):
     assert (codes[~rows] == 0).all() and (scales[~rows] == 0).all()
 
 
-# few rows (16 and fewer, short K), every tile size plain and in groups, ragged in every direction; the sides are the product's for 2N
-PRODUCTS = [(1, 1, 1, 0), (16, 130, 8193, 0), (1, 17, 300, 0), (16, 33, 256, 0), (16, 4100, 4096, 0), (7, 1000, 9000, 0), (17, 15, 31, 0), (130, 150, 520, 0),
+# few rows and little work (one kernel), every tile size plain and in groups, ragged in every direction; the sides are the product's for 2N
+PRODUCTS = [(1, 1, 1, 0), (16, 130, 8193, 0), (1, 17, 300, 0), (16, 33, 256, 0), (16, 4100, 4096, 0), (7, 1000, 9000, 0), (17, 15, 31, 0), (130, 150, 520, 0), (300, 700, 2600, 0),
             (64, 32, 257, 0), (200, 47, 1300, 3), (1700, 1025, 300, 0), (1540, 901, 40, 0), (1700, 1025, 1300, 5),
             (3400, 1801, 520, 0), (3330, 1825, 33, 0), (3400, 1801, 777, 4)]
 
@@ -327,7 +327,7 @@ def test_gated_refusals(b):
     with pytest.raises(ValueError):
         b.apb_mx4_gated_linear(x, w4, 40, Y=torch.empty(4, 41, device="cuda"))
     with pytest.raises(ValueError):
-        b.apb_mx4_gated_linear(torch.zeros(100, 64, device="cuda"), w4, 40, scratch=torch.empty(5, dtype=torch.uint8, device="cuda"))
+        b.apb_mx4_gated_linear(torch.zeros(100, 64, device="cuda"), w4, 40, scratch=torch.empty(5, dtype=torch.uint8, device="cuda"), saved=b.alloc_mx8(200, 40))
     with pytest.raises(ValueError):
         b.apb_gated_forward(torch.zeros(4, 7, device="cuda"))
     with pytest.raises(TypeError):
