@@ -944,10 +944,10 @@ def apb_mx8_bytes(rows: int, K: int) -> int:
 
 def alloc_mx8(rows: int, K: int, device=None) -> torch.Tensor:
     """Memory for an 8-bit matrix of `rows` rows of K values (uint8, see the header for the layout)."""
-    nbytes = apb_mx8_bytes(rows, K)
-    if nbytes == 0:
+    blocks = (K + 31) // 32                                           # (apb_mx8_bytes without the call)
+    if rows <= 0 or K <= 0 or K > 1 << 22 or rows * blocks > (1 << 30) - 64:
         raise ApbError(APB_ERR_SHAPE, "apb_mx8_bytes")
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda" if device is None else device)
+    return torch.empty(rows * blocks * 33, dtype=torch.uint8, device="cuda" if device is None else device)
 
 
 def _mx8_ptr(mx8: Optional[torch.Tensor], rows: int, K: int, name: str) -> Optional[int]:

@@ -97,8 +97,11 @@ def test_mx8_bytes(b):
     assert b.apb_mx8_bytes(1, 1) == 33 and b.apb_mx8_bytes(3, 32) == 99 and b.apb_mx8_bytes(3, 33) == 198
     assert b.apb_mx8_bytes(0, 5) == 0 and b.apb_mx8_bytes(5, 0) == 0 and b.apb_mx8_bytes(1, (1 << 22) + 1) == 0
     assert b.apb_mx8_bytes((1 << 30) - 64, 32) == ((1 << 30) - 64) * 33 and b.apb_mx8_bytes((1 << 30) - 63, 32) == 0
-    with pytest.raises(b.ApbError):
-        b.alloc_mx8(0, 4)
+    for rows, K in ((0, 4), (4, 0), (1, (1 << 22) + 1), ((1 << 30) - 63, 32)):
+        with pytest.raises(b.ApbError):
+            b.alloc_mx8(rows, K)
+    for rows, K in ((1, 1), (3, 32), (7, 517), (2, 1 << 22)):
+        assert b.alloc_mx8(rows, K, device="meta").numel() == b.apb_mx8_bytes(rows, K)
 
 
 def test_mx8_refusals(b):
