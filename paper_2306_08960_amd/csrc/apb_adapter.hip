@@ -3,17 +3,16 @@
 // in whole lines and all directions are these three kernels.
 #include <type_traits>
 
+#include "apb_adapter_shape.h"
 #include "apb_mx8.h"
 
 namespace apb {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kWaves = kAdapterWaves;
+static_assert(kThreads == kWaves * kWave, "a workgroup of up and gradient");
 constexpr int kList = 1024;                    // rows of an adapter whose numbers a workgroup of the gradient holds at a time
-constexpr int kUpRows = 64;                    // of a workgroup that streams them past B, at most
-constexpr int kMaxParts = APB_ADAPTER_MAX_PARTS;
-constexpr int kCols = 128;                    // of a wave, in up and gradient: eight to a lane
 constexpr int kStage = 64;                    // ranks of T that are in LDS at a time
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -94,8 +93,6 @@ __device__ __forceinline__ f32x4 multiply8(const Eight<TYPE>& a, const Eight<TYP
 // next lines are under way while these are multiplied.  In LDS the eight 16-byte pieces of a line are permuted by the row's number, so
 // that eight lanes reading the same piece of eight rows meet every bank once.  8196 rows of 4096 in bfloat16: rank 16 16 us, rank 64
 // 25 (67 MB are 13), in the order of the operands 24 and 50.
-template <int RT, int JT>
-constexpr int kDownWaves = RT + JT <= 4 ? 16 : 8;
 template <int TYPE, int RT, int JT, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void k_adapter_down(const void* __restrict__ X, long long ldx, const void* __restrict__ A,
                                                                 Segments seg, const float* __restrict__ scale, int K, int r, int lines_each,
@@ -549,9 +546,6 @@ __device__ __forceinline__ Span span_of(const Segments& seg, int a, int& its, in
     rows = min(__builtin_amdgcn_readfirstlane(rows), seg.M);
     return Span{rows, min(__builtin_amdgcn_readfirstlane(before), seg.M - rows)};
 }
-// Where slice z of an adapter of more than `each` rows leaves its sum: slices of different adapters never meet, as n rows have
-// ceil(n / each) <= floor(2 n / each) slices, and there are at most 2 M / each places.
-__device__ __forceinline__ int place_of_slice(const Span& s, int each, int z) { return (int)(2LL * s.before / each) + z; }
 
 // Rows of X as they are loaded: what a lane has of 32 of them.  16 bits: eight columns of eight rows 8 g ..; float32: eight columns
 // of rows g, g + 4, ...; 8 bits: as 16 bits, and each row's scale.
@@ -762,7 +756,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gradient(const float* __re
     if (WHOLE || whole) multiply(std::true_type{});
     else multiply(std::false_type{});
     if (!there) return;
-    float* out = span.rows > each ? shared + (size_t)place_of_slice(span, each, blockIdx.z) * r * K : dA + (size_t)a * r * K;
+    float* out = span.rows > each ? shared + (size_t)(place_of_slices(span.before, each) + blockIdx.z) * r * K : dA + (size_t)a * r * K;
 #pragma unroll
     for (int j = 0; j < JT; ++j)
 #pragma unroll
@@ -784,7 +778,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restri
     const Span span = span_of(seg, a, its, first, count);
     if (span.rows <= each) return;
     const int slices = (span.rows + each - 1) / each;
-    const float* from = shared + (size_t)place_of_slice(span, each, 0) * n;
+    const float* from = shared + (size_t)place_of_slices(span.before, each) * n;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     __shared__ f32x4 sums[kWaves][kWave];
     // four neighbours to a lane; a wave takes every fourth slice, eight at a time
@@ -827,55 +821,10 @@ bool bad_adapter(int S, int L, int M, int K, int r, const int32_t* offsets, cons
            r > APB_ADAPTER_MAX_R || (!offsets && S != 1) || (!adapter && S != L);
 }
 
-int rank_groups(int r) { return r <= 16 ? 1 : r <= 32 ? 2 : 4; }
-
-// Rows to a workgroup that streams them past its share of B.
-int up_rows(int S, int M, int N) {
-    const long long columns = (N + kCols * kWaves - 1) / (kCols * kWaves);
-    int rows = 16;
-    while (rows < kUpRows && rows < (M + S - 1) / S && M / (2 * rows) * columns >= 1024) rows *= 2;
-    return rows;
-}
-
-// Rows of an adapter to a workgroup of its gradient: so many that a workgroup comes to each compute unit, were they spread evenly, but at
-// least 128, and no more than 16384 workgroups that may find none.  4100 rows of 4096, rank 16, four adapters (us): 512 workgroups 21.5,
-// 256 16.0, 128 18.9; 8196 rows, rank 64: 55, 43, 48.  Up to 256 rows are never shared: joining takes 4 us and another launch.
-int gradient_rows(int L, int M, int K, int r) {
-    const int ranks = 16 * rank_groups(r);
-    const long long columns = (long long)((K + kCols * kWaves - 1) / (kCols * kWaves)) * ((r + ranks - 1) / ranks);
-    const long long rows = std::max<long long>(M * columns / 256, M * columns * L / 16384);
-    return M <= 256 ? 256 : (int)std::min<long long>(1 << 24, std::max<long long>(128, (rows + 63) / 64 * 64));
-}
-
-// Groups of rows and of ranks to a workgroup of down, and parts of K: what takes least by a count of the bytes that the busiest compute
-// unit brings (40 GB/s each), a quarter of a microsecond for each part that the readers of T will add up, and parts only where T stays
-// small.  Measured (us; groups of rows, of ranks, parts): one row of 4096, rank 16: 1 1 1 5.8, 1 1 4 4.3, 1 1 8 4.1; 512 rows, rank 16:
-// 1 1 1 10.0, 1 1 4 4.7; 4100 rows, rank 16: 1 1 1 12.2, 2 1 1 11.6; 8196 rows, rank 64: 1 1 1 68, 2 2 1 34, 4 4 1 25.
-struct DownPlan {
-    int rt, jt, parts;
-};
-DownPlan down_plan(int S, int M, int K, int r) {
-    DownPlan best{1, 1, 1};
-    double least = 1e30;
-    for (int rt = 1; rt <= 4; rt *= 2)
-        for (int jt = 1; jt <= rank_groups(r); jt *= 2)
-            for (int parts = 1; parts <= kMaxParts; parts *= 2) {
-                if (parts > 1 && ((long long)parts * M > 8192 || K < 512 * parts)) continue;
-                const long long tiles = std::max<long long>((M + 16 * rt - 1) / (16 * rt), std::min(S, M)) * ((r + 16 * jt - 1) / (16 * jt));
-                const long long rounds = (tiles * parts + 255) / 256;
-                const double cost = (double)rounds * (rt + jt) / parts * K * 32 / 40e3 + 0.25 * parts;
-                if (cost < least) {
-                    least = cost;
-                    best = DownPlan{rt, jt, parts};
-                }
-            }
-    return best;
-}
-
 template <int TYPE, int RT, int JT>
 void down_tiles(const void* X, long long ldx, const void* A, const Segments& seg, const float* scale, int K, int r, int parts, float* T,
                 hipStream_t s) {
-    constexpr int kLine = TYPE == APB_F32 ? 32 : 64, kW = kDownWaves<RT, JT>;
+    constexpr int kLine = TYPE == APB_F32 ? 32 : 64, kW = down_waves(RT, JT);
     const int lines = (K + kLine - 1) / kLine, each = (lines + parts - 1) / parts;
     const dim3 grid((unsigned)max_row_tiles(seg.M, seg.S, seg.offsets != nullptr, 16 * RT), (unsigned)((r + 16 * JT - 1) / (16 * JT)), (unsigned)parts);
     hipLaunchKernelGGL((k_adapter_down<TYPE, RT, JT, kW>), grid, dim3(kW * kWave), 0, s, X, ldx, A, seg, scale, K, r, each, T);
@@ -1002,7 +951,7 @@ size_t apb_adapter_gradient_workspace_bytes(int L, int M, int K, int r) {
     static const int32_t some = 0;
     if (bad_adapter(1, L, M, K, r, &some, &some)) return 0;
     const int each = gradient_rows(L, M, K, r);
-    return M > each ? (size_t)(2LL * M / each + 1) * r * K * sizeof(float) : 0;
+    return M > each ? (size_t)places_of_slices(M, each) * r * K * sizeof(float) : 0;
 }
 
 int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, long long ldx, const int32_t* offsets,

@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 import torch
 
+import adapter_cases as cases
 from oracle import block_oracle as o
 
 pytestmark = pytest.mark.gpu
@@ -53,33 +54,8 @@ def _wide(x, extra=5, at=3, fill=99.0):
     return w[:, at:at + x.shape[1]]
 
 
-def _segments(kind, M, L, seed):
-    """(offsets, adapter): requests of one token, of any length with empty ones and rows behind the last, all rows, one per adapter."""
-    g = np.random.default_rng(seed)
-    if kind == "all":
-        return None, np.array([L - 1], np.int32)
-    if kind == "tokens":
-        return np.arange(M + 1, dtype=np.int32), g.integers(-1, L + 1, M).astype(np.int32)
-    S = L if kind == "own" else 70 if kind == "many" else 6
-    cut = np.sort(g.integers(0, M - M // 8 + 1, S))
-    off = np.concatenate([[0], cut]).astype(np.int32)
-    if S > 2:
-        off[2] = off[1]
-    return off, None if kind == "own" else g.integers(-1, L, S).astype(np.int32)
-
-
-# M, K, N, r, L, segments: every number of ranks and rows to a workgroup, parts of sums, ragged in every direction
-CASES = [
-    (1, 1, 1, 1, 1, "all"), (1, 4096, 4096, 16, 3, "all"), (1, 1000, 517, 5, 2, "tokens"), (64, 4096, 600, 16, 8, "tokens"),
-    (33, 517, 1000, 3, 2, "mixed"), (100, 300, 130, 17, 4, "mixed"), (40, 64, 512, 33, 5, "own"), (16, 70, 31, 64, 2, "mixed"),
-    (333, 517, 1000, 16, 2, "mixed"), (900, 1000, 515, 8, 3, "own"), (700, 2048, 1100, 32, 1, "all"), (1500, 300, 260, 64, 3, "mixed"),
-    (2600, 40, 24, 4, 1, "all"), (4096, 16, 40, 3, 7, "tokens"), (3000, 5, 6, 18, 2, "mixed"),
-    (400, 200, 140, 100, 2, "mixed"), (300, 96, 520, 256, 2, "all"), (2000, 130, 70, 20, 9, "many"), (8, 9000, 100, 130, 4, "tokens"),
-]
-
-
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("M,K,N,r,L,kind", CASES)
+@pytest.mark.parametrize("M,K,N,r,L,kind", cases.CASES)
 def test_adapter_forward_and_gradients(b, M, K, N, r, L, kind, t):
     g = np.random.default_rng(M * 31 + K + r)
     x, xv = _in(g.standard_normal((M, K)) * np.exp(g.standard_normal(K) * 0.5), t)
@@ -89,7 +65,7 @@ def test_adapter_forward_and_gradients(b, M, K, N, r, L, kind, t):
     dy, dyv = _in(g.standard_normal((M, N)) * 0.1, t)
     scale = torch.from_numpy(g.uniform(0.5, 2.0, L).astype(np.float32))
     sv = scale.double().numpy()
-    off, adapter = _segments(kind, M, L, r)
+    off, adapter = cases.segments(kind, M, L, r)
     which = o.rows_by_adapter(off, adapter, M, L)
     if kind == "all" and adapter is not None:
         which[:] = adapter[0]

@@ -10,6 +10,7 @@ import numpy as np
 import pytest
 import torch
 
+import gated_cases as gated
 import mx4_tile_cases as cases
 from oracle import block_oracle as o
 from oracle import mx4_oracle as o4
@@ -218,14 +219,8 @@ def _check_saved(saved, gu, mag, K, M, N, inside):
     assert (codes[~rows] == 0).all() and (scales[~rows] == 0).all()
 
 
-# few rows and little work (one kernel), every tile size plain and in groups, ragged in every direction; the sides are the product's for 2N
-PRODUCTS = [(1, 1, 1, 0), (16, 130, 8193, 0), (1, 17, 300, 0), (16, 33, 256, 0), (16, 4100, 4096, 0), (7, 1000, 9000, 0), (17, 15, 31, 0), (130, 150, 520, 0), (300, 700, 2600, 0),
-            (64, 32, 257, 0), (200, 47, 1300, 3), (1700, 1025, 300, 0), (1540, 901, 40, 0), (1700, 1025, 1300, 5),
-            (3400, 1801, 520, 0), (3330, 1825, 33, 0), (3400, 1801, 777, 4)]
-
-
 @pytest.mark.parametrize("kind,t", [("silu", "bf16"), ("gelu", "f32"), ("relu", "f16")])
-@pytest.mark.parametrize("M,N,K,E", PRODUCTS)
+@pytest.mark.parametrize("M,N,K,E", [c[:4] for c in gated.PRODUCTS])
 def test_gated_gemm(b, M, N, K, E, kind, t):
     x, w = _acts(M + N + K, M, K), (np.random.default_rng(N).standard_normal((max(E, 1) * 2 * N, K)) * K ** -0.5).astype(np.float32)
     xc, wc = o4.quantize(x), o4.quantize(w)
