@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kAdapterWaves;
-static_assert(kThreads == kWaves * kWave, "a workgroup of up and gradient");
+static_assert(kThreads == kWaves * kWave, "a workgroup of up and of the join");
 constexpr int kList = 1024;                    // rows of an adapter whose numbers a workgroup of the gradient holds at a time
 constexpr int kStage = 64;                    // ranks of T that are in LDS at a time
 
@@ -340,27 +340,17 @@ __device__ __forceinline__ Eight<TYPE> settle(const Eight<TYPE>& x, int c, int n
     if constexpr (WHOLE) return x;
     const int by = n < 8 ? 0 : max(c - (n - 8), 0) & 7;          // elements to move by
     Eight<TYPE> v = x;
-    if constexpr (TYPE == APB_F32) {
 #pragma unroll
-        for (int d = 4; d >= 1; d >>= 1)
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const uint32_t from = q + d < 8 ? v.w[(q + d) / 4 & 1][(q + d) & 3] : 0u;
-                v.w[q / 4][q & 3] = by & d ? from : v.w[q / 4][q & 3];
-            }
-    } else {
-#pragma unroll
-        for (int d = 2; d >= 1; d >>= 1)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t from = q + d < 4 ? v.w[0][(q + d) & 3] : 0u;
-                v.w[0][q] = by & (2 * d) ? from : v.w[0][q];
-            }
+    for (int d = 2; d >= 1; d >>= 1)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const uint32_t next = q < 3 ? v.w[0][(q + 1) & 3] : 0u;
-            v.w[0][q] = by & 1 ? v.w[0][q] >> 16 | next << 16 : v.w[0][q];
+            const uint32_t from = q + d < 4 ? v.w[0][(q + d) & 3] : 0u;
+            v.w[0][q] = by & (2 * d) ? from : v.w[0][q];
         }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t next = q < 3 ? v.w[0][(q + 1) & 3] : 0u;
+        v.w[0][q] = by & 1 ? v.w[0][q] >> 16 | next << 16 : v.w[0][q];
     }
     return v;
 }
@@ -547,110 +537,112 @@ __device__ __forceinline__ Span span_of(const Segments& seg, int a, int& its, in
     return Span{rows, min(__builtin_amdgcn_readfirstlane(before), seg.M - rows)};
 }
 
-// Rows of X as they are loaded: what a lane has of 32 of them.  16 bits: eight columns of eight rows 8 g ..; float32: eight columns
-// of rows g, g + 4, ...; 8 bits: as 16 bits, and each row's scale.
-template <int XT>
+// 32 rows of X as they are loaded: of eight of them NC neighbours to a lane.  Rows 8 g + e, for operands that sum over eight rows; an X of
+// float32 goes into products over four rows, row 4 e + g of a lane.
+template <int XT, int NC>
 struct Rows32 {
-    Eight<XT == APB_F32 ? APB_F32 : APB_BF16> v[8];
-};
-template <>
-struct Rows32<APB_MX8> {
-    u32x2 v[8];
+    uint32_t w[8][NC * (XT == APB_F32 ? 4 : XT == APB_MX8 ? 1 : 2) / 4];
     uint8_t scale[8];
 };
-// `rows`: the numbers of the 32 rows.  (Fewer than eight columns: one by one.)
-template <int XT, bool WHOLE>
-__device__ __forceinline__ void load_rows(Rows32<XT>& x, const void* X, long long ldx, const Mx8& x8, const int* rows, int g, int c, int K) {
-    long long row[8];
+template <int XT>
+__device__ __forceinline__ int row_of(int e, int g) { return XT == APB_F32 ? 4 * e + g : 8 * g + e; }
+
+// `rows`: the numbers of the 32 rows.  WHOLE: all columns of the workgroup are there; otherwise the values come one by one, the row's
+// last one in the place of those that are not (loads without a branch, which would make the loads before it be waited for).
+template <int XT, int NC, bool WHOLE>
+__device__ __forceinline__ void load_rows(Rows32<XT, NC>& x, const void* X, long long ldx, const Mx8& x8, const int* rows, int g, int c, int K) {
+    constexpr int kWords = sizeof(x.w[0]) / 4;
+    typedef uint32_t words __attribute__((ext_vector_type(kWords)));
+    typedef words words_any __attribute__((aligned(1)));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) row[e] = rows[XT == APB_F32 ? 4 * e + g : 8 * g + e];
-    if constexpr (XT == APB_MX8) {
-        const int at = min(c, x8.blocks * kMx8Block - 8);
+    for (int e = 0; e < 8; ++e) {
+        const long long row = rows[row_of<XT>(e, g)];
+        if constexpr (XT == APB_MX8) {
+            const int at = min(c, x8.blocks * kMx8Block - NC);   // (its rows are padded)
+            if constexpr (kWords == 1) x.w[e][0] = *reinterpret_cast<const uint32_t*>(x8.codes + row * x8.blocks * kMx8Block + at);
+            else __builtin_memcpy(x.w[e], x8.codes + row * x8.blocks * kMx8Block + at, sizeof(x.w[e]));
+            x.scale[e] = x8.scales[row * x8.blocks + at / kMx8Block];
+        } else if constexpr (WHOLE) {
+            const words v = *reinterpret_cast<const words_any*>(static_cast<const uint8_t*>(X) + (row * ldx + c) * (XT == APB_F32 ? 4 : 2));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x.v[e] = *reinterpret_cast<const u32x2*>(x8.codes + row[e] * x8.blocks * kMx8Block + at);
-            x.scale[e] = x8.scales[row[e] * x8.blocks + at / kMx8Block];
-        }
-    } else {
-        constexpr int kAs = XT == APB_F32 ? APB_F32 : APB_BF16;
-        if (WHOLE || K >= 8) {
+            for (int q = 0; q < kWords; ++q) x.w[e][q] = v[q];
+        } else if constexpr (XT == APB_F32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x.v[e] = load_row<kAs, WHOLE>(X, row[e] * ldx, c, K);
+            for (int q = 0; q < NC; ++q) x.w[e][q] = static_cast<const uint32_t*>(X)[row * ldx + min(c + q, K - 1)];
         } else {
+            const uint16_t* p = static_cast<const uint16_t*>(X) + row * ldx;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x.v[e] = load_some<kAs>(X, row[e] * ldx + c, K - c);
+            for (int q = 0; q < kWords; ++q) x.w[e][q] = p[min(c + 2 * q, K - 1)] | (uint32_t)p[min(c + 2 * q + 1, K - 1)] << 16;
         }
     }
 }
 // Rows that are not there as zeros (they repeat the last one, and zero times infinity is not zero).
-template <int XT>
-__device__ __forceinline__ void clear_rows(Rows32<XT>& x, int rows, int g) {
+template <int XT, int NC>
+__device__ __forceinline__ void clear_rows(Rows32<XT, NC>& x, int rows, int g) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if ((XT == APB_F32 ? 4 * e + g : 8 * g + e) >= rows) {
-            if constexpr (XT == APB_MX8) {
-                x.v[e] = u32x2{0u, 0u};
-                x.scale[e] = 0;
-            } else {
-                x.v[e].w[0] = u32x4{0u, 0u, 0u, 0u};
-                if constexpr (XT == APB_F32) x.v[e].w[1] = u32x4{0u, 0u, 0u, 0u};
-            }
-        }
+    for (int e = 0; e < 8; ++e) {
+        const bool there = row_of<XT>(e, g) < rows;
+#pragma unroll
+        for (int q = 0; q < (int)sizeof(x.w[0]) / 4; ++q) x.w[e][q] = there ? x.w[e][q] : 0u;
+        if (XT == APB_MX8) x.scale[e] = there ? x.scale[e] : (uint8_t)0;
+    }
 }
-// Column n of the lane's eight as bfloat16 operands of eight rows: 16-bit floats in one or two parts, 8-bit values in one.
+// Column n of the lane's as bfloat16 operands of eight rows: 16-bit floats in one or two parts, 8-bit values in one.
 template <int XT>
 constexpr int kXParts = XT == APB_F16 ? 2 : 1;
-template <int XT>
-__device__ __forceinline__ void column(const Rows32<XT>& x, int n, Eight<APB_BF16> (&out)[kXParts<XT>]) {
+template <int XT, int NC>
+__device__ __forceinline__ void column(const Rows32<XT, NC>& x, int n, Eight<APB_BF16> (&out)[kXParts<XT>]) {
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
-        if constexpr (XT == APB_BF16) {
-            out[0].w[0][d] = __builtin_amdgcn_perm(x.v[2 * d + 1].w[0][n / 2], x.v[2 * d].w[0][n / 2], n & 1 ? 0x07060302u : 0x05040100u);
-        } else if constexpr (XT == APB_MX8) {
-            out[0].w[0][d] = pack2(APB_BF16, decode8(x.v[2 * d][n / 4], n & 3, scale_value(x.scale[2 * d])),
-                                   decode8(x.v[2 * d + 1][n / 4], n & 3, scale_value(x.scale[2 * d + 1])));
+        if constexpr (XT == APB_MX8) {
+            out[0].w[0][d] = pack2(APB_BF16, decode8(x.w[2 * d][n / 4], n & 3, scale_value(x.scale[2 * d])),
+                                   decode8(x.w[2 * d + 1][n / 4], n & 3, scale_value(x.scale[2 * d + 1])));
         } else {
-            const uint32_t w = __builtin_amdgcn_perm(x.v[2 * d + 1].w[0][n / 2], x.v[2 * d].w[0][n / 2], n & 1 ? 0x07060302u : 0x05040100u);
-            const f16x2 h = __builtin_bit_cast(f16x2, w);
-            const uint32_t hi = pack2(APB_BF16, (float)h[0], (float)h[1]);
-            out[0].w[0][d] = hi;
-            out[1].w[0][d] = pack2(APB_BF16, (float)h[0] - __builtin_bit_cast(float, hi << 16),
-                                   (float)h[1] - __builtin_bit_cast(float, hi & 0xffff0000u));
+            const uint32_t w = __builtin_amdgcn_perm(x.w[2 * d + 1][n / 2], x.w[2 * d][n / 2], n & 1 ? 0x07060302u : 0x05040100u);
+            if constexpr (XT == APB_BF16) {
+                out[0].w[0][d] = w;
+            } else {
+                const f16x2 h = __builtin_bit_cast(f16x2, w);
+                const uint32_t hi = pack2(APB_BF16, (float)h[0], (float)h[1]);
+                out[0].w[0][d] = hi;
+                out[1].w[0][d] = pack2(APB_BF16, (float)h[0] - __builtin_bit_cast(float, hi << 16),
+                                       (float)h[1] - __builtin_bit_cast(float, hi & 0xffff0000u));
+            }
         }
     }
 }
 
-// A workgroup takes one adapter, 16 * JT ranks, kCols columns a wave, and `each` of the adapter's rows, counted through all of its
-// segments, whose numbers it lists in LDS, and of these 32 at a time: while one such chunk is multiplied, the next one's X comes to
-// registers, where it is transposed, and T, its parts added up, on its way to LDS, where it is in three bfloat16 operands of eight
-// rows, or in float32 for an X of float32.  Bound by reading X: 4100 rows of 4096 in bfloat16, rank 16, four adapters, 16 us with the
-// joining, of which 34 MB are 7; a row's numbers come from a list so that 64 requests of one row are two chunks (7 us), not 64 (69).
-template <int XT, int JT, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void k_adapter_gradient(const float* __restrict__ T, int parts, const void* __restrict__ X,
-                                                               long long ldx, Mx8 x8, Segments seg, int K, int r, int rank_tiles, int each,
-                                                               float* __restrict__ dA, float* __restrict__ shared) {
-    constexpr bool kWide = XT == APB_F32;
-    constexpr int kRanks = 16 * JT, kChunk = 32;
-    constexpr int kPitch = kWide ? 4 * (kRanks + 1) : 2 * kChunk + 16;            // of a row of T; of a rank
-    constexpr int kStageBytes = ((kWide ? kChunk * kPitch : 3 * kRanks * kPitch) + 15) / 16 * 16;
-    static_assert(kRanks * kChunk / 8 <= kThreads, "a thread brings eight values of T");
-    __shared__ __align__(16) uint8_t lds[2 * kStageBytes];
+// WHOLE: K is 16 * NC or more; the last workgroup's columns then end with the row's, and those that two workgroups have get the same
+// values twice.  (Rows of 8 bits are padded, and their columns stay in blocks.)
+//
+// A workgroup takes one adapter, 16 * JT ranks, 16 * NC columns, and `each` of the adapter's rows, counted through all of its segments,
+// whose numbers it lists in LDS; its waves take 32 of them at a time in turn, by themselves, the next ones under way, and join their sums in
+// LDS.  T, its parts added up, comes to registers in the order of the operand and is split there into three bfloat16 parts (an X of
+// float32 goes with T as it is through float32 products); X is transposed in registers.  With waves that share a tile of rows in LDS and
+// each take columns of their own, every wave waits at barriers for the slowest load, and an adapter's rows have to be shared out much
+// sooner: 16384 rows of 8192, rank 32, bfloat16 65 us and now 62 (268 MB are 52); 8196 of 4096, rank 64 43 and 35 (67 MB are 13; the
+// splitting of T by each of 64 workgroups is most of it); 4100 of 4096, rank 16 16 and 11.7 (34 MB are 7); 512 of 4096, rank 32 13.4 and 7.0.
+template <int XT, int JT, int NC, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float* __restrict__ T, int parts, const void* __restrict__ X,
+                                                                    long long ldx, Mx8 x8, Segments seg, int K, int r, int rank_tiles,
+                                                                    int each, float* __restrict__ dA, float* __restrict__ shared) {
+    constexpr int kChunk = 32, kRanks = 16 * JT;
+    __shared__ f32x4 sums[WAVES][JT * NC][kWave];
     __shared__ int list[kList + kChunk];
     const int a = blockIdx.y / rank_tiles, j0 = blockIdx.y % rank_tiles * kRanks;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
-    const int c0 = (blockIdx.x * kWaves + wave) * kCols, c = c0 + 8 * i;
-    const bool there = c0 < K, whole = WHOLE || c0 + kCols <= K;
+    const int c0 = XT == APB_MX8 ? blockIdx.x * 16 * NC : WHOLE ? min((int)blockIdx.x * 16 * NC, K - 16 * NC) : 0, c = c0 + NC * i;
     int its, first, count;
     const Span span = span_of(seg, a, its, first, count);
     const int lo = blockIdx.z * each, hi = min(lo + each, span.rows);
     if (blockIdx.z > 0 && lo >= hi) return;
-    f32x4 acc[JT][8];
+    f32x4 acc[JT][NC];
 #pragma unroll
     for (int j = 0; j < JT; ++j)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) acc[j][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int n = 0; n < NC; ++n) acc[j][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // the numbers of the adapter's rows start .. start + count - 1; behind them the last one again, up to a whole chunk
+    // the numbers of the adapter's rows start .. start + rows - 1; behind them the last one again, up to a whole chunk
     auto list_rows = [&](int start, int rows) {
         if (wave == 0) {
             int before = 0;
@@ -669,105 +661,94 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gradient(const float* __re
         }
         __syncthreads();
     };
-    const int tj = threadIdx.x % kRanks, octet = threadIdx.x / kRanks;
-    const bool brings = octet < kChunk / 8;
-    Rows32<XT> x;
-    float tv[8];
-    auto fetch = [&](int m, auto all) {
-        if (there) load_rows<XT, decltype(all)::value>(x, X, ldx, x8, list + m, g, c, K);
-        if (brings) {
-            // (rows and ranks that are not there repeat the last ones, and are cleared)
-            size_t at[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) at[e] = (size_t)list[m + 8 * octet + e] * r + min(j0 + tj, r - 1);
-            sum_parts<8>(T, at, parts, (size_t)seg.M * r, tv);
-        }
+    struct Chunk {
+        Rows32<XT, NC> x;
+        float t[JT][8];
     };
-    auto multiply = [&](auto all) {
-        uint32_t stage = 0;
-        for (int start = lo; start < hi; start += kList) {
-            const int rows_listed = min(hi - start, kList);
-            list_rows(start, rows_listed);
-            fetch(0, all);
-            for (int m = 0; m < rows_listed; m += kChunk) {
-                const int rows = min(rows_listed - m, kChunk);
-                uint8_t* to = lds + stage;
-                stage = kStageBytes - stage;
-                if (brings) {
+    auto fetch = [&](Chunk& v, int m) {
+        load_rows<XT, NC, WHOLE>(v.x, X, ldx, x8, list + m, g, c, K);
+        size_t at[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) tv[e] = 8 * octet + e < rows && j0 + tj < r ? tv[e] : 0.0f;
-                    if constexpr (kWide) {
+        for (int e = 0; e < 8; ++e) at[e] = (size_t)list[m + row_of<XT>(e, g)] * r;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) *reinterpret_cast<float*>(to + (8 * octet + e) * kPitch + 4 * tj) = tv[e];
-                    } else {
-                        Eight<APB_BF16> part[3];
-                        bf16_parts<3>(tv, part);
+        for (int j = 0; j < JT; ++j) sum_parts<8>(T + min(j0 + 16 * j + i, r - 1), at, parts, (size_t)seg.M * r, v.t[j]);
+    };
+    auto multiply = [&](Chunk& v, int rows) {
+        if (rows < kChunk) {
+            clear_rows<XT, NC>(v.x, rows, g);
 #pragma unroll
-                        for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(to + (p * kRanks + tj) * kPitch + 16 * octet) = part[p].w[0];
+            for (int j = 0; j < JT; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.t[j][e] = row_of<XT>(e, g) < rows ? v.t[j][e] : 0.0f;
+        }
+        if constexpr (XT == APB_F32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int j = 0; j < JT; ++j)
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) {
+                        const uint32_t bits = v.x.w[e][n];
+                        acc[j][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.t[j][e], __builtin_bit_cast(float, bits), acc[j][n], 0, 0, 0);
                     }
-                }
-                Rows32<XT> now = x;
-                if (m + kChunk < rows_listed) fetch(m + kChunk, all);
-                __syncthreads();                                 // (of the other stage, everybody has read by the time they are here)
-                if (!there) continue;
-                if constexpr (XT != APB_MX8)
+        } else {
+            Eight<APB_BF16> t[JT][3];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) now.v[e] = settle<XT == APB_F32 ? APB_F32 : APB_BF16, decltype(all)::value>(now.v[e], c, K);
-                if (rows < kChunk) clear_rows<XT>(now, rows, g);
-                if constexpr (kWide) {
+            for (int j = 0; j < JT; ++j) bf16_parts<3>(v.t[j], t[j]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float v[8];
-                        floats(now.v[e], v);
+            for (int n = 0; n < NC; ++n) {
+                Eight<APB_BF16> xv[kXParts<XT>];
+                column<XT, NC>(v.x, n, xv);
 #pragma unroll
-                        for (int j = 0; j < JT; ++j) {
-                            const float t = *reinterpret_cast<const float*>(to + (4 * e + g) * kPitch + 4 * (16 * j + i));
-#pragma unroll
-                            for (int n = 0; n < 8; ++n) acc[j][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(t, v[n], acc[j][n], 0, 0, 0);
-                        }
+                for (int j = 0; j < JT; ++j) {
+                    // (the smallest first; the third part of T times the second of X is below 2^-24)
+                    if constexpr (kXParts<XT> == 2) {
+                        acc[j][n] = multiply8<APB_BF16>(t[j][1], xv[1], acc[j][n]);
+                        acc[j][n] = multiply8<APB_BF16>(t[j][0], xv[1], acc[j][n]);
                     }
-                } else {
-                    Eight<APB_BF16> t[JT][3];
 #pragma unroll
-                    for (int j = 0; j < JT; ++j)
-#pragma unroll
-                        for (int p = 0; p < 3; ++p)
-                            t[j][p].w[0] = *reinterpret_cast<const u32x4*>(to + (p * kRanks + 16 * j + i) * kPitch + 16 * g);
-#pragma unroll
-                    for (int n = 0; n < 8; ++n) {
-                        Eight<APB_BF16> xv[kXParts<XT>];
-                        column<XT>(now, n, xv);
-#pragma unroll
-                        for (int j = 0; j < JT; ++j) {
-                            // (the smallest first; the third part of T times the second of X is below 2^-24)
-                            if constexpr (kXParts<XT> == 2) {
-                                acc[j][n] = multiply8<APB_BF16>(t[j][1], xv[1], acc[j][n]);
-                                acc[j][n] = multiply8<APB_BF16>(t[j][0], xv[1], acc[j][n]);
-                            }
-#pragma unroll
-                            for (int p = 2; p >= 0; --p) acc[j][n] = multiply8<APB_BF16>(t[j][p], xv[0], acc[j][n]);
-                        }
-                    }
+                    for (int p = 2; p >= 0; --p) acc[j][n] = multiply8<APB_BF16>(t[j][p], xv[0], acc[j][n]);
                 }
             }
-            if (start + kList < hi) __syncthreads();             // (the list has been read)
         }
     };
-    if (WHOLE || whole) multiply(std::true_type{});
-    else multiply(std::false_type{});
-    if (!there) return;
-    float* out = span.rows > each ? shared + (size_t)(place_of_slices(span.before, each) + blockIdx.z) * r * K : dA + (size_t)a * r * K;
+    for (int start = lo; start < hi; start += kList) {
+        const int rows = min(hi - start, kList);
+        list_rows(start, rows);
+        Chunk v;
+        int m = wave * kChunk;
+        if (m < rows) fetch(v, m);
+        for (; m < rows; m += WAVES * kChunk) {
+            Chunk now = v;
+            if (m + WAVES * kChunk < rows) fetch(v, m + WAVES * kChunk);
+            multiply(now, rows - m);
+        }
+        if (start + kList < hi) __syncthreads();                 // (the list has been read)
+    }
 #pragma unroll
     for (int j = 0; j < JT; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int rank = j0 + 16 * j + 4 * g + q;
-            if (rank >= r) continue;
-            float v[8];
+        for (int n = 0; n < NC; ++n) sums[wave][j * NC + n][lane] = acc[j][n];
+    __syncthreads();
+    // rank 16 j + 4 g + q of columns NC i ..
+    float* out = span.rows > each ? shared + (size_t)(place_of_slices(span.before, each) + blockIdx.z) * r * K : dA + (size_t)a * r * K;
+    for (int n = threadIdx.x; n < JT * 256; n += WAVES * kWave) {
+        const int q = n & 3, from = n >> 2 & 63, j = n >> 8;
+        const int rank = j0 + 16 * j + 4 * (from >> 4) + q, col = c0 + NC * (from & 15);
+        if (rank >= r || col >= K) continue;
+        float v[NC];
 #pragma unroll
-            for (int n = 0; n < 8; ++n) v[n] = acc[j][n][q];
-            store8<APB_F32>(out, (long long)rank * K + c, K - c, v);
+        for (int e = 0; e < NC; ++e) {
+            v[e] = sums[0][j * NC + e][from][q];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v[e] += sums[w][j * NC + e][from][q];
         }
+#pragma unroll
+        for (int e = 0; e < NC; e += 4) {
+            const float four[4] = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+            store4(out, APB_F32, (long long)rank * K + col + e, four, K - col - e);
+        }
+    }
 }
 
 // The slices of the adapters that have several, added up in order.
@@ -878,26 +859,34 @@ void up(const float* T, int parts, const void* B, const Segments& seg, int N, in
     else up_tiles<TYPE, 1>(T, parts, B, seg, N, r, Y0, ldy0, Y, ldy, s);
 }
 
-template <int XT, int JT>
-void gradient_tiles(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int each,
-                    float* dA, float* shared, hipStream_t s) {
+template <int XT, int JT, int NC, int WAVES>
+void gradient_form(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int each,
+                   float* dA, float* shared, hipStream_t s) {
     const int rank_tiles = (r + 16 * JT - 1) / (16 * JT);
-    const dim3 grid((unsigned)((K + kCols * kWaves - 1) / (kCols * kWaves)), (unsigned)(seg.L * rank_tiles), (unsigned)((seg.M + each - 1) / each));
+    const dim3 grid((unsigned)((K + 16 * NC - 1) / (16 * NC)), (unsigned)(seg.L * rank_tiles), (unsigned)((seg.M + each - 1) / each));
     auto launch = [&](auto whole) {
-        hipLaunchKernelGGL((k_adapter_gradient<XT, JT, decltype(whole)::value>), grid, dim3(kThreads), 0, s, T, parts, X, ldx, x8, seg, K, r,
-                           rank_tiles, each, dA, shared);
+        hipLaunchKernelGGL((k_adapter_gradient<XT, JT, NC, WAVES, decltype(whole)::value>), grid, dim3(WAVES * kWave), 0, s, T, parts, X, ldx, x8,
+                           seg, K, r, rank_tiles, each, dA, shared);
     };
-    if constexpr (XT == APB_MX8) launch(std::true_type{});       // (its rows are padded)
-    else if (K % kCols == 0) launch(std::true_type{});
+    if constexpr (XT == APB_MX8 || NC == 8) launch(std::true_type{});
+    else if (K >= 16 * NC) launch(std::true_type{});
     else launch(std::false_type{});
 }
 template <int XT>
 void gradient(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int each,
               float* dA, float* shared, hipStream_t s) {
-    const int j = rank_groups(r);
-    if (j == 1) gradient_tiles<XT, 1>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
-    else if (j == 2) gradient_tiles<XT, 2>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
-    else gradient_tiles<XT, 4>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+    const GradientForm form = gradient_form_of(XT, seg.L, seg.M, K, r);
+    auto with = [&](auto ranks) {
+        constexpr int kJt = decltype(ranks)::value;
+        if (form.waves == 1) return gradient_form<XT, kJt, 4, 1>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+        if (form.waves == 4) return gradient_form<XT, kJt, 4, 4>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+        if constexpr (XT != APB_F32 && kJt <= 2)
+            if (form.nc == 8) return gradient_form<XT, kJt, 8, 8>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+        if constexpr (XT != APB_F32 || kJt <= 2) gradient_form<XT, kJt, 4, 8>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
+    };
+    if (form.jt == 1) with(std::integral_constant<int, 1>{});
+    else if (form.jt == 2) with(std::integral_constant<int, 2>{});
+    else with(std::integral_constant<int, 4>{});
 }
 
 }  // namespace

@@ -15,7 +15,7 @@
 namespace apb {
 
 constexpr int kMaxParts = APB_ADAPTER_MAX_PARTS;
-constexpr int kCols = 128;                    // of a wave, in up and gradient: eight to a lane
+constexpr int kCols = 128;                    // of a wave of up: eight to a lane
 constexpr int kAdapterWaves = 4;              // of a workgroup there
 constexpr int kUpRows = 64;                   // of a workgroup that streams them past B, at most
 
@@ -29,14 +29,33 @@ inline int up_rows(int S, int M, int N) {
     return rows;
 }
 
-// Rows of an adapter to a workgroup of its gradient: so many that a workgroup comes to each compute unit, were they spread evenly, but at
-// least 128, and no more than 16384 workgroups that may find none.  4100 rows of 4096, rank 16, four adapters (us): 512 workgroups 21.5,
-// 256 16.0, 128 18.9; 8196 rows, rank 64: 55, 43, 48.  Up to 256 rows are never shared: joining takes 4 us and another launch.
-inline int gradient_rows(int L, int M, int K, int r) {
+// Columns of X that all adapters' gradients make, in groups of 64, times the groups of ranks: workgroups, were the rows not shared.
+inline long long gradient_groups(int L, int K, int r) {
     const int ranks = 16 * rank_groups(r);
-    const long long columns = (long long)((K + kCols * kAdapterWaves - 1) / (kCols * kAdapterWaves)) * ((r + ranks - 1) / ranks);
-    const long long rows = std::max<long long>(M * columns / 256, M * columns * L / 16384);
-    return M <= 256 ? 256 : (int)std::min<long long>(1 << 24, std::max<long long>(128, (rows + 63) / 64 * 64));
+    return (long long)((K + 63) / 64) * L * ((r + ranks - 1) / ranks);
+}
+// Rows of an adapter to a workgroup of its gradient.  Where one workgroup for each of those fills the compute units, more than 8192 and
+// four times the average are shared out, and otherwise so many that there is a workgroup to each unit, but at least 256 (sharing costs a
+// launch and 4 us).  bfloat16, us: 4100 rows of 4096, rank 16, four adapters (256 groups) not shared 11.7, in pieces of 2048 rows 14.2, of
+// 1024 17.7; one adapter (64 groups) 27.0, 18.4, 16.5; 2000 rows of 1024, rank 64, one adapter (16 groups) not shared 39, in pieces of 1024
+// 25, of 512 16.5, of 256 13.1.
+inline int gradient_rows(int L, int M, int K, int r) {
+    const long long mean = (M + L - 1) / L, slices = 256 / gradient_groups(L, K, r);
+    return (int)(slices <= 1 ? std::max(8192LL, 4 * mean) : std::max(256LL, (mean / slices + 31) / 32 * 32));
+}
+// Groups of 16 ranks, columns to a lane and waves of such a workgroup.  A wave takes 32 rows at a time: as many waves as an adapter has
+// rows for on average, and one for each 256 rows in case one adapter has most of them.  128 columns instead of 64, which halves how often T
+// is read and split, where that leaves a workgroup to each compute unit.  bfloat16, us, with 64 and with 128: 16384 rows of 8192, rank 32
+// 91 and 62, 4100 rows of 8192, rank 16 21 and 18, 2000 rows of 4096, rank 32, eight adapters 16 and 11; with half the workgroups
+// 4100 rows of 4096, rank 32, four adapters 14 and 17.
+struct GradientForm {
+    int jt, nc, waves;
+};
+inline GradientForm gradient_form_of(int x_type, int L, int M, int K, int r) {
+    const int jt = rank_groups(r), chunks = std::max((M / L + 31) / 32, (M + 255) / 256);
+    const bool wide = x_type == APB_F32;                         // (its operands take twice the registers)
+    const int waves = chunks > 4 && !(wide && jt == 4) ? 8 : chunks > 1 ? 4 : 1;
+    return GradientForm{jt, waves == 8 && !wide && jt <= 2 && K >= 128 && gradient_groups(L, K, r) >= 512 ? 8 : 4, waves};
 }
 
 // Groups of rows and of ranks to a workgroup of down, and parts of K: what takes least by a count of the bytes that the busiest compute

@@ -13,6 +13,9 @@ CASES = [
     (4100, 24, 8300, 100, 2, "mixed"), (2100, 24, 8300, 200, 2, "mixed"), (4100, 24, 8192, 20, 2, "own"),
     (12100, 40, 30, 9, 3, "mixed"), (9000, 70, 50, 30, 2, "mixed"), (9000, 70, 40, 100, 2, "mixed"), (700, 8300, 40, 20, 2, "mixed"),
     (40, 4100, 100, 70, 30, "own"), (2000, 130, 70, 20, 9, "many"), (8, 9000, 100, 130, 4, "tokens"),
+    (600, 200, 40, 10, 7, "mixed"), (600, 130, 30, 24, 7, "own"), (500, 150, 50, 60, 9, "mixed"), (1300, 4100, 40, 12, 8, "mixed"),
+    (1100, 8300, 48, 30, 4, "own"), (9000, 4100, 16, 9, 8, "all"), (50, 30, 20, 40, 3, "mixed"), (70, 24, 40, 20, 4, "own"),
+    (300, 60, 9, 16, 2, "many"),
 ]
 
 

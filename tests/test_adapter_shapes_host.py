@@ -22,7 +22,10 @@ int main() {
         const DownPlan p = down_plan(S, M, K, r);
         if (what == 'd') std::printf("%d %d %d %d\n", p.rt, p.jt, p.parts, down_waves(p.rt, p.jt));
         else if (what == 'u') std::printf("%d\n", up_rows(S, M, K));
-        else if (what == 'g') std::printf("%d %d\n", gradient_rows(L, M, K, r), rank_groups(r));
+        else if (what == 'g' || what == 'w') {                        // (w: an X of float32)
+            const GradientForm f = gradient_form_of(what == 'w' ? APB_F32 : APB_BF16, L, M, K, r);
+            std::printf("%d %d %d %d\n", gradient_rows(L, M, K, r), f.jt, f.nc, f.waves);
+        }
         else std::printf("%d %lld\n", place_of_slices(S, L), places_of_slices(M, L));      // (S: rows before, L: rows to a slice)
     }
 }
@@ -65,9 +68,13 @@ def test_cases_reach_every_form(ask):
     assert reached == {(h, many) for h in (0, 1, 2, 4, None) for many in (False, True)}
     assert {rows[0] for rows in up} == {16, 32, 64}
     assert {(s[3] % 128 == 0, s[3] < 8, s[3] < 128) for s in sizes} == {(True, False, False), (False, False, False), (False, True, True), (False, False, True)}
-    grad = ask([("g", *s) for s in sizes])
-    assert {(g[1], s[2] > g[0], s[3] % 128 == 0) for s, g in zip(sizes, grad)} >= {(j, shared, False) for j in (1, 2, 4) for shared in (False, True)}
-    assert {(g[1], True) for s, g in zip(sizes, grad) if s[3] % 128 == 0} == {(j, True) for j in (1, 2, 4)}
+    grad, wide = ask([("g", *s) for s in sizes]), ask([("w", *s) for s in sizes])
+    assert {g[1:] for g in grad} == {(j, 4, w) for j in (1, 2, 4) for w in (1, 4, 8)} | {(j, 8, 8) for j in (1, 2)}
+    assert {g[1:] for g in wide} == {(j, 4, w) for j in (1, 2, 4) for w in (1, 4, 8) if (j, w) != (4, 8)}
+    assert {(g[1], g[3], s[3] < 64) for s, g in zip(sizes, grad)} == {(j, w, tiny) for j in (1, 2, 4) for w in (1, 4, 8) for tiny in (False, True)}
+    assert {(g[1], s[2] > g[0]) for s, g in zip(sizes, grad)} == {(j, shared) for j in (1, 2, 4) for shared in (False, True)}
+    assert any(s[2] > g[0] and g[2] == 8 for s, g in zip(sizes, grad))
+    assert any(s[3] % 128 and g[2] == 8 for s, g in zip(sizes, grad))
     assert any(s[2] > 1024 and s[1] == 1 for s in sizes)             # (more rows of one adapter than a list holds, without a workspace)
 
 
@@ -93,5 +100,8 @@ def test_plans_over_the_range(ask):
     for (rt, jt, parts, waves), (S, L, M, K, r) in zip(ask([("d", *s) for s in sizes]), sizes):
         assert rt in (1, 2, 4) and jt in (1, 2, 4) and 1 <= parts <= 8 and (parts == 1 or K >= 512 * parts)
         assert waves * 2 * (rt + jt) * 1024 <= 160 * 1024 and waves * rt * jt * 1024 <= 160 * 1024      # (LDS)
-    for (each, _), (S, L, M, K, r) in zip(ask([("g", *s) for s in sizes]), sizes):
-        assert 64 <= each <= 1 << 24 and -(-M // each) <= 65535
+    for what in "gw":
+        for (each, jt, nc, waves), (S, L, M, K, r) in zip(ask([(what, *s) for s in sizes]), sizes):
+            assert 256 <= each and -(-M // each) <= 65535 and 2 * M // each < 1 << 31 and L * -(-r // (16 * jt)) <= 65535
+            assert waves * jt * nc * 1024 + (1024 + 32) * 4 <= 160 * 1024      # (LDS)
+            assert nc == 4 or K >= 128                                         # (no form for fewer columns)
