@@ -87,15 +87,15 @@ __device__ __forceinline__ f32x4 multiply8(const Eight<TYPE>& a, const Eight<TYP
     }
 }
 
-// A workgroup takes 16 * RT rows of a segment, 16 * JT ranks and one part of K; its waves take lines of 128 bytes of all those rows in
+// A workgroup takes `tile` rows of a segment, up to 16 * RT, 16 * JT ranks and one part of K; its waves take lines of 128 bytes of all those rows in
 // turn and join their sums in LDS.  A line is loaded by eight neighbouring lanes and goes through LDS of the wave's own: in the order
 // of the operands, sixteen neighbouring lanes would ask for sixteen lines, and a compute unit would be brought 17 bytes a cycle.  The
 // next lines are under way while these are multiplied.  In LDS the eight 16-byte pieces of a line are permuted by the row's number, so
 // that eight lanes reading the same piece of eight rows meet every bank once.  8196 rows of 4096 in bfloat16: rank 16 16 us, rank 64
-// 25 (67 MB are 13), in the order of the operands 24 and 50.
+// 24 (67 MB are 13), in the order of the operands 24 and 50.
 template <int TYPE, int RT, int JT, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void k_adapter_down(const void* __restrict__ X, long long ldx, const void* __restrict__ A,
-                                                                Segments seg, const float* __restrict__ scale, int K, int r, int lines_each,
+                                                                Segments seg, const float* __restrict__ scale, int K, int r, int lines_each, int tile,
                                                                 float* __restrict__ T) {
     constexpr int kW = WAVES, kPiece = TYPE == APB_F32 ? 4 : 8, kLine = 8 * kPiece;       // values of 16 and of 128 bytes
     constexpr int kLoads = 2 * (RT + JT);                        // of a wave for a line of all rows, eight rows each
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_down(const void* __re
         uint8_t lines[kW][kLoads * 1024];
         f32x4 sums[kW][RT * JT][kWave];
     } lds;
-    const SegmentTile t = find_tile(seg, 16 * RT, blockIdx.x);
+    const SegmentTile t = find_tile(seg, tile, blockIdx.x);
     if (t.rows <= 0) return;
     const int j0 = blockIdx.y * 16 * JT, ranks = min(16 * JT, r - j0);
     float* out = T + ((size_t)blockIdx.z * seg.M + t.row0) * r + j0;
@@ -803,18 +803,18 @@ bool bad_adapter(int S, int L, int M, int K, int r, const int32_t* offsets, cons
 }
 
 template <int TYPE, int RT, int JT>
-void down_tiles(const void* X, long long ldx, const void* A, const Segments& seg, const float* scale, int K, int r, int parts, float* T,
-                hipStream_t s) {
+void down_tiles(const void* X, long long ldx, const void* A, const Segments& seg, const float* scale, int K, int r, int tile, int parts,
+                float* T, hipStream_t s) {
     constexpr int kLine = TYPE == APB_F32 ? 32 : 64, kW = down_waves(RT, JT);
     const int lines = (K + kLine - 1) / kLine, each = (lines + parts - 1) / parts;
-    const dim3 grid((unsigned)max_row_tiles(seg.M, seg.S, seg.offsets != nullptr, 16 * RT), (unsigned)((r + 16 * JT - 1) / (16 * JT)), (unsigned)parts);
-    hipLaunchKernelGGL((k_adapter_down<TYPE, RT, JT, kW>), grid, dim3(kW * kWave), 0, s, X, ldx, A, seg, scale, K, r, each, T);
+    const dim3 grid((unsigned)max_row_tiles(seg.M, seg.S, seg.offsets != nullptr, tile), (unsigned)((r + 16 * JT - 1) / (16 * JT)), (unsigned)parts);
+    hipLaunchKernelGGL((k_adapter_down<TYPE, RT, JT, kW>), grid, dim3(kW * kWave), 0, s, X, ldx, A, seg, scale, K, r, each, tile, T);
 }
 template <int TYPE>
 void down(const void* X, long long ldx, const void* A, const Segments& seg, const float* scale, int K, int r, float* T, hipStream_t s) {
     const DownPlan p = down_plan(seg.S, seg.M, K, r);
     auto with = [&](auto rt, auto jt) {
-        down_tiles<TYPE, decltype(rt)::value, decltype(jt)::value>(X, ldx, A, seg, scale, K, r, p.parts, T, s);
+        down_tiles<TYPE, decltype(rt)::value, decltype(jt)::value>(X, ldx, A, seg, scale, K, r, p.tile, p.parts, T, s);
     };
     auto with_rows = [&](auto rt) {
         if (p.jt == 1) with(rt, std::integral_constant<int, 1>{});

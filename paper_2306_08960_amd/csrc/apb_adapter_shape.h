@@ -58,26 +58,32 @@ inline GradientForm gradient_form_of(int x_type, int L, int M, int K, int r) {
     return GradientForm{jt, waves == 8 && !wide && jt <= 2 && K >= 128 && gradient_groups(L, K, r) >= 512 ? 8 : 4, waves};
 }
 
-// Groups of rows and of ranks to a workgroup of down, and parts of K: what takes least by a count of the bytes that the busiest compute
-// unit brings (40 GB/s each), a quarter of a microsecond for each part that the readers of T will add up, and parts only where T stays
-// small.  Measured (us; groups of rows, of ranks, parts): one row of 4096, rank 16: 1 1 1 5.8, 1 1 4 4.3, 1 1 8 4.1; 512 rows, rank 16:
-// 1 1 1 10.0, 1 1 4 4.7; 4100 rows, rank 16: 1 1 1 12.2, 2 1 1 11.6; 8196 rows, rank 64: 1 1 1 68, 2 2 1 34, 4 4 1 25.
+// Groups of rows, rows, and groups of ranks to a workgroup of down, and parts of K: what takes least by a count of the bytes that the busiest
+// compute unit brings (40 GB/s each), a quarter of a microsecond for each part that the readers of T will add up, and parts only where T
+// stays small.  Rows may be fewer than their groups hold, where more workgroups then share the work with still one to a compute unit.
+// Measured (us; rows, groups of ranks, parts; X from memory where there is more than one row): one row of 4096, rank 16: 16 1 1 5.8, 16 1 4
+// 4.3, 16 1 8 4.1; 512 rows, rank 16: 16 1 1 10.0, 16 1 4 4.7; 4100 rows, rank 16: 16 1 1 14.8, 17 1 1 11.0, 24 1 1 12.0, 32 1 1 12.9;
+// 8196 rows, rank 64: 16 4 1 36, 32 4 1 33, 33 4 1 24, 48 4 1 27, 64 4 1 29.
 struct DownPlan {
-    int rt, jt, parts;
+    int rt, tile, jt, parts;
 };
 inline DownPlan down_plan(int S, int M, int K, int r) {
-    DownPlan best{1, 1, 1};
+    DownPlan best{1, 16, 1, 1};
     double least = 1e30;
     for (int rt = 1; rt <= 4; rt *= 2)
         for (int jt = 1; jt <= rank_groups(r); jt *= 2)
             for (int parts = 1; parts <= kMaxParts; parts *= 2) {
                 if (parts > 1 && ((long long)parts * M > 8192 || K < 512 * parts)) continue;
-                const long long tiles = std::max<long long>((M + 16 * rt - 1) / (16 * rt), std::min(S, M)) * ((r + 16 * jt - 1) / (16 * jt));
-                const long long rounds = (tiles * parts + 255) / 256;
-                const double cost = (double)rounds * (rt + jt) / parts * K * 32 / 40e3 + 0.25 * parts;
+                const long long segments = std::min(S, M), each = (long long)((r + 16 * jt - 1) / (16 * jt)) * parts;
+                const long long tiles = std::max<long long>((M + 16 * rt - 1) / (16 * rt), segments), rounds = (tiles * each + 255) / 256;
+                // as few rows as still leave one workgroup to a compute unit, with a last tile in each segment
+                int tile = 16 * rt;
+                while (tile > 8 * rt + 1 && ((M + tile - 2) / (tile - 1) + segments - 1) * each <= 256) --tile;
+                if (rt == 1) tile = 16;
+                const double cost = (double)rounds * (tile + 16 * jt) / parts * K * 2 / 40e3 + 0.25 * parts;
                 if (cost < least) {
                     least = cost;
-                    best = DownPlan{rt, jt, parts};
+                    best = DownPlan{rt, tile, jt, parts};
                 }
             }
     return best;

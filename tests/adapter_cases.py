@@ -15,7 +15,7 @@ CASES = [
     (40, 4100, 100, 70, 30, "own"), (2000, 130, 70, 20, 9, "many"), (8, 9000, 100, 130, 4, "tokens"),
     (600, 200, 40, 10, 7, "mixed"), (600, 130, 30, 24, 7, "own"), (500, 150, 50, 60, 9, "mixed"), (1300, 4100, 40, 12, 8, "mixed"),
     (1100, 8300, 48, 30, 4, "own"), (9000, 4100, 16, 9, 8, "all"), (50, 30, 20, 40, 3, "mixed"), (70, 24, 40, 20, 4, "own"),
-    (300, 60, 9, 16, 2, "many"),
+    (300, 60, 9, 16, 2, "many"), (1747, 30, 40, 130, 3, "many"), (1422, 40, 30, 256, 3, "mixed"),
 ]
 
 

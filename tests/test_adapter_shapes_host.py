@@ -20,7 +20,7 @@ int main() {
     int S, L, M, K, r;
     while (std::scanf(" %c %d %d %d %d %d", &what, &S, &L, &M, &K, &r) == 6) {
         const DownPlan p = down_plan(S, M, K, r);
-        if (what == 'd') std::printf("%d %d %d %d\n", p.rt, p.jt, p.parts, down_waves(p.rt, p.jt));
+        if (what == 'd') std::printf("%d %d %d %d %d\n", p.rt, p.jt, p.parts, down_waves(p.rt, p.jt), p.tile);
         else if (what == 'u') std::printf("%d\n", up_rows(S, M, K));
         else if (what == 'g' || what == 'w') {                        // (w: an X of float32)
             const GradientForm f = gradient_form_of(what == 'w' ? APB_F32 : APB_BF16, L, M, K, r);
@@ -61,6 +61,7 @@ def test_cases_reach_every_form(ask):
     down = ask([("d", *s) for s in sizes])
     assert {d[:2] for d in down} == {(rt, jt) for rt in (1, 2, 4) for jt in (1, 2, 4)}
     assert {d[2] for d in down} >= {1, 2, 4, 8}
+    assert {(d[0], d[4] < 16 * d[0]) for d in down} == {(1, False), (2, False), (2, True), (4, False), (4, True)}
     # the kernel that streams rows past B, by ranks held (16, 32, 64, 128; above, and in float32, the other one), rows and width
     up = ask([("u", *s) for s in sizes])
     held = lambda r: 0 if r <= 16 else 1 if r <= 32 else 2 if r <= 64 else 4 if r <= 128 else None
@@ -97,8 +98,9 @@ def test_plans_over_the_range(ask):
     g = np.random.default_rng(1)
     sizes = [(int(np.exp(g.uniform(0, 8.3))), int(np.exp(g.uniform(0, 8.3))), int(np.exp(g.uniform(0, 16.6))), int(np.exp(g.uniform(0, 15.2))),
               int(g.integers(1, 257))) for _ in range(2000)] + [(4096, 4096, 1 << 24, 1 << 22, 256), (1, 1, 1, 1, 1)]
-    for (rt, jt, parts, waves), (S, L, M, K, r) in zip(ask([("d", *s) for s in sizes]), sizes):
+    for (rt, jt, parts, waves, tile), (S, L, M, K, r) in zip(ask([("d", *s) for s in sizes]), sizes):
         assert rt in (1, 2, 4) and jt in (1, 2, 4) and 1 <= parts <= 8 and (parts == 1 or K >= 512 * parts)
+        assert tile == 16 if rt == 1 else 8 * rt < tile <= 16 * rt
         assert waves * 2 * (rt + jt) * 1024 <= 160 * 1024 and waves * rt * jt * 1024 <= 160 * 1024      # (LDS)
     for what in "gw":
         for (each, jt, nc, waves), (S, L, M, K, r) in zip(ask([(what, *s) for s in sizes]), sizes):
