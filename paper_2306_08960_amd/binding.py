@@ -1086,15 +1086,19 @@ def _factors(F: torch.Tensor, type_: torch.dtype, name: str) -> Tuple[int, int, 
 
 def _segments(offsets: Optional[torch.Tensor], adapter: Optional[torch.Tensor]):
     """(pointer of offsets, pointer of adapter, number of segments)."""
-    off, S = _experts(offsets)
-    return off, _array(adapter, torch.int32, S, "adapter"), S
+    if offsets is None:
+        return None, _array(adapter, torch.int32, 1, "adapter"), 1
+    S = offsets.numel() - 1
+    if S < 1:
+        raise ValueError("offsets must hold S + 1 int32")
+    return _array(offsets, torch.int32, None, "offsets"), _array(adapter, torch.int32, S, "adapter"), S
 
 
-def _low_rank(T: torch.Tensor, M: int) -> Tuple[int, int, int]:
-    """(pointer, parts, r) of what apb_adapter_down returned."""
-    if T.dim() != 3 or T.shape[1] != M:
+def _low_rank(T: torch.Tensor) -> Tuple[int, int, int, int]:
+    """(pointer, parts, M, r) of what apb_adapter_down returned."""
+    if T.dim() != 3:
         raise ValueError("T must be [parts, M, r]")
-    return _array(T, torch.float32, None, "T"), T.shape[0], T.shape[2]
+    return (_array(T, torch.float32, None, "T"), *T.shape)
 
 
 def apb_adapter_parts(S: int, M: int, K: int, r: int) -> int:
@@ -1118,10 +1122,13 @@ def apb_adapter_down(X: torch.Tensor, A: torch.Tensor, offsets: Optional[torch.T
         if parts == 0:
             raise ApbError(APB_ERR_SHAPE, "apb_adapter_down")
         T = _new(X, (parts, M, r), torch.float32, stream)
-    elif tuple(T.shape) != (parts, M, r):
+        tp = T.data_ptr()
+    elif T.shape != (parts, M, r):
         raise ValueError(f"T must be [{parts}, {M}, {r}]")
-    _check(lib.apb_adapter_down(xp, xt, ldx, ap, off, adp, _array(scale, torch.float32, L, "scale"), S, L, M, K, r,
-                                _array(T, torch.float32, None, "T"), _stream(stream)), "apb_adapter_down")
+    else:
+        tp = _array(T, torch.float32, None, "T")
+    _check(lib.apb_adapter_down(xp, xt, ldx, ap, off, adp, _array(scale, torch.float32, L, "scale"), S, L, M, K, r, tp, _stream(stream)),
+           "apb_adapter_down")
     return T
 
 
@@ -1129,17 +1136,14 @@ def apb_adapter_up(T: torch.Tensor, B: torch.Tensor, Y0: Optional[torch.Tensor] 
                    offsets: Optional[torch.Tensor] = None, adapter: Optional[torch.Tensor] = None,
                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Y = Y0 + T B[a] for B [L, r, N], in B's type (Y0 None: zeros).  Y may be Y0: rows without an adapter are then not touched."""
-    if T.dim() != 3:
-        raise ValueError("T must be [parts, M, r]")
-    M = T.shape[1]
-    tp, parts, r = _low_rank(T, M)
+    tp, parts, M, r = _low_rank(T)
     bp, L, rb, N = _factors(B, B.dtype, "B")
     if rb != r:
         raise ValueError("B must be [L, r, N]")
     off, adp, S = _segments(offsets, adapter)
     p0, ld0 = None, N
     if Y0 is not None:
-        if tuple(Y0.shape) != (M, N) or Y0.dtype != B.dtype:
+        if Y0.shape != (M, N) or Y0.dtype != B.dtype:
             raise ValueError("Y0 must be [M, N] in B's type")
         p0, _, ld0 = _matrix(Y0, "Y0")
     Y, yp, yt, ldy = _result(Y, (M, N), B.dtype, B, "Y", stream)
@@ -1158,10 +1162,7 @@ def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[i
                          adapter: Optional[torch.Tensor] = None, dA: Optional[torch.Tensor] = None,
                          workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """dA[a] = sum over a's rows of T^T X, float32 [L, r, K].  X: [M, K], or its 8-bit form (uint8) with K given."""
-    if T.dim() != 3:
-        raise ValueError("T must be [parts, M, r]")
-    M = T.shape[1]
-    tp, parts, r = _low_rank(T, M)
+    tp, parts, M, r = _low_rank(T)
     if X.dtype == torch.uint8:
         if K is None:
             raise ValueError("K must be given for an 8-bit X")
@@ -1177,9 +1178,12 @@ def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[i
         if L <= 0:
             raise ApbError(APB_ERR_SHAPE, "apb_adapter_gradient")
         dA = _new(T, (L, r, K), torch.float32, stream)
-    elif tuple(dA.shape) != (L, r, K):
+        dp = dA.data_ptr()
+    elif dA.shape != (L, r, K):
         raise ValueError(f"dA must be [{L}, {r}, {K}]")
+    else:
+        dp = _array(dA, torch.float32, None, "dA")
     keep, sp, sb = _scratch(workspace, lib.apb_adapter_gradient_workspace_bytes(L, M, K, r), T, stream)
-    _check(lib.apb_adapter_gradient(tp, parts, xp, xt, ldx, off, adp, S, int(L), M, int(K), r, _array(dA, torch.float32, None, "dA"), sp, sb,
-                                    _stream(stream)), "apb_adapter_gradient")
+    _check(lib.apb_adapter_gradient(tp, parts, xp, xt, ldx, off, adp, S, int(L), M, int(K), r, dp, sp, sb, _stream(stream)),
+           "apb_adapter_gradient")
     return dA
