@@ -202,3 +202,23 @@ def test_example_runs(ex):
     losses, batch, step = ex.main(steps=3)
     assert len(losses) == 3 and all(np.isfinite(losses))
     assert (batch.float() - step.float()).norm() <= NORM[torch.bfloat16] * batch.float().norm()
+
+
+def test_another_device_is_refused(monkeypatch):
+    """Kernels go to the current device: with another one current (as far as the binding is told) no call gets as far as a launch."""
+    from paper_2306_08960_amd import binding as b
+    x, A = torch.randn(4, 64, device="cuda"), torch.randn(1, 3, 64, device="cuda")
+    w, seg = b.apb_mx4_quantize(torch.randn(64, 64, device="cuda")), dict(adapter=torch.zeros(1, dtype=torch.int32, device="cuda"))
+    T, x8, saved, x4 = b.apb_adapter_down(x, A, **seg), b.apb_mx8_quantize(x), b.alloc_mx8(8, 32), b.apb_mx4_quantize(x)
+    calls = [lambda: b.apb_mx8_quantize(x), lambda: b.apb_mx8_dequantize(x8, 4, 64), lambda: b.apb_mx4_gated_gemm(x4, w, 4, 32, 64),
+             lambda: b.apb_mx4_gated_linear(x, w, 32), lambda: b.apb_gated_forward(x, saved=saved),
+             lambda: b.apb_gated_backward(saved, x[:, :32]), lambda: b.apb_adapter_down(x, A, **seg), lambda: b.apb_adapter_up(T, A, **seg),
+             lambda: b.apb_adapter_gradient(T, x, 1, **seg)]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    here = torch.cuda.current_device()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: here + 1)
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
