@@ -533,7 +533,7 @@ int apb_adapter_up(const float* T, int parts, const void* B, int type, const int
  *   dA  DEVICE, [L][r][K] floats, fully overwritten (0 for an adapter without rows).
  *   workspace, workspace_bytes  optional DEVICE scratch (NULL, 0: none), 4-byte aligned: with as many bytes as the function says
  *       (0: no use for any), workgroups share the sum over many rows and join it in a fixed order. */
-size_t apb_adapter_gradient_workspace_bytes(int L, int M, int K, int r);
+size_t apb_adapter_gradient_workspace_bytes(int S, int L, int M, int K, int r);
 int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, long long ldx, const int32_t* offsets,
                          const int32_t* adapter, int S, int L, int M, int K, int r, float* dA, void* workspace,
                          size_t workspace_bytes, void* stream);

@@ -148,7 +148,7 @@ def load() -> ctypes.CDLL:
                        ("apb_adapter_gradient", [vp, ci, vp, ci, ll, vp, vp, ci, ci, ci, ci, ci, vp, vp, ctypes.c_size_t, vp])):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = ci
-    for name, sizes in (("apb_mx8_bytes", 2), ("apb_mx4_gated_linear_scratch_bytes", 6), ("apb_adapter_gradient_workspace_bytes", 4)):
+    for name, sizes in (("apb_mx8_bytes", 2), ("apb_mx4_gated_linear_scratch_bytes", 6), ("apb_adapter_gradient_workspace_bytes", 5)):
         getattr(lib, name).argtypes = [ci] * sizes
         getattr(lib, name).restype = ctypes.c_size_t
     lib.apb_strerror.argtypes = [ci]
@@ -1161,9 +1161,9 @@ def apb_adapter_up(T: torch.Tensor, B: torch.Tensor, Y0: Optional[torch.Tensor] 
     return Y
 
 
-def apb_adapter_gradient_workspace_bytes(L: int, M: int, K: int, r: int) -> int:
+def apb_adapter_gradient_workspace_bytes(S: int, L: int, M: int, K: int, r: int) -> int:
     """Bytes of scratch that apb_adapter_gradient has a use for."""
-    return int(load().apb_adapter_gradient_workspace_bytes(int(L), int(M), int(K), int(r)))
+    return int(load().apb_adapter_gradient_workspace_bytes(int(S), int(L), int(M), int(K), int(r)))
 
 
 def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[int] = None, offsets: Optional[torch.Tensor] = None,
@@ -1191,7 +1191,7 @@ def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[i
         raise ValueError(f"dA must be [{L}, {r}, {K}]")
     else:
         dp = _array(dA, torch.float32, None, "dA")
-    keep, sp, sb = _scratch(workspace, lib.apb_adapter_gradient_workspace_bytes(L, M, K, r), T, stream)
+    keep, sp, sb = _scratch(workspace, lib.apb_adapter_gradient_workspace_bytes(S, L, M, K, r), T, stream)
     _check(lib.apb_adapter_gradient(tp, parts, xp, xt, ldx, off, adp, S, int(L), M, int(K), r, dp, sp, sb, _stream_at(T, stream)),
            "apb_adapter_gradient")
     return dA

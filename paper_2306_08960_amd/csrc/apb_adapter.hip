@@ -537,6 +537,16 @@ __device__ __forceinline__ Span span_of(const Segments& seg, int a, int& its, in
     return Span{rows, min(__builtin_amdgcn_readfirstlane(before), seg.M - rows)};
 }
 
+// The adapter of segment s, if it is the first segment of it; -1 otherwise.
+__device__ __forceinline__ int first_segment_of(const Segments& seg, int s) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int first, count;
+    const int a = rows_of(seg, s, first, count);
+    for (int base = 0; base < s; base += kWave)
+        if (__ballot(base + lane < s && rows_of(seg, base + lane, first, count) == a)) return -1;
+    return __builtin_amdgcn_readfirstlane(a);
+}
+
 // 32 rows of X as they are loaded: of eight of them NC neighbours to a lane.  Rows 8 g + e, for operands that sum over eight rows; an X of
 // float32 goes into products over four rows, row 4 e + g of a lane.
 template <int XT, int NC>
@@ -612,24 +622,56 @@ __device__ __forceinline__ void column(const Rows32<XT, NC>& x, int n, Eight<APB
     }
 }
 
+// The sums of adapters without rows, n each, in pieces of kPiece: part `part` of `parts`.
+__device__ __forceinline__ void clear_adapters(const Segments& seg, long long n, int part, int parts, float* dA) {
+    constexpr int kPiece = 4096;
+    const int pieces = (int)((n + kPiece - 1) / kPiece);
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    int known = -1;
+    bool empty = false;
+    const long long all = (long long)pieces * seg.L, each = (all + parts - 1) / parts;
+    for (long long u = part * each; u < std::min(all, (part + 1) * each); ++u) {
+        const int a = (int)(u / pieces);
+        if (a != known) {
+            int its, first, count;
+            empty = span_of(seg, a, its, first, count).rows == 0;
+            known = a;
+        }
+        if (!empty) continue;
+        const long long from = (u - (long long)a * pieces) * kPiece, end = std::min<long long>(from + kPiece, n);
+        for (long long k = from + 4 * threadIdx.x; k < end; k += 4 * blockDim.x) store4(dA, APB_F32, a * n + k, zero, (int)(end - k));
+    }
+}
+
 // WHOLE: K is 16 * NC or more; the last workgroup's columns then end with the row's, and those that two workgroups have get the same
 // values twice.  (Rows of 8 bits are padded, and their columns stay in blocks.)
 //
-// A workgroup takes one adapter, 16 * JT ranks, 16 * NC columns, and `each` of the adapter's rows, counted through all of its segments,
-// whose numbers it lists in LDS; its waves take 32 of them at a time in turn, by themselves, the next ones under way, and join their sums in
-// LDS.  T, its parts added up, comes to registers in the order of the operand and is split there into three bfloat16 parts (an X of
-// float32 goes with T as it is through float32 products); X is transposed in registers.  With waves that share a tile of rows in LDS and
-// each take columns of their own, every wave waits at barriers for the slowest load, and an adapter's rows have to be shared out much
-// sooner: 16384 rows of 8192, rank 32, bfloat16 65 us and now 62 (268 MB are 52); 8196 of 4096, rank 64 43 and 35 (67 MB are 13; the
-// splitting of T by each of 64 workgroups is most of it); 4100 of 4096, rank 16 16 and 11.7 (34 MB are 7); 512 of 4096, rank 32 13.4 and 7.0.
+// A workgroup takes one adapter (by_segment: that of a segment), 16 * JT ranks, 16 * NC columns, and `each` of the adapter's rows, counted
+// through all of its segments, whose numbers it lists in LDS; its waves take 32 of them at a time in turn, by themselves, the next ones under
+// way, and join their sums in LDS.  T, its parts added up, comes to registers in the order of the operand and is split there into three
+// bfloat16 parts (an X of float32 goes with T as it is through float32 products); X is transposed in registers.  With waves that share a
+// tile of rows in LDS and each take columns of their own, every wave waits at barriers for the slowest load, and an adapter's rows have
+// to be shared out much sooner: 16384 rows of 8192, rank 32, bfloat16 65 us and now 62 (268 MB are 52); 8196 of 4096, rank 64 43 and 35 (67 MB are 13; T is
+// split anew for each of 64 groups of columns); 4100 of 4096, rank 16 16 and 11.7 (34 MB are 7); 512 of 4096, rank 32 13.4 and 7.0.
 template <int XT, int JT, int NC, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float* __restrict__ T, int parts, const void* __restrict__ X,
                                                                     long long ldx, Mx8 x8, Segments seg, int K, int r, int rank_tiles,
-                                                                    int each, float* __restrict__ dA, float* __restrict__ shared) {
+                                                                    int by_segment, int each, float* __restrict__ dA,
+                                                                    float* __restrict__ shared) {
     constexpr int kChunk = 32, kRanks = 16 * JT;
     __shared__ f32x4 sums[WAVES][JT * NC][kWave];
     __shared__ int list[kList + kChunk];
-    const int a = blockIdx.y / rank_tiles, j0 = blockIdx.y % rank_tiles * kRanks;
+    int a = blockIdx.y / rank_tiles;
+    const int j0 = blockIdx.y % rank_tiles * kRanks;
+    if (by_segment) {
+        if (a >= seg.S) {
+            if (blockIdx.z == 0) clear_adapters(seg, (long long)r * K, (blockIdx.y - seg.S * rank_tiles) * gridDim.x + blockIdx.x,
+                                                (gridDim.y - seg.S * rank_tiles) * gridDim.x, dA);
+            return;
+        }
+        a = first_segment_of(seg, a);
+        if (a < 0) return;
+    }
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
     const int c0 = XT == APB_MX8 ? blockIdx.x * 16 * NC : WHOLE ? min((int)blockIdx.x * 16 * NC, K - 16 * NC) : 0, c = c0 + NC * i;
     int its, first, count;
@@ -752,9 +794,10 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float*
 }
 
 // The slices of the adapters that have several, added up in order.
-__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int each, long long n,
-                                                           float* __restrict__ dA) {
-    const int a = blockIdx.y;
+__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int by_segment, int each,
+                                                           long long n, float* __restrict__ dA) {
+    const int a = by_segment ? first_segment_of(seg, blockIdx.y) : blockIdx.y;
+    if (a < 0) return;
     int its, first, count;
     const Span span = span_of(seg, a, its, first, count);
     if (span.rows <= each) return;
@@ -863,10 +906,13 @@ template <int XT, int JT, int NC, int WAVES>
 void gradient_form(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int each,
                    float* dA, float* shared, hipStream_t s) {
     const int rank_tiles = (r + 16 * JT - 1) / (16 * JT);
-    const dim3 grid((unsigned)((K + 16 * NC - 1) / (16 * NC)), (unsigned)(seg.L * rank_tiles), (unsigned)((seg.M + each - 1) / each));
+    const int by_segment = gradient_by_segment(seg.S, seg.L, K, r);
+    const unsigned columns = (unsigned)((K + 16 * NC - 1) / (16 * NC));
+    const dim3 grid(columns, by_segment ? seg.S * rank_tiles + (1024 + columns - 1) / columns : seg.L * rank_tiles,
+                    (unsigned)((seg.M + each - 1) / each));
     auto launch = [&](auto whole) {
         hipLaunchKernelGGL((k_adapter_gradient<XT, JT, NC, WAVES, decltype(whole)::value>), grid, dim3(WAVES * kWave), 0, s, T, parts, X, ldx, x8,
-                           seg, K, r, rank_tiles, each, dA, shared);
+                           seg, K, r, rank_tiles, by_segment, each, dA, shared);
     };
     if constexpr (XT == APB_MX8 || NC == 8) launch(std::true_type{});
     else if (K >= 16 * NC) launch(std::true_type{});
@@ -875,7 +921,7 @@ void gradient_form(const float* T, int parts, const void* X, long long ldx, cons
 template <int XT>
 void gradient(const float* T, int parts, const void* X, long long ldx, const Mx8& x8, const Segments& seg, int K, int r, int each,
               float* dA, float* shared, hipStream_t s) {
-    const GradientForm form = gradient_form_of(XT, seg.L, seg.M, K, r);
+    const GradientForm form = gradient_form_of(XT, seg.S, seg.L, seg.M, K, r);
     auto with = [&](auto ranks) {
         constexpr int kJt = decltype(ranks)::value;
         if (form.waves == 1) return gradient_form<XT, kJt, 4, 1>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
@@ -936,10 +982,10 @@ int apb_adapter_up(const float* T, int parts, const void* B, int type, const int
     return APB_OK;
 }
 
-size_t apb_adapter_gradient_workspace_bytes(int L, int M, int K, int r) {
+size_t apb_adapter_gradient_workspace_bytes(int S, int L, int M, int K, int r) {
     static const int32_t some = 0;
-    if (bad_adapter(1, L, M, K, r, &some, &some)) return 0;
-    const int each = gradient_rows(L, M, K, r);
+    if (bad_adapter(S, L, M, K, r, &some, &some)) return 0;
+    const int each = gradient_rows(S, L, M, K, r);
     return M > each ? (size_t)places_of_slices(M, each) * r * K * sizeof(float) : 0;
 }
 
@@ -956,9 +1002,9 @@ int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, l
         return APB_ERR_ALIGN;
     const Segments seg{offsets, adapter, S, L, M};
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const size_t need = apb_adapter_gradient_workspace_bytes(L, M, K, r);
+    const size_t need = apb_adapter_gradient_workspace_bytes(S, L, M, K, r);
     const bool join = need != 0 && workspace != nullptr && workspace_bytes >= need;
-    const int each = join ? gradient_rows(L, M, K, r) : M;
+    const int each = join ? gradient_rows(S, L, M, K, r) : M;
     float* shared = static_cast<float*>(workspace);
     const Mx8 x8 = mx8_view(X, M, K);
     if (x_type == APB_F32) gradient<APB_F32>(T, parts, X, ldx, x8, seg, K, r, each, dA, shared, s);
@@ -968,8 +1014,10 @@ int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, l
     APB_HIP(hipGetLastError());
     if (join) {
         const long long n = (long long)r * K;
-        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096), (unsigned)L);
-        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, each, n, dA);
+        const int by_segment = gradient_by_segment(S, L, K, r);
+        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096),
+                        (unsigned)(by_segment ? S : L));
+        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, by_segment, each, n, dA);
         APB_HIP(hipGetLastError());
     }
     return APB_OK;

@@ -29,18 +29,25 @@ inline int up_rows(int S, int M, int N) {
     return rows;
 }
 
-// Columns of X that all adapters' gradients make, in groups of 64, times the groups of ranks: workgroups, were the rows not shared.
-inline long long gradient_groups(int L, int K, int r) {
+// Columns of X that the gradients of `adapters` make, in groups of 64, times the groups of ranks: workgroups, were the rows not shared.
+inline long long gradient_groups(int adapters, int K, int r) {
     const int ranks = 16 * rank_groups(r);
-    return (long long)((K + 63) / 64) * L * ((r + ranks - 1) / ranks);
+    return (long long)((K + 63) / 64) * adapters * ((r + ranks - 1) / ranks);
 }
+// No more adapters than these have rows.
+inline int active_adapters(int S, int L) { return std::min(S, L); }
+// The gradient's workgroups go by adapter, or, where many adapters cannot have rows, by segment (the first of its adapter), and some that
+// only clear.  us by adapter and by segment (clearing alone): 4100 rows of 4096 in four segments, 64 adapters of rank 16 24 and 19 (5), of
+// rank 64 60 and 34 (11), 1024 of rank 16 255 and 53 (34); 64 segments of a row, 512 adapters 31 and 25 (19).
+inline bool gradient_by_segment(int S, int L, int K, int r) { return L > S && gradient_groups(L - S, K, r) >= 1024; }
 // Rows of an adapter to a workgroup of its gradient.  Where one workgroup for each of those fills the compute units, more than 8192 and
 // four times the average are shared out, and otherwise so many that there is a workgroup to each unit, but at least 256 (sharing costs a
 // launch and 4 us).  bfloat16, us: 4100 rows of 4096, rank 16, four adapters (256 groups) not shared 11.7, in pieces of 2048 rows 14.2, of
 // 1024 17.7; one adapter (64 groups) 27.0, 18.4, 16.5; 2000 rows of 1024, rank 64, one adapter (16 groups) not shared 39, in pieces of 1024
 // 25, of 512 16.5, of 256 13.1.
-inline int gradient_rows(int L, int M, int K, int r) {
-    const long long mean = (M + L - 1) / L, slices = 256 / gradient_groups(L, K, r);
+inline int gradient_rows(int S, int L, int M, int K, int r) {
+    const int active = active_adapters(S, L);
+    const long long mean = (M + active - 1) / active, slices = 256 / gradient_groups(active, K, r);
     return (int)(slices <= 1 ? std::max(8192LL, 4 * mean) : std::max(256LL, (mean / slices + 31) / 32 * 32));
 }
 // Groups of 16 ranks, columns to a lane and waves of such a workgroup.  A wave takes 32 rows at a time: as many waves as an adapter has
@@ -51,11 +58,11 @@ inline int gradient_rows(int L, int M, int K, int r) {
 struct GradientForm {
     int jt, nc, waves;
 };
-inline GradientForm gradient_form_of(int x_type, int L, int M, int K, int r) {
-    const int jt = rank_groups(r), chunks = std::max((M / L + 31) / 32, (M + 255) / 256);
+inline GradientForm gradient_form_of(int x_type, int S, int L, int M, int K, int r) {
+    const int active = active_adapters(S, L), jt = rank_groups(r), chunks = std::max((M / active + 31) / 32, (M + 255) / 256);
     const bool wide = x_type == APB_F32;                         // (its operands take twice the registers)
     const int waves = chunks > 4 && !(wide && jt == 4) ? 8 : chunks > 1 ? 4 : 1;
-    return GradientForm{jt, waves == 8 && !wide && jt <= 2 && K >= 128 && gradient_groups(L, K, r) >= 512 ? 8 : 4, waves};
+    return GradientForm{jt, waves == 8 && !wide && jt <= 2 && K >= 128 && gradient_groups(active, K, r) >= 512 ? 8 : 4, waves};
 }
 
 // Groups of rows, rows, and groups of ranks to a workgroup of down, and parts of K: what takes least by a count of the bytes that the busiest

@@ -23,8 +23,8 @@ int main() {
         if (what == 'd') std::printf("%d %d %d %d %d\n", p.rt, p.jt, p.parts, down_waves(p.rt, p.jt), p.tile);
         else if (what == 'u') std::printf("%d\n", up_rows(S, M, K));
         else if (what == 'g' || what == 'w') {                        // (w: an X of float32)
-            const GradientForm f = gradient_form_of(what == 'w' ? APB_F32 : APB_BF16, L, M, K, r);
-            std::printf("%d %d %d %d\n", gradient_rows(L, M, K, r), f.jt, f.nc, f.waves);
+            const GradientForm f = gradient_form_of(what == 'w' ? APB_F32 : APB_BF16, S, L, M, K, r);
+            std::printf("%d %d %d %d %d\n", gradient_rows(S, L, M, K, r), f.jt, f.nc, f.waves, gradient_by_segment(S, L, K, r));
         }
         else std::printf("%d %lld\n", place_of_slices(S, L), places_of_slices(M, L));      // (S: rows before, L: rows to a slice)
     }
@@ -70,10 +70,11 @@ def test_cases_reach_every_form(ask):
     assert {rows[0] for rows in up} == {16, 32, 64}
     assert {(s[3] % 128 == 0, s[3] < 8, s[3] < 128) for s in sizes} == {(True, False, False), (False, False, False), (False, True, True), (False, False, True)}
     grad, wide = ask([("g", *s) for s in sizes]), ask([("w", *s) for s in sizes])
-    assert {g[1:] for g in grad} == {(j, 4, w) for j in (1, 2, 4) for w in (1, 4, 8)} | {(j, 8, 8) for j in (1, 2)}
-    assert {g[1:] for g in wide} == {(j, 4, w) for j in (1, 2, 4) for w in (1, 4, 8) if (j, w) != (4, 8)}
+    assert {g[1:4] for g in grad} == {(j, 4, w) for j in (1, 2, 4) for w in (1, 4, 8)} | {(j, 8, 8) for j in (1, 2)}
+    assert {g[1:4] for g in wide} == {(j, 4, w) for j in (1, 2, 4) for w in (1, 4, 8) if (j, w) != (4, 8)}
     assert {(g[1], g[3], s[3] < 64) for s, g in zip(sizes, grad)} == {(j, w, tiny) for j in (1, 2, 4) for w in (1, 4, 8) for tiny in (False, True)}
     assert {(g[1], s[2] > g[0]) for s, g in zip(sizes, grad)} == {(j, shared) for j in (1, 2, 4) for shared in (False, True)}
+    assert {(g[4], s[2] > g[0]) for s, g in zip(sizes, grad)} == {(b, shared) for b in (0, 1) for shared in (False, True)}
     assert any(s[2] > g[0] and g[2] == 8 for s, g in zip(sizes, grad))
     assert any(s[3] % 128 and g[2] == 8 for s, g in zip(sizes, grad))
     assert any(s[2] > 1024 and s[1] == 1 for s in sizes)             # (more rows of one adapter than a list holds, without a workspace)
@@ -103,7 +104,7 @@ def test_plans_over_the_range(ask):
         assert tile == 16 if rt == 1 else 8 * rt < tile <= 16 * rt
         assert waves * 2 * (rt + jt) * 1024 <= 160 * 1024 and waves * rt * jt * 1024 <= 160 * 1024      # (LDS)
     for what in "gw":
-        for (each, jt, nc, waves), (S, L, M, K, r) in zip(ask([(what, *s) for s in sizes]), sizes):
+        for (each, jt, nc, waves, by_segment), (S, L, M, K, r) in zip(ask([(what, *s) for s in sizes]), sizes):
             assert 256 <= each and -(-M // each) <= 65535 and 2 * M // each < 1 << 31 and L * -(-r // (16 * jt)) <= 65535
             assert waves * jt * nc * 1024 + (1024 + 32) * 4 <= 160 * 1024      # (LDS)
             assert nc == 4 or K >= 128                                         # (no form for fewer columns)

@@ -198,4 +198,4 @@ def test_adapter_refusals(b):
     assert up(Y0=P, ld0=63) == b.APB_ERR_SHAPE and up(Y0=P, ld0=65, X=P) == b.APB_ERR_SHAPE
     assert gradient(t=3, X=ODD) == b.APB_ERR_ALIGN and gradient(A=ODD) == b.APB_ERR_ALIGN and gradient(ws=ODD) == b.APB_ERR_ALIGN
     assert b.apb_adapter_parts(0, 4, 4, 4) == 0 and b.apb_adapter_parts(1, 1, 1, 1) == 1 and b.apb_adapter_parts(1, 1, 1, 257) == 0
-    assert b.apb_adapter_gradient_workspace_bytes(0, 4, 4, 4) == 0 and b.apb_adapter_gradient_workspace_bytes(1, 1, 1, 1) == 0
+    assert b.apb_adapter_gradient_workspace_bytes(1, 0, 4, 4, 4) == 0 and b.apb_adapter_gradient_workspace_bytes(1, 1, 1, 1, 1) == 0
