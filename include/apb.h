@@ -452,7 +452,7 @@ int apb_mx8_dequantize(const void* mx8, int rows, int K, int type, void* X, long
  *      APB_SILU   x * s(x)                                            s(z) = 1 / (1 + e^-z)
  *      APB_GELU   x * s(2 sqrt(2/pi) (x + 0.044715 x^3))              (the same as x/2 (1 + tanh(sqrt(2/pi) (x + ...))))
  *      APB_RELU   max(x, 0)
- * in float32; at the infinities their limits, NaN for NaN.  An s below 2^-126 counts as 0.
+ * in float32; at the infinities their limits, NaN for NaN (act' likewise).  An s below 2^-126 counts as 0.
  *
  * A gated layer has ONE 4-bit matrix of weights, for every expert first the N rows of the gate, then the N rows of the up
  * projection (E * 2N rows of K): what the gradients of the 4-bit products take with 2N in the place of N, and [dG | dU]

@@ -45,7 +45,7 @@ def act(x, kind):
     """(act(x), act'(x), |z|, z'): z the argument of the sigmoid."""
     x = np.asarray(x, dtype=np.float64)
     if kind == "relu":
-        return np.where(x < 0, 0.0, x), (x > 0).astype(np.float64), np.zeros_like(x), np.zeros_like(x)
+        return np.where(x < 0, 0.0, x), np.where(np.isnan(x), x, x > 0), np.zeros_like(x), np.zeros_like(x)
     with np.errstate(over="ignore", invalid="ignore"):
         z, dz = (x, np.ones_like(x)) if kind == "silu" else (2 * ROOT * (x + 0.044715 * x ** 3), 2 * ROOT * (1 + 0.134145 * x * x))
         small = np.exp(-np.abs(z))

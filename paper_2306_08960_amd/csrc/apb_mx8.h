@@ -79,9 +79,9 @@ __device__ __forceinline__ float act_value(const Act& k, float x) {
     return act_times(x, act_sigmoid<KIND>(k, x, KIND == APB_SILU ? 0.0f : act_square(x)));
 }
 __device__ __forceinline__ void act_both(const Act& k, float x, float& value, float& slope) {
-    if (k.relu) {
+    if (k.relu) {                                                // (a NaN is neither below nor above: both stay NaN)
         value = x < 0.0f ? 0.0f : x;
-        slope = x > 0.0f ? 1.0f : 0.0f;
+        slope = x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
         return;
     }
     const float sq = act_square(x), s = act_sigmoid(k, x, sq);

@@ -1,0 +1,45 @@
+"""Gated blocks, 8-bit checkpoints and adapters: what NaN, infinities and memory beside the operands may reach, and the precision that
+the header promises for single terms."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TYPE = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def b():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2306_08960_amd import binding
+    binding.load()
+    return binding
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_nan_gate_reaches_its_gradients(b, t, kind):
+    """A gate that is NaN has NaN gradients, and nobody else has: from the float matrix one value, from 8 bits its block."""
+    M, N = 5, 70
+    g = torch.Generator(device="cuda").manual_seed(3)
+    gu = torch.randn(M, 2 * N, generator=g, device="cuda").to(TYPE[t])
+    dy = torch.ones(M, N, device="cuda").to(TYPE[t])
+    gu[1, 5], gu[3, 66] = float("nan"), float("nan")
+    saved = b.alloc_mx8(2 * M, N)
+    b.apb_gated_forward(gu, kind, saved=saved)
+    one = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    one[1, 5] = one[3, 66] = True
+    block = torch.zeros_like(one)
+    block[1, :32] = block[3, 64:] = True
+    for source, want in ((gu, one), (saved, block)):
+        y = torch.empty(M, N, dtype=TYPE[t], device="cuda")
+        d = b.apb_gated_backward(source, dy, kind, Y=y)
+        for got in (y, d[:, :N], d[:, N:]):
+            assert torch.equal(torch.isnan(got), want)
+    gu[1, 5] = gu[3, 66] = 0.0
+    gu[2, N + 7] = float("nan")                                      # an up projection that is NaN: Y and dG
+    one[:] = False
+    one[2, 7] = True
+    d = b.apb_gated_backward(gu, dy, kind, Y=y)
+    assert torch.equal(torch.isnan(y), one) and torch.equal(torch.isnan(d[:, :N]), one) and bool(torch.isfinite(d[:, N:]).all())
