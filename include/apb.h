@@ -510,9 +510,11 @@ int apb_gated_backward(const void* GU, int gu_type, long long ldgu, const void* 
  *
  * T is float32, as `parts` sums whose total it is ([parts][M][r], parts = apb_adapter_parts(), fixed by the sizes): where rows
  * are few, workgroups share a row's sum, and whoever reads T adds the parts up, in order.  X, A, Y0, Y are of one `type`;
- * products are exact or float32, sums float32 in a fixed order (repeating a call repeats its bits); Y is rounded once.  With a 16-bit `type`, T enters Y as two 16-bit parts, which is off by 2^-16 of each
- * term (and for APB_F16 by up to 2^-39 of the largest |T| of the row), and the gradients as three (2^-24).  Rows and factors that
- * a result does not depend on do not reach it, whatever they hold; an infinity among those it depends on may come out as a NaN.
+ * products are exact or float32, sums float32 in a fixed order (repeating a call repeats its bits); Y is rounded once.
+ * With a 16-bit `type`, T enters Y as two 16-bit parts, which is off by 2^-16 of each term (APB_F16: 2^-22, and by up to 2^-39 of the
+ * largest |T| of the row), and the gradients as three (2^-24).  Where |T| is below 2^-109, bfloat16 parts end at 2^-133, and T is off by
+ * up to 2^-134.  Rows and factors that a result does not depend on do not reach it, whatever they hold; an infinity among those it
+ * depends on may come out as a NaN.
  *   r <= APB_ADAPTER_MAX_R, S <= APB_ADAPTER_MAX_S, L <= APB_ADAPTER_MAX_L, K, N <= 2^22, M <= 2^24. */
 #define APB_ADAPTER_MAX_R 256
 #define APB_ADAPTER_MAX_S 4096
