@@ -175,12 +175,18 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return int(stream.cuda_stream)
 
 
-def _stream_at(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
-    """_stream for a call that reads `t`, which has to be on the current device: kernels are launched there."""
+def _stream_at(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> int:
+    """_stream for a call with these operands (None: not given), all of which have to be on the current device, like the stream: that
+    is where kernels are launched."""
     here = torch._C._cuda_getDevice()
-    if t.get_device() != here:
-        raise ValueError("the tensors must be on the current device")
-    return torch._C._cuda_getCurrentRawStream(here) if stream is None else int(stream.cuda_stream)
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("the tensors must be on the current device")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(here)
+    if stream.device_index != here:
+        raise ValueError("the stream must be one of the current device")
+    return int(stream.cuda_stream)
 
 
 def _dev_ptr(t: torch.Tensor, dtype: torch.dtype, name: str) -> int:
@@ -976,14 +982,14 @@ def apb_mx8_quantize(X: torch.Tensor, mx8: Optional[torch.Tensor] = None,
         if nbytes == 0:
             raise ApbError(APB_ERR_SHAPE, "apb_mx8_bytes")
         mx8 = _new(X, nbytes, torch.uint8, stream)
-    _check(load().apb_mx8_quantize(ptr, t, ld, rows, K, _mx8_ptr(mx8, rows, K, "mx8"), _stream_at(X, stream)), "apb_mx8_quantize")
+    _check(load().apb_mx8_quantize(ptr, t, ld, rows, K, _mx8_ptr(mx8, rows, K, "mx8"), _stream_at(stream, X, mx8)), "apb_mx8_quantize")
     return mx8
 
 
 def apb_mx8_dequantize(mx8: torch.Tensor, rows: int, K: int, dtype: torch.dtype = torch.float32,
                        X: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     X, ptr, t, ld = _result(X, (rows, K), dtype, mx8, "X", stream)
-    _check(load().apb_mx8_dequantize(_mx8_ptr(mx8, rows, K, "mx8"), int(rows), int(K), t, ptr, ld, _stream_at(mx8, stream)),
+    _check(load().apb_mx8_dequantize(_mx8_ptr(mx8, rows, K, "mx8"), int(rows), int(K), t, ptr, ld, _stream_at(stream, mx8, X)),
            "apb_mx8_dequantize")
     return X
 
@@ -1010,7 +1016,7 @@ def apb_mx4_gated_gemm(A: torch.Tensor, W: torch.Tensor, M: int, N: int, K: int,
     act = _activation(activation)
     Y, ptr, t, ld = _result(Y, (M, N), dtype, A, "Y", stream)
     _check(load().apb_mx4_gated_gemm(_mx4_ptr(A, M, K, "A"), _mx4_ptr(W, E * 2 * N, K, "W"), off, E, int(M), int(N), int(K), act, t, ptr,
-                                     ld, _mx8_ptr(saved, 2 * M, N, "saved"), _stream_at(A, stream)), "apb_mx4_gated_gemm")
+                                     ld, _mx8_ptr(saved, 2 * M, N, "saved"), _stream_at(stream, A, W, offsets, Y, saved)), "apb_mx4_gated_gemm")
     return Y
 
 
@@ -1040,8 +1046,8 @@ def apb_mx4_gated_linear(X: torch.Tensor, W: torch.Tensor, N: int, activation: s
         sp = scratch.data_ptr() if need else wp                       # (none needed: not touched, but not NULL)
     Y, yp, yt, ldy = _result(Y, (M, N), dtype or X.dtype, X, "Y", stream)
     _check(lib.apb_mx4_gated_linear(xp, xt, ldx, rows_in, _array(rows_from, torch.int32, M, "rows_from"), wp, off, E, M, int(N), K, act,
-                                    sp if need else wp, yt, yp, ldy, _mx8_ptr(saved, 2 * M, N, "saved"), _stream_at(X, stream)),
-           "apb_mx4_gated_linear")
+                                    sp if need else wp, yt, yp, ldy, _mx8_ptr(saved, 2 * M, N, "saved"),
+                                    _stream_at(stream, X, W, rows_from, offsets, scratch, Y, saved)), "apb_mx4_gated_linear")
     return Y
 
 
@@ -1056,7 +1062,8 @@ def apb_gated_forward(GU: torch.Tensor, activation: str = "silu", Y: Optional[to
     Y, yp, yt, ldy = _result(Y, (M, N), GU.dtype, GU, "Y", stream)
     if yt != gt:
         raise TypeError("Y must have GU's type")
-    _check(load().apb_gated_forward(gp, gt, ldg, M, N, act, yp, ldy, _mx8_ptr(saved, 2 * M, N, "saved"), _stream_at(GU, stream)), "apb_gated_forward")
+    _check(load().apb_gated_forward(gp, gt, ldg, M, N, act, yp, ldy, _mx8_ptr(saved, 2 * M, N, "saved"), _stream_at(stream, GU, Y, saved)),
+           "apb_gated_forward")
     return Y
 
 
@@ -1079,7 +1086,7 @@ def apb_gated_backward(GU: torch.Tensor, dY: torch.Tensor, activation: str = "si
         Y, yp, yt, ldy = _result(Y, (M, N), dY.dtype, dY, "Y", stream)
     if ot != dt or yt != dt:
         raise TypeError("dGU and Y must have dY's type")
-    _check(load().apb_gated_backward(gp, gt, ldg, dp, dt, ldd, M, N, act, op, ldo, yp, ldy, _stream_at(dY, stream)), "apb_gated_backward")
+    _check(load().apb_gated_backward(gp, gt, ldg, dp, dt, ldd, M, N, act, op, ldo, yp, ldy, _stream_at(stream, GU, dY, dGU, Y)), "apb_gated_backward")
     return dGU
 
 
@@ -1135,8 +1142,8 @@ def apb_adapter_down(X: torch.Tensor, A: torch.Tensor, offsets: Optional[torch.T
         raise ValueError(f"T must be [{parts}, {M}, {r}]")
     else:
         tp = _array(T, torch.float32, None, "T")
-    _check(lib.apb_adapter_down(xp, xt, ldx, ap, off, adp, _array(scale, torch.float32, L, "scale"), S, L, M, K, r, tp, _stream_at(X, stream)),
-           "apb_adapter_down")
+    _check(lib.apb_adapter_down(xp, xt, ldx, ap, off, adp, _array(scale, torch.float32, L, "scale"), S, L, M, K, r, tp,
+                                _stream_at(stream, X, A, offsets, adapter, scale, T)), "apb_adapter_down")
     return T
 
 
@@ -1157,7 +1164,8 @@ def apb_adapter_up(T: torch.Tensor, B: torch.Tensor, Y0: Optional[torch.Tensor] 
     Y, yp, yt, ldy = _result(Y, (M, N), B.dtype, B, "Y", stream)
     if Y.dtype != B.dtype:
         raise TypeError("Y must have B's type")
-    _check(load().apb_adapter_up(tp, parts, bp, yt, off, adp, S, L, M, N, r, p0, ld0, yp, ldy, _stream_at(T, stream)), "apb_adapter_up")
+    _check(load().apb_adapter_up(tp, parts, bp, yt, off, adp, S, L, M, N, r, p0, ld0, yp, ldy,
+                                 _stream_at(stream, T, B, Y0, Y, offsets, adapter)), "apb_adapter_up")
     return Y
 
 
@@ -1192,6 +1200,6 @@ def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[i
     else:
         dp = _array(dA, torch.float32, None, "dA")
     keep, sp, sb = _scratch(workspace, lib.apb_adapter_gradient_workspace_bytes(S, L, M, K, r), T, stream)
-    _check(lib.apb_adapter_gradient(tp, parts, xp, xt, ldx, off, adp, S, int(L), M, int(K), r, dp, sp, sb, _stream_at(T, stream)),
-           "apb_adapter_gradient")
+    _check(lib.apb_adapter_gradient(tp, parts, xp, xt, ldx, off, adp, S, int(L), M, int(K), r, dp, sp, sb,
+                                    _stream_at(stream, T, X, offsets, adapter, dA, keep)), "apb_adapter_gradient")
     return dA

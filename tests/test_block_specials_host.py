@@ -1,11 +1,86 @@
 """Gated blocks, 8-bit checkpoints and adapters without a GPU: NaN in the oracle, sizes at the limits, operands of another device."""
+import os
+import types
+
 import numpy as np
 import pytest
+import torch
 
 from oracle import block_oracle as o
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2306_08960_amd", "libapb.so")
+needs_lib = pytest.mark.skipif(not os.path.exists(LIB), reason="libapb.so not built")
 
 
 @pytest.mark.parametrize("kind", ["silu", "gelu", "relu"])
 def test_nan_has_no_value_and_no_slope(kind):
     v, d, _, _ = o.act(np.array([np.nan, 1.0, -1.0]), kind)
     assert np.isnan(v[0]) and np.isnan(d[0]) and np.isfinite(v[1:]).all() and np.isfinite(d[1:]).all()
+
+
+# ---- operands of another device: kernels are launched on the current one --------------------------------------------------
+
+class _On(torch.Tensor):
+    """Host memory that says it is on a GPU: nothing here gets as far as a launch."""
+    where = 0
+    is_cuda = True
+
+    def get_device(self):
+        return self.where
+
+
+def _on(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(_On)
+
+
+def _operands():
+    """Every entry point with every tensor it takes, by name, and its other arguments."""
+    M, N, K, r, L, S = 40, 64, 96, 4, 2, 3
+    bytes_, ints = (lambda n: _on(n, dtype=torch.uint8)), (lambda n: _on(n, dtype=torch.int32))
+    mx4, mx8 = (lambda rows, k: bytes_(rows * (k + 255) // 256 * 136)), (lambda rows, k: bytes_(rows * (k + 31) // 32 * 33))
+    seg = dict(offsets=ints(S + 1), adapter=ints(S))
+    T = _on(1, M, r, dtype=torch.float32)
+    return [
+        ("apb_mx8_quantize", dict(X=_on(M, K), mx8=mx8(M, K)), {}),
+        ("apb_mx8_dequantize", dict(mx8=mx8(M, K), X=_on(M, K)), dict(rows=M, K=K)),
+        ("apb_mx4_gated_gemm", dict(A=mx4(M, K), W=mx4(2 * 2 * N, K), Y=_on(M, N), offsets=ints(3), saved=mx8(2 * M, N)), dict(M=M, N=N, K=K)),
+        ("apb_mx4_gated_linear", dict(X=_on(M, K), W=mx4(2 * 2 * N, K), Y=_on(M, N), rows_from=ints(M), offsets=ints(3), scratch=mx4(M, K),
+                                      saved=mx8(2 * M, N)), dict(N=N)),
+        ("apb_gated_forward", dict(GU=_on(M, 2 * N), Y=_on(M, N), saved=mx8(2 * M, N)), {}),
+        ("apb_gated_backward", dict(GU=_on(M, 2 * N), dY=_on(M, N), dGU=_on(M, 2 * N), Y=_on(M, N)), {}),
+        ("apb_gated_backward", dict(GU=mx8(2 * M, N), dY=_on(M, N), dGU=_on(M, 2 * N), Y=_on(M, N)), {}),
+        ("apb_adapter_down", dict(X=_on(M, K), A=_on(L, r, K), scale=_on(L, dtype=torch.float32), T=T, **seg), {}),
+        ("apb_adapter_up", dict(T=T, B=_on(L, r, N), Y0=_on(M, N), Y=_on(M, N), **seg), {}),
+        ("apb_adapter_gradient", dict(T=T, X=_on(M, K), dA=_on(L, r, K, dtype=torch.float32), workspace=bytes_(64), **seg), dict(L=L)),
+        ("apb_adapter_gradient", dict(T=T, X=mx8(M, K), dA=_on(L, r, K, dtype=torch.float32), workspace=bytes_(64), **seg), dict(L=L, K=K)),
+    ]
+
+
+@needs_lib
+@pytest.mark.parametrize("at", range(len(_operands())), ids=lambda i: f"{_operands()[i][0]}-{i}")
+def test_no_operand_is_taken_from_another_device(monkeypatch, at):
+    from paper_2306_08960_amd import binding
+    real, launched = binding.load(), []
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith("_bytes") or name.endswith("_parts"):
+                return getattr(real, name)
+            return lambda *args: launched.append(name) or 0
+    monkeypatch.setattr(binding, "load", Library)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    name, tensors, sizes = _operands()[at]
+    call = getattr(binding, name)
+    call(**tensors, **sizes)
+    call(**tensors, **sizes, stream=types.SimpleNamespace(cuda_stream=7, device_index=0))
+    assert launched == [name] * 2
+    for which in tensors:
+        other = tensors[which].clone()
+        other.where = 1
+        with pytest.raises(ValueError, match="current device"):
+            call(**{**tensors, which: other}, **sizes)
+    with pytest.raises(ValueError, match="current device"):
+        call(**tensors, **sizes, stream=types.SimpleNamespace(cuda_stream=7, device_index=1))
+    assert launched == [name] * 2
