@@ -167,7 +167,7 @@ int apb_gated_forward(const void* GU, int type, long long ldgu, int M, int N, in
     if (!GU || !Y) return APB_ERR_NULL;
     if (bad_type(type)) return APB_ERR_TYPE;
     if (bad_activation(activation)) return APB_ERR_VALUE;
-    if (bad_shape_mx8(2LL * M, N) || ldgu < 2LL * N || ldy < N) return APB_ERR_SHAPE;
+    if (bad_shape_mx8(saved ? 2LL * M : M, N) || ldgu < 2LL * N || ldy < N) return APB_ERR_SHAPE;
     if (!aligned(GU, type_size(type)) || !aligned(Y, type_size(type)) || !aligned(saved, 16)) return APB_ERR_ALIGN;
     const dim3 grid(workgroups(M, N));
     const FastDiv by((uint32_t)mx8_blocks(N));
@@ -186,7 +186,7 @@ int apb_gated_backward(const void* GU, int gu_type, long long ldgu, const void* 
     if (!GU || !dY || !dGU) return APB_ERR_NULL;
     if ((bad_type(gu_type) && gu_type != APB_MX8) || bad_type(type)) return APB_ERR_TYPE;
     if (bad_activation(activation)) return APB_ERR_VALUE;
-    if (bad_shape_mx8(2LL * M, N) || (gu_type != APB_MX8 && ldgu < 2LL * N) || lddy < N || lddgu < 2LL * N || (Y && ldy < N) ||
+    if (bad_shape_mx8(gu_type == APB_MX8 ? 2LL * M : M, N) || (gu_type != APB_MX8 && ldgu < 2LL * N) || lddy < N || lddgu < 2LL * N || (Y && ldy < N) ||
         (GU == dGU && (gu_type != type || ldgu != lddgu)))
         return APB_ERR_SHAPE;
     if (!aligned(GU, gu_type == APB_MX8 ? 16 : type_size(gu_type)) || !aligned(dY, type_size(type)) || !aligned(dGU, type_size(type)) ||

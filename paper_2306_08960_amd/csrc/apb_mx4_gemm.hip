@@ -331,9 +331,9 @@ int launch_mx4_gated(const Mx& A, const Mx& B, const int32_t* offsets, int E, in
     return APB_OK;
 }
 
-// The sizes of a gated product; N counts the columns of Y.
-bool bad_gated(int E, int M, int N, int K, const int32_t* offsets) {
-    return N <= 0 || N > kMxMaxK || bad_product(E, M, 2 * N, K, offsets) || bad_shape_mx8(2LL * M, N);
+// The sizes of a gated product; N counts the columns of Y.  saved: both projections go to an 8-bit matrix, which has limits of its own.
+bool bad_gated(int E, int M, int N, int K, const int32_t* offsets, bool saved) {
+    return N <= 0 || N > kMxMaxK || bad_product(E, M, 2 * N, K, offsets) || (saved && bad_shape_mx8(2LL * M, N));
 }
 
 }  // namespace
@@ -396,7 +396,7 @@ int apb_mx4_gated_gemm(const void* A, const void* W, const int32_t* offsets, int
     if (!A || !W || !Y) return APB_ERR_NULL;
     if (bad_type(type)) return APB_ERR_TYPE;
     if (bad_activation(activation)) return APB_ERR_VALUE;
-    if (bad_gated(E, M, N, K, offsets) || ldy < N) return APB_ERR_SHAPE;
+    if (bad_gated(E, M, N, K, offsets, saved != nullptr) || ldy < N) return APB_ERR_SHAPE;
     if (!aligned(A, 16) || !aligned(W, 16) || !aligned(Y, type_size(type)) || !aligned(offsets, 4) || !aligned(saved, 16)) return APB_ERR_ALIGN;
     const Mx a = mx_view(A, M, K), w = mx_view(W, E * 2 * N, K);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -406,7 +406,7 @@ int apb_mx4_gated_gemm(const void* A, const void* W, const int32_t* offsets, int
 
 size_t apb_mx4_gated_linear_scratch_bytes(int grouped, int E, int M, int N, int K, int with_saved) {
     const int32_t some = 0, *offsets = grouped ? &some : nullptr;
-    if (bad_gated(E, M, N, K, offsets) || (!with_saved && mx4_few_gated_applies(offsets, E, M, N, K))) return 0;
+    if (bad_gated(E, M, N, K, offsets, with_saved != 0) || (!with_saved && mx4_few_gated_applies(offsets, E, M, N, K))) return 0;
     return apb_mx4_bytes(M, K);
 }
 
@@ -416,7 +416,8 @@ int apb_mx4_gated_linear(const void* X, int x_type, long long ldx, int rows_in, 
     if (!X || !W || !scratch || !Y) return APB_ERR_NULL;
     if (bad_type(x_type) || bad_type(y_type)) return APB_ERR_TYPE;
     if (bad_activation(activation)) return APB_ERR_VALUE;
-    if (bad_gated(E, M, N, K, offsets) || ldy < N || ldx < K || rows_in <= 0 || (!rows_from && rows_in != M)) return APB_ERR_SHAPE;
+    if (bad_gated(E, M, N, K, offsets, saved != nullptr) || ldy < N || ldx < K || rows_in <= 0 || (!rows_from && rows_in != M))
+        return APB_ERR_SHAPE;
     if (!aligned(X, type_size(x_type)) || !aligned(W, 16) || !aligned(scratch, 16) || !aligned(Y, type_size(y_type)) ||
         !aligned(offsets, 4) || !aligned(rows_from, 4) || !aligned(saved, 16))
         return APB_ERR_ALIGN;

@@ -1,4 +1,5 @@
 """Gated blocks, 8-bit checkpoints and adapters without a GPU: NaN in the oracle, sizes at the limits, operands of another device."""
+import ctypes
 import os
 import types
 
@@ -84,3 +85,44 @@ def test_no_operand_is_taken_from_another_device(monkeypatch, at):
     with pytest.raises(ValueError, match="current device"):
         call(**tensors, **sizes, stream=types.SimpleNamespace(cuda_stream=7, device_index=1))
     assert launched == [name] * 2
+
+
+# ---- sizes at the limits -------------------------------------------------------------------------------------------------------
+
+P, ODD = ctypes.c_void_p(1 << 20), ctypes.c_void_p((1 << 20) + 1)     # never followed: the odd one is refused once the sizes are taken
+
+
+@needs_lib
+def test_limits_of_the_8_bit_form_hold_only_with_it():
+    """2 M rows of N in 8 bits are bounded; a product that saves nothing takes what the plain 4-bit product takes."""
+    from paper_2306_08960_amd import binding as b
+    lib = b.load()
+    gemm = lambda M, N, K, saved: lib.apb_mx4_gated_gemm(P, P, None, 1, M, N, K, 0, 1, ODD, N, saved, None)
+    plain = lambda M, N, K: lib.apb_mx4_gemm(P, P, None, 1, M, N, K, 1, ODD, N, None)
+    linear = lambda M, N, K, saved: lib.apb_mx4_gated_linear(P, 1, K, M, None, P, None, 1, M, N, K, 0, P, 1, ODD, N, saved, None)
+    scratch = lambda M, N, K, saved: b.apb_mx4_gated_linear_scratch_bytes(False, 1, M, N, K, saved)
+    M, N, K = 1 << 20, 16384, 4096                                   # 2 M * 512 blocks = 2^30
+    assert plain(M, 2 * N, K) == b.APB_ERR_ALIGN
+    assert gemm(M, N, K, None) == b.APB_ERR_ALIGN and gemm(M, N, K, P) == b.APB_ERR_SHAPE
+    assert linear(M, N, K, None) == b.APB_ERR_ALIGN and linear(M, N, K, P) == b.APB_ERR_SHAPE
+    assert scratch(M, N, K, False) == b.apb_mx4_bytes(M, K) > 0 and scratch(M, N, K, True) == 0
+    most = ((1 << 30) - 64) // 512 // 2
+    assert gemm(most, N, K, P) == b.APB_ERR_ALIGN and gemm(most + 1, N, K, P) == b.APB_ERR_SHAPE
+    assert scratch(most, N, K, True) == b.apb_mx4_bytes(most, K) and scratch(most + 1, N, K, True) == 0
+    N = 64 * 65535                                                   # (columns: 2 N is what the plain product takes at most)
+    assert plain(1, 2 * N, 256) == b.APB_ERR_ALIGN and plain(1, 2 * N + 2, 256) == b.APB_ERR_SHAPE
+    assert gemm(1, N, 256, None) == b.APB_ERR_ALIGN and gemm(1, N + 1, 256, None) == b.APB_ERR_SHAPE
+
+
+@needs_lib
+def test_limits_of_the_activation():
+    """M rows of N, or 2 M where they are read from or written in 8 bits."""
+    from paper_2306_08960_amd import binding as b
+    lib = b.load()
+    forward = lambda M, N, saved: lib.apb_gated_forward(P, 1, 2 * N, M, N, 0, ODD, N, saved, None)
+    backward = lambda M, N, t: lib.apb_gated_backward(P, t, 2 * N, P, 1, N, M, N, 0, ODD, 2 * N, None, N, None)
+    N, all_ = 32 * 512, ((1 << 30) - 64) // 512
+    assert forward(all_, N, None) == b.APB_ERR_ALIGN and forward(all_ + 1, N, None) == b.APB_ERR_SHAPE
+    assert forward(all_ // 2, N, P) == b.APB_ERR_ALIGN and forward(all_ // 2 + 1, N, P) == b.APB_ERR_SHAPE
+    assert backward(all_, N, 1) == b.APB_ERR_ALIGN and backward(all_ + 1, N, 1) == b.APB_ERR_SHAPE
+    assert backward(all_ // 2, N, 3) == b.APB_ERR_ALIGN and backward(all_ // 2 + 1, N, 3) == b.APB_ERR_SHAPE

@@ -43,3 +43,21 @@ def test_nan_gate_reaches_its_gradients(b, t, kind):
     one[2, 7] = True
     d = b.apb_gated_backward(gu, dy, kind, Y=y)
     assert torch.equal(torch.isnan(y), one) and torch.equal(torch.isnan(d[:, :N]), one) and bool(torch.isfinite(d[:, N:]).all())
+
+
+def test_product_beyond_the_8_bit_form(b):
+    """More rows than both projections could be saved of in 8 bits, and more than 2^34 outputs: the last rows against themselves alone."""
+    M, N, K, tail = 1 << 20, 16385, 32, 300
+    assert b.apb_mx8_bytes(2 * M, N) == 0
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    w4 = b.apb_mx4_quantize(torch.randn(2 * N, K, generator=g, device="cuda"))
+    last = b.apb_mx4_gated_linear(x[M - tail:], w4, N)
+    y = b.apb_mx4_gated_linear(x, w4, N)
+    assert torch.equal(y[M - tail:], last)
+    assert bool(torch.isfinite(last).all()) and int((last != 0).sum()) > last.numel() // 2
+    y.zero_()
+    b.apb_mx4_gated_gemm(b.apb_mx4_quantize(x), w4, M, N, K, Y=y)
+    assert torch.equal(y[M - tail:], last)
+    with pytest.raises(ValueError):
+        b.apb_mx4_gated_linear(x, w4, N, saved=torch.empty(64, dtype=torch.uint8, device="cuda"))
