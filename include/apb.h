@@ -525,7 +525,7 @@ int apb_adapter_parts(int S, int M, int K, int r);   /* 0 on bad arguments */
  *   T  DEVICE, apb_adapter_parts(S, M, K, r) * M * r floats, fully overwritten. */
 int apb_adapter_down(const void* X, int type, long long ldx, const void* A, const int32_t* offsets, const int32_t* adapter,
                      const float* scale, int S, int L, int M, int K, int r, float* T, void* stream);
-/*   T   as apb_adapter_down left it, or any `parts` sums of M rows of r floats.   B  DEVICE, [L][r][N].
+/*   T   as apb_adapter_down left it, or any `parts` <= APB_ADAPTER_MAX_PARTS sums of M rows of r floats.   B  DEVICE, [L][r][N].
  *   Y0  DEVICE, M rows of N elements, or NULL: zeros.      Y  DEVICE, the same, fully overwritten; may be Y0 itself
  *       (with the same row stride), then rows without an adapter are not touched.  Otherwise the two do not overlap. */
 int apb_adapter_up(const float* T, int parts, const void* B, int type, const int32_t* offsets, const int32_t* adapter, int S,

@@ -996,6 +996,7 @@ def apb_mx8_dequantize(mx8: torch.Tensor, rows: int, K: int, dtype: torch.dtype 
 
 # ----------------------------------------------------------------------------- gated feed-forward blocks
 
+# "gelu" is the form by the hyperbolic tangent (torch.nn.GELU(approximate="tanh")), not the one by the error function.
 _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}                      # apb_activation
 
 
@@ -1010,7 +1011,8 @@ def apb_mx4_gated_gemm(A: torch.Tensor, W: torch.Tensor, M: int, N: int, K: int,
                        dtype: torch.dtype = torch.float32, Y: Optional[torch.Tensor] = None,
                        offsets: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """Y[M, N] = act(A^ Wg^T) * (A^ Wu^T); W: for every expert N rows of the gate, then N of the up projection.  saved: memory from
+    """Y[M, N] = act(A^ Wg^T) * (A^ Wu^T); W: for every expert N rows of the gate, then N of the up projection.  activation: "silu", "gelu"
+    (the tanh form, 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3)))) or "relu", here and in what follows.  saved: memory from
     alloc_mx8(2 * M, N) that receives both projections in 8 bits for apb_gated_backward."""
     off, E = _experts(offsets)
     act = _activation(activation)

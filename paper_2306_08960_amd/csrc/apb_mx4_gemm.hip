@@ -137,9 +137,9 @@ __device__ __forceinline__ void store_gated(const f32x16 (&acc)[F][F], uint32_t 
 // rows meet every bank once.  Lane (r, h) holds 32 values of row r: step s multiplies blocks s (h = 0) and 2 + s (h = 1) of the
 // half segment.  Rows of B go in the first operand: a lane then holds four neighbours of a row of Y.
 //
-// ACT, if not -1, is an apb_activation: both projections of a gated block.  Of the 32 * F rows of B that a wave multiplies, the first half are the gate's, the second
-// the up projection's for the same 16 * F columns of Y, so a lane holds both factors of each of its outputs; N counts the columns
-// of Y, the tile has 32 * F of them.  `saved`: where G and U go in 8 bits, if anywhere.
+// ACT, if not -1, is an apb_activation: both projections of a gated block.  Of the 32 * F rows of B that a wave multiplies, the first
+// half are the gate's, the second the up projection's for the same 16 * F columns of Y, so a lane holds both factors of each of its
+// outputs; N counts the columns of Y, the tile has 32 * F of them.  `saved`: where G and U go in 8 bits, if anywhere.
 template <int F, int ACT>
 __global__ __launch_bounds__(kThreads, F == 4 ? 1 : 2) void k_mx4_gemm(Mx A, Mx B, const int32_t* __restrict__ offsets, int E, int N,
                                                                        int tiles_n, int type, void* __restrict__ Y, long long ldy,

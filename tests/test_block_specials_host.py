@@ -126,3 +126,13 @@ def test_limits_of_the_activation():
     assert forward(all_ // 2, N, P) == b.APB_ERR_ALIGN and forward(all_ // 2 + 1, N, P) == b.APB_ERR_SHAPE
     assert backward(all_, N, 1) == b.APB_ERR_ALIGN and backward(all_ + 1, N, 1) == b.APB_ERR_SHAPE
     assert backward(all_ // 2, N, 3) == b.APB_ERR_ALIGN and backward(all_ // 2 + 1, N, 3) == b.APB_ERR_SHAPE
+
+
+@needs_lib
+def test_limits_of_parts():
+    from paper_2306_08960_amd import binding as b
+    lib = b.load()
+    up = lambda parts: lib.apb_adapter_up(P, parts, P, 1, P, P, 3, 2, 20, 64, 8, None, 64, ODD, 64, None)
+    gradient = lambda parts: lib.apb_adapter_gradient(P, parts, P, 1, 64, P, P, 3, 2, 20, 64, 8, ODD, None, 0, None)
+    for f in (up, gradient):
+        assert f(8) == b.APB_ERR_ALIGN and f(9) == b.APB_ERR_SHAPE and f(0) == b.APB_ERR_SHAPE
