@@ -229,17 +229,8 @@ bool mx4_few_applies(const int32_t* offsets, int E, int M, int K) {
     const int mean = offsets ? (M + E - 1) / E : M;              // rows of an expert, were they all alike
     return mean <= 16 && (long long)mean * K <= (offsets ? 8192 : 65536) && lds_bytes(std::min(M, 16), mx_segs(K), false) <= kMaxLds;
 }
-// Both projections: twice the weights to the same rows, and one launch instead of two.  Few rows, measured likewise (us): 2 x 4096 x 4096,
-// 1 row 5.9 : 12.9, 16 rows 11.3 : 12.8, 32 rows 13.6 : 13.0; 2 x 8192 x 8192, 16 rows 25.0 : 32.5; 64 experts of 2 x 1024 x 2048, a row
-// each 26.7 : 27.4, 4 rows 29.2 : 28.0; 16 experts of 2 x 2048 x 4096, 4 rows each 36.4 : 27.0.  More rows of little work, tiles of 16
-// rows that read the weights again: 1024 x 512 x 512 6.1 : 6.6, 256 x 2048 x 512 6.1 : 6.5, 128 x 2048 x 2048 10.9 : 8.5, 16384 x 64 x 64
-// 10.6 : 8.8; 256 rows on 16 experts of 2 x 512 x 512 6.1 : 6.9, 1024 rows 8.5 : 7.1, 64 rows on 8 of 2 x 1024 x 4096 18.4 : 12.5.  Called
-// from Python, each of those is 4 us less with one launch.
 bool mx4_few_gated_applies(const int32_t* offsets, int E, int M, int N, int K) {
-    const int mean = offsets ? (M + E - 1) / E : M;
-    if (lds_bytes(std::min(M, 16), mx_segs(K), true) > kMaxLds) return false;
-    if (mean <= 16 && (!offsets || (long long)mean * K <= 8192)) return true;
-    return K <= 2048 && (offsets || M <= 4096) && (long long)M * N <= (1LL << (offsets ? 27 : 28)) / K;
+    return mx4_gated_is_little(M, N, K, E, offsets != nullptr) && lds_bytes(std::min(M, 16), mx_segs(K), true) <= kMaxLds;
 }
 
 int launch_mx4_few(const void* X, int x_type, long long ldx, int rows_in, const int32_t* rows_from, const Mx& W, const int32_t* offsets,

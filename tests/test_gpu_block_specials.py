@@ -61,3 +61,21 @@ def test_product_beyond_the_8_bit_form(b):
     assert torch.equal(y[M - tail:], last)
     with pytest.raises(ValueError):
         b.apb_mx4_gated_linear(x, w4, N, saved=torch.empty(64, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("M,N,E", [(40, 30001, 0), (200, 24600, 0), (512, 8200, 16), (2000, 2111, 64)])
+def test_few_rows_and_many_columns(b, M, N, E):
+    """The kernel for few rows where tiles would be mostly empty, against the tiles (which a call takes that saves both projections): with
+    one block a row every sum is exact, so the two agree to the bit."""
+    K = 32
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    w4 = b.apb_mx4_quantize(torch.randn(max(E, 1) * 2 * N, K, generator=g, device="cuda"))
+    off = None
+    if E:
+        off = torch.sort(torch.randint(0, M - 8, (E + 1,), generator=g, device="cuda")).values.int()
+        off[0] = 0
+    assert b.apb_mx4_gated_linear_scratch_bytes(E > 0, max(E, 1), M, N, K) == 0
+    few = b.apb_mx4_gated_linear(x, w4, N, offsets=off)
+    tiles = b.apb_mx4_gated_linear(x, w4, N, offsets=off, saved=b.alloc_mx8(2 * M, N))
+    assert torch.equal(few, tiles) and bool(torch.isfinite(few).all())
