@@ -512,29 +512,53 @@ __global__ __launch_bounds__(kThreads) void k_adapter_up16(const float* __restri
 
 // ---- gradients --------------------------------------------------------------------------------------------------------------
 
+// The sum over a wave's lanes.
+__device__ __forceinline__ int total(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // (lanes 1, 2, 4, 8 before, of a row of sixteen)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // (the last lane of the row before, to rows 1 and 3)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // (of the first half, to the second)
+    return __builtin_amdgcn_readlane(v, kWave - 1);
+}
+
+// What a wave knows of the segments: lane s of the s-th one's adapter, first row and rows, if there are no more of them than lanes.
+struct Known {
+    int its, first, count;
+};
+__device__ __forceinline__ Known know(const Segments& seg) {
+    Known k;
+    k.its = rows_of(seg, threadIdx.x & (kWave - 1), k.first, k.count);
+    return k;
+}
+// add(adapter, rows) of all segments, by lanes.  (Four loads at a time that do not wait for one another.)
+template <class ADD>
+__device__ __forceinline__ void over_segments(const Segments& seg, const Known& known, ADD add) {
+    if (seg.S <= kWave) return add(known.its, known.count);
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int base = 0; base < seg.S; base += 4 * kWave) {
+        int a[4], first, n[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) a[u] = rows_of(seg, base + u * kWave + lane, first, n[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) add(a[u], n[u]);
+    }
+}
+
 // The rows of adapter a, and of all adapters before it.
 struct Span {
     int rows, before;
 };
-// its, first, count: the last segment that the lane has looked at.
-__device__ __forceinline__ Span span_of(const Segments& seg, int a, int& its, int& first, int& count) {
-    const int lane = threadIdx.x & (kWave - 1);
+__device__ __forceinline__ Span span_of(const Segments& seg, const Known& known, int a) {
     int rows = 0, before = 0;
-    for (int base = 0; base < seg.S; base += kWave) {
-        its = rows_of(seg, base + lane, first, count);
-        rows += its == a ? count : 0;
-        before += its >= 0 && its < a ? count : 0;
-    }
+    over_segments(seg, known, [&](int its, int n) {
+        rows += its == a ? n : 0;
+        before += its >= 0 && its < a ? n : 0;
+    });
     // (together they are no more than M; of offsets that do not ascend, that much is kept)
-    rows = min(rows, seg.M);
-    before = min(before, seg.M);
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        rows += __shfl_xor(rows, d, kWave);
-        before += __shfl_xor(before, d, kWave);
-    }
-    rows = min(__builtin_amdgcn_readfirstlane(rows), seg.M);
-    return Span{rows, min(__builtin_amdgcn_readfirstlane(before), seg.M - rows)};
+    rows = min(total(min(rows, seg.M)), seg.M);
+    return Span{rows, min(total(min(before, seg.M)), seg.M - rows)};
 }
 
 // The adapter of segment s, if it is the first segment of it; -1 otherwise.
@@ -545,6 +569,34 @@ __device__ __forceinline__ int first_segment_of(const Segments& seg, int s) {
     for (int base = 0; base < s; base += kWave)
         if (__ballot(base + lane < s && rows_of(seg, base + lane, first, count) == a)) return -1;
     return __builtin_amdgcn_readfirstlane(a);
+}
+
+// Slice `number` of adapter a, which has these rows; a < 0: none.
+struct Slice {
+    int a, number;
+    Span span;
+};
+// What the place k * each stands for (slice_at_place).  Adapters are looked for in eighths: a pass over the segments adds up the rows
+// before seven of them.
+__device__ __forceinline__ Slice slice_at(const Segments& seg, const Known& known, int k, int each) {
+    const int place = k * each;
+    int from = 0, to = seg.L;
+    while (to - from > 1) {
+        const int step = (to - from + 7) / 8;
+        int before[7] = {};
+        over_segments(seg, known, [&](int its, int n) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i) before[i] += its >= 0 && its < from + (i + 1) * step ? n : 0;
+        });
+        int steps = 0;
+#pragma unroll
+        for (int i = 0; i < 7; ++i) steps += total(min(before[i], seg.M)) <= place ? 1 : 0;
+        from = min(from + steps * step, to - 1);
+        to = min(from + step, to);
+    }
+    const Span span = span_of(seg, known, from);
+    const int number = slice_at_place(k, span.before, each);
+    return Slice{number > 0 && number < (span.rows + each - 1) / each ? from : -1, number, span};
 }
 
 // 32 rows of X as they are loaded: of eight of them NC neighbours to a lane.  Rows 8 g + e, for operands that sum over eight rows; an X of
@@ -627,15 +679,15 @@ __device__ __forceinline__ void clear_adapters(const Segments& seg, long long n,
     constexpr int kPiece = 4096;
     const int pieces = (int)((n + kPiece - 1) / kPiece);
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    int known = -1;
+    const Known all_of = know(seg);
+    int last = -1;
     bool empty = false;
     const long long all = (long long)pieces * seg.L, each = (all + parts - 1) / parts;
     for (long long u = part * each; u < std::min(all, (part + 1) * each); ++u) {
         const int a = (int)(u / pieces);
-        if (a != known) {
-            int its, first, count;
-            empty = span_of(seg, a, its, first, count).rows == 0;
-            known = a;
+        if (a != last) {
+            empty = span_of(seg, all_of, a).rows == 0;
+            last = a;
         }
         if (!empty) continue;
         const long long from = (u - (long long)a * pieces) * kPiece, end = std::min<long long>(from + kPiece, n);
@@ -646,8 +698,9 @@ __device__ __forceinline__ void clear_adapters(const Segments& seg, long long n,
 // WHOLE: K is 16 * NC or more; the last workgroup's columns then end with the row's, and those that two workgroups have get the same
 // values twice.  (Rows of 8 bits are padded, and their columns stay in blocks.)
 //
-// A workgroup takes one adapter (by_segment: that of a segment), 16 * JT ranks, 16 * NC columns, and `each` of the adapter's rows, counted
-// through all of its segments, whose numbers it lists in LDS; its waves take 32 of them at a time in turn, by themselves, the next ones under
+// A workgroup takes one adapter (by_segment: that of a segment), 16 * JT ranks, 16 * NC columns, and the first `each` of the adapter's rows,
+// or those of another of its slices (`more`: how many places for them there are), counted through all of its segments, whose numbers it
+// lists in LDS; its waves take 32 of them at a time in turn, by themselves, the next ones under
 // way, and join their sums in LDS.  T, its parts added up, comes to registers in the order of the operand and is split there into three
 // bfloat16 parts (an X of float32 goes with T as it is through float32 products); X is transposed in registers.  With waves that share a
 // tile of rows in LDS and each take columns of their own, every wave waits at barriers for the slowest load, and an adapter's rows have
@@ -656,28 +709,28 @@ __device__ __forceinline__ void clear_adapters(const Segments& seg, long long n,
 template <int XT, int JT, int NC, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float* __restrict__ T, int parts, const void* __restrict__ X,
                                                                     long long ldx, Mx8 x8, Segments seg, int K, int r, int rank_tiles,
-                                                                    int by_segment, int each, float* __restrict__ dA,
+                                                                    int by_segment, int each, int more, float* __restrict__ dA,
                                                                     float* __restrict__ shared) {
     constexpr int kChunk = 32, kRanks = 16 * JT;
     __shared__ f32x4 sums[WAVES][JT * NC][kWave];
     __shared__ int list[kList + kChunk];
-    int a = blockIdx.y / rank_tiles;
+    const int unit = blockIdx.y / rank_tiles, firsts = by_segment ? seg.S : seg.L;
     const int j0 = blockIdx.y % rank_tiles * kRanks;
-    if (by_segment) {
-        if (a >= seg.S) {
-            if (blockIdx.z == 0) clear_adapters(seg, (long long)r * K, (blockIdx.y - seg.S * rank_tiles) * gridDim.x + blockIdx.x,
-                                                (gridDim.y - seg.S * rank_tiles) * gridDim.x, dA);
-            return;
-        }
-        a = first_segment_of(seg, a);
-        if (a < 0) return;
+    if (unit >= firsts + more) {
+        const int behind = (firsts + more) * rank_tiles;
+        clear_adapters(seg, (long long)r * K, (blockIdx.y - behind) * gridDim.x + blockIdx.x, (gridDim.y - behind) * gridDim.x, dA);
+        return;
     }
+    Known known = know(seg);
+    Slice slice{unit, 0, {}};
+    if (unit >= firsts) slice = slice_at(seg, known, unit - firsts + 1, each);
+    else if (by_segment) slice.a = first_segment_of(seg, unit);
+    const int a = slice.a;
+    if (a < 0) return;
+    const Span span = unit < firsts ? span_of(seg, known, a) : slice.span;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
     const int c0 = XT == APB_MX8 ? blockIdx.x * 16 * NC : WHOLE ? min((int)blockIdx.x * 16 * NC, K - 16 * NC) : 0, c = c0 + NC * i;
-    int its, first, count;
-    const Span span = span_of(seg, a, its, first, count);
-    const int lo = blockIdx.z * each, hi = min(lo + each, span.rows);
-    if (blockIdx.z > 0 && lo >= hi) return;
+    const int lo = slice.number * each, hi = min(lo + each, span.rows);
     f32x4 acc[JT][NC];
 #pragma unroll
     for (int j = 0; j < JT; ++j)
@@ -689,10 +742,10 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float*
         if (wave == 0) {
             int before = 0;
             for (int base = 0; base < seg.S && before < start + rows; base += kWave) {
-                if (seg.S > kWave) its = rows_of(seg, base + lane, first, count);
-                for (unsigned long long left = __ballot(its == a && count > 0); left; left &= left - 1) {
+                if (seg.S > kWave) known.its = rows_of(seg, base + lane, known.first, known.count);
+                for (unsigned long long left = __ballot(known.its == a && known.count > 0); left; left &= left - 1) {
                     const int src = __builtin_amdgcn_readfirstlane(__ffsll((long long)left) - 1);
-                    const int from = __builtin_amdgcn_readlane(first, src), n = __builtin_amdgcn_readlane(count, src);
+                    const int from = __builtin_amdgcn_readlane(known.first, src), n = __builtin_amdgcn_readlane(known.count, src);
                     const int skip = max(start - before, 0), end = min(n, start + rows - before);
                     for (int k = skip + lane; k < end; k += kWave) list[before + k - start] = from + k;
                     if (before + n >= start + rows && lane < kChunk && end > skip) list[rows + lane] = from + end - 1;
@@ -773,7 +826,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float*
         for (int n = 0; n < NC; ++n) sums[wave][j * NC + n][lane] = acc[j][n];
     __syncthreads();
     // rank 16 j + 4 g + q of columns NC i ..
-    float* out = span.rows > each ? shared + (size_t)(place_of_slices(span.before, each) + blockIdx.z) * r * K : dA + (size_t)a * r * K;
+    float* out = span.rows > each ? shared + (size_t)(place_of_slices(span.before, each) + slice.number) * r * K : dA + (size_t)a * r * K;
     for (int n = threadIdx.x; n < JT * 256; n += WAVES * kWave) {
         const int q = n & 3, from = n >> 2 & 63, j = n >> 8;
         const int rank = j0 + 16 * j + 4 * (from >> 4) + q, col = c0 + NC * (from & 15);
@@ -793,14 +846,14 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float*
     }
 }
 
-// The slices of the adapters that have several, added up in order.
-__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int by_segment, int each,
-                                                           long long n, float* __restrict__ dA) {
-    const int a = by_segment ? first_segment_of(seg, blockIdx.y) : blockIdx.y;
-    if (a < 0) return;
-    int its, first, count;
-    const Span span = span_of(seg, a, its, first, count);
-    if (span.rows <= each) return;
+// The slices of the adapters that have several, added up in order.  A workgroup for the place of each slice behind an adapter's first:
+// that of its second one has the adapter.
+__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int each, long long n,
+                                                           float* __restrict__ dA) {
+    const Slice slice = slice_at(seg, know(seg), blockIdx.y + 1, each);
+    if (slice.a < 0 || slice.number != 1) return;
+    const int a = slice.a;
+    const Span span = slice.span;
     const int slices = (span.rows + each - 1) / each;
     const float* from = shared + (size_t)place_of_slices(span.before, each) * n;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -908,11 +961,11 @@ void gradient_form(const float* T, int parts, const void* X, long long ldx, cons
     const int rank_tiles = (r + 16 * JT - 1) / (16 * JT);
     const int by_segment = gradient_by_segment(seg.S, seg.L, K, r);
     const unsigned columns = (unsigned)((K + 16 * NC - 1) / (16 * NC));
-    const dim3 grid(columns, by_segment ? seg.S * rank_tiles + (1024 + columns - 1) / columns : seg.L * rank_tiles,
-                    (unsigned)((seg.M + each - 1) / each));
+    const int firsts = by_segment ? seg.S : seg.L, more = more_slices(seg.M, each);
+    const dim3 grid(columns, (unsigned)((firsts + more) * rank_tiles + (by_segment ? (1024 + columns - 1) / columns : 0)));
     auto launch = [&](auto whole) {
         hipLaunchKernelGGL((k_adapter_gradient<XT, JT, NC, WAVES, decltype(whole)::value>), grid, dim3(WAVES * kWave), 0, s, T, parts, X, ldx, x8,
-                           seg, K, r, rank_tiles, by_segment, each, dA, shared);
+                           seg, K, r, rank_tiles, by_segment, each, more, dA, shared);
     };
     if constexpr (XT == APB_MX8 || NC == 8) launch(std::true_type{});
     else if (K >= 16 * NC) launch(std::true_type{});
@@ -1014,10 +1067,8 @@ int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, l
     APB_HIP(hipGetLastError());
     if (join) {
         const long long n = (long long)r * K;
-        const int by_segment = gradient_by_segment(S, L, K, r);
-        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096),
-                        (unsigned)(by_segment ? S : L));
-        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, by_segment, each, n, dA);
+        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096), (unsigned)more_slices(M, each));
+        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, each, n, dA);
         APB_HIP(hipGetLastError());
     }
     return APB_OK;

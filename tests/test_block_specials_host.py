@@ -1,6 +1,7 @@
 """Gated blocks, 8-bit checkpoints and adapters without a GPU: NaN in the oracle, sizes at the limits, operands of another device."""
 import ctypes
 import os
+import subprocess
 import types
 
 import numpy as np
@@ -159,3 +160,45 @@ def test_little_work_is_counted_with_what_rows_are_padded_to():
     for E, M, N, K in ((0, 4096, 256, 32), (16, 4096, 128, 32), (16, 16384, 32, 200), (0, 32, 262144, 8), (0, 64, 8192, 256), (0, 256, 24576, 32),
                        (16, 512, 8192, 32), (64, 2048, 16384, 256)):
         assert one(E, M, N, K)
+
+
+# ---- slices of the adapters' gradient: workgroups for those that there are ------------------------------------------------
+
+SLICES = r"""
+#include <cstdio>
+#include "apb_adapter_shape.h"
+
+int main() {                                                          // rows before an adapter, to a slice, all rows
+    int before, each, M;
+    while (std::scanf("%d %d %d", &before, &each, &M) == 3) {
+        std::printf("%d", apb::more_slices(M, each));
+        for (int k = 1; k <= apb::more_slices(M, each); ++k) std::printf(" %d", apb::slice_at_place(k, before, each));
+        std::printf("\n");
+    }
+}
+"""
+
+
+def test_every_slice_has_one_workgroup(tmp_path):
+    """First slices have one for each adapter; the others one place each among M / each, and no place stands for two."""
+    src, exe = tmp_path / "slices.cpp", tmp_path / "slices"
+    src.write_text(SLICES)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-ftrapv", "-I", os.path.join(ROOT, "include"),
+                    "-I", os.path.join(ROOT, "paper_2306_08960_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    g = np.random.default_rng(1)
+    for case in range(150):
+        L, each = int(g.integers(1, 30)), int(g.choice([1, 2, 3, 64, 128, 320]))
+        rows = np.where(g.random(L) < 0.3, 0, np.exp(g.uniform(0, 7, L))).astype(int)
+        rows[g.integers(L)] = int(g.choice([1, each, each + 1, 3 * each, 3 * each - 1]))
+        behind = int(g.integers(0, 300))                             # (rows of no adapter)
+        before, M = np.concatenate([[0], np.cumsum(rows)]), int(rows.sum()) + behind
+        text = "\n".join(f"{b} {each} {M}" for b in before[:-1])
+        p = subprocess.run([str(exe)], input=text, stdout=subprocess.PIPE, text=True, check=True, timeout=60)
+        answers = [list(map(int, line.split())) for line in p.stdout.splitlines()]
+        taken, places = [], answers[0][0]
+        assert places * each < M
+        for k in range(1, places + 1):
+            a = int(np.searchsorted(before, k * each, side="right")) - 1
+            if a < L and 0 < answers[a][k] < -(-int(rows[a]) // each):
+                taken.append((a, answers[a][k]))
+        assert sorted(taken) == [(a, z) for a in range(L) for z in range(1, -(-int(rows[a]) // each))]

@@ -169,3 +169,35 @@ def test_up_keeps_its_bits(b, M, N, r, t):
     err = np.abs(got - want)
     at = np.unravel_index(np.argmax(err - tol), err.shape)
     assert (err <= tol).all(), (at, err[at], tol[at], want[at])
+
+
+# L adapters, S segments, M rows, K, r
+@pytest.mark.parametrize("L,S,M,K,r", [(1, 3, 5000, 64, 4), (3, 9, 6000, 130, 20), (9, 40, 9000, 64, 16), (70, 200, 20000, 64, 4), (300, 30, 20000, 100, 5),
+                                       (1500, 5, 9000, 64, 4), (2000, 4096, 30000, 64, 3), (4096, 4096, 40000, 40, 2), (8, 64, 40000, 4100, 9),
+                                       (20, 65, 40000, 2000, 40)])
+@pytest.mark.parametrize("spread", [True, False])
+def test_slices_of_many_adapters(b, L, S, M, K, r, spread):
+    """Adapters whose rows workgroups share, in segments wherever they are, evenly or most of them one adapter's.  Whole numbers below
+    2^24 all the way: every order of the sums gives the same."""
+    g = np.random.default_rng(L + S)
+    cut = np.sort(g.integers(0, M - 50, S + 1)) if spread else np.concatenate([np.sort(g.integers(0, M // 5, S)), [M - 50]])
+    cut[0] = 0
+    which = g.integers(-1, L, S)
+    which[-1] = L - 1 if L % 2 else L // 2
+    seg = dict(offsets=torch.from_numpy(cut.astype(np.int32)).cuda(), adapter=torch.from_numpy(which.astype(np.int32)).cuda())
+    row = torch.full((M,), -1, dtype=torch.long)
+    for s in range(S):
+        row[cut[s]:cut[s + 1]] = int(which[s])
+    T = torch.from_numpy(g.integers(-8, 9, (1, M, r)).astype(np.float32)).cuda()
+    x = torch.from_numpy(g.integers(-8, 9, (M, K)).astype(np.float32)).cuda().bfloat16()
+    need = b.apb_adapter_gradient_workspace_bytes(S, L, M, K, r)
+    assert need > 0 and 64 * 50000 < 1 << 24
+    want = torch.zeros(L, r, K, dtype=torch.float64)
+    for a in set(row.tolist()) - {-1}:
+        mine = (row == a).nonzero().flatten().cuda()
+        want[a] = (T[0, mine].double().t().contiguous() @ x[mine].double()).cpu()
+    for X, k in ((x, None), (b.apb_mx8_quantize(x), K), (x.float(), None)):
+        got = b.apb_adapter_gradient(T, X, L, K=k, workspace=torch.full((need,), 0xff, dtype=torch.uint8, device="cuda"), **seg)
+        assert torch.equal(got.cpu().double(), want)
+    none = b.apb_adapter_gradient(T, x, L, workspace=torch.empty(4, dtype=torch.uint8, device="cuda"), **seg)
+    assert torch.equal(none.cpu().double(), want)
