@@ -650,11 +650,14 @@ def _type(dtype: torch.dtype) -> int:
     return t
 
 
+# (The C entry points count in int, and ctypes passes the low 32 bits of what is larger: such sizes end here.)
 def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
     """(pointer, apb_type, row stride) of a 2-D float matrix whose rows are contiguous."""
     if not t.is_cuda or t.dim() != 2:
         raise TypeError(f"{name} must be a 2-D tensor on the GPU")
     rows, cols = t.shape
+    if rows >> 31 or cols >> 31:
+        raise ApbError(APB_ERR_SHAPE, name)
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise TypeError(f"the rows of {name} must be contiguous")
@@ -673,7 +676,7 @@ def _result(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dtyp
             stream: Optional[torch.cuda.Stream]):
     """(tensor, pointer, apb_type, row stride) of an output: `t`, or a new one beside `like`."""
     if t is None:
-        if shape[0] < 0 or shape[1] < 0:
+        if shape[0] >> 31 or shape[1] >> 31:                              # (negative ones as well)
             raise ApbError(APB_ERR_SHAPE, name)
         t = _new(like, shape, dtype, stream)
         return t, t.data_ptr(), _type(dtype), shape[1]
@@ -724,9 +727,12 @@ def _experts(offsets: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
     """(pointer, number of groups) of the offsets; (None, 1) without."""
     if offsets is None:
         return None, 1
-    if offsets.numel() < 2:
+    E = offsets.numel() - 1
+    if E < 1:
         raise ValueError("offsets must hold E + 1 int32")
-    return _array(offsets, torch.int32, None, "offsets"), offsets.numel() - 1
+    if E >> 31:
+        raise ApbError(APB_ERR_SHAPE, "offsets")
+    return _array(offsets, torch.int32, None, "offsets"), E
 
 
 def apb_mx4_quantize(X: torch.Tensor, mx: Optional[torch.Tensor] = None, rows_from: Optional[torch.Tensor] = None,
@@ -953,7 +959,8 @@ _MX8 = 3                                                              # APB_MX8
 
 
 def apb_mx8_bytes(rows: int, K: int) -> int:
-    return int(load().apb_mx8_bytes(int(rows), int(K)))
+    rows, K = int(rows), int(K)
+    return 0 if rows >> 31 or K >> 31 else int(load().apb_mx8_bytes(rows, K))
 
 
 def alloc_mx8(rows: int, K: int, device=None) -> torch.Tensor:
@@ -1016,6 +1023,8 @@ def apb_mx4_gated_gemm(A: torch.Tensor, W: torch.Tensor, M: int, N: int, K: int,
     alloc_mx8(2 * M, N) that receives both projections in 8 bits for apb_gated_backward."""
     off, E = _experts(offsets)
     act = _activation(activation)
+    if int(K) >> 31:
+        raise ApbError(APB_ERR_SHAPE, "apb_mx4_gated_gemm")
     Y, ptr, t, ld = _result(Y, (M, N), dtype, A, "Y", stream)
     _check(load().apb_mx4_gated_gemm(_mx4_ptr(A, M, K, "A"), _mx4_ptr(W, E * 2 * N, K, "W"), off, E, int(M), int(N), int(K), act, t, ptr,
                                      ld, _mx8_ptr(saved, 2 * M, N, "saved"), _stream_at(stream, A, W, offsets, Y, saved)), "apb_mx4_gated_gemm")
@@ -1023,7 +1032,9 @@ def apb_mx4_gated_gemm(A: torch.Tensor, W: torch.Tensor, M: int, N: int, K: int,
 
 
 def apb_mx4_gated_linear_scratch_bytes(grouped: bool, E: int, M: int, N: int, K: int, with_saved: bool = False) -> int:
-    """Bytes of scratch that apb_mx4_gated_linear uses: 0 where it runs as one kernel."""
+    """Bytes of scratch that apb_mx4_gated_linear uses: 0 where it runs as one kernel, and for sizes that it refuses."""
+    if E >> 31 or M >> 31 or N >> 31 or K >> 31:
+        return 0
     return int(load().apb_mx4_gated_linear_scratch_bytes(int(grouped), E, M, N, K, int(with_saved)))
 
 
@@ -1098,7 +1109,10 @@ def _factors(F: torch.Tensor, type_: torch.dtype, name: str) -> Tuple[int, int, 
     """(pointer, L, r, long side) of an adapters' factor."""
     if F.dim() != 3:
         raise ValueError(f"{name} must be [L, r, long side]")
-    return (_array(F, type_, None, name), *F.shape)
+    L, r, side = F.shape
+    if L >> 31 or r >> 31 or side >> 31:
+        raise ApbError(APB_ERR_SHAPE, name)
+    return _array(F, type_, None, name), L, r, side
 
 
 def _segments(offsets: Optional[torch.Tensor], adapter: Optional[torch.Tensor]):
@@ -1108,6 +1122,8 @@ def _segments(offsets: Optional[torch.Tensor], adapter: Optional[torch.Tensor]):
     S = offsets.numel() - 1
     if S < 1:
         raise ValueError("offsets must hold S + 1 int32")
+    if S >> 31:
+        raise ApbError(APB_ERR_SHAPE, "offsets")
     return _array(offsets, torch.int32, None, "offsets"), _array(adapter, torch.int32, S, "adapter"), S
 
 
@@ -1115,11 +1131,15 @@ def _low_rank(T: torch.Tensor) -> Tuple[int, int, int, int]:
     """(pointer, parts, M, r) of what apb_adapter_down returned."""
     if T.dim() != 3:
         raise ValueError("T must be [parts, M, r]")
-    return (_array(T, torch.float32, None, "T"), *T.shape)
+    parts, M, r = T.shape
+    if parts >> 31 or M >> 31 or r >> 31:
+        raise ApbError(APB_ERR_SHAPE, "T")
+    return _array(T, torch.float32, None, "T"), parts, M, r
 
 
 def apb_adapter_parts(S: int, M: int, K: int, r: int) -> int:
-    return int(load().apb_adapter_parts(int(S), int(M), int(K), int(r)))
+    sizes = int(S), int(M), int(K), int(r)
+    return 0 if any(n >> 31 for n in sizes) else int(load().apb_adapter_parts(*sizes))
 
 
 def apb_adapter_down(X: torch.Tensor, A: torch.Tensor, offsets: Optional[torch.Tensor] = None, adapter: Optional[torch.Tensor] = None,
@@ -1173,7 +1193,8 @@ def apb_adapter_up(T: torch.Tensor, B: torch.Tensor, Y0: Optional[torch.Tensor] 
 
 def apb_adapter_gradient_workspace_bytes(S: int, L: int, M: int, K: int, r: int) -> int:
     """Bytes of scratch that apb_adapter_gradient has a use for."""
-    return int(load().apb_adapter_gradient_workspace_bytes(int(S), int(L), int(M), int(K), int(r)))
+    sizes = int(S), int(L), int(M), int(K), int(r)
+    return 0 if any(n >> 31 for n in sizes) else int(load().apb_adapter_gradient_workspace_bytes(*sizes))
 
 
 def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[int] = None, offsets: Optional[torch.Tensor] = None,
@@ -1192,9 +1213,9 @@ def apb_adapter_gradient(T: torch.Tensor, X: torch.Tensor, L: int, K: Optional[i
         K = X.shape[1]
     off, adp, S = _segments(offsets, adapter)
     lib = load()
+    if L <= 0 or int(L) >> 31 or int(K) >> 31:
+        raise ApbError(APB_ERR_SHAPE, "apb_adapter_gradient")
     if dA is None:
-        if L <= 0:
-            raise ApbError(APB_ERR_SHAPE, "apb_adapter_gradient")
         dA = _new(T, (L, r, K), torch.float32, stream)
         dp = dA.data_ptr()
     elif dA.shape != (L, r, K):

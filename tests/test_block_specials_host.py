@@ -202,3 +202,69 @@ def test_every_slice_has_one_workgroup(tmp_path):
             if a < L and 0 < answers[a][k] < -(-int(rows[a]) // each):
                 taken.append((a, answers[a][k]))
         assert sorted(taken) == [(a, z) for a in range(L) for z in range(1, -(-int(rows[a]) // each))]
+
+
+# ---- sizes beyond 32 bits: refused, not cut to what is left of them ---------------------------------------------------------
+
+def _vast(*shape, dtype=torch.bfloat16):
+    return torch.empty(*shape, dtype=dtype, device="meta").as_subclass(_On)
+
+
+BIG = (1 << 32) + 3
+VAST = [
+    lambda b: b.apb_mx8_quantize(_vast(BIG, 2)), lambda b: b.apb_mx8_quantize(_vast(2, BIG)),
+    lambda b: b.apb_mx8_dequantize(_vast(BIG * 33, dtype=torch.uint8), BIG, 32), lambda b: b.alloc_mx8(BIG, 2, device="meta"),
+    lambda b: b.apb_gated_forward(_vast(BIG, 2)), lambda b: b.apb_gated_backward(_vast(BIG, 2), _vast(BIG, 1)),
+    lambda b: b.apb_gated_backward(_vast(2 * BIG * 33, dtype=torch.uint8), _vast(BIG, 1)),
+    lambda b: b.apb_mx4_gated_linear(_vast(BIG, 32), _vast(2 * 136, dtype=torch.uint8), 1),
+    lambda b: b.apb_mx4_gated_linear(_vast(4, 32), _vast(2 * 136, dtype=torch.uint8), 1, rows_from=_vast(BIG, dtype=torch.int32)),
+    lambda b: b.apb_mx4_gated_linear(_vast(4, 32), _vast(BIG * 2 * 136, dtype=torch.uint8), 1, offsets=_vast(BIG + 1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_down(_vast(BIG, 8), _vast(1, 2, 8), adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_down(_vast(4, 8), _vast(BIG, 2, 8), adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_down(_vast(4, 8), _vast(1, BIG, 8), adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_down(_vast(4, 8), _vast(1, 2, 8), _vast(BIG + 1, dtype=torch.int32), _vast(BIG, dtype=torch.int32)),
+    lambda b: b.apb_adapter_up(_vast(1, BIG, 2, dtype=torch.float32), _vast(1, 2, 8), adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_up(_vast(1, 4, BIG, dtype=torch.float32), _vast(1, BIG, 8), adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_up(_vast(BIG, 4, 2, dtype=torch.float32), _vast(1, 2, 8), adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_gradient(_vast(1, BIG, 2, dtype=torch.float32), _vast(BIG, 8), 1, adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_gradient(_vast(1, BIG, 2, dtype=torch.float32), _vast(BIG * 33, dtype=torch.uint8), 1, K=8, adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_gradient(_vast(1, 4, BIG, dtype=torch.float32), _vast(4, 8), 1, adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_gradient(_vast(1, 4, 2, dtype=torch.float32), _vast(4, 8), BIG, adapter=_vast(1, dtype=torch.int32)),
+    lambda b: b.apb_adapter_gradient(_vast(1, 4, 2, dtype=torch.float32), _vast(4 * 33, dtype=torch.uint8), 1, K=BIG, adapter=_vast(1, dtype=torch.int32)),
+]
+
+
+@needs_lib
+@pytest.mark.parametrize("at", range(len(VAST)))
+def test_no_size_is_cut_to_32_bits(monkeypatch, at):
+    from paper_2306_08960_amd import binding
+    real, launched = binding.load(), []
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith("_bytes") or name.endswith("_parts") or name == "apb_strerror":
+                return getattr(real, name)
+            return lambda *args: launched.append(name) or 0
+    monkeypatch.setattr(binding, "load", Library)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    with pytest.raises((binding.ApbError, ValueError)):
+        VAST[at](binding)
+    assert not launched
+    with pytest.raises((binding.ApbError, ValueError)):
+        binding.apb_mx4_gated_gemm(_vast(BIG * 136, dtype=torch.uint8), _vast(2 * 136, dtype=torch.uint8), BIG, 1, 32)
+    with pytest.raises((binding.ApbError, ValueError)):
+        binding.apb_mx4_gated_gemm(_vast(136, dtype=torch.uint8), _vast(BIG * 2 * 136, dtype=torch.uint8), 1, BIG, 32)
+    assert not launched
+
+
+@needs_lib
+def test_sizes_are_asked_for_whole():
+    from paper_2306_08960_amd import binding as b
+    assert b.apb_mx8_bytes(BIG, 32) == 0 and b.apb_mx8_bytes(32, BIG) == 0
+    for i in range(4):
+        assert b.apb_adapter_parts(*[BIG if k == i else 4 for k in range(4)]) == 0
+    for i in range(5):
+        assert b.apb_adapter_gradient_workspace_bytes(*[BIG if k == i else v for k, v in enumerate((1, 1, 5000, 64, 4))]) == 0
+    for i in range(1, 5):
+        assert b.apb_mx4_gated_linear_scratch_bytes(True, *[BIG if k == i else v for k, v in enumerate((0, 2, 500, 4096, 4096)) if k]) == 0
