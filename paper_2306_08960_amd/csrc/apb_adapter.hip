@@ -528,21 +528,21 @@ struct Known {
     int its, first, count;
 };
 __device__ __forceinline__ Known know(const Segments& seg) {
-    Known k;
-    k.its = rows_of(seg, threadIdx.x & (kWave - 1), k.first, k.count);
+    Known k = {};
+    if (seg.S <= kWave) k.its = rows_of(seg, threadIdx.x & (kWave - 1), k.first, k.count);
     return k;
 }
-// add(adapter, rows) of all segments, by lanes.  (Four loads at a time that do not wait for one another.)
-template <class ADD>
+// add(adapter, rows) of all segments, by lanes, WIDE * 64 of them by loads that do not wait for one another.
+template <int WIDE, class ADD>
 __device__ __forceinline__ void over_segments(const Segments& seg, const Known& known, ADD add) {
     if (seg.S <= kWave) return add(known.its, known.count);
     const int lane = threadIdx.x & (kWave - 1);
-    for (int base = 0; base < seg.S; base += 4 * kWave) {
-        int a[4], first, n[4];
+    for (int base = 0; base < seg.S; base += WIDE * kWave) {
+        int a[WIDE], first, n[WIDE];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) a[u] = rows_of(seg, base + u * kWave + lane, first, n[u]);
+        for (int u = 0; u < WIDE; ++u) a[u] = rows_of(seg, base + u * kWave + lane, first, n[u]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) add(a[u], n[u]);
+        for (int u = 0; u < WIDE; ++u) add(a[u], n[u]);
     }
 }
 
@@ -552,7 +552,7 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const Segments& seg, const Known& known, int a) {
     int rows = 0, before = 0;
-    over_segments(seg, known, [&](int its, int n) {
+    over_segments<2>(seg, known, [&](int its, int n) {
         rows += its == a ? n : 0;
         before += its >= 0 && its < a ? n : 0;
     });
@@ -576,27 +576,48 @@ struct Slice {
     int a, number;
     Span span;
 };
-// What the place k * each stands for (slice_at_place).  Adapters are looked for in eighths: a pass over the segments adds up the rows
-// before seven of them.
+// The k-th slice behind the adapters' first ones, k = 1 ..  Up to eight adapters' slices are counted, so that those k that have no work come
+// last (16384 rows of 512, four adapters of rank 16, which are 256 workgroups: 9.8 us, 15.0 with such k among them).  More adapters: the
+// place k * each stands for one (slice_at_place).  Adapters are looked for in eighths, a pass over the segments adds up the rows before
+// seven of them.
 __device__ __forceinline__ Slice slice_at(const Segments& seg, const Known& known, int k, int each) {
-    const int place = k * each;
-    int from = 0, to = seg.L;
-    while (to - from > 1) {
-        const int step = (to - from + 7) / 8;
-        int before[7] = {};
-        over_segments(seg, known, [&](int its, int n) {
+    const bool counted = seg.L > 1 && seg.L <= 8;
+    int sums[8] = {}, a = 0, number = k;
+    if (counted) {
+        over_segments<4>(seg, known, [&](int its, int n) {
 #pragma unroll
-            for (int i = 0; i < 7; ++i) before[i] += its >= 0 && its < from + (i + 1) * step ? n : 0;
+            for (int i = 0; i < 8; ++i) sums[i] += its == i ? n : 0;
         });
-        int steps = 0;
+        a = -1;
 #pragma unroll
-        for (int i = 0; i < 7; ++i) steps += total(min(before[i], seg.M)) <= place ? 1 : 0;
-        from = min(from + steps * step, to - 1);
-        to = min(from + step, to);
+        for (int i = 0; i < 8; ++i) {
+            const int rows = total(min(sums[i], seg.M));
+            if (a >= 0 || rows <= each) continue;
+            const int mine = (min(rows, seg.M) - 1) / each;
+            if (number <= mine) a = i;
+            else number -= mine;
+        }
+        if (a < 0) return Slice{-1, 0, {}};
+    } else {
+        const int place = k * each;
+        for (int to = seg.L; to - a > 1;) {
+            const int step = (to - a + 7) / 8;
+#pragma unroll
+            for (int i = 0; i < 7; ++i) sums[i] = 0;
+            over_segments<4>(seg, known, [&](int its, int n) {
+#pragma unroll
+                for (int i = 0; i < 7; ++i) sums[i] += its >= 0 && its < a + (i + 1) * step ? n : 0;
+            });
+            int steps = 0;
+#pragma unroll
+            for (int i = 0; i < 7; ++i) steps += total(min(sums[i], seg.M)) <= place ? 1 : 0;
+            a = min(a + steps * step, to - 1);
+            to = min(a + step, to);
+        }
     }
-    const Span span = span_of(seg, known, from);
-    const int number = slice_at_place(k, span.before, each);
-    return Slice{number > 0 && number < (span.rows + each - 1) / each ? from : -1, number, span};
+    const Span span = span_of(seg, known, a);
+    if (!counted) number = slice_at_place(k, span.before, each);
+    return Slice{number > 0 && number < (span.rows + each - 1) / each ? a : -1, number, span};
 }
 
 // 32 rows of X as they are loaded: of eight of them NC neighbours to a lane.  Rows 8 g + e, for operands that sum over eight rows; an X of
@@ -846,12 +867,15 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float*
     }
 }
 
-// The slices of the adapters that have several, added up in order.  A workgroup for the place of each slice behind an adapter's first:
-// that of its second one has the adapter.
-__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int each, long long n,
-                                                           float* __restrict__ dA) {
-    const Slice slice = slice_at(seg, know(seg), blockIdx.y + 1, each);
-    if (slice.a < 0 || slice.number != 1) return;
+// The slices of the adapters that have several, added up in order.  Where there are more adapters than slices behind their first ones, a
+// workgroup takes one of those, and that of its second slice has the adapter.
+__global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int by_slice, int each,
+                                                           long long n, float* __restrict__ dA) {
+    const Known known = know(seg);
+    Slice slice{(int)blockIdx.y, 1, {}};
+    if (by_slice) slice = slice_at(seg, known, blockIdx.y + 1, each);
+    else slice.span = span_of(seg, known, slice.a);
+    if (slice.a < 0 || slice.number != 1 || slice.span.rows <= each) return;
     const int a = slice.a;
     const Span span = slice.span;
     const int slices = (span.rows + each - 1) / each;
@@ -1067,8 +1091,9 @@ int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, l
     APB_HIP(hipGetLastError());
     if (join) {
         const long long n = (long long)r * K;
-        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096), (unsigned)more_slices(M, each));
-        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, each, n, dA);
+        const int more = more_slices(M, each);
+        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096), (unsigned)std::min(L, more));
+        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, L > more, each, n, dA);
         APB_HIP(hipGetLastError());
     }
     return APB_OK;

@@ -105,11 +105,12 @@ APB_BOTH inline int place_of_slices(int before, int each) { return (int)(2LL * b
 // ... and how many places M rows take at most.
 inline long long places_of_slices(int M, int each) { return 2LL * M / each + 1; }
 
-// The slices of an adapter behind its first one.  Were all rows ordered by their adapter, the place k * each lies among the rows of one
-// adapter, with `before` rows of others before it, and stands for that adapter's slice number slice_at_place(k, before, each): 0, or more
-// than it has, where there is none to stand for.  Every slice but the first ones has one place, k = 1 .. more_slices(M, each): at most
-// M / each workgroups beside one for each adapter, instead of M / each for each of them (bfloat16: 65536 rows of 4096 on 256 adapters
-// of rank 16 239 us, with workgroups for all of those 622; 262144 rows of 1024 on 4096 adapters of rank 8 4.0 ms and 80).
+// The slices of adapters behind their first ones: at most M / each of them, which have a workgroup each beside one for each adapter, instead
+// of M / each for each adapter (bfloat16: 65536 rows of 4096 on 64 adapters of rank 16 129 us, with workgroups for all of those 181; on
+// 256 adapters 233 and 622; 262144 rows of 1024 on 4096 adapters of rank 8 4.1 ms and 80).  Were all rows ordered by their adapter, the
+// place k * each, k = 1 .. more_slices(M, each), lies among the rows of one adapter, with `before` rows of others before it, and stands
+// for that adapter's slice number slice_at_place(k, before, each): 0, or more than it has, where there is none to stand for.  Every slice
+// but the first ones has one place.
 inline int more_slices(int M, int each) { return (M - 1) / each; }
 APB_BOTH inline int slice_at_place(int k, int before, int each) { return k - before / each; }
 
