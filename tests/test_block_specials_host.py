@@ -73,6 +73,7 @@ def test_no_operand_is_taken_from_another_device(monkeypatch, at):
     monkeypatch.setattr(binding, "load", Library)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    monkeypatch.setattr(binding, "_several_devices", True)
     name, tensors, sizes = _operands()[at]
     call = getattr(binding, name)
     call(**tensors, **sizes)
