@@ -66,8 +66,9 @@ inline GradientForm gradient_form_of(int x_type, int S, int L, int M, int K, int
 }
 
 // Groups of rows, rows, and groups of ranks to a workgroup of down, and parts of K: what takes least by a count of the bytes that the busiest
-// compute unit brings (40 GB/s each), a quarter of a microsecond for each part that the readers of T will add up, and parts only where T
-// stays small.  Rows may be fewer than their groups hold, where more workgroups then share the work with still one to a compute unit.
+// compute unit brings (40 GB/s each; two a value, whatever the type, so that the parts depend on the sizes alone), a quarter of a
+// microsecond for each part that the readers of T will add up, and parts only where T stays small.  Rows may be fewer than their groups
+// hold, where more workgroups then share the work with still one to a compute unit.
 // Measured (us; rows, groups of ranks, parts; X from memory where there is more than one row): one row of 4096, rank 16: 16 1 1 5.8, 16 1 4
 // 4.3, 16 1 8 4.1; 512 rows, rank 16: 16 1 1 10.0, 16 1 4 4.7; 4100 rows, rank 16: 16 1 1 14.8, 17 1 1 11.0, 24 1 1 12.0, 32 1 1 12.9;
 // 8196 rows, rank 64: 16 4 1 36, 32 4 1 33, 33 4 1 24, 48 4 1 27, 64 4 1 29.
