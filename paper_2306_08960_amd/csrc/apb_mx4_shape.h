@@ -50,19 +50,20 @@ inline int mx4_gated_side(int M, int N, int E, bool grouped) {
 // 11.3 : 12.8, 32 rows 13.6 : 13.0; 2 x 8192 x 8192, 16 rows 25.0 : 32.5; 64 experts of 2 x 1024 x 2048, a row each 26.7 : 27.4, 4 rows
 // 29.2 : 28.0; 16 experts of 2 x 2048 x 4096, 4 rows each 36.4 : 27.0.  More rows of little work, tiles of 16 rows that read the weights
 // again: 1024 x 512 x 512 6.1 : 6.6, 256 x 2048 x 512 6.1 : 6.5, 128 x 2048 x 2048 10.9 : 8.5, 16384 x 64 x 64 10.6 : 8.8; 256 rows on 16
-// experts of 2 x 512 x 512 6.1 : 6.9, 1024 rows 8.5 : 7.1, 64 rows on 8 of 2 x 1024 x 4096 18.4 : 12.5.  Called from Python, each of those
-// is 4 us less with one launch.  Rows are padded to whole segments, and what counts is that: 4096 x 256 x 32 6.9 : 6.1, 4096 x 2048 x 32
-// 26 : 15, 1024 x 8192 x 32 26 : 15; on 16 experts 4096 x 128 x 32 5.8 : 6.2, 4096 x 1024 x 32 23 : 11, 16384 x 32 x 32 10.3 : 8.6, 131072
-// x 4 x 32 63 : 41.  One segment, many outputs and tiles that are mostly empty: 32 x 262144 x 32 34 : 229, 64 x
-// 8192 x 256 4.8 : 7.4, 64 x 524288 x 256 93 : 457, 256 x 24576 x 256 (tiles of 256 a side) 22 : 28, 256 x 24000 (of 128) 22 : 17; on 16
-// experts 512 x 8192 x 32 22 : 24, 512 x 2048 9.5 : 8.1, on 64 2048 x 16384 x 256 98 : 166, 4096 x 2048 31 : 27.  (Of the two kernels'
-// times 2.5 us are the quantization, which a call with 4-bit rows does not have.)
+// experts of 2 x 512 x 512 6.1 : 6.9, 1024 rows 8.5 : 7.1, 64 rows on 8 of 2 x 1024 x 4096 18.4 : 12.5.  Called from Python, a launch less
+// is 4 us less, and two are 12.9 whatever they do.  Below a K of 256 the work no longer falls with K (rows are padded to segments), so the
+// outputs are bounded: 512 x 4096 x 32 11.2 : 7.2, 512 x 8192 x 32 20 : 9.4, 4096 x 2048 x 32 26 : 15; on 16 experts 512 x 2048 x 32
+// 9.5 : 8.1, 16384 x 32 x 32 10.3 : 8.6, 4096 x 1024 x 32 23 : 11, 131072 x 4 x 32 63 : 41.  One segment, many outputs and tiles that are
+// mostly empty: 32 x 262144 x 32 34 : 229, 64 x 8192 x 256 4.8 : 7.4, 64 x 524288 x 256 93 : 457, 256 x 24576 x 256 (tiles of 256 a side)
+// 22 : 28, 256 x 24000 (of 128) 22 : 17; on 16 experts 512 x 8192 x 32 22 : 24, on 64 2048 x 16384 x 256 98 : 166, 4096 x 2048 31 : 27.
+// (Of the two kernels' times 2.5 us are the quantization, which a call with 4-bit rows does not have.)
 inline bool mx4_gated_is_little(int M, int N, int K, int E, bool grouped) {
     const int mean = grouped ? (M + E - 1) / E : M;              // rows of an expert, were they all alike
     const long long outputs = (long long)M * N;
     if (mean <= 16 && (!grouped || (long long)mean * K <= 8192)) return true;
     if (K <= kMxSeg && (grouped ? mean <= 32 && outputs >= 1 << 22 : M <= 64 || (M <= 256 && mx4_product_side(M, 2 * N) == 256))) return true;
-    return K <= 2048 && M <= (grouped ? 16384 : 4096) && outputs <= (1LL << (grouped ? 19 : 20)) / mx_segs(K);
+    return K <= 2048 && M <= (grouped ? 16384 : 4096) &&
+           outputs <= std::min<long long>((1LL << (grouped ? 27 : 28)) / K, 1 << (grouped ? 20 : 21));
 }
 
 constexpr int kMx4Pass = 64;                  // rows of the 4-bit matrix that a pass of the gradients sums over

@@ -141,25 +141,27 @@ def test_limits_of_parts():
 
 
 @needs_lib
-def test_little_work_is_counted_with_what_rows_are_padded_to():
-    """A product of less than 256 values a row costs what one of 256 does: whether it runs as one kernel does not depend on how many."""
+def test_little_work_is_bounded():
+    """A product of less than 256 values a row costs what one of 256 does: how much runs as one kernel does not grow without end as there
+    are fewer, and a launch of it is never more than a launch can be."""
     from paper_2306_08960_amd import binding as b
     one = lambda E, M, N, K: b.apb_mx4_gated_linear_scratch_bytes(E > 0, max(E, 1), M, N, K) == 0
     g = np.random.default_rng(0)
     taken = set()
     for _ in range(4000):
         E, M, N = int(g.choice([0, 16])), int(np.exp(g.uniform(3, 14))), int(np.exp(g.uniform(0, 11)))
-        padded = one(E, M, N, 256)
-        taken.add((E, padded))
-        for K in (1, 8, 32, 100, 255):
-            assert one(E, M, N, K) == padded, (E, M, N, K)
-        if padded and M > 16 * max(E, 1) and not (M * N >= 1 << 22 and M <= 32 * E if E else M <= 64 or M <= 256 and N > 24320):
-            assert M <= (16384 if E else 4096) and M * N <= 1 << (19 if E else 20)
-    assert taken == {(E, o) for E in (0, 16) for o in (False, True)}
-    for E, M, N, K in ((0, 4096, 2048, 32), (0, 1024, 8192, 8), (16, 131072, 4, 128), (16, 131072, 32, 32), (16, (1 << 27) - 8, 1, 1), (16, 512, 2048, 32)):
+        few = M <= 16 * max(E, 1) or (M * N >= 1 << 22 and M <= 32 * E if E else M <= 64 or M <= 256 and N > 24320)
+        for K in (1, 8, 32, 100, 128, 255, 256):
+            o = one(E, M, N, K)
+            taken.add((E, K, few, o))
+            assert o == few or not few
+            if o and not few:
+                assert M <= (16384 if E else 4096) and M * N <= 1 << (20 if E else 21) and M * N * K <= 1 << (27 if E else 28)
+    assert {(E, K, o) for E, K, few, o in taken if not few} == {(E, K, o) for E in (0, 16) for K in (1, 8, 32, 100, 128, 255, 256) for o in (False, True)}
+    for E, M, N, K in ((0, 4096, 2048, 32), (0, 1024, 8192, 8), (16, 131072, 4, 128), (16, 131072, 32, 32), (16, (1 << 27) - 8, 1, 1)):
         assert not one(E, M, N, K)
     for E, M, N, K in ((0, 4096, 256, 32), (16, 4096, 128, 32), (16, 16384, 32, 200), (0, 32, 262144, 8), (0, 64, 8192, 256), (0, 256, 24576, 32),
-                       (16, 512, 8192, 32), (64, 2048, 16384, 256)):
+                       (16, 512, 8192, 32), (64, 2048, 16384, 256), (0, 310, 3664, 66), (9, 192, 4168, 160), (0, 1024, 512, 512)):
         assert one(E, M, N, K)
 
 
