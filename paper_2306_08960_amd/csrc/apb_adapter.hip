@@ -523,39 +523,25 @@ __device__ __forceinline__ int total(int v) {
     return __builtin_amdgcn_readlane(v, kWave - 1);
 }
 
-// What a wave knows of the segments: lane s of the s-th one's adapter, first row and rows, if there are no more of them than lanes.
+// What a wave knows of the segments, a lane each: the last ones that it has looked at, or all if there are no more of them than lanes.
 struct Known {
     int its, first, count;
 };
-__device__ __forceinline__ Known know(const Segments& seg) {
-    Known k = {};
-    if (seg.S <= kWave) k.its = rows_of(seg, threadIdx.x & (kWave - 1), k.first, k.count);
-    return k;
-}
-// add(adapter, rows) of all segments, by lanes, WIDE * 64 of them by loads that do not wait for one another.
-template <int WIDE, class ADD>
-__device__ __forceinline__ void over_segments(const Segments& seg, const Known& known, ADD add) {
-    if (seg.S <= kWave) return add(known.its, known.count);
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int base = 0; base < seg.S; base += WIDE * kWave) {
-        int a[WIDE], first, n[WIDE];
-#pragma unroll
-        for (int u = 0; u < WIDE; ++u) a[u] = rows_of(seg, base + u * kWave + lane, first, n[u]);
-#pragma unroll
-        for (int u = 0; u < WIDE; ++u) add(a[u], n[u]);
-    }
-}
-
-// The rows of adapter a, and of all adapters before it.
+// The rows of adapter a, and of all adapters before it.  (A loop of few instructions rather than loads side by side: a workgroup
+// comes here once, and fetching instructions takes as long as waiting for the loads.)
 struct Span {
     int rows, before;
 };
-__device__ __forceinline__ Span span_of(const Segments& seg, const Known& known, int a) {
+// fresh: `known` is nothing yet.
+__device__ __forceinline__ Span span_of(const Segments& seg, int a, Known& known, bool fresh) {
+    const int lane = threadIdx.x & (kWave - 1);
     int rows = 0, before = 0;
-    over_segments<2>(seg, known, [&](int its, int n) {
-        rows += its == a ? n : 0;
-        before += its >= 0 && its < a ? n : 0;
-    });
+#pragma unroll 1
+    for (int base = 0; base < seg.S; base += kWave) {
+        if (fresh || seg.S > kWave) known.its = rows_of(seg, base + lane, known.first, known.count);
+        rows += known.its == a ? known.count : 0;
+        before += known.its >= 0 && known.its < a ? known.count : 0;
+    }
     // (together they are no more than M; of offsets that do not ascend, that much is kept)
     rows = min(total(min(rows, seg.M)), seg.M);
     return Span{rows, min(total(min(before, seg.M)), seg.M - rows)};
@@ -576,48 +562,27 @@ struct Slice {
     int a, number;
     Span span;
 };
-// The k-th slice behind the adapters' first ones, k = 1 ..  Up to eight adapters' slices are counted, so that those k that have no work come
-// last (16384 rows of 512, four adapters of rank 16, which are 256 workgroups: 9.8 us, 15.0 with such k among them).  More adapters: the
-// place k * each stands for one (slice_at_place).  Adapters are looked for in eighths, a pass over the segments adds up the rows before
-// seven of them.
-__device__ __forceinline__ Slice slice_at(const Segments& seg, const Known& known, int k, int each) {
-    const bool counted = seg.L > 1 && seg.L <= 8;
-    int sums[8] = {}, a = 0, number = k;
-    if (counted) {
-        over_segments<4>(seg, known, [&](int its, int n) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sums[i] += its == i ? n : 0;
-        });
-        a = -1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int rows = total(min(sums[i], seg.M));
-            if (a >= 0 || rows <= each) continue;
-            const int mine = (min(rows, seg.M) - 1) / each;
-            if (number <= mine) a = i;
-            else number -= mine;
-        }
-        if (a < 0) return Slice{-1, 0, {}};
-    } else {
-        const int place = k * each;
-        for (int to = seg.L; to - a > 1;) {
-            const int step = (to - a + 7) / 8;
-#pragma unroll
-            for (int i = 0; i < 7; ++i) sums[i] = 0;
-            over_segments<4>(seg, known, [&](int its, int n) {
-#pragma unroll
-                for (int i = 0; i < 7; ++i) sums[i] += its >= 0 && its < a + (i + 1) * step ? n : 0;
-            });
-            int steps = 0;
-#pragma unroll
-            for (int i = 0; i < 7; ++i) steps += total(min(sums[i], seg.M)) <= place ? 1 : 0;
-            a = min(a + steps * step, to - 1);
-            to = min(a + step, to);
+// What the place k * each stands for (slice_at_place): a slice of the last adapter with no more rows before it, or none.
+__device__ __forceinline__ Slice slice_at(const Segments& seg, int k, int each, Known& known) {
+    Slice slice{0, 0, {}};
+    bool fresh = true;
+    int to = seg.L;
+#pragma unroll 1
+    for (;;) {
+        const int middle = (slice.a + to) / 2;                   // (at last slice.a itself)
+        const Span span = span_of(seg, middle, known, fresh);
+        fresh = false;
+        if (span.before > k * each) {
+            to = middle;
+        } else {
+            slice.span = span;
+            if (middle == slice.a) break;
+            slice.a = middle;
         }
     }
-    const Span span = span_of(seg, known, a);
-    if (!counted) number = slice_at_place(k, span.before, each);
-    return Slice{number > 0 && number < (span.rows + each - 1) / each ? a : -1, number, span};
+    slice.number = slice_at_place(k, slice.span.before, each);
+    if (slice.number <= 0 || slice.number >= (slice.span.rows + each - 1) / each) slice.a = -1;
+    return slice;
 }
 
 // 32 rows of X as they are loaded: of eight of them NC neighbours to a lane.  Rows 8 g + e, for operands that sum over eight rows; an X of
@@ -700,14 +665,14 @@ __device__ __forceinline__ void clear_adapters(const Segments& seg, long long n,
     constexpr int kPiece = 4096;
     const int pieces = (int)((n + kPiece - 1) / kPiece);
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const Known all_of = know(seg);
+    Known known;
     int last = -1;
     bool empty = false;
     const long long all = (long long)pieces * seg.L, each = (all + parts - 1) / parts;
     for (long long u = part * each; u < std::min(all, (part + 1) * each); ++u) {
         const int a = (int)(u / pieces);
         if (a != last) {
-            empty = span_of(seg, all_of, a).rows == 0;
+            empty = span_of(seg, a, known, true).rows == 0;
             last = a;
         }
         if (!empty) continue;
@@ -720,8 +685,8 @@ __device__ __forceinline__ void clear_adapters(const Segments& seg, long long n,
 // values twice.  (Rows of 8 bits are padded, and their columns stay in blocks.)
 //
 // A workgroup takes one adapter (by_segment: that of a segment), 16 * JT ranks, 16 * NC columns, and the first `each` of the adapter's rows,
-// or those of another of its slices (`more`: how many places for them there are), counted through all of its segments, whose numbers it
-// lists in LDS; its waves take 32 of them at a time in turn, by themselves, the next ones under
+// or those of another of its slices (`more` workgroups, for every adapter as many or by_slice), counted through all of its segments, whose
+// numbers it lists in LDS; its waves take 32 of them at a time in turn, by themselves, the next ones under
 // way, and join their sums in LDS.  T, its parts added up, comes to registers in the order of the operand and is split there into three
 // bfloat16 parts (an X of float32 goes with T as it is through float32 products); X is transposed in registers.  With waves that share a
 // tile of rows in LDS and each take columns of their own, every wave waits at barriers for the slowest load, and an adapter's rows have
@@ -730,7 +695,7 @@ __device__ __forceinline__ void clear_adapters(const Segments& seg, long long n,
 template <int XT, int JT, int NC, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float* __restrict__ T, int parts, const void* __restrict__ X,
                                                                     long long ldx, Mx8 x8, Segments seg, int K, int r, int rank_tiles,
-                                                                    int by_segment, int each, int more, float* __restrict__ dA,
+                                                                    int by_segment, int by_slice, int each, int more, float* __restrict__ dA,
                                                                     float* __restrict__ shared) {
     constexpr int kChunk = 32, kRanks = 16 * JT;
     __shared__ f32x4 sums[WAVES][JT * NC][kWave];
@@ -742,13 +707,19 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float*
         clear_adapters(seg, (long long)r * K, (blockIdx.y - behind) * gridDim.x + blockIdx.x, (gridDim.y - behind) * gridDim.x, dA);
         return;
     }
-    Known known = know(seg);
-    Slice slice{unit, 0, {}};
-    if (unit >= firsts) slice = slice_at(seg, known, unit - firsts + 1, each);
-    else if (by_segment) slice.a = first_segment_of(seg, unit);
+    Known known;
+    Slice slice{unit % firsts, unit / firsts, {}};
+    if (unit >= firsts && by_slice) {
+        slice = slice_at(seg, unit - firsts + 1, each, known);
+        if (slice.a < 0) return;
+    } else {
+        if (by_segment) slice.a = first_segment_of(seg, slice.a);
+        if (slice.a < 0) return;
+        slice.span = span_of(seg, slice.a, known, true);
+        if (slice.number > 0 && slice.number * each >= slice.span.rows) return;
+    }
     const int a = slice.a;
-    if (a < 0) return;
-    const Span span = unit < firsts ? span_of(seg, known, a) : slice.span;
+    const Span span = slice.span;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane & 15, g = lane >> 4;
     const int c0 = XT == APB_MX8 ? blockIdx.x * 16 * NC : WHOLE ? min((int)blockIdx.x * 16 * NC, K - 16 * NC) : 0, c = c0 + NC * i;
     const int lo = slice.number * each, hi = min(lo + each, span.rows);
@@ -867,14 +838,14 @@ __global__ __launch_bounds__(WAVES * kWave) void k_adapter_gradient(const float*
     }
 }
 
-// The slices of the adapters that have several, added up in order.  Where there are more adapters than slices behind their first ones, a
-// workgroup takes one of those, and that of its second slice has the adapter.
+// The slices of the adapters that have several, added up in order.  by_slice: a workgroup takes a slice behind an adapter's first one, and
+// that of its second has the adapter.
 __global__ __launch_bounds__(kThreads) void k_adapter_join(const float* __restrict__ shared, Segments seg, int by_slice, int each,
                                                            long long n, float* __restrict__ dA) {
-    const Known known = know(seg);
+    Known known;
     Slice slice{(int)blockIdx.y, 1, {}};
-    if (by_slice) slice = slice_at(seg, known, blockIdx.y + 1, each);
-    else slice.span = span_of(seg, known, slice.a);
+    if (by_slice) slice = slice_at(seg, blockIdx.y + 1, each, known);
+    else slice.span = span_of(seg, slice.a, known, true);
     if (slice.a < 0 || slice.number != 1 || slice.span.rows <= each) return;
     const int a = slice.a;
     const Span span = slice.span;
@@ -985,11 +956,13 @@ void gradient_form(const float* T, int parts, const void* X, long long ldx, cons
     const int rank_tiles = (r + 16 * JT - 1) / (16 * JT);
     const int by_segment = gradient_by_segment(seg.S, seg.L, K, r);
     const unsigned columns = (unsigned)((K + 16 * NC - 1) / (16 * NC));
-    const int firsts = by_segment ? seg.S : seg.L, more = more_slices(seg.M, each);
+    const int firsts = by_segment ? seg.S : seg.L;
+    const bool by_slice = gradient_by_slice(firsts, seg.M, each, (long long)columns * rank_tiles);
+    const int more = by_slice ? more_slices(seg.M, each) : firsts * ((seg.M - 1) / each);
     const dim3 grid(columns, (unsigned)((firsts + more) * rank_tiles + (by_segment ? (1024 + columns - 1) / columns : 0)));
     auto launch = [&](auto whole) {
         hipLaunchKernelGGL((k_adapter_gradient<XT, JT, NC, WAVES, decltype(whole)::value>), grid, dim3(WAVES * kWave), 0, s, T, parts, X, ldx, x8,
-                           seg, K, r, rank_tiles, by_segment, each, more, dA, shared);
+                           seg, K, r, rank_tiles, by_segment, by_slice, each, more, dA, shared);
     };
     if constexpr (XT == APB_MX8 || NC == 8) launch(std::true_type{});
     else if (K >= 16 * NC) launch(std::true_type{});
@@ -1091,9 +1064,10 @@ int apb_adapter_gradient(const float* T, int parts, const void* X, int x_type, l
     APB_HIP(hipGetLastError());
     if (join) {
         const long long n = (long long)r * K;
-        const int more = more_slices(M, each);
-        const dim3 grid((unsigned)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096), (unsigned)std::min(L, more));
-        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, L > more, each, n, dA);
+        const int columns = (int)std::min<long long>((n + 4 * kWave - 1) / (4 * kWave), 4096);
+        const bool by_slice = join_by_slice(L, M, each, columns);
+        const dim3 grid((unsigned)columns, (unsigned)(by_slice ? more_slices(M, each) : L));
+        hipLaunchKernelGGL(k_adapter_join, grid, dim3(kThreads), 0, s, shared, seg, by_slice, each, n, dA);
         APB_HIP(hipGetLastError());
     }
     return APB_OK;

@@ -106,13 +106,19 @@ APB_BOTH inline int place_of_slices(int before, int each) { return (int)(2LL * b
 // ... and how many places M rows take at most.
 inline long long places_of_slices(int M, int each) { return 2LL * M / each + 1; }
 
-// The slices of adapters behind their first ones: at most M / each of them, which have a workgroup each beside one for each adapter, instead
-// of M / each for each adapter (bfloat16: 65536 rows of 4096 on 64 adapters of rank 16 129 us, with workgroups for all of those 181; on
-// 256 adapters 233 and 622; 262144 rows of 1024 on 4096 adapters of rank 8 4.1 ms and 80).  Were all rows ordered by their adapter, the
-// place k * each, k = 1 .. more_slices(M, each), lies among the rows of one adapter, with `before` rows of others before it, and stands
-// for that adapter's slice number slice_at_place(k, before, each): 0, or more than it has, where there is none to stand for.  Every slice
-// but the first ones has one place.
+// The slices of adapters behind their first ones: at most M / each of them, which have a workgroup each beside one for each adapter
+// (bfloat16: 65536 rows of 4096 on 64 adapters of rank 16 131 us, with M / each workgroups for each adapter 181; on 256 adapters 247 and
+// 622; 262144 rows of 1024 on 4096 adapters of rank 8 4.5 ms and 80).  Were all rows ordered by their adapter, the place k * each, k = 1 ..
+// more_slices(M, each), lies among the rows of one adapter, with `before` rows of others before it, and stands for that adapter's slice
+// number slice_at_place(k, before, each): 0, or more than it has, where there is none to stand for.  Every slice but the first ones has
+// one place.
 inline int more_slices(int M, int each) { return (M - 1) / each; }
 APB_BOTH inline int slice_at_place(int k, int before, int each) { return k - before / each; }
+// To find out which adapter's a slice is takes a few microseconds.  So there are workgroups for each of `firsts` adapters or segments and each
+// of M / each slices, `groups` of them, as long as those that only exit are few.  us, so and by slice: 2506 of them (17979 rows of 435, 179
+// adapters of rank 5) 28 and 31; 3710 (27505 of 28, 35 of rank 24) 22 and 12; 6963 (8469 of 12, 211 of rank 2) 30 and 11.
+inline bool gradient_by_slice(int firsts, int M, int each, long long groups) { return firsts * groups * ((M - 1) / each) > 3072; }
+// The same for the workgroups that join them, `columns` for each adapter, which exit sooner.
+inline bool join_by_slice(int L, int M, int each, long long columns) { return L > more_slices(M, each) && L * columns > 8192; }
 
 }  // namespace apb

@@ -170,24 +170,59 @@ def test_little_work_is_bounded():
 SLICES = r"""
 #include <cstdio>
 #include "apb_adapter_shape.h"
+using namespace apb;
 
-int main() {                                                          // rows before an adapter, to a slice, all rows
-    int before, each, M;
-    while (std::scanf("%d %d %d", &before, &each, &M) == 3) {
-        std::printf("%d", apb::more_slices(M, each));
-        for (int k = 1; k <= apb::more_slices(M, each); ++k) std::printf(" %d", apb::slice_at_place(k, before, each));
-        std::printf("\n");
+int main() {
+    char what;
+    int a, b, c, K, r;
+    while (std::scanf(" %c %d %d %d %d %d", &what, &a, &b, &c, &K, &r) == 6) {
+        if (what == 's') {                                            // rows before an adapter, to a slice, all rows
+            std::printf("%d", more_slices(c, b));
+            for (int k = 1; k <= more_slices(c, b); ++k) std::printf(" %d", slice_at_place(k, a, b));
+            std::printf("\n");
+        } else {                                                      // segments, adapters, rows, long side, rank: the launch's rows and how many
+            const GradientForm form = gradient_form_of(APB_BF16, a, b, c, K, r);      // ... of its workgroups may have nothing to do
+            const int each = gradient_rows(a, b, c, K, r), tiles = (r + 16 * form.jt - 1) / (16 * form.jt);
+            const long long groups = (long long)((K + 16 * form.nc - 1) / (16 * form.nc)) * tiles;
+            const int firsts = gradient_by_segment(a, b, K, r) ? a : b;
+            const bool by_slice = gradient_by_slice(firsts, c, each, groups);
+            const long long more = by_slice ? more_slices(c, each) : (long long)firsts * ((c - 1) / each);
+            std::printf("%lld %lld %lld %d\n", (firsts + more) * tiles + 1024, more * groups, more_slices(c, each) * groups, by_slice);
+        }
     }
 }
 """
 
 
-def test_every_slice_has_one_workgroup(tmp_path):
-    """First slices have one for each adapter; the others one place each among M / each, and no place stands for two."""
-    src, exe = tmp_path / "slices.cpp", tmp_path / "slices"
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    at = tmp_path_factory.mktemp("slices")
+    src, exe = at / "slices.cpp", at / "slices"
     src.write_text(SLICES)
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-ftrapv", "-I", os.path.join(ROOT, "include"),
                     "-I", os.path.join(ROOT, "paper_2306_08960_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+
+    def answers(questions):
+        text = "\n".join(" ".join(map(str, q)) for q in questions)
+        p = subprocess.run([str(exe)], input=text, stdout=subprocess.PIPE, text=True, check=True, timeout=60)
+        return [list(map(int, line.split())) for line in p.stdout.splitlines()]
+    return answers
+
+
+def test_no_more_idle_workgroups_than_a_few(ask):
+    """However many adapters there are: as many workgroups beside their first slices' as there can be slices, or few."""
+    g = np.random.default_rng(2)
+    sizes = [(int(np.exp(g.uniform(0, 8.3))), int(np.exp(g.uniform(0, 8.3))), int(np.exp(g.uniform(0, 16.6))), int(np.exp(g.uniform(0, 11))),
+              int(g.integers(1, 257))) for _ in range(3000)] + [(4096, 4096, 1 << 24, 1 << 22, 256), (1, 1, 1, 1, 1), (256, 256, 65536, 4096, 16)]
+    seen = set()
+    for (rows, extra, useful, by_slice), size in zip(ask([("w", *s) for s in sizes]), sizes):
+        assert rows <= 65535 and extra <= max(useful, 3072), size
+        seen.add(by_slice)
+    assert seen == {0, 1}
+
+
+def test_every_slice_has_one_workgroup(ask):
+    """First slices have one for each adapter; the others one place each among M / each, and no place stands for two."""
     g = np.random.default_rng(1)
     for case in range(150):
         L, each = int(g.integers(1, 30)), int(g.choice([1, 2, 3, 64, 128, 320]))
@@ -195,9 +230,7 @@ def test_every_slice_has_one_workgroup(tmp_path):
         rows[g.integers(L)] = int(g.choice([1, each, each + 1, 3 * each, 3 * each - 1]))
         behind = int(g.integers(0, 300))                             # (rows of no adapter)
         before, M = np.concatenate([[0], np.cumsum(rows)]), int(rows.sum()) + behind
-        text = "\n".join(f"{b} {each} {M}" for b in before[:-1])
-        p = subprocess.run([str(exe)], input=text, stdout=subprocess.PIPE, text=True, check=True, timeout=60)
-        answers = [list(map(int, line.split())) for line in p.stdout.splitlines()]
+        answers = ask([("s", int(b), each, M, 1, 1) for b in before[:-1]])
         taken, places = [], answers[0][0]
         assert places * each < M
         for k in range(1, places + 1):
